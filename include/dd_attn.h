@@ -274,6 +274,77 @@ int dd_swiglu_bwd(const void *U, const void *V, const void *dY, void *dU, void *
 int dd_transpose(const void *X, long long ldx, void *Y, long long ldy, int rows, int cols,
                  void *stream);
 
+/*
+ * Rows in 8 bits.  Codes of a row z with largest magnitude A: int8 q = the
+ * integer nearest to 127 z / A, ties to even (so in [-127, 127]), and an fp32
+ * scale; the row's values are scale * q.  A row of zeros has codes and scale
+ * 0; a row that holds a NaN or an infinity has codes 0 and a NaN scale (all
+ * its values are NaN, and no other row's).  rows >= 1, 1 <= d <= 16384, rows
+ * * d < 2^40; row strides (elements) at least d; bf16 pointers 2-byte, fp32
+ * pointers 4-byte aligned.  Rows of 16-byte aligned pieces (d and the strides
+ * multiples of 8, pointers 16-byte, codes 8-byte aligned) run with wide
+ * accesses, others element by element.  Outputs must not overlap inputs or
+ * each other.
+ *
+ * dd_quantize    codes and scales (A / 127) of the rows of a bf16 matrix X.
+ * dd_dequantize  Y = bf16(scale * q).
+ * dd_rmsnorm_fwd RMSNorm over the rows of X + R: H = bf16(X + R) (X itself
+ *                where R is NULL; H is then NULL too), rstd = 1 /
+ *                sqrt(mean(H^2) + eps) (fp32 [rows], kept for the backward),
+ *                Y = H rstd w, w bf16 [d].  H and Y contiguous, eps finite
+ *                and > 0.
+ * dd_rmsnorm_int8_fwd  the same with the output as codes of the rows of
+ *                H w and scales A rstd / 127.
+ * dd_rmsnorm_bwd its backward (of either form; codes pass the gradient
+ *                straight through) for the upstream gradient dY: dX is the
+ *                gradient of X and of R alike, plus dRes (optional: the
+ *                gradient of H from its other uses), added before rounding;
+ *                dw bf16 [d], summed over the rows in fp32 in a fixed order.  All
+ *                contiguous.  workspace: fp32 scratch of
+ *                dd_rmsnorm_bwd_workspace_bytes(rows, d) bytes.
+ */
+int dd_quantize(const void *X, long long ldx, int8_t *Q, long long ldq, float *scales, int rows,
+                int d, void *stream);
+int dd_dequantize(const int8_t *Q, long long ldq, const float *scales, void *Y, long long ldy,
+                  int rows, int d, void *stream);
+int dd_rmsnorm_fwd(const void *X, long long ldx, const void *R, long long ldr, const void *w,
+                   void *H, void *Y, float *rstd, int rows, int d, float eps, void *stream);
+int dd_rmsnorm_int8_fwd(const void *X, long long ldx, const void *R, long long ldr, const void *w,
+                        void *H, int8_t *Q, long long ldq, float *scales, float *rstd, int rows,
+                        int d, float eps, void *stream);
+int dd_rmsnorm_bwd(const void *H, const void *w, const float *rstd, const void *dY,
+                   const void *dRes, void *dX, void *dw, int rows, int d, void *workspace,
+                   size_t workspace_bytes, void *stream);
+size_t dd_rmsnorm_bwd_workspace_bytes(int rows, int d);
+
+/*
+ * Products of codes.
+ *
+ * dd_gemm_i8: C[m, n] = bf16(sa[m] sb[n] sum_k A[m, k] B[n, k] (+ R[m, n])),
+ * A [M][K] and B [N][K] int8 with row strides lda and ldb, an fp32 scale per
+ * row of each (per token, per output channel); the sum is exact in int32, the
+ * rest fp32 with one rounding.  R: NULL, or a bf16 [M][N] matrix of row
+ * stride ldc, which may be C itself.  Any M and N >= 1 (together at most
+ * 2^23 - 1 tiles of 64 x 64), K a multiple of 16 below 2^17; lda and ldb
+ * multiples of 16 below 2^23, A and B 16-byte aligned.  C must not overlap
+ * the other inputs.
+ *
+ * dd_gemm_i8_wgrad: the weight gradient of a layer y = x W whose input was
+ * kept as codes: dW [M][N] = X^T dY with X = bf16(scales Q), Q [T][M] int8,
+ * dY [T][N] bf16, fp32 sums.  T >= 1, M and N multiples of 8; strides
+ * multiples of 8, ldq and ldy below 2^23; Q 8-byte, dY and dW 16-byte aligned.
+ * dW must not overlap the inputs.  workspace: scratch of
+ * dd_gemm_i8_wgrad_workspace_bytes(T, M, N) bytes, 16-byte aligned (may be
+ * NULL where that is 0).
+ */
+int dd_gemm_i8(const int8_t *A, long long lda, const float *sa, const int8_t *B, long long ldb,
+               const float *sb, const void *R, void *C, long long ldc, int M, int N, int K,
+               void *stream);
+int dd_gemm_i8_wgrad(const int8_t *Q, long long ldq, const float *scales, const void *dY,
+                     long long ldy, void *dW, long long ldw, int T, int M, int N, void *workspace,
+                     size_t workspace_bytes, void *stream);
+size_t dd_gemm_i8_wgrad_workspace_bytes(int T, int M, int N); /* 0: none needed, or invalid */
+
 /* Workspace bytes dd_attn_bwd needs for this shape (0 for an invalid shape). */
 size_t dd_attn_bwd_workspace_bytes(int B, int L, int H, int D);
 

@@ -1,11 +1,19 @@
 """Python binding of the block kernels around the attention (argument
-marshalling only): the bf16 GEMM, LayerNorm and SwiGLU of include/dd_attn.h.
+marshalling only): the bf16 GEMM, LayerNorm and SwiGLU of include/dd_attn.h,
+and its 8-bit operators: RMSNorm, rows as codes, and their products.
 
 Every computation runs in the HIP kernels behind the C ABI; this module
 checks tensor metadata, allocates outputs and scratch with torch on the
 tensors' device and passes raw pointers, strides and the current stream.
 Matrices are 2-D bf16 tensors with unit column stride (row-major, possibly
 a column slice of a wider matrix: the row stride is passed through).
+
+8-bit matrices are int8 codes [rows, d] with one fp32 scale per row: row r's
+values are scales[r] * codes[r].  ``quantize`` forms them (the nearest codes
+to 127 x / max |x| of each row, ties to even) and so does ``rms_norm_int8``;
+``gemm_int8`` multiplies two of them, ``gemm_int8_wgrad`` takes one as the
+kept input of a linear layer.  Their calls run on the tensors' device, on
+its current stream; matrices without rows or columns give empty results.
 """
 from __future__ import annotations
 
@@ -221,3 +229,213 @@ def swiglu_backward(u, v, dy):
                              _stream(u.device))
     check(st, "dd_swiglu_bwd")
     return du, dv
+
+
+# ---------------------------------------------------------------------------
+# rows in 8 bits
+
+
+def _call(dev, name, *args):
+    """Runs an entry point on the current stream of ``dev``."""
+    fn = getattr(lib(), name)
+    if dev.index == torch.cuda.current_device():
+        st = fn(*args, _stream(dev))
+    else:
+        with torch.cuda.device(dev):
+            st = fn(*args, _stream(dev))
+    check(st, name)
+
+
+def _on(t, name, dev):
+    if t.device != dev:
+        raise ValueError(f"{name} is on {t.device}, not on {dev}")
+
+
+def _ld(t):
+    """Row stride; of a single row, whose stride is never used, its length."""
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def _vec(t, name, n, dtype, dev):
+    if (isinstance(t, torch.Tensor) and t.dtype is dtype and t.shape == (n,)
+            and t.device == dev and t.is_contiguous()):
+        return
+    raise ValueError(f"{name} must be a contiguous {dtype} tensor of {n} elements on {dev}")
+
+
+def _code_matrix(t, name, dev=None):
+    if not isinstance(t, torch.Tensor) or t.dim() != 2:
+        raise ValueError(f"{name} must be a 2-D tensor")
+    if t.dtype is not torch.int8 or not t.is_cuda:
+        raise ValueError(f"{name} must be an int8 GPU tensor")
+    if t.stride(1) != 1:
+        raise ValueError(f"{name} must have unit column stride")
+    if dev is not None:
+        _on(t, name, dev)
+
+
+def _rows(t, name, shape, dev):
+    """A contiguous bf16 matrix of this shape on ``dev``."""
+    _mat(t, name)
+    _on(t, name, dev)
+    if t.shape != shape:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+
+
+def _norm_inputs(x, w, residual):
+    _mat(x, "x")
+    dev = x.device
+    _vec(w, "w", x.shape[1], torch.bfloat16, dev)
+    if residual is None:
+        return dev, None
+    _mat(residual, "residual")
+    _on(residual, "residual", dev)
+    if residual.shape != x.shape:
+        raise ValueError("residual must match x in shape")
+    return dev, torch.empty(x.shape, dtype=torch.bfloat16, device=dev)
+
+
+def rms_norm(x, w, residual=None, eps: float = LN_EPS):
+    """(y, h, rstd) of RMSNorm over the rows of h = x + residual (rounded to
+    bf16; x itself without one): rstd = 1 / sqrt(mean(h^2) + eps), y = h rstd w."""
+    dev, h = _norm_inputs(x, w, residual)
+    rows, d = x.shape
+    y = torch.empty((rows, d), dtype=torch.bfloat16, device=dev)
+    rstd = torch.empty(rows, dtype=torch.float32, device=dev)
+    if y.numel():
+        _call(dev, "dd_rmsnorm_fwd", _p(x), _ld(x), _p(residual),
+              0 if residual is None else _ld(residual), _p(w), _p(h), _p(y), _p(rstd), rows, d,
+              eps)
+    return y, x if h is None else h, rstd
+
+
+def rms_norm_int8(x, w, residual=None, eps: float = LN_EPS):
+    """(codes, scales, h, rstd): ``rms_norm`` with its output as codes."""
+    dev, h = _norm_inputs(x, w, residual)
+    rows, d = x.shape
+    codes = torch.empty((rows, d), dtype=torch.int8, device=dev)
+    scales, rstd = (torch.empty(rows, dtype=torch.float32, device=dev) for _ in range(2))
+    if codes.numel():
+        _call(dev, "dd_rmsnorm_int8_fwd", _p(x), _ld(x), _p(residual),
+              0 if residual is None else _ld(residual), _p(w), _p(h), _p(codes), d, _p(scales),
+              _p(rstd), rows, d, eps)
+    return codes, scales, x if h is None else h, rstd
+
+
+def rms_norm_backward(h, w, rstd, dy, dres=None):
+    """(dx, dw) of either norm for the gradient dy of its output; dx is the
+    gradient of x and of the residual, ``dres`` (optional, the gradient of h
+    from its other uses) is added to it."""
+    _mat(h, "h")
+    dev, (rows, d) = h.device, h.shape
+    _rows(h, "h", h.shape, dev)
+    _vec(w, "w", d, torch.bfloat16, dev)
+    _vec(rstd, "rstd", rows, torch.float32, dev)
+    for t, n in ((dy, "dy"), (dres, "dres")):
+        if t is not None or n == "dy":
+            _rows(t, n, h.shape, dev)
+    dx = torch.empty((rows, d), dtype=torch.bfloat16, device=dev)
+    if not dx.numel():
+        return dx, torch.zeros(d, dtype=torch.bfloat16, device=dev)
+    dw = torch.empty(d, dtype=torch.bfloat16, device=dev)
+    need = lib().dd_rmsnorm_bwd_workspace_bytes(rows, d)
+    ws = torch.empty(need, dtype=torch.uint8, device=dev)
+    _call(dev, "dd_rmsnorm_bwd", _p(h), _p(w), _p(rstd), _p(dy), _p(dres), _p(dx), _p(dw), rows,
+          d, _p(ws), need)
+    return dx, dw
+
+
+def quantize(x):
+    """(codes, scales) of the rows of a bf16 matrix."""
+    _mat(x, "x")
+    rows, d = x.shape
+    codes = torch.empty((rows, d), dtype=torch.int8, device=x.device)
+    scales = torch.empty(rows, dtype=torch.float32, device=x.device)
+    if codes.numel():
+        _call(x.device, "dd_quantize", _p(x), _ld(x), _p(codes), d, _p(scales), rows, d)
+    return codes, scales
+
+
+def dequantize(codes, scales, out=None):
+    """The bf16 values of codes (into ``out`` if given)."""
+    _code_matrix(codes, "codes")
+    dev, (rows, d) = codes.device, codes.shape
+    _vec(scales, "scales", rows, torch.float32, dev)
+    if out is None:
+        out = torch.empty((rows, d), dtype=torch.bfloat16, device=dev)
+    else:
+        _mat(out, "out")
+        _on(out, "out", dev)
+        if out.shape != codes.shape:
+            raise ValueError(f"out has shape {tuple(out.shape)}, expected {(rows, d)}")
+    if codes.numel():
+        _call(dev, "dd_dequantize", _p(codes), _ld(codes), _p(scales), _p(out), _ld(out), rows, d)
+    return out
+
+
+def gemm_int8(a, a_scales, b, b_scales, residual=None, out=None):
+    """(a_scales * a) @ (b_scales * b).T (+ residual) in bf16, from codes a
+    [M, K] (tokens) and b [N, K] (output channels; a weight W [K, N] is kept
+    as ``quantize(W.T.contiguous())``), K a multiple of 16 below 2^17.
+
+    The sums are exact, scaled in fp32 and rounded once.  ``out`` (optional)
+    receives the result and may be ``residual`` itself."""
+    _code_matrix(a, "a")
+    dev, (M, K) = a.device, a.shape
+    _code_matrix(b, "b", dev)
+    N = b.shape[0]
+    if b.shape[1] != K:
+        raise ValueError(f"inner dimensions differ: {K} vs {b.shape[1]}")
+    if K % 16 or not 0 < K < 1 << 17:
+        raise ValueError(f"the inner dimension must be a multiple of 16 below 2^17 (got {K})")
+    _vec(a_scales, "a_scales", M, torch.float32, dev)
+    _vec(b_scales, "b_scales", N, torch.float32, dev)
+    if out is None:
+        out = torch.empty((M, N), dtype=torch.bfloat16, device=dev)
+    else:
+        _mat(out, "out")
+        _on(out, "out", dev)
+        if out.shape != (M, N):
+            raise ValueError(f"out has shape {tuple(out.shape)}, expected {(M, N)}")
+    if residual is not None:
+        _mat(residual, "residual")
+        _on(residual, "residual", dev)
+        if residual.shape != (M, N) or _ld(residual) != _ld(out):
+            raise ValueError("residual must match out in shape and row stride")
+    if out.numel():
+        _call(dev, "dd_gemm_i8", _p(a), _ld(a), _p(a_scales), _p(b), _ld(b), _p(b_scales),
+              _p(residual), _p(out), _ld(out), M, N, K)
+    return out
+
+
+def gemm_int8_wgrad(codes, scales, dy, out=None):
+    """``dequantize(codes, scales).T @ dy``: the weight gradient [M, N] of a
+    linear layer from its input, kept as codes [T, M], and the gradient dy
+    [T, N] of its output; M and N multiples of 8."""
+    _code_matrix(codes, "codes")
+    dev, (T, M) = codes.device, codes.shape
+    _vec(scales, "scales", T, torch.float32, dev)
+    _mat(dy, "dy")
+    _on(dy, "dy", dev)
+    N = dy.shape[1]
+    if dy.shape[0] != T:
+        raise ValueError(f"codes have {T} rows, dy has {dy.shape[0]}")
+    if M % 8 or N % 8:
+        raise ValueError(f"the columns of codes and dy must be multiples of 8 (got {M} and {N})")
+    if out is None:
+        out = torch.empty((M, N), dtype=torch.bfloat16, device=dev)
+    else:
+        _mat(out, "out")
+        _on(out, "out", dev)
+        if out.shape != (M, N):
+            raise ValueError(f"out has shape {tuple(out.shape)}, expected {(M, N)}")
+    if not T:
+        return out.zero_()
+    if out.numel():
+        need = lib().dd_gemm_i8_wgrad_workspace_bytes(T, M, N)
+        ws = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
+        _call(dev, "dd_gemm_i8_wgrad", _p(codes), _ld(codes), _p(scales), _p(dy), _ld(dy),
+              _p(out), _ld(out), T, M, N, _p(ws), need)
+    return out

@@ -1,7 +1,7 @@
 """Build ``libdd_attn.so`` in-tree for gfx950 with hipcc.
 
 The HIP sources (``csrc/*.hip``) are compiled for gfx950 only; the C ABI and
-its validation (``csrc/dd_api.cpp``) is plain C++ compiled with g++.  Objects
+its validation (``csrc/dd_api*.cpp``) is plain C++ compiled with g++.  Objects
 go to ``_build/`` at the repository root; the library lands next to this file.
 
     python -m paper_2405_13226_amd.build
@@ -22,7 +22,8 @@ LIB = os.path.join(PKG, "libdd_attn.so")
 
 ARCH = "gfx950"
 HIP_SOURCES = ["dd_fwd.hip", "dd_bwd.hip", "dd_dkdv.hip", "dd_bwd_short.hip", "dd_prof.hip",
-               "dd_rope.hip", "dd_noalloc.hip", "dd_gemm.hip", "dd_block.hip"]
+               "dd_rope.hip", "dd_noalloc.hip", "dd_gemm.hip", "dd_block.hip", "dd_rms.hip",
+               "dd_gemm_i8.hip", "dd_wgrad_i8.hip"]
 # Extra flags per source.  The D = 128 dK/dV kernel, the one-kernel
 # short-row backward and the GEMM are scheduled for instruction-level
 # parallelism (measured: dK/dV ~6% faster at L = 8192, neutral at L = 256;
@@ -31,7 +32,7 @@ HIP_SOURCES = ["dd_fwd.hip", "dd_bwd.hip", "dd_dkdv.hip", "dd_bwd_short.hip", "d
 # faster for every other kernel.
 _ILP = ["-mllvm", "-amdgpu-sched-strategy=max-ilp"]
 HIP_SOURCE_FLAGS = {"dd_dkdv.hip": _ILP, "dd_bwd_short.hip": _ILP, "dd_gemm.hip": _ILP}
-CXX_SOURCES = ["dd_api.cpp"]
+CXX_SOURCES = ["dd_api.cpp", "dd_api8.cpp"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 # Packed fp32 VALU forms are disabled for all device code.
 HIP_FLAGS = ["-O3", "-std=c++17", f"--offload-arch={ARCH}", "-fPIC",

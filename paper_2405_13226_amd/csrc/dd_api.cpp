@@ -5,34 +5,20 @@
 // dd_bwd.hip behind the internal interface of dd_internal.h.  Every check
 // runs before any launch, so an invalid call leaves all outputs untouched.
 #include "dd_attn.h"
+#include "dd_check.hpp"
 #include "dd_internal.h"
 
 #include <cmath>
 #include <cstdint>
 #include <initializer_list>
 
+using namespace dd::check;
+
 namespace {
 
 // Bound on B * H * ceil(L / 128): (2^23 - 8) workgroups of 512 work-items
 // stay below 2^32 work-items.
 constexpr long long kMaxBlocks = (1LL << 23) - 8;
-
-struct Range {
-    uintptr_t lo, hi;  // [lo, hi)
-};
-
-Range range_of(const void *p, size_t bytes)
-{
-    uintptr_t a = reinterpret_cast<uintptr_t>(p);
-    return Range{a, a + bytes};
-}
-
-bool overlaps(Range a, Range b) { return a.lo < b.hi && b.lo < a.hi; }
-
-bool aligned(const void *p, uintptr_t n)
-{
-    return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0;
-}
 
 int check_shape(int B, int L, int H, int D)
 {

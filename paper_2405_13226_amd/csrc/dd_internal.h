@@ -125,6 +125,66 @@ struct TransposeArgs {
 };
 int launch_transpose(const TransposeArgs &a);
 
+// Rows of a bf16 matrix through the norm or into codes (dd_rms.hip):
+//   w == NULL            codes of X's rows
+//   w, Q == NULL         RMSNorm of X (+ R) in bf16
+//   w and Q              RMSNorm of X (+ R) as codes
+// H receives X + R where R is given.
+struct RowArgs {
+    const void *X, *R, *w;
+    void *H, *Y, *Q;
+    float *scales, *rstd;
+    long long ldx, ldr, ldq;  // row strides in elements (H and Y: d)
+    int rows, d;
+    float eps;
+    void *stream;
+};
+int launch_rows(const RowArgs &a);
+
+struct DequantizeArgs {
+    const void *Q;
+    const float *scales;
+    void *Y;
+    long long ldq, ldy;
+    int rows, d;
+    void *stream;
+};
+int launch_dequantize(const DequantizeArgs &a);
+
+struct RmsBackArgs {
+    const void *H, *w, *dY, *dRes;
+    const float *rstd;
+    void *dX, *dw, *workspace;
+    int rows, d;
+    void *stream;
+};
+size_t rmsnorm_workspace_bytes(int rows, int d);
+int launch_rmsnorm_bwd(const RmsBackArgs &a);
+
+// C = (A sa) (B sb)^T (+ R) from int8 codes A [M][K], B [N][K] (dd_gemm_i8.hip).
+struct GemmI8Args {
+    const void *A, *B, *R;
+    const float *sa, *sb;
+    void *C;
+    long long lda, ldb, ldc;  // R has ldc
+    int M, N, K;
+    void *stream;
+};
+int launch_gemm_i8(const GemmI8Args &a);
+
+// dW [M][N] = X^T dY with X = bf16(scales Q), Q [T][M] int8, dY [T][N] bf16
+// (dd_wgrad_i8.hip).
+struct WgradI8Args {
+    const void *Q, *dY;
+    const float *scales;
+    void *dW, *workspace;
+    long long ldq, ldy, ldw;
+    int T, M, N;
+    void *stream;
+};
+size_t wgrad_i8_workspace_bytes(int T, int M, int N);
+int launch_wgrad_i8(const WgradI8Args &a);
+
 // Both return a dd_status value (DD_OK or DD_ERR_HIP).
 int launch_fwd(const FwdArgs &a);
 int launch_bwd(const BwdArgs &a);

@@ -1,0 +1,551 @@
+// dd_rms.hip -- rows into 8 bits: RMSNorm (with the residual's addition, its
+// output in bf16 or as codes, and its backward), and the codes of any matrix's
+// rows and back.  All are passes over [rows, d] tensors with fp32 arithmetic,
+// bound by HBM, or at a few rows by latency.
+//
+// RMSNorm:   h = bf16(x + r), rstd = 1 / sqrt(mean(h^2) + eps), y = h rstd w.
+// Codes:     a row z with largest magnitude A is held as int8 codes
+//            q = the integer nearest to 127 z / A (ties to even) and one fp32
+//            scale; the row's values are scale q.
+// For the norm's codes z = h w: rstd cancels out of the codes, so they need no
+// sum over the row, and h w is exact in fp32 (two 8-bit significands).  The
+// scale is A rstd / 127.
+//
+// Backward, with xh = h rstd and g = dy w:
+//            dx = rstd (g - xh mean(g xh)) (+ dres),  dw = sum over rows dy xh.
+#include "dd_device.hpp"
+#include "dd_internal.h"
+#include "dd_launch.hpp"
+#include "dd_attn.h"
+
+#include <algorithm>
+
+namespace dd {
+
+namespace {
+
+enum RowKind { kNorm, kNormCodes, kCodes };
+
+// Row `row` of a matrix belongs to TPR threads of a workgroup: one wave (four
+// rows per workgroup), or a whole workgroup of 256 or 1024 threads.  Thread t
+// holds the 8-element chunks t, t + TPR, ... of it, CH of them.
+template <int TPR>
+struct RowThreads {
+    static constexpr int THREADS = TPR == 64 ? 256 : TPR;
+    static constexpr int ROWS = THREADS / TPR;
+    static constexpr int WAVES = TPR / 64;  // per row
+};
+
+// Eight elements from `p`, of which `left` (or more) exist; zeros for the
+// others.  VEC: left is a multiple of 8 and p 16-byte aligned.
+template <bool VEC>
+__device__ __forceinline__ void load8(const uint16_t *p, int left, float (&f)[8])
+{
+    if constexpr (VEC) {
+        u32x4 u = {0u, 0u, 0u, 0u};
+        if (left > 0)
+            u = *reinterpret_cast<const u32x4 *>(p);
+        unpack8(u, f);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            f[i] = i < left ? __uint_as_float(static_cast<uint32_t>(p[i]) << 16) : 0.f;
+    }
+}
+
+template <bool VEC>
+__device__ __forceinline__ void store8(uint16_t *p, int left, const float (&f)[8])
+{
+    if constexpr (VEC) {
+        if (left > 0)
+            *reinterpret_cast<u32x4 *>(p) = pack8f(f);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < left)
+                p[i] = __builtin_bit_cast(uint16_t, static_cast<__bf16>(f[i]));
+    }
+}
+
+// The sum of s and the maximum of m over a row's threads, in each of them.
+// `red` is LDS of 2 x WAVES floats and as many words; `flip` alternates from
+// row to row, so that one barrier a row is enough.
+template <int TPR>
+__device__ __forceinline__ void row_reduce(float &s, uint32_t &m, float *red, int flip)
+{
+    constexpr int W = RowThreads<TPR>::WAVES;
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) {
+        s += __shfl_xor(s, o);
+        m = max(m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), o)));
+    }
+    if constexpr (W > 1) {
+        float *rs = red + flip * 2 * W;
+        uint32_t *rm = reinterpret_cast<uint32_t *>(rs + W);
+        if ((threadIdx.x & 63) == 0) {
+            rs[threadIdx.x >> 6] = s;
+            rm[threadIdx.x >> 6] = m;
+        }
+        __syncthreads();
+        s = rs[0];
+        m = rm[0];
+#pragma unroll
+        for (int i = 1; i < W; ++i) {
+            s += rs[i];
+            m = max(m, rm[i]);
+        }
+    }
+}
+
+// How a row's codes are formed from its largest magnitude: z is multiplied by
+// a power of two that keeps every step below normal and finite (1 for ordinary
+// rows), then by 127 / A.  A row of zeros has codes and scale 0; one that
+// holds a NaN or an infinity has codes 0 and a NaN scale, so that all its
+// values are NaN.
+struct CodeScale {
+    float fit, amax, inv, scale;
+
+    __device__ __forceinline__ explicit CodeScale(uint32_t amax_bits)
+    {
+        const float a = __uint_as_float(amax_bits);
+        fit = a < 0x1p-60f ? 0x1p64f : a > 0x1p60f ? 0x1p-64f : 1.0f;
+        amax = a * fit;
+        inv = 127.0f / amax;
+        scale = a / 127.0f;
+        if (amax_bits == 0 || amax_bits >= 0x7f800000u) {
+            fit = inv = 0.0f;
+            amax = 1.0f;
+            scale = amax_bits == 0 ? 0.0f : __uint_as_float(0x7fc00000u);
+        }
+    }
+    __device__ __forceinline__ bool usable() const { return inv != 0.0f; }
+    // The nearest integer to 127 z / amax, ties to even, exactly: the rounded
+    // product of the reciprocal is at most one off, and 127 z - q amax is
+    // exact in fp32 (z and amax have 16 significant bits at most, q and 127
+    // seven), so it tells which side of the border z is on.
+    __device__ __forceinline__ int code(float z) const
+    {
+        z *= fit;
+        float q = rintf(z * inv);
+        const float r = fmaf(-q, amax, 127.0f * z), r2 = 2.0f * fabsf(r);
+        const int qi = static_cast<int>(q);
+        const bool step = r2 > amax || (r2 == amax && (qi & 1));
+        return qi + (step ? (r > 0.f ? 1 : -1) : 0);
+    }
+};
+
+__device__ __forceinline__ uint32_t abs_bits(float x) { return __float_as_uint(x) & 0x7fffffffu; }
+
+template <bool VEC>
+__device__ __forceinline__ void store_codes(int8_t *p, int left, const float (&z)[8],
+                                            const CodeScale &cs, bool usable)
+{
+    int c[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        c[i] = usable ? cs.code(z[i]) : 0;
+    if constexpr (VEC) {
+        u32x2 u;
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            u[i] = (c[4 * i] & 255) | (c[4 * i + 1] & 255) << 8 | (c[4 * i + 2] & 255) << 16 |
+                   static_cast<uint32_t>(c[4 * i + 3]) << 24;
+        if (left > 0)
+            *reinterpret_cast<u32x2 *>(p) = u;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < left)
+                p[i] = static_cast<int8_t>(c[i]);
+    }
+}
+
+}  // namespace
+
+// One pass over the rows: the row stays in registers from its load to its
+// stores.  H and Y have a row stride of d.
+struct RowOperands {
+    const uint16_t *X, *R, *W;
+    uint16_t *H, *Y;
+    int8_t *Q;
+    float *scales, *rstd;
+    long long ldx, ldr, ldq;
+    int rows, d;
+    float eps;
+};
+
+template <int TPR, int CH, bool VEC, int KIND>
+__global__ void __launch_bounds__(RowThreads<TPR>::THREADS)
+row_kernel(RowOperands op)
+{
+    using T = RowThreads<TPR>;
+    __shared__ float red[T::WAVES > 1 ? 4 * T::WAVES : 1];
+    const int t = threadIdx.x % TPR, d = op.d;
+    const int step = static_cast<int>(gridDim.x) * T::ROWS;
+    int flip = 0;
+    for (long long row = static_cast<long long>(blockIdx.x) * T::ROWS + threadIdx.x / TPR;
+         row < op.rows; row += step, flip ^= 1) {
+        float v[CH][8];
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            const int col = (t + TPR * c) * 8;
+            load8<VEC>(op.X + row * op.ldx + col, d - col, v[c]);
+        }
+        if (KIND != kCodes && op.R != nullptr) {
+#pragma unroll
+            for (int c = 0; c < CH; ++c) {
+                const int col = (t + TPR * c) * 8;
+                float r[8];
+                load8<VEC>(op.R + row * op.ldr + col, d - col, r);
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    v[c][i] = static_cast<float>(static_cast<__bf16>(v[c][i] + r[i]));
+                store8<VEC>(op.H + row * d + col, d - col, v[c]);
+            }
+        }
+        float s = 0.f;
+        uint32_t m = 0;
+        float w[CH][8];
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            const int col = (t + TPR * c) * 8;
+            if constexpr (KIND != kCodes)
+                load8<VEC>(op.W + col, d - col, w[c]);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                if constexpr (KIND != kCodes)
+                    s += v[c][i] * v[c][i];
+                if constexpr (KIND == kNormCodes)
+                    v[c][i] *= w[c][i];
+                if constexpr (KIND != kNorm)
+                    m = max(m, abs_bits(v[c][i]));
+            }
+        }
+        row_reduce<TPR>(s, m, red, flip);
+        float rstd = 1.f;
+        if constexpr (KIND != kCodes) {
+            rstd = 1.0f / sqrtf(s / d + op.eps);
+            if (t == 0)
+                op.rstd[row] = rstd;
+        }
+        if constexpr (KIND == kNorm) {
+#pragma unroll
+            for (int c = 0; c < CH; ++c) {
+                const int col = (t + TPR * c) * 8;
+                float y[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    y[i] = v[c][i] * rstd * w[c][i];
+                store8<VEC>(op.Y + row * d + col, d - col, y);
+            }
+        } else {
+            const CodeScale cs(m);
+            if (t == 0)
+                op.scales[row] = KIND == kCodes ? cs.scale
+                                 : cs.usable()  ? __uint_as_float(m) * rstd / 127.0f
+                                                : cs.scale;
+#pragma unroll
+            for (int c = 0; c < CH; ++c) {
+                const int col = (t + TPR * c) * 8;
+                store_codes<VEC>(op.Q + row * op.ldq + col, d - col, v[c], cs, cs.usable());
+            }
+        }
+    }
+}
+
+// Codes to bf16: one wave per row and 2048 columns, 8 codes per lane and load.
+template <bool VEC>
+__global__ void __launch_bounds__(256)
+dequantize_kernel(const int8_t *__restrict__ Q, long long ldq, const float *__restrict__ scales,
+                  uint16_t *__restrict__ Y, long long ldy, int rows, int d)
+{
+    const int lane = threadIdx.x & 63;
+    const int step = static_cast<int>(gridDim.x) * 4;
+    for (long long row = static_cast<long long>(blockIdx.x) * 4 + (threadIdx.x >> 6); row < rows;
+         row += step) {
+        const float s = scales[row];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            const int col = static_cast<int>(blockIdx.y) * 2048 + (lane + 64 * c) * 8;
+            const int left = d - col;
+            const int8_t *q = Q + row * ldq + col;
+            float f[8];
+            if constexpr (VEC) {
+                u32x2 u = {0u, 0u};
+                if (left > 0)
+                    u = *reinterpret_cast<const u32x2 *>(q);
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    f[i] = s * static_cast<float>(static_cast<int8_t>(u[i >> 2] >> 8 * (i & 3)));
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    f[i] = i < left ? s * static_cast<float>(q[i]) : 0.f;
+            }
+            store8<VEC>(Y + row * ldy + col, left, f);
+        }
+    }
+}
+
+// Backward of rms_rows_per_wg rows per workgroup: dx of each, and their column
+// sums of dy xh into row blockIdx.x of an fp32 workspace.
+struct RmsBackOperands {
+    const uint16_t *H, *W, *dY, *dRes;
+    const float *rstd;
+    uint16_t *dX;
+    float *part;
+    int rows, d, per_wg;
+};
+
+template <int TPR, int CH, bool VEC>
+__global__ void __launch_bounds__(RowThreads<TPR>::THREADS)
+rms_bwd_kernel(RmsBackOperands op)
+{
+    using T = RowThreads<TPR>;
+    constexpr int COLS = TPR * CH * 8;
+    // TPR = 64: the four waves' column sums; else the reductions.
+    __shared__ float red[T::ROWS > 1 ? T::ROWS * COLS : 4 * T::WAVES];
+    const int t = threadIdx.x % TPR, d = op.d;
+    float w[CH][8], dw[CH][8];
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+        const int col = (t + TPR * c) * 8;
+        load8<VEC>(op.W + col, d - col, w[c]);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            dw[c][i] = 0.f;
+    }
+    const long long row0 = static_cast<long long>(blockIdx.x) * op.per_wg;
+    const int n = static_cast<int>(min(static_cast<long long>(op.per_wg), op.rows - row0));
+    int flip = 0;
+    for (int rr = threadIdx.x / TPR; rr < n; rr += T::ROWS, flip ^= 1) {
+        const long long row = row0 + rr, base = row * d;
+        const float rstd = op.rstd[row];
+        float xh[CH][8], g[CH][8];
+        float s = 0.f;
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            const int col = (t + TPR * c) * 8;
+            load8<VEC>(op.H + base + col, d - col, xh[c]);
+            load8<VEC>(op.dY + base + col, d - col, g[c]);
+        }
+#pragma unroll
+        for (int c = 0; c < CH; ++c)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                xh[c][i] *= rstd;
+                dw[c][i] += g[c][i] * xh[c][i];
+                g[c][i] *= w[c][i];
+                s += g[c][i] * xh[c][i];
+            }
+        uint32_t none = 0;
+        row_reduce<TPR>(s, none, red, flip);
+        const float mean = s / d;
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            const int col = (t + TPR * c) * 8;
+            float out[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                out[i] = rstd * (g[c][i] - xh[c][i] * mean);
+            if (op.dRes != nullptr) {
+                float r[8];
+                load8<VEC>(op.dRes + base + col, d - col, r);
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    out[i] += r[i];
+            }
+            store8<VEC>(op.dX + base + col, d - col, out);
+        }
+    }
+    float *dst = op.part + static_cast<long long>(blockIdx.x) * d;
+    if constexpr (T::ROWS > 1) {
+        float *mine = red + threadIdx.x / TPR * COLS;
+#pragma unroll
+        for (int c = 0; c < CH; ++c)
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                mine[(t + TPR * c) * 8 + i] = dw[c][i];
+        __syncthreads();
+        for (int col = threadIdx.x; col < d; col += T::THREADS) {
+            float sum = 0.f;
+#pragma unroll
+            for (int k = 0; k < T::ROWS; ++k)
+                sum += red[k * COLS + col];
+            dst[col] = sum;
+        }
+    } else {
+#pragma unroll
+        for (int c = 0; c < CH; ++c)
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if ((t + TPR * c) * 8 + i < d)
+                    dst[(t + TPR * c) * 8 + i] = dw[c][i];
+    }
+}
+
+// Sums of the columns of `part` [n][d]: 16 waves sum 64 columns over the rows
+// of chunk blockIdx.y (`per` rows); the result goes to `sums` (fp32, one row
+// per chunk), or rounded to bf16 to `dw`.
+__global__ void __launch_bounds__(1024)
+rms_columns_kernel(const float *__restrict__ part, int n, int per, int d, float *__restrict__ sums,
+                   uint16_t *__restrict__ dw)
+{
+    __shared__ float red[16][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int col = static_cast<int>(blockIdx.x) * 64 + lane;
+    const int p0 = static_cast<int>(blockIdx.y) * per, p1 = min(p0 + per, n);
+    float s = 0.f;
+    if (col < d) {
+#pragma unroll 4
+        for (int p = p0 + wave; p < p1; p += 16)
+            s += part[static_cast<long long>(p) * d + col];
+    }
+    red[wave][lane] = s;
+    __syncthreads();
+    if (wave == 0 && col < d) {
+        float sum = 0.f;
+#pragma unroll
+        for (int w = 0; w < 16; ++w)
+            sum += red[w][lane];
+        if (dw != nullptr)
+            dw[col] = __builtin_bit_cast(uint16_t, static_cast<__bf16>(sum));
+        else
+            sums[static_cast<long long>(blockIdx.y) * d + col] = sum;
+    }
+}
+
+namespace {
+
+// Partial rows of the backward that one launch sums; more go through
+// kRmsChunks chunk sums.
+constexpr int kRmsOneStage = 256, kRmsChunks = 32;
+
+int rms_rows_per_wg(int rows)
+{
+    const long long wgs = (rows <= 16384 ? 1 : rows <= 32768 ? 2 : 4) * kRmsOneStage;
+    const int per = static_cast<int>((rows + wgs - 1) / wgs + 3) / 4 * 4;
+    return std::max(per, 8);
+}
+
+bool aligned16(std::initializer_list<const void *> ps)
+{
+    for (const void *p : ps)
+        if (reinterpret_cast<uintptr_t>(p) & 15)
+            return false;
+    return true;
+}
+
+// Threads per row and chunks per thread for rows of d elements.
+struct RowShape {
+    int tpr, ch;
+};
+
+RowShape row_shape(int rows, int d)
+{
+    const int tpr = d <= 2048 && (rows >= 512 || d <= 512) ? 64 : d <= 8192 ? 256 : 1024;
+    return RowShape{tpr, (d + 8 * tpr - 1) / (8 * tpr)};
+}
+
+// Calls f(IC<TPR>, IC<CH>) for the shape.
+template <typename F>
+auto with_shape(RowShape s, F f)
+{
+    if (s.tpr == 64)
+        return s.ch == 1   ? f(IC<64>{}, IC<1>{})
+               : s.ch == 2 ? f(IC<64>{}, IC<2>{})
+               : s.ch == 3 ? f(IC<64>{}, IC<3>{})
+                           : f(IC<64>{}, IC<4>{});
+    if (s.tpr == 256)
+        return s.ch == 1   ? f(IC<256>{}, IC<1>{})
+               : s.ch == 2 ? f(IC<256>{}, IC<2>{})
+               : s.ch == 3 ? f(IC<256>{}, IC<3>{})
+                           : f(IC<256>{}, IC<4>{});
+    return f(IC<1024>{}, IC<2>{});
+}
+
+// Workgroups of a grid over `n` units: below 2^20, the kernels walk further.
+unsigned grid_of(long long n) { return static_cast<unsigned>(std::min<long long>(n, 1 << 20)); }
+
+}  // namespace
+
+int launch_rows(const RowArgs &a)
+{
+    hipStream_t st = static_cast<hipStream_t>(a.stream);
+    const RowOperands op{static_cast<const uint16_t *>(a.X), static_cast<const uint16_t *>(a.R),
+                         static_cast<const uint16_t *>(a.w), static_cast<uint16_t *>(a.H),
+                         static_cast<uint16_t *>(a.Y),       static_cast<int8_t *>(a.Q),
+                         a.scales, a.rstd, a.ldx, a.ldr, a.ldq, a.rows, a.d, a.eps};
+    const bool vec = a.d % 8 == 0 && a.ldx % 8 == 0 && a.ldr % 8 == 0 && a.ldq % 8 == 0 &&
+                     aligned16({a.X, a.R, a.w, a.H, a.Y}) &&
+                     reinterpret_cast<uintptr_t>(a.Q) % 8 == 0;
+    const hipError_t e = with_shape(row_shape(a.rows, a.d), [&](auto tpr, auto ch) {
+        using T = RowThreads<decltype(tpr)::value>;
+        constexpr int TPR = decltype(tpr)::value, CH = decltype(ch)::value;
+        auto run = [&](auto kind) {
+            constexpr int K = decltype(kind)::value;
+            return launch_kernel(vec ? row_kernel<TPR, CH, true, K> : row_kernel<TPR, CH, false, K>,
+                                 dim3(grid_of((a.rows + T::ROWS - 1LL) / T::ROWS)),
+                                 dim3(T::THREADS), st, op);
+        };
+        return a.w == nullptr ? run(IC<kCodes>{}) : a.Q ? run(IC<kNormCodes>{}) : run(IC<kNorm>{});
+    });
+    return e == hipSuccess ? DD_OK : DD_ERR_HIP;
+}
+
+int launch_dequantize(const DequantizeArgs &a)
+{
+    const bool vec = a.d % 8 == 0 && a.ldq % 8 == 0 && a.ldy % 8 == 0 && aligned16({a.Y}) &&
+                     reinterpret_cast<uintptr_t>(a.Q) % 8 == 0;
+    const dim3 grid(grid_of((a.rows + 3LL) / 4), static_cast<unsigned>((a.d + 2047) / 2048));
+    const hipError_t e =
+        launch_kernel(vec ? dequantize_kernel<true> : dequantize_kernel<false>, grid, dim3(256),
+                      static_cast<hipStream_t>(a.stream), static_cast<const int8_t *>(a.Q), a.ldq,
+                      a.scales, static_cast<uint16_t *>(a.Y), a.ldy, a.rows, a.d);
+    return e == hipSuccess ? DD_OK : DD_ERR_HIP;
+}
+
+size_t rmsnorm_workspace_bytes(int rows, int d)
+{
+    const int per = rms_rows_per_wg(rows);
+    const long long parts = (rows + per - 1LL) / per;
+    return static_cast<size_t>(parts + kRmsChunks) * d * sizeof(float);
+}
+
+int launch_rmsnorm_bwd(const RmsBackArgs &a)
+{
+    hipStream_t st = static_cast<hipStream_t>(a.stream);
+    const int per = rms_rows_per_wg(a.rows), parts = static_cast<int>((a.rows + per - 1LL) / per);
+    auto *part = static_cast<float *>(a.workspace);
+    auto *dw = static_cast<uint16_t *>(a.dw);
+    const RmsBackOperands op{static_cast<const uint16_t *>(a.H), static_cast<const uint16_t *>(a.w),
+                             static_cast<const uint16_t *>(a.dY), static_cast<const uint16_t *>(a.dRes),
+                             a.rstd, static_cast<uint16_t *>(a.dX), part, a.rows, a.d, per};
+    const bool vec = a.d % 8 == 0 && aligned16({a.H, a.w, a.dY, a.dRes, a.dX});
+    hipError_t e = with_shape(row_shape(a.rows, a.d), [&](auto tpr, auto ch) {
+        constexpr int TPR = decltype(tpr)::value, CH = decltype(ch)::value;
+        return launch_kernel(vec ? rms_bwd_kernel<TPR, CH, true> : rms_bwd_kernel<TPR, CH, false>,
+                             dim3(static_cast<unsigned>(parts)), dim3(RowThreads<TPR>::THREADS), st,
+                             op);
+    });
+    if (e != hipSuccess)
+        return DD_ERR_HIP;
+    const unsigned cols = static_cast<unsigned>((a.d + 63) / 64);
+    const float *from = part;
+    int n = parts;
+    if (parts > kRmsOneStage) {
+        float *sums = part + static_cast<long long>(parts) * a.d;
+        const int rows = (parts + kRmsChunks - 1) / kRmsChunks;
+        e = launch_kernel(rms_columns_kernel, dim3(cols, kRmsChunks), dim3(1024), st, from, parts,
+                          rows, a.d, sums, nullptr);
+        if (e != hipSuccess)
+            return DD_ERR_HIP;
+        from = sums;
+        n = kRmsChunks;
+    }
+    e = launch_kernel(rms_columns_kernel, dim3(cols, 1), dim3(1024), st, from, n, n, a.d, nullptr,
+                      dw);
+    return e == hipSuccess ? DD_OK : DD_ERR_HIP;
+}
+
+}  // namespace dd

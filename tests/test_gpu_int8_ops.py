@@ -1,0 +1,431 @@
+"""GPU parity of the 8-bit operators (RMSNorm, rows as codes, int8 products,
+weight gradients from codes) against their float64 definitions.
+
+Tolerances, elementwise, from the roundings on the way (u = 2^-24 is the
+fp32 rounding, 2^-8 the bf16 one, both relative to the value):
+
+* h, codes, the scales of ``quantize`` and the values of ``dequantize`` are
+  exact: equal to the definition.
+* rstd: a sum of d squares of which a thread adds at most 32 and the rest is a
+  tree of at most ten levels and 15 waves: 57 u of a positive sum, halved by
+  the root, and four roundings after it: 34 u.  The norm's scales: two more.
+* y: 2^-8 and 37 u.
+* dx: 2^-8 of the result and (57 + 34 + 10) u of the magnitudes added.
+* dw of the norm: 2^-8 and the depth of its sum (rows of a wave, waves,
+  partial rows: below 128 at these sizes) u of the magnitudes.
+* int8 products: the sum is exact; its conversion, two products and the
+  residual's addition: 2^-8 and 4 u of the magnitudes.
+* weight gradients: 2^-8 and T u of the magnitudes (a sum of T products), and
+  relative L2 <= 3e-3 (the rounding of the result alone: 1.7e-3).
+"""
+import numpy as np
+import pytest
+import torch
+
+from paper_2405_13226_amd import block_ops as ops
+
+import int8_oracle as O
+from int8_oracle import bf16, f64
+from parity import log, rel_l2
+
+pytestmark = pytest.mark.gpu
+U, B = 2.0 ** -24, 2.0 ** -8
+EPS = 1e-5
+
+# every form of a row: one wave of 1-4 chunks per lane, a workgroup of 256
+# with 1-4, one of 1024; whole and ragged, one row to several workgroups
+ROWS = [(1, 1), (3, 7), (2, 8), (1, 64), (5, 100), (9, 512), (2, 520), (1, 2048), (700, 2048),
+        (601, 1416), (513, 1000), (3, 1021), (515, 1029), (2, 2056), (7, 4100), (3, 5632),
+        (2, 8192), (2, 8200), (3, 10001), (2, 16384)]
+
+
+def close(got, ref, tol, what):
+    got, ref = np.asarray(got, dtype=np.float64), np.asarray(ref, dtype=np.float64)
+    assert got.shape == ref.shape, what
+    off = np.abs(got - ref) - tol
+    assert np.isfinite(got).all(), what
+    assert (off <= 1e-37).all(), (what, float(off.max()), int((off > 0).sum()))
+
+
+def norm_case(rows, d, seed, residual):
+    x = bf16((rows, d), seed, 2.0)
+    r = bf16((rows, d), seed + 1) if residual else None
+    w = (1 + 0.2 * bf16((d,), seed + 2).float()).to(torch.bfloat16)
+    return x, r, w, (O.add(x, r) if residual else x)
+
+
+@pytest.mark.parametrize("residual", [False, True])
+@pytest.mark.parametrize("rows,d", ROWS)
+def test_rms_norm(cuda, rows, d, residual):
+    log(f"rms_norm {rows} x {d} residual={residual}")
+    x, r, w, h = norm_case(rows, d, rows + d, residual)
+    rg = None if r is None else r.to(cuda)
+    y, hg, rstd = ops.rms_norm(x.to(cuda), w.to(cuda), residual=rg, eps=EPS)
+    assert torch.equal(hg.cpu(), h)
+    ref = O.rstd(f64(h), EPS)
+    close(rstd.cpu().numpy(), ref, 34 * U * ref, "rstd")
+    want = f64(h) * ref[:, None] * f64(w)
+    close(f64(y), want, (B + 37 * U) * np.abs(want), "y")
+    codes, scales, hg, rstd8 = ops.rms_norm_int8(x.to(cuda), w.to(cuda), residual=rg, eps=EPS)
+    assert torch.equal(hg.cpu(), h) and torch.equal(rstd8, rstd)
+    q, top = O.codes(f64(h) * f64(w))
+    assert np.array_equal(codes.cpu().numpy(), q)
+    close(scales.cpu().numpy(), top * ref / 127, 36 * U * top * ref / 127, "scales")
+
+
+@pytest.mark.parametrize("rows,d", ROWS)
+def test_quantize_and_back(cuda, rows, d):
+    log(f"quantize {rows} x {d}")
+    x = bf16((rows, d), d)
+    codes, scales = ops.quantize(x.to(cuda))
+    q, top = O.codes(f64(x))
+    assert np.array_equal(codes.cpu().numpy(), q)
+    assert np.array_equal(scales.cpu().numpy(), top.astype(np.float32) / np.float32(127))
+    back = ops.dequantize(codes, scales)
+    want = (torch.from_numpy(q).float() * scales.cpu()[:, None]).to(torch.bfloat16)
+    assert torch.equal(back.cpu(), want)
+
+
+def test_codes_at_the_borders(cuda):
+    # 127 z / 254 = z / 2: every odd z is on a border and goes to the even code
+    z = torch.arange(-254, 255, dtype=torch.float32)
+    rows = [z, z * 2.0 ** -40, z * 2.0 ** 100, z * 2.0 ** -135]  # the last holds subnormals
+    # every bf16 value of the top eight binades, under maxima of all significands
+    bits = torch.arange(0x3f80 - 8 * 128, 0x3f80, dtype=torch.int32).to(torch.int16)
+    ladder = bits.view(torch.bfloat16).float()
+    for k in range(128, 256, 7):
+        rows.append(torch.cat([ladder, torch.tensor([k / 128.0])]))
+    for i, row in enumerate(rows):
+        x = row.to(torch.bfloat16)[None]
+        codes, scales = ops.quantize(x.to(cuda))
+        q, top = O.codes(f64(x))
+        assert np.array_equal(codes.cpu().numpy(), q), i
+        assert np.array_equal(scales.cpu().numpy(), top.astype(np.float32) / np.float32(127)), i
+
+
+@pytest.mark.parametrize("d", [64, 1416, 5632])
+def test_rows_that_are_zero_or_not_finite(cuda, d):
+    x = bf16((7, d), 3)
+    x[1] = 0
+    x[2, d // 2] = float("nan")
+    x[4, 0] = float("inf")
+    x[5, d - 1] = -float("inf")
+    bad = [2, 4, 5]
+    w = torch.ones(d, dtype=torch.bfloat16)
+    codes, scales = ops.quantize(x.to(cuda))
+    c8, s8, _, _ = ops.rms_norm_int8(x.to(cuda), w.to(cuda), eps=EPS)
+    good = [i for i in range(7) if i not in bad]
+    for c, s in ((codes, scales), (c8, s8)):
+        c, s = c.cpu(), s.cpu()
+        assert torch.isnan(s[bad]).all() and not c[bad].any()
+        assert s[1] == 0 and not c[1].any()
+        assert torch.isfinite(s[good]).all()
+        assert np.array_equal(c[good].numpy(), O.codes(f64(x[good]))[0])
+        v = ops.dequantize(c.to(cuda), s.to(cuda)).float().cpu()
+        assert torch.isnan(v[bad]).all() and torch.isfinite(v[good]).all()
+    y, _, rstd = ops.rms_norm(x.to(cuda), w.to(cuda), eps=EPS)
+    y = y.float().cpu()
+    assert torch.isfinite(y[good]).all() and not y[1].any()
+    assert abs(float(rstd[1]) * EPS ** 0.5 - 1) < 1e-6
+    assert torch.isnan(y[2]).all()
+
+
+@pytest.mark.parametrize("off", [1, 8])
+def test_rows_of_wider_matrices(cuda, off):
+    # column slices, aligned and not, and a longer output around the values
+    rows, d, wide = 37, 1000, 1100
+    x, r = bf16((rows, wide), 1).to(cuda), bf16((rows, wide + 8), 2).to(cuda)
+    w = bf16((d,), 3).to(cuda)
+    xs, rs = x[:, off:off + d], r[:, 2 * off:2 * off + d]
+    a = ops.rms_norm_int8(xs, w, residual=rs)
+    b = ops.rms_norm_int8(xs.contiguous(), w, residual=rs.contiguous())
+    for s, t in zip(a, b):
+        assert torch.equal(s, t)
+    for s, t in zip(ops.rms_norm(xs, w, rs), ops.rms_norm(xs.contiguous(), w, rs.contiguous())):
+        assert torch.equal(s, t)
+    q, s = ops.quantize(xs)
+    q2, s2 = ops.quantize(xs.contiguous())
+    assert torch.equal(q, q2) and torch.equal(s, s2)
+    out = torch.full((rows + 2, wide), 7.0, dtype=torch.bfloat16, device=cuda)
+    into = out[1:-1, off:off + d]
+    ops.dequantize(q, s, out=into)
+    assert torch.equal(into, ops.dequantize(q, s))
+    keep = torch.ones_like(out, dtype=torch.bool)
+    keep[1:-1, off:off + d] = False
+    assert (out[keep] == 7.0).all()
+
+
+@pytest.mark.parametrize("dres", [False, True])
+@pytest.mark.parametrize("rows,d", ROWS + [(5000, 64), (17000, 520), (33000, 128)])
+def test_rms_norm_backward(cuda, rows, d, dres):
+    log(f"rms_norm_backward {rows} x {d} dres={dres}")
+    h, dy = bf16((rows, d), 5, 2.0), bf16((rows, d), 6)
+    w = (1 + 0.2 * bf16((d,), 7).float()).to(torch.bfloat16)
+    r = bf16((rows, d), 8) if dres else None
+    rs = torch.from_numpy(O.rstd(f64(h), EPS)).float()
+    dx, dw = ops.rms_norm_backward(h.to(cuda), w.to(cuda), rs.to(cuda), dy.to(cuda),
+                                   None if r is None else r.to(cuda))
+    rx, rw, mag = O.norm_backward(f64(h), f64(w), f64(rs), f64(dy), None if r is None else f64(r))
+    close(f64(dx), rx, B * np.abs(rx) + 101 * U * mag, "dx")
+    sums = np.abs(f64(dy) * f64(h) * f64(rs)[:, None]).sum(0)
+    close(f64(dw), rw, B * np.abs(rw) + 128 * U * sums, "dw")
+
+
+def test_rms_norm_backward_is_the_gradient(cuda):
+    # against differences of the norm itself in float64
+    rows, d = 3, 40
+    x, w, dy = (f64(bf16(s, i)) for i, s in enumerate([(rows, d), (d,), (rows, d)]))
+    w = f64(round_to_bf16(1 + 0.1 * w))
+    f = lambda x, w: (dy * (x * O.rstd(x, EPS)[:, None] * w)).sum()
+    t = lambda a: torch.from_numpy(a).to(torch.bfloat16).to(cuda)
+    rs = torch.from_numpy(O.rstd(x, EPS)).float().to(cuda)
+    dx, dw = ops.rms_norm_backward(t(x), t(w), rs, t(dy))
+    e = 1e-5
+    for i, j in [(0, 0), (1, 7), (2, 39)]:
+        p, m = x.copy(), x.copy()
+        p[i, j] += e
+        m[i, j] -= e
+        num = (f(p, w) - f(m, w)) / (2 * e)
+        # the difference: e^2 times a third derivative of order one
+        assert abs(f64(dx)[i, j] - num) <= B * abs(num) + 1e-5
+        p, m = w.copy(), w.copy()
+        p[j] += e
+        m[j] -= e
+        num = (f(x, p) - f(x, m)) / (2 * e)
+        assert abs(f64(dw)[j] - num) <= B * abs(num) + 1e-5
+
+
+def round_to_bf16(a):
+    return torch.from_numpy(a).to(torch.bfloat16)
+
+
+def random_codes(rows, d, seed, dev, full=False):
+    g = torch.Generator(device="cpu").manual_seed(seed)
+    q = torch.randint(-128 if full else -127, 128, (rows, d), generator=g).to(torch.int8)
+    s = torch.rand(rows, generator=g) * 0.02 + 1e-3
+    return q.to(dev), s.to(dev)
+
+
+def check_product(q, s, p, t, r, c):
+    ref = O.product(q.cpu().numpy(), f64(s), p.cpu().numpy(), f64(t))
+    mag = np.abs(ref)
+    if r is not None:
+        ref, mag = ref + f64(r), mag + np.abs(f64(r))
+    close(f64(c), ref, B * np.abs(ref) + 4 * U * mag, "c")
+
+
+SIZES = [(1, 1, 16), (1, 48, 64), (1, 1000, 2048), (2, 17, 80), (3, 5, 16), (5, 300, 1040),
+         (16, 64, 128), (16, 2000, 2048), (17, 33, 48), (31, 640, 512), (33, 257, 4096),
+         (64, 64, 64), (64, 1000, 528), (65, 63, 144), (100, 128, 128), (127, 129, 256),
+         (128, 128, 272), (200, 500, 1040), (257, 255, 384), (300, 1029, 1808), (512, 512, 2048),
+         (1000, 130, 96), (1531, 777, 640), (2, 9000, 16), (2300, 2600, 128), (2304, 4352, 400)]
+
+
+@pytest.mark.parametrize("residual", [False, True])
+@pytest.mark.parametrize("M,N,K", SIZES)
+def test_gemm_int8(cuda, M, N, K, residual):
+    log(f"gemm_int8 M={M} N={N} K={K} residual={residual}")
+    q, s = random_codes(M, K, M + K, cuda, full=True)
+    p, t = random_codes(N, K, N + K + 1, cuda, full=True)
+    r = bf16((M, N), 9, 3.0).to(cuda) if residual else None
+    c = ops.gemm_int8(q, s, p, t, residual=r)
+    check_product(q, s, p, t, r, c)
+
+
+def test_gemm_int8_extreme_codes_sum_exactly(cuda):
+    # all codes -128: the longest sum is 131056 * 2^14, just below 2^31
+    for M, N in ((1, 20), (70, 70)):
+        K = (1 << 17) - 16
+        q = torch.full((M, K), -128, dtype=torch.int8, device=cuda)
+        p = torch.full((N, K), -128, dtype=torch.int8, device=cuda)
+        one = torch.ones(max(M, N), device=cuda)
+        c = ops.gemm_int8(q, one[:M].contiguous(), p, one[:N].contiguous())
+        want = torch.tensor(float(K * 128 * 128)).to(torch.bfloat16).float()
+        assert (c.float().cpu() == want).all()
+
+
+@pytest.mark.parametrize("M,N,K", [(1, 100, 256), (40, 100, 272), (300, 264, 400)])
+def test_gemm_int8_strided_and_in_place(cuda, M, N, K):
+    q, s = random_codes(M, K + 48, 1, cuda)
+    p, t = random_codes(N, K + 32, 2, cuda)
+    qs, ps = q[:, 16:16 + K], p[:, 32:32 + K]
+    want = ops.gemm_int8(qs.contiguous(), s, ps.contiguous(), t)
+    for off in (0, 1, 8):
+        out = torch.full((M + 2, N + 24), 5.0, dtype=torch.bfloat16, device=cuda)
+        into = out[1:-1, off:off + N]
+        ops.gemm_int8(qs, s, ps, t, out=into)
+        assert torch.equal(into, want)
+        keep = torch.ones_like(out, dtype=torch.bool)
+        keep[1:-1, off:off + N] = False
+        assert (out[keep] == 5.0).all()
+        r = bf16((M, N), 4).to(cuda)
+        into.copy_(r)
+        ops.gemm_int8(qs, s, ps, t, residual=into, out=into)
+        assert torch.equal(into, ops.gemm_int8(qs, s, ps, t, residual=r))
+        assert (out[keep] == 5.0).all()
+
+
+def test_gemm_int8_scales_that_are_not_finite(cuda):
+    # a poisoned token poisons its row, a zero one gives the residual
+    M, N, K = 70, 90, 128
+    q, s = random_codes(M, K, 1, cuda)
+    p, t = random_codes(N, K, 2, cuda)
+    r = bf16((M, N), 3).to(cuda)
+    clean = ops.gemm_int8(q, s, p, t, residual=r)
+    s2 = s.clone()
+    s2[5], s2[66] = float("nan"), 0.0
+    c = ops.gemm_int8(q, s2, p, t, residual=r)
+    assert torch.isnan(c[5]).all() and torch.equal(c[66], r[66])
+    others = [i for i in range(M) if i not in (5, 66)]
+    assert torch.equal(c[others], clean[others])
+
+
+WGRAD = [(1, 8, 8), (2, 16, 40), (63, 64, 64), (64, 72, 128), (65, 128, 72), (200, 256, 256),
+         (129, 264, 520), (1000, 520, 264), (3001, 1040, 1416), (64, 512, 768), (192, 256, 512),
+         (4096, 256, 256), (8200, 512, 264), (300, 2304, 2560), (20000, 136, 200)]
+
+
+@pytest.mark.parametrize("T,M,N", WGRAD)
+def test_gemm_int8_wgrad(cuda, T, M, N):
+    log(f"gemm_int8_wgrad T={T} M={M} N={N}")
+    q, s = random_codes(T, M, T + M, cuda)
+    dy = bf16((T, N), N).to(cuda)
+    dw = ops.gemm_int8_wgrad(q, s, dy)
+    x = f64(ops.dequantize(q, s))
+    ref = x.T @ f64(dy)
+    mag = np.abs(x).T @ np.abs(f64(dy))
+    close(f64(dw), ref, B * np.abs(ref) + T * U * mag, "dw")
+    assert rel_l2(f64(dw), ref) <= 3e-3
+
+
+@pytest.mark.parametrize("T,M,N", [(100, 40, 72), (500, 264, 264)])
+def test_gemm_int8_wgrad_strided(cuda, T, M, N):
+    q, s = random_codes(T, M + 24, 1, cuda)
+    dy = bf16((T, N + 16), 2).to(cuda)
+    want = ops.gemm_int8_wgrad(q[:, 8:8 + M].contiguous(), s, dy[:, 8:8 + N].contiguous())
+    out = torch.full((M + 2, N + 24), 5.0, dtype=torch.bfloat16, device=cuda)
+    into = out[1:-1, 8:8 + N]
+    ops.gemm_int8_wgrad(q[:, 8:8 + M], s, dy[:, 8:8 + N], out=into)
+    assert torch.equal(into, want)
+    keep = torch.ones_like(out, dtype=torch.bool)
+    keep[1:-1, 8:8 + N] = False
+    assert (out[keep] == 5.0).all()
+
+
+def test_gemm_int8_wgrad_rows_behind_the_last_token(cuda):
+    # what lies behind the last token is not read into the sums
+    T, M, N = 70, 264, 520
+    q, s = random_codes(T + 60, M, 1, cuda)
+    dy = bf16((T + 60, N), 2).to(cuda)
+    want = ops.gemm_int8_wgrad(q[:T].clone(), s[:T].clone(), dy[:T].clone())
+    dy[T:] = float("nan")
+    s[T:] = float("inf")
+    assert torch.equal(ops.gemm_int8_wgrad(q[:T], s[:T].contiguous(), dy[:T]), want)
+
+
+def test_empty_matrices(cuda):
+    e = lambda *s, t=torch.bfloat16: torch.empty(s, dtype=t, device=cuda)
+    y, h, rstd = ops.rms_norm(e(0, 64), e(64))
+    assert y.shape == (0, 64) and rstd.shape == (0,)
+    assert ops.rms_norm_int8(e(0, 64), e(64))[0].shape == (0, 64)
+    dx, dw = ops.rms_norm_backward(e(0, 64), e(64), e(0, t=torch.float32), e(0, 64))
+    assert dx.shape == (0, 64) and not dw.any()
+    q, s = ops.quantize(e(0, 64))
+    assert ops.dequantize(q, s).shape == (0, 64)
+    b, sb = ops.quantize(e(32, 64).zero_())
+    assert ops.gemm_int8(q, s, b, sb).shape == (0, 32)
+    dw = ops.gemm_int8_wgrad(q, s, e(0, 16))
+    assert dw.shape == (64, 16) and not dw.any()
+    assert ops.gemm_int8_wgrad(b[:, :0].contiguous(), sb, e(32, 16)).shape == (0, 16)
+
+
+def layer_step(x, r, nw, w8, sw, w, dy, dh):
+    """A linear layer behind the norm, forward in 8 bits, and its backward
+    from the codes it kept."""
+    q, s, h, rstd = ops.rms_norm_int8(x, nw, residual=r)
+    y = ops.gemm_int8(q, s, w8, sw)
+    dw = ops.gemm_int8_wgrad(q, s, dy)
+    da = ops.gemm(dy, w, trans_b=True)
+    dx, dnw = ops.rms_norm_backward(h, nw, rstd, da, dres=dh)
+    return y, dw, dx, dnw
+
+
+def layer_inputs(T, d, n, dev):
+    x, r, dy, dh = bf16((T, d), 1), bf16((T, d), 2), bf16((T, n), 3), bf16((T, d), 4)
+    nw, w = (1 + 0.1 * bf16((d,), 5).float()).to(torch.bfloat16), bf16((d, n), 6, 0.05)
+    w8, sw = ops.quantize(w.t().contiguous().to(dev))
+    return [t.to(dev) for t in (x, r, nw)] + [w8, sw] + [t.to(dev) for t in (w, dy, dh)]
+
+
+def test_layer_forward_and_backward_together(cuda):
+    T, d, n = 512, 768, 1024
+    args = layer_inputs(T, d, n, cuda)
+    x, r, nw, w8, sw, w, dy, dh = args
+    y, dw, dx, dnw = layer_step(*args)
+    h = f64(O.add(x.cpu(), r.cpu()))
+    rs = O.rstd(h, ops.LN_EPS)
+    q, top = O.codes(h * f64(nw))
+    a = q * (top * rs / 127)[:, None]
+    # one bf16 rounding of each result (1.7e-3); dw also rounds its restored
+    # input, dx and dnw the gradient between the two products
+    assert rel_l2(f64(y), a @ (w8.cpu().numpy() * f64(sw)[:, None]).T) <= 3e-3
+    assert rel_l2(f64(dw), a.T @ f64(dy)) <= 5e-3
+    rx, rnw, _ = O.norm_backward(h, f64(nw), rs, f64(dy) @ f64(w).T, f64(dh))
+    assert rel_l2(f64(dx), rx) <= 5e-3 and rel_l2(f64(dnw), rnw) <= 5e-3
+    # and the 8-bit layer is the bf16 one up to its codes: each operand is off
+    # by up to half a step of A / 127 with A about four deviations, 0.9% of a
+    # deviation (rms), the two together 1.3%
+    plain = (h * rs[:, None] * f64(nw)) @ f64(w)
+    assert rel_l2(f64(y), plain) <= 2e-2
+
+
+def test_repeated_calls_are_bit_identical(cuda):
+    args = layer_inputs(768, 512, 768, cuda)
+    first = layer_step(*args)
+    for _ in range(2):
+        for a, b in zip(layer_step(*args), first):
+            assert torch.equal(a, b)
+
+
+def test_on_another_stream(cuda):
+    args = layer_inputs(256, 256, 512, cuda)
+    ref = layer_step(*args)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream(cuda)
+    with torch.cuda.stream(side):
+        out = layer_step(*args)
+    side.synchronize()
+    for a, b in zip(out, ref):
+        assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("T,d,n", [(256, 256, 512), (2048, 1024, 2816)])
+def test_graph_replay_matches_eager(cuda, T, d, n):
+    args = layer_inputs(T, d, n, cuda)
+    one = [args[0][:1], args[1][:1]] + args[2:5]  # and the single-token form
+
+    def step():
+        q, s, h, _ = ops.rms_norm_int8(one[0], one[2], residual=one[1])
+        return layer_step(*args) + (ops.gemm_int8(q, s, one[3], one[4]), h)
+
+    ref = [t.clone() for t in step()]
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream(cuda)
+    side.wait_stream(torch.cuda.current_stream(cuda))
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream(cuda).wait_stream(side)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        out = step()
+    other = layer_inputs(256, 512, 256, cuda)
+    for rep in range(3):
+        for t in out:
+            t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        for i, (a, b) in enumerate(zip(out, ref)):
+            assert torch.equal(a, b), (rep, i)
+        layer_step(*other)
+        torch.cuda.synchronize()

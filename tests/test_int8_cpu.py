@@ -1,0 +1,155 @@
+"""The 8-bit operators without a GPU: every refusal of the C ABI (validation
+runs on the host before any launch) and of the Python wrappers."""
+import ctypes
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2405_13226_amd import _lib, block_ops as ops
+
+import int8_oracle as O
+
+OK, NULL, SHAPE, HEADDIM, DOCLENS, WORKSPACE, ALIGN, ALIAS = range(8)
+
+
+def fake(i, off=0):
+    """Addresses 2^30 apart; never read."""
+    return ctypes.c_void_p((i + 1) * (1 << 30) + off)
+
+
+@pytest.fixture(scope="module")
+def lib():
+    return _lib.lib()
+
+
+def call(lib, fn, defaults, **kw):
+    a = dict(defaults)
+    assert set(kw) <= set(a), kw
+    a.update(kw)
+    return getattr(lib, fn)(*a.values(), None)
+
+
+NORM = dict(X=fake(0), ldx=512, R=fake(1), ldr=512, w=fake(2), H=fake(3), Y=fake(4),
+            rstd=fake(5), rows=8, d=512, eps=1e-5)
+NORM8 = dict(X=fake(0), ldx=512, R=fake(1), ldr=512, w=fake(2), H=fake(3), Q=fake(4), ldq=512,
+             scales=fake(6), rstd=fake(5), rows=8, d=512, eps=1e-5)
+
+
+@pytest.mark.parametrize("fn,base", [("dd_rmsnorm_fwd", NORM), ("dd_rmsnorm_int8_fwd", NORM8)])
+def test_norm_refusals(lib, fn, base):
+    for n in ("X", "w", "H", "R", "rstd") + (("Y",) if "Y" in base else ("Q", "scales")):
+        assert call(lib, fn, base, **{n: None}) == NULL, n
+    for kw in (dict(rows=0), dict(d=0), dict(d=16385, ldx=1 << 15, ldr=1 << 15), dict(ldx=511),
+               dict(ldr=511), dict(eps=0.0), dict(eps=-1.0), dict(eps=float("nan")),
+               dict(eps=float("inf")), dict(rows=(1 << 31) - 1, d=1024, ldx=1024, ldr=1024)):
+        assert call(lib, fn, base, **kw) == SHAPE, kw
+    assert call(lib, fn, base, X=fake(0, 1)) == ALIGN
+    assert call(lib, fn, base, rstd=fake(5, 2)) == ALIGN
+    out = "Y" if "Y" in base else "Q"
+    assert call(lib, fn, base, **{out: fake(0, 64)}) == ALIAS
+    assert call(lib, fn, base, H=fake(1)) == ALIAS
+    assert call(lib, fn, base, H=fake(4)) == ALIAS
+    if fn == "dd_rmsnorm_int8_fwd":
+        assert call(lib, fn, base, ldq=500) == SHAPE
+        assert call(lib, fn, base, scales=fake(6, 1)) == ALIGN
+        assert call(lib, fn, base, scales=fake(5)) == ALIAS
+
+
+def test_norm_backward_refusals(lib):
+    need = lib.dd_rmsnorm_bwd_workspace_bytes(8, 512)
+    assert need > 0 and lib.dd_rmsnorm_bwd_workspace_bytes(0, 512) == 0
+    assert lib.dd_rmsnorm_bwd_workspace_bytes(8, 16385) == 0
+    base = dict(H=fake(0), w=fake(1), rstd=fake(2), dY=fake(3), dRes=fake(4), dX=fake(5),
+                dw=fake(6), rows=8, d=512, ws=fake(7), bytes=need)
+    for n in ("H", "w", "rstd", "dY", "dX", "dw"):
+        assert call(lib, "dd_rmsnorm_bwd", base, **{n: None}) == NULL, n
+    assert call(lib, "dd_rmsnorm_bwd", base, rows=0) == SHAPE
+    assert call(lib, "dd_rmsnorm_bwd", base, d=20000) == SHAPE
+    assert call(lib, "dd_rmsnorm_bwd", base, ws=None) == WORKSPACE
+    assert call(lib, "dd_rmsnorm_bwd", base, bytes=need - 1) == WORKSPACE
+    assert call(lib, "dd_rmsnorm_bwd", base, ws=fake(7, 2)) == ALIGN
+    assert call(lib, "dd_rmsnorm_bwd", base, dX=fake(3)) == ALIAS
+    assert call(lib, "dd_rmsnorm_bwd", base, dX=fake(4, 16)) == ALIAS
+    assert call(lib, "dd_rmsnorm_bwd", base, ws=fake(6, 16)) == ALIAS
+
+
+def test_codes_refusals(lib):
+    q = dict(X=fake(0), ldx=512, Q=fake(1), ldq=512, scales=fake(2), rows=8, d=512)
+    for n in ("X", "Q", "scales"):
+        assert call(lib, "dd_quantize", q, **{n: None}) == NULL
+    for kw in (dict(rows=0), dict(d=0), dict(d=16385), dict(ldx=500), dict(ldq=500)):
+        assert call(lib, "dd_quantize", q, **kw) == SHAPE, kw
+    assert call(lib, "dd_quantize", q, X=fake(0, 1)) == ALIGN
+    assert call(lib, "dd_quantize", q, Q=fake(0, 512)) == ALIAS
+    d = dict(Q=fake(0), ldq=512, scales=fake(1), Y=fake(2), ldy=512, rows=8, d=512)
+    for n in ("Q", "scales", "Y"):
+        assert call(lib, "dd_dequantize", d, **{n: None}) == NULL
+    for kw in (dict(rows=0), dict(d=16385), dict(ldy=500), dict(ldq=500)):
+        assert call(lib, "dd_dequantize", d, **kw) == SHAPE, kw
+    assert call(lib, "dd_dequantize", d, Y=fake(0, 512)) == ALIAS
+    assert call(lib, "dd_dequantize", d, Y=fake(2, 1)) == ALIGN
+
+
+def test_product_refusals(lib):
+    g = dict(A=fake(0), lda=128, sa=fake(1), B=fake(2), ldb=128, sb=fake(3), R=None, C=fake(4),
+             ldc=96, M=64, N=96, K=128)
+    for n in ("A", "sa", "B", "sb", "C"):
+        assert call(lib, "dd_gemm_i8", g, **{n: None}) == NULL, n
+    for kw in (dict(M=0), dict(N=0), dict(K=0), dict(K=8), dict(K=120), dict(lda=112),
+               dict(ldb=112), dict(ldc=95), dict(K=1 << 17, lda=1 << 17, ldb=1 << 17),
+               dict(lda=1 << 23), dict(ldb=1 << 23), dict(M=1 << 20, N=1 << 20, ldc=1 << 20)):
+        assert call(lib, "dd_gemm_i8", g, **kw) == SHAPE, kw
+    for kw in (dict(lda=136), dict(ldb=136), dict(A=fake(0, 8)), dict(B=fake(2, 4)),
+               dict(sa=fake(1, 2)), dict(C=fake(4, 1)), dict(R=fake(5, 1))):
+        assert call(lib, "dd_gemm_i8", g, **kw) == ALIGN, kw
+    for kw in (dict(C=fake(0, 64)), dict(C=fake(2)), dict(C=fake(1)), dict(C=fake(3, 128)),
+               dict(R=fake(4, 2))):
+        assert call(lib, "dd_gemm_i8", g, **kw) == ALIAS, kw
+
+
+def test_weight_gradient_refusals(lib):
+    need = lib.dd_gemm_i8_wgrad_workspace_bytes(64, 96, 128)
+    assert lib.dd_gemm_i8_wgrad_workspace_bytes(0, 96, 128) == 0
+    assert lib.dd_gemm_i8_wgrad_workspace_bytes(64, 92, 128) == 0
+    g = dict(Q=fake(0), ldq=96, scales=fake(1), dY=fake(2), ldy=128, dW=fake(3), ldw=128, T=64,
+             M=96, N=128, ws=fake(4), bytes=need)
+    for n in ("Q", "scales", "dY", "dW"):
+        assert call(lib, "dd_gemm_i8_wgrad", g, **{n: None}) == NULL, n
+    for kw in (dict(T=0), dict(M=0), dict(M=92), dict(N=100), dict(ldq=88), dict(ldy=120),
+               dict(ldw=120), dict(ldq=1 << 23), dict(ldy=1 << 23)):
+        assert call(lib, "dd_gemm_i8_wgrad", g, **kw) == SHAPE, kw
+    for kw in (dict(ldq=100), dict(ldy=132), dict(ldw=132), dict(Q=fake(0, 4)), dict(dY=fake(2, 8)),
+               dict(dW=fake(3, 8)), dict(scales=fake(1, 1))):
+        assert call(lib, "dd_gemm_i8_wgrad", g, **kw) == ALIGN, kw
+    for kw in (dict(dW=fake(0)), dict(dW=fake(1, 64)), dict(dW=fake(2, 16))):
+        assert call(lib, "dd_gemm_i8_wgrad", g, **kw) == ALIAS, kw
+    # a product whose T axis is split needs its scratch
+    T, M, N = 65536, 256, 256
+    need = lib.dd_gemm_i8_wgrad_workspace_bytes(T, M, N)
+    if need:
+        g.update(T=T, M=M, N=N, ldq=M, ldy=N, ldw=N)
+        assert call(lib, "dd_gemm_i8_wgrad", g, bytes=need - 1) == WORKSPACE
+        assert call(lib, "dd_gemm_i8_wgrad", g, ws=None) == WORKSPACE
+        assert call(lib, "dd_gemm_i8_wgrad", g, ws=fake(4, 8), bytes=need) == ALIGN
+        assert call(lib, "dd_gemm_i8_wgrad", g, ws=fake(3, 16), bytes=need) == ALIAS
+
+
+def test_wrappers_refuse_what_is_not_on_a_gpu_or_of_another_type():
+    x = torch.zeros(4, 32, dtype=torch.bfloat16)
+    q, s = torch.zeros(4, 32, dtype=torch.int8), torch.zeros(4)
+    w = torch.zeros(32, dtype=torch.bfloat16)
+    for f in (lambda: ops.rms_norm(x, w), lambda: ops.rms_norm_int8(x, w),
+              lambda: ops.rms_norm(x[0], w), lambda: ops.rms_norm_backward(x, w, s, x),
+              lambda: ops.quantize(x), lambda: ops.quantize([1.0]),
+              lambda: ops.dequantize(q, s), lambda: ops.dequantize(x, s),
+              lambda: ops.gemm_int8(q, s, q, s), lambda: ops.gemm_int8_wgrad(q, s, x)):
+        with pytest.raises(ValueError):
+            f()
+
+
+def test_oracle_codes_take_ties_to_even():
+    z = np.array([[254.0, 1.0, 3.0, -5.0, 0.0], [0.0] * 5, [np.nan, 1.0, 2.0, 3.0, 4.0]])
+    q, top = O.codes(z)
+    assert q.tolist() == [[127, 0, 2, -2, 0], [0] * 5, [0] * 5]
+    assert top[0] == 254.0 and top[1] == 0.0
