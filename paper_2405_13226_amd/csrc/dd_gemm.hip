@@ -54,6 +54,7 @@
 // caller's workspace and a second kernel sums them.
 #include "dd_device.hpp"
 #include "dd_tile.hpp"
+#include "dd_gemm.hpp"
 #include "dd_internal.h"
 #include "dd_launch.hpp"
 #include "dd_routes.hpp"
@@ -69,30 +70,6 @@ struct GemmTile {
     static constexpr int HALF = 2 * SUB;       // half of the A (or B) tile of one K step
     static constexpr int SIDE = 4 * HALF;      // A (or B): two halves x two stages
 };
-
-// Waits until at most N of this wave's vector-memory operations are in
-// flight and all its LDS reads have returned, then joins the workgroup's
-// barrier.
-template <int N>
-__device__ __forceinline__ void wait_and_barrier()
-{
-    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"(N) : "memory");
-    __builtin_amdgcn_sched_barrier(0);
-}
-
-__device__ __forceinline__ void plain_barrier()
-{
-    __builtin_amdgcn_sched_barrier(0);
-    asm volatile("s_barrier" : : : "memory");
-    __builtin_amdgcn_sched_barrier(0);
-}
-
-// Chunk swizzle of the sub-tiles that are read along rows: 64 lanes read 16
-// consecutive rows at four neighbouring chunks, and the LDS serves them in
-// groups of 16 lanes that are not consecutive (lanes 0-3, 12-15, 20-23,
-// 24-27 and so on).  With swz<64>, made for 32 rows at two chunks, such a
-// read has two-way bank conflicts.
-__device__ __forceinline__ int row_swz(int r) { return (r >> 1) & 7; }
 
 __device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c)
 {
@@ -133,30 +110,6 @@ struct GemmSizes {
     int M, N, K, k_len, tiles_n, xm;
     long long lda, ldb, ldc;
 };
-
-// Tile of block `id`.  Workgroups are dispatched round-robin over the 8 XCDs
-// (block id % 8), each with its own L2.  XCD x takes every xm-th tile row
-// from row x % xm on and one of 8 / xm blocks of columns, in bands of kGR of
-// its rows; a band is walked in groups of 32 tiles (one per CU of the XCD),
-// each group column by column, so the tiles that run at the same time share
-// their A and B panels in one L2.  xm = 0: row by row (tile_rows_step).
-constexpr int kGR = 4;
-
-__device__ __forceinline__ void tile_of(int id, int tiles_m, int tiles_n, int xm, int &tm, int &tn)
-{
-    if (xm == 0) {
-        tm = id / tiles_n;
-        tn = id - tm * tiles_n;
-        return;
-    }
-    const int x = id % kXcds, k = id / kXcds;
-    const int rows_x = tiles_m / xm, cols_x = tiles_n * xm / kXcds;
-    const int band = k / (kGR * cols_x), rem = k - band * kGR * cols_x;
-    const int gr = min(kGR, rows_x - band * kGR);  // rows of this band
-    const int gc = 32 / gr, grp = rem / (gr * gc), w = rem - grp * gr * gc;
-    tm = (band * kGR + w % gr) * xm + x % xm;
-    tn = x / xm * cols_x + grp * gc + w / gr;
-}
 
 // LDS position (elements) of the four columns c .. c + 3 of row r of the
 // finished BM x BN bf16 tile.  With kEpiSwiglu the column halves are two
@@ -785,28 +738,6 @@ DD_GEMM_INST(false, true, kEpiSwigluBwd);
 static GemmPlan plan_on_device(int M, long long N, long long K, bool may_split)
 {
     return gemm_plan(M, N, K, may_split, device_cu_count());
-}
-
-// xm of tile_of: the one whose groups of 32 tiles read the fewest panels per
-// tile, of those that divide the tiles evenly (0: none does).  Eight tile rows
-// of a weight gradient, taken a row per XCD, read 24 B panels for 24 tiles
-// (2048 x 6144, K = 16,384: 430 us); as 4 x 6 tiles per XCD 400 us.
-static int tile_rows_step(int tiles_m, int tiles_n)
-{
-    int best = 0;
-    double least = 0;
-    for (int xm = kXcds; xm >= 1; xm /= 2) {
-        if (tiles_m % xm || tiles_n * xm % kXcds)
-            continue;
-        const double gr = std::min(kGR, tiles_m / xm);
-        const double gc = std::min(32 / gr, static_cast<double>(tiles_n * xm / kXcds));
-        const double panels = (gr + gc) / (gr * gc);
-        if (best == 0 || panels < least) {
-            best = xm;
-            least = panels;
-        }
-    }
-    return best;
 }
 
 size_t gemm_workspace_bytes(int M, int N, int K, int groups)

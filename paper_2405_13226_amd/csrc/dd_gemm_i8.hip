@@ -5,8 +5,11 @@
 // (K < 2^17); it is scaled and the residual added in fp32, with one rounding to
 // bf16 at the end.  Any M, N and K (a multiple of 16).
 #include "dd_device.hpp"
+#include "dd_tile.hpp"
+#include "dd_gemm.hpp"
 #include "dd_internal.h"
 #include "dd_launch.hpp"
+#include "dd_routes.hpp"
 #include "dd_attn.h"
 
 namespace dd {
@@ -22,73 +25,501 @@ __device__ __forceinline__ i32x4 mfma_i8(u32x4 a, u32x4 b, i32x4 c)
                                                  __builtin_bit_cast(i32x4, b), c, 0, 0, 0);
 }
 
+// `wide`: the rows of C (and R) are made of 16-byte aligned pieces.
 struct GemmI8Operands {
     const int8_t *A, *B;
     const float *sa, *sb;
     const uint16_t *R;
     uint16_t *C;
     long long lda, ldb, ldc;
-    int M, N, K, tiles_n;
+    int M, N, K, tiles_m, tiles_n, xm;
+    bool wide;
 };
 
-// One workgroup per 64 x 64 tile, 32 x 32 per wave, operands straight from
-// memory.
-__global__ void __launch_bounds__(256)
+__device__ __forceinline__ float bf16_at(const uint16_t *p)
+{
+    return __uint_as_float(static_cast<uint32_t>(*p) << 16);
+}
+
+// sa sb acc + R of row m, columns n .. n + 3, in bf16 (junk where they do not
+// exist).  ra: sa of the row, rb: sb of the columns.
+__device__ __forceinline__ bf16x4 scaled(const GemmI8Operands &op, i32x4 acc, float ra,
+                                         const float (&rb)[4], int m, int n)
+{
+    float c[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        c[e] = static_cast<float>(acc[e]) * ra * rb[e];
+    if (op.R != nullptr && m < op.M) {
+        const uint16_t *r = op.R + m * op.ldc + n;
+        if (op.wide && n + 4 <= op.N) {
+            const bf16x4 v = *reinterpret_cast<const bf16x4 *>(r);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                c[e] += static_cast<float>(v[e]);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (n + e < op.N)
+                    c[e] += bf16_at(r + e);
+        }
+    }
+    return pack4(c[0], c[1], c[2], c[3]);
+}
+
+// The finished BM x BN tile in LDS, and from there to memory in 16-byte pieces
+// of rows.  A row's 4-element group x sits at x ^ (2 (r mod 16)), which keeps
+// the two groups of a piece adjacent and spreads one write instruction's 16
+// rows over the LDS banks.
+template <int BN>
+__device__ __forceinline__ int image_off(int r, int c)
+{
+    return r * BN + 4 * ((c >> 2) ^ (2 * (r & 15)));
+}
+
+template <int BM, int BN>
+__device__ __forceinline__ void store_image(const uint16_t *lds, const GemmI8Operands &op, int m0,
+                                            int n0, int tid)
+{
+    constexpr int CPR = BN / 8;
+#pragma unroll 4
+    for (int it = 0; it < BM * CPR / 512; ++it) {
+        const int idx = it * 512 + tid, r = idx / CPR, c = idx % CPR * 8, m = m0 + r, n = n0 + c;
+        const u32x4 v = *reinterpret_cast<const u32x4 *>(lds + image_off<BN>(r, c));
+        if (m >= op.M || n >= op.N)
+            continue;
+        uint16_t *p = op.C + m * op.ldc + n;
+        if (op.wide && n + 8 <= op.N) {
+            *reinterpret_cast<u32x4 *>(p) = v;
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (n + e < op.N)
+                    p[e] = static_cast<uint16_t>(v[e >> 1] >> 16 * (e & 1));
+        }
+    }
+}
+
+// The direct loads of both operands of a tile.  Every 64 rows x 128 bytes of
+// an operand are a sub-tile of 8 KiB in LDS, whose 16-byte chunk x of row r
+// sits at x ^ row_swz(r); one instruction of wave w loads its rows 8 w .. +7.
+// Rows behind the matrix and bytes behind K read as zeros.
+struct I8Loads {
+    u32x4 a, b;
+    uint32_t va, vb;     // this lane's byte offset in a sub-tile of the step
+    uint32_t sa, sb;     // from sub-tile to sub-tile
+    int kx, k, K;        // this lane's first k in a step, the next step, the end
+
+    __device__ __forceinline__ void init(const GemmI8Operands &op, int m0, int n0, int wave,
+                                         int lane)
+    {
+        a = buffer_of(op.A + m0 * op.lda, (op.M - 1LL - m0) * op.lda + op.K);
+        b = buffer_of(op.B + n0 * op.ldb, (op.N - 1LL - n0) * op.ldb + op.K);
+        const int r = 8 * wave + (lane >> 3);
+        kx = ((lane & 7) ^ row_swz(r)) * 16;
+        va = static_cast<uint32_t>(r * op.lda + kx);
+        vb = static_cast<uint32_t>(r * op.ldb + kx);
+        sa = static_cast<uint32_t>(64 * op.lda);
+        sb = static_cast<uint32_t>(64 * op.ldb);
+        k = 0;
+        K = op.K;
+    }
+    // Sub-tile s of the step's A (B) to LDS address l.
+    __device__ __forceinline__ void load_a(int s, uint32_t l) const
+    {
+        dma_b128_buf(a, kx + k < K ? va + (s * sa + k) : kBufferEnd, l);
+    }
+    __device__ __forceinline__ void load_b(int s, uint32_t l) const
+    {
+        dma_b128_buf(b, kx + k < K ? vb + (s * sb + k) : kBufferEnd, l);
+    }
+};
+
+// 256 x 256 tiles, K in steps of 128: the loop of the bf16 product (dd_gemm.hip,
+// which has its phases), since an int8 product instruction takes the bytes and
+// the time of a bf16 one with twice the k.
+__global__ void __launch_bounds__(512, 1)
 gemm_i8_kernel(GemmI8Operands op)
 {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, g = lane >> 4;
-    const int m0 = static_cast<int>(blockIdx.x) / op.tiles_n * 64 + (wave >> 1) * 32;
-    const int n0 = static_cast<int>(blockIdx.x) % op.tiles_n * 64 + (wave & 1) * 32;
-    const int8_t *pa[2], *pb[2];
+    constexpr int SUB = 64 * 128, HALF = 2 * SUB, SIDE = 4 * HALF;  // bytes
+    __shared__ __attribute__((aligned(1024))) int8_t lds[2 * SIDE];
+    const int tid = threadIdx.x;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+    const int l16 = lane & 15, g = lane >> 4;
+    const int wm = wave >> 2, wn = wave & 3;
+    int tm, tn;
+    tile_of(static_cast<int>(blockIdx.x), op.tiles_m, op.tiles_n, op.xm, tm, tn);
+    const int m0 = tm * 256, n0 = tn * 256;
+    const int nkt = (op.K + 127) / 128;
+    I8Loads at;
+    at.init(op, m0, n0, wave, lane);
+    const uint32_t lds0 = lds_base_sgpr(lds) + 1024u * wave;
+    auto load_a = [&](int h, int S) __attribute__((always_inline)) {
+        at.load_a(2 * h, lds0 + (2 * h + S) * HALF);
+        at.load_a(2 * h + 1, lds0 + (2 * h + S) * HALF + SUB);
+    };
+    auto load_b = [&](int h, int S) __attribute__((always_inline)) {
+        at.load_b(2 * h, lds0 + SIDE + (2 * h + S) * HALF);
+        at.load_b(2 * h + 1, lds0 + SIDE + (2 * h + S) * HALF + SUB);
+    };
+    const int8_t *fa[2], *fb[2];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        pa[i] = op.A + min(m0 + 16 * i + l16, op.M - 1) * op.lda;
-        pb[i] = op.B + min(n0 + 16 * i + l16, op.N - 1) * op.ldb;
+    for (int kk = 0; kk < 2; ++kk) {
+        const int x = ((4 * kk + g) ^ row_swz(l16)) * 16;
+        fa[kk] = lds + wm * SUB + 128 * l16 + x;
+        fb[kk] = lds + SIDE + (wn >> 1) * SUB + 128 * (32 * (wn & 1) + l16) + x;
     }
-    i32x4 acc[2][2] = {};
-    for (int k0 = 0; k0 < op.K; k0 += 64) {
-        const int k = k0 + 16 * g;
-        u32x4 a[2], b[2];
+    u32x4 a0[4][2], a1[4][2], b0[2][2], b1[2][2];
+    auto read_a = [&](u32x4 (&f)[4][2], int h, int S) __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            a[i] = b[i] = u32x4{0u, 0u, 0u, 0u};
-            if (k < op.K) {
-                a[i] = *reinterpret_cast<const u32x4 *>(pa[i] + k);
-                b[i] = *reinterpret_cast<const u32x4 *>(pb[i] + k);
-            }
-        }
+        for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-            for (int j = 0; j < 2; ++j)
-                acc[i][j] = mfma_i8(b[j], a[i], acc[i][j]);  // rows n, columns m
-    }
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
+            for (int kk = 0; kk < 2; ++kk)
+                f[i][kk] = *reinterpret_cast<const u32x4 *>(fa[kk] + ((2 * h + S) * HALF + 2048 * i));
+    };
+    auto read_b = [&](u32x4 (&f)[2][2], int h, int S) __attribute__((always_inline)) {
 #pragma unroll
         for (int j = 0; j < 2; ++j)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int m = m0 + 16 * i + l16, n = n0 + 16 * j + 4 * g + e;
-                if (m >= op.M || n >= op.N)
-                    continue;
-                const long long at = m * op.ldc + n;
-                float c = static_cast<float>(acc[i][j][e]) * op.sa[m] * op.sb[n];
-                if (op.R != nullptr)
-                    c += __uint_as_float(static_cast<uint32_t>(op.R[at]) << 16);
-                op.C[at] = __builtin_bit_cast(uint16_t, static_cast<__bf16>(c));
-            }
+            for (int kk = 0; kk < 2; ++kk)
+                f[j][kk] = *reinterpret_cast<const u32x4 *>(fb[kk] + ((2 * h + S) * HALF + 2048 * j));
+    };
+    i32x4 acc[2][2][4][2];  // [A half][B half][i][j]
+#pragma unroll
+    for (int x = 0; x < 4; ++x)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+                acc[x >> 1][x & 1][i][j] = i32x4{};
+    auto multiply = [&](i32x4 (&c)[4][2], const u32x4 (&a)[4][2],
+                        const u32x4 (&b)[2][2]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+                    c[i][j] = mfma_i8(b[j][kk], a[i][kk], c[i][j]);  // rows n, columns m
+    };
+    auto products = [&](i32x4 (&c)[4][2], const u32x4 (&a)[4][2],
+                        const u32x4 (&b)[2][2]) __attribute__((always_inline)) {
+        __builtin_amdgcn_s_setprio(1);
+        multiply(c, a, b);
+        __builtin_amdgcn_s_setprio(0);
+        plain_barrier();
+    };
+    // One K step from stage S.  MODE 0: also starts the loads of the step
+    // after the next one; 1, 2: the last step but one, the last step.
+    auto step = [&](auto stage, auto mode) __attribute__((always_inline)) {
+        constexpr int S = decltype(stage)::value, MODE = decltype(mode)::value;
+        read_b(b0, 0, S);
+        if constexpr (MODE == 0)
+            load_a(0, S);
+        wait_and_barrier<MODE == 0 ? 12 : MODE == 1 ? 10 : 2>();
+        products(acc[0][0], a0, b0);
+        read_b(b1, 1, S);
+        if constexpr (MODE == 0)
+            load_b(0, S);
+        wait_and_barrier<MODE == 0 ? 12 : MODE == 1 ? 8 : 0>();
+        products(acc[0][1], a0, b1);
+        read_a(a1, 1, S);
+        if constexpr (MODE == 0)
+            load_b(1, S);
+        wait_and_barrier<MODE == 0 ? 12 : MODE == 1 ? 6 : 0>();
+        products(acc[1][1], a1, b1);
+        if constexpr (MODE != 2)
+            read_a(a0, 0, 1 - S);
+        if constexpr (MODE == 0) {
+            load_a(1, S);
+            at.k += 128;
+        }
+        wait_and_barrier<MODE == 0 ? 12 : MODE == 1 ? 4 : 0>();
+        products(acc[1][0], a1, b0);
+    };
+    auto load_step = [&](int S) __attribute__((always_inline)) {
+        load_a(0, S);
+        load_b(0, S);
+        load_b(1, S);
+        load_a(1, S);
+        at.k += 128;
+    };
+    if (nkt == 1) {
+        load_step(0);
+        wait_and_barrier<0>();
+        read_a(a0, 0, 0);
+        read_b(b0, 0, 0);
+        multiply(acc[0][0], a0, b0);
+        read_b(b1, 1, 0);
+        multiply(acc[0][1], a0, b1);
+        read_a(a1, 1, 0);
+        multiply(acc[1][1], a1, b1);
+        multiply(acc[1][0], a1, b0);
+    } else {
+        const int s0 = nkt & 1;
+        load_step(s0);
+        load_step(1 - s0);
+        wait_and_barrier<8>();
+        read_a(a0, 0, s0);
+        // Phase 1 refills the half just read: only after a barrier that every
+        // wave reaches with its reads returned.
+        wait_and_barrier<8>();
+        // Waves 4-7 run half a phase behind waves 0-3.
+        if (wm == 1)
+            plain_barrier();
+        for (int kt = 2 - s0; kt < nkt; kt += 2) {
+            if (kt > 1)
+                step(IC<0>{}, IC<0>{});
+            step(IC<1>{}, IC<0>{});
+        }
+        step(IC<0>{}, IC<1>{});
+        step(IC<1>{}, IC<2>{});
+        if (wm == 0)
+            plain_barrier();
+    }
+
+    // Accumulator (ha, hb, i, j), register e: row m = 128 ha + 64 wm + 16 i +
+    // l16, column n = 128 hb + 32 wn + 16 j + 4 g + e of the tile.
+    float rb[2][2][4];
+#pragma unroll
+    for (int hb = 0; hb < 2; ++hb)
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                rb[hb][j][e] = op.sb[min(n0 + 128 * hb + 32 * wn + 16 * j + 4 * g + e, op.N - 1)];
+    __syncthreads();
+    uint16_t *image = reinterpret_cast<uint16_t *>(lds);
+#pragma unroll
+    for (int x = 0; x < 8; ++x) {
+        const int ha = x >> 2, i = x & 3, r = 128 * ha + 64 * wm + 16 * i + l16;
+        const float ra = op.sa[min(m0 + r, op.M - 1)];
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+            const int hb = y >> 1, j = y & 1, c = 128 * hb + 32 * wn + 16 * j + 4 * g;
+            *reinterpret_cast<bf16x4 *>(image + image_off<256>(r, c)) =
+                scaled(op, acc[ha][hb][i][j], ra, rb[hb][j], m0 + r, n0 + c);
+        }
+    }
+    __syncthreads();
+    store_image<256, 256>(image, op, m0, n0, tid);
+}
+
+// 128 x 128 tiles for products whose large tiles would leave CUs idle: eight
+// waves in two groups that run half a phase apart, a phase of 16 products of
+// every wave per K step of 128, four stages in LDS of which three are in
+// flight (128 KiB).
+__global__ void __launch_bounds__(512, 1)
+gemm_i8_small_kernel(GemmI8Operands op)
+{
+    constexpr int SUB = 64 * 128, STAGE = 4 * SUB, NST = 4;  // bytes
+    __shared__ __attribute__((aligned(1024))) int8_t lds[NST * STAGE];
+    const int tid = threadIdx.x;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+    const int l16 = lane & 15, g = lane >> 4;
+    const int wm = wave >> 2, wn = wave & 3;
+    int tm, tn;
+    tile_of(static_cast<int>(blockIdx.x), op.tiles_m, op.tiles_n, op.xm, tm, tn);
+    const int m0 = tm * 128, n0 = tn * 128;
+    const int nkt = (op.K + 127) / 128;
+    I8Loads at;
+    at.init(op, m0, n0, wave, lane);
+    const uint32_t lds0 = lds_base_sgpr(lds) + 1024u * wave;
+    auto load_step = [&](int st) __attribute__((always_inline)) {
+        at.load_a(0, lds0 + STAGE * st);
+        at.load_a(1, lds0 + STAGE * st + SUB);
+        at.load_b(0, lds0 + STAGE * st + 2 * SUB);
+        at.load_b(1, lds0 + STAGE * st + 3 * SUB);
+        at.k += 128;
+    };
+    int fa[2], fb[2];  // byte offsets in a stage
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk) {
+        const int x = ((4 * kk + g) ^ row_swz(l16)) * 16;
+        fa[kk] = wm * SUB + 128 * l16 + x;
+        fb[kk] = (2 + (wn >> 1)) * SUB + 128 * (32 * (wn & 1) + l16) + x;
+    }
+    i32x4 acc[4][2];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+            acc[i][j] = i32x4{};
+    const int first = min(nkt, NST - 1);
+    for (int kt = 0; kt < first; ++kt)
+        load_step(kt);
+    if (nkt > NST - 2)
+        wait_and_barrier<4 * (NST - 2)>();
+    else
+        wait_and_barrier<0>();
+    if (wm == 1)
+        plain_barrier();
+    int rs = 0, ws = NST - 1;  // the stages read and refilled by a step
+    for (int kt = 0; kt < nkt; ++kt) {
+        const int8_t *st = lds + rs * STAGE;
+        u32x4 a[4][2], b[2][2];
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk) {
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+                b[j][kk] = *reinterpret_cast<const u32x4 *>(st + fb[kk] + 2048 * j);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                a[i][kk] = *reinterpret_cast<const u32x4 *>(st + fa[kk] + 2048 * i);
+        }
+        // The stage that the step before has read is refilled; before the
+        // next step starts, its own loads have to be there (the steps after
+        // it may be in flight).
+        const int ahead = nkt - 1 - kt;  // steps after this one
+        if (ahead >= NST - 1) {
+            load_step(ws);
+            wait_and_barrier<4 * (NST - 2)>();
+        } else if (ahead == 2) {
+            wait_and_barrier<4>();
+        } else {
+            wait_and_barrier<0>();
+        }
+        ws = rs;
+        rs = rs + 1 == NST ? 0 : rs + 1;
+        __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+                    acc[i][j] = mfma_i8(b[j][kk], a[i][kk], acc[i][j]);  // rows n, columns m
+        __builtin_amdgcn_s_setprio(0);
+        plain_barrier();
+    }
+    if (wm == 0)
+        plain_barrier();
+
+    // Accumulator (i, j), register e: row m = 64 wm + 16 i + l16, column n =
+    // 32 wn + 16 j + 4 g + e of the tile.
+    __syncthreads();
+    uint16_t *image = reinterpret_cast<uint16_t *>(lds);
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        const int c = 32 * wn + 16 * j + 4 * g;
+        float rb[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            rb[e] = op.sb[min(n0 + c + e, op.N - 1)];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int r = 64 * wm + 16 * i + l16;
+            *reinterpret_cast<bf16x4 *>(image + image_off<128>(r, c)) =
+                scaled(op, acc[i][j], op.sa[min(m0 + r, op.M - 1)], rb, m0 + r, n0 + c);
+        }
+    }
+    __syncthreads();
+    store_image<128, 128>(image, op, m0, n0, tid);
+}
+
+// At most 64 tokens: the weights are read once, straight into registers, 16
+// NB rows of them per workgroup; its eight waves share K in turns of 64 and add
+// their sums through LDS.  MB blocks of 16 tokens.
+template <int MB, int NB>
+__global__ void __launch_bounds__(512)
+gemm_i8_few_kernel(GemmI8Operands op)
+{
+    constexpr int UN = MB * NB > 4 ? 2 : 4;  // turns whose loads are in flight
+    __shared__ __attribute__((aligned(16))) int sums[8][MB * NB][4][64];
+    const int tid = threadIdx.x;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+    const int l16 = lane & 15, g = lane >> 4;
+    const int n0 = static_cast<int>(blockIdx.x) * 16 * NB;
+    const int8_t *pa[MB], *pb[NB];
+#pragma unroll
+    for (int i = 0; i < MB; ++i)
+        pa[i] = op.A + min(16 * i + l16, op.M - 1) * op.lda + 16 * g;
+#pragma unroll
+    for (int j = 0; j < NB; ++j)
+        pb[j] = op.B + min(n0 + 16 * j + l16, op.N - 1) * op.ldb + 16 * g;
+    i32x4 acc[MB][NB];
+#pragma unroll
+    for (int i = 0; i < MB; ++i)
+#pragma unroll
+        for (int j = 0; j < NB; ++j)
+            acc[i][j] = i32x4{};
+    for (int k0 = wave * 64; k0 < op.K; k0 += 512 * UN) {
+        u32x4 a[UN][MB], b[UN][NB];
+#pragma unroll
+        for (int u = 0; u < UN; ++u) {
+            const int k = k0 + 512 * u;
+            const bool in = k + 16 * g < op.K;
+#pragma unroll
+            for (int j = 0; j < NB; ++j)
+                b[u][j] = in ? *reinterpret_cast<const u32x4 *>(pb[j] + k) : u32x4{0u, 0u, 0u, 0u};
+#pragma unroll
+            for (int i = 0; i < MB; ++i)
+                a[u][i] = in ? *reinterpret_cast<const u32x4 *>(pa[i] + k) : u32x4{0u, 0u, 0u, 0u};
+        }
+#pragma unroll
+        for (int u = 0; u < UN; ++u)
+#pragma unroll
+            for (int i = 0; i < MB; ++i)
+#pragma unroll
+                for (int j = 0; j < NB; ++j)
+                    acc[i][j] = mfma_i8(b[u][j], a[u][i], acc[i][j]);  // rows n, columns m
+    }
+#pragma unroll
+    for (int i = 0; i < MB; ++i)
+#pragma unroll
+        for (int j = 0; j < NB; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                sums[wave][i * NB + j][e][lane] = acc[i][j][e];
+    __syncthreads();
+    // Element (m, n) of the workgroup: block (m / 16, n / 16), register n % 4
+    // of lane 16 (n % 16 / 4) + m % 16.
+    for (int idx = tid; idx < 256 * MB * NB; idx += 512) {
+        const int m = idx / (16 * NB), c = idx % (16 * NB), n = n0 + c;
+        if (m >= op.M || n >= op.N)
+            continue;
+        const int blk = (m >> 4) * NB + (c >> 4), ln = 16 * ((c & 15) >> 2) + (m & 15);
+        int s = 0;
+#pragma unroll
+        for (int w = 0; w < 8; ++w)
+            s += sums[w][blk][c & 3][ln];
+        const long long at = m * op.ldc + n;
+        float v = static_cast<float>(s) * op.sa[m] * op.sb[n];
+        if (op.R != nullptr)
+            v += bf16_at(op.R + at);
+        op.C[at] = __builtin_bit_cast(uint16_t, static_cast<__bf16>(v));
+    }
 }
 
 int launch_gemm_i8(const GemmI8Args &a)
 {
-    const GemmI8Operands op{static_cast<const int8_t *>(a.A), static_cast<const int8_t *>(a.B),
-                            a.sa, a.sb, static_cast<const uint16_t *>(a.R),
-                            static_cast<uint16_t *>(a.C), a.lda, a.ldb, a.ldc, a.M, a.N, a.K,
-                            (a.N + 63) / 64};
-    const dim3 grid(static_cast<unsigned>((a.M + 63) / 64) * op.tiles_n);
-    const hipError_t e =
-        launch_kernel(gemm_i8_kernel, grid, dim3(256), static_cast<hipStream_t>(a.stream), op);
+    hipStream_t st = static_cast<hipStream_t>(a.stream);
+    GemmI8Operands op{static_cast<const int8_t *>(a.A), static_cast<const int8_t *>(a.B), a.sa,
+                      a.sb, static_cast<const uint16_t *>(a.R), static_cast<uint16_t *>(a.C),
+                      a.lda, a.ldb, a.ldc, a.M, a.N, a.K, 0, 0, 0, false};
+    op.wide = a.ldc % 8 == 0 && reinterpret_cast<uintptr_t>(a.C) % 16 == 0 &&
+              reinterpret_cast<uintptr_t>(a.R) % 16 == 0;
+    const GemmI8Tile tile = gemm_i8_tile(a.M, a.N, a.K, device_cu_count());
+    if (tile == GemmI8Tile::kFew) {
+        const int mb = (a.M + 15) / 16;
+        const bool two = a.N > 16 * 1024;
+        auto run = [&](auto m) {
+            constexpr int MB = decltype(m)::value;
+            const int cols = two ? 32 : 16;
+            return launch_kernel(two ? gemm_i8_few_kernel<MB, 2> : gemm_i8_few_kernel<MB, 1>,
+                                 dim3(static_cast<unsigned>((a.N + cols - 1) / cols)), dim3(512),
+                                 st, op);
+        };
+        const hipError_t e = mb == 1 ? run(IC<1>{}) : mb == 2 ? run(IC<2>{}) : run(IC<4>{});
+        return e == hipSuccess ? DD_OK : DD_ERR_HIP;
+    }
+    const int edge = tile == GemmI8Tile::kLarge ? 256 : 128;
+    op.tiles_m = (a.M + edge - 1) / edge;
+    op.tiles_n = (a.N + edge - 1) / edge;
+    op.xm = tile_rows_step(op.tiles_m, op.tiles_n);
+    const dim3 grid(static_cast<unsigned>(op.tiles_m) * static_cast<unsigned>(op.tiles_n));
+    const hipError_t e = launch_kernel(
+        tile == GemmI8Tile::kLarge ? gemm_i8_kernel : gemm_i8_small_kernel, grid, dim3(512), st, op);
     return e == hipSuccess ? DD_OK : DD_ERR_HIP;
 }
 

@@ -171,4 +171,23 @@ inline GemmPlan gemm_plan(int M, long long N, long long K, bool may_split, int c
     }
 }
 
+// How an int8 product of M x N over K runs: few tokens with the weights
+// straight into registers, or on tiles of 128 x 128 or 256 x 256.
+enum class GemmI8Tile { kFew, kSmall, kLarge };
+
+inline GemmI8Tile gemm_i8_tile(int M, int N, int K, int cus)
+{
+    if (M <= 64)
+        return GemmI8Tile::kFew;
+    cus = std::max(cus, 1);
+    auto rounds = [&](int edge) {
+        const double tiles = std::ceil(M / static_cast<double>(edge)) * std::ceil(N / static_cast<double>(edge));
+        return std::ceil(tiles / cus);
+    };
+    const double steps = std::ceil(K / 128.0);
+    return rounds(128) * (steps * 0.5 + 6.0) < rounds(256) * (steps * 1.2 + 6.0)
+               ? GemmI8Tile::kSmall
+               : GemmI8Tile::kLarge;
+}
+
 }  // namespace dd
