@@ -32,7 +32,7 @@ HIP_SOURCES = ["dd_fwd.hip", "dd_bwd.hip", "dd_dkdv.hip", "dd_bwd_short.hip", "d
 # faster for every other kernel.
 _ILP = ["-mllvm", "-amdgpu-sched-strategy=max-ilp"]
 HIP_SOURCE_FLAGS = {"dd_dkdv.hip": _ILP, "dd_bwd_short.hip": _ILP, "dd_gemm.hip": _ILP,
-                    "dd_gemm_i8.hip": _ILP}
+                    "dd_gemm_i8.hip": _ILP, "dd_wgrad_i8.hip": _ILP}
 CXX_SOURCES = ["dd_api.cpp", "dd_api8.cpp"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 # Packed fp32 VALU forms are disabled for all device code.

@@ -190,4 +190,32 @@ inline GemmI8Tile gemm_i8_tile(int M, int N, int K, int cus)
                : GemmI8Tile::kLarge;
 }
 
+// How a weight gradient of M x N over T tokens runs: tiles of 256 x 256 or
+// 128 x 128 (`edge`), T in `splits` parts of k_len tokens (a multiple of 64).
+struct WgradPlan {
+    int edge, splits, k_len, tiles_m, tiles_n;
+};
+
+inline WgradPlan wgrad_plan(int T, int M, int N, int cus)
+{
+    cus = std::max(cus, 1);
+    const long long steps = (T + 63LL) / 64;
+    WgradPlan best{};
+    double cost = -1;
+    for (const int edge : {256, 128}) {
+        const long long tm = (M + edge - 1LL) / edge, tn = (N + edge - 1LL) / edge;
+        for (int s = 1; s == 1 || (s <= 32 && steps / s >= 8); ++s) {
+            const double c = gemm_cost(static_cast<double>(tm * tn), cus, static_cast<double>(steps), s,
+                                       static_cast<double>(tm * tn) * edge * edge,
+                                       edge == 256 ? GemmPlan::kLarge : GemmPlan::kSmall);
+            if (cost < 0 || c < cost) {
+                cost = c;
+                best = WgradPlan{edge, s, static_cast<int>((steps + s - 1) / s * 64),
+                                 static_cast<int>(tm), static_cast<int>(tn)};
+            }
+        }
+    }
+    return best;
+}
+
 }  // namespace dd

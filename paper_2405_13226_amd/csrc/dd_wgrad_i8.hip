@@ -4,93 +4,539 @@
 // The restored input is bf16, as the activation that was saved; the products
 // are bf16 matrix-core products with fp32 sums.  Any T, M and N (M and N
 // multiples of 8).
+//
+// Two launches, or three.  The first restores X, transposed: XT [M][T] in the
+// workspace, T padded with zeros to whole K steps.  The product then reads XT
+// along its rows and dY, as it is stored, transposed, with the loop of the
+// bf16 product (dd_gemm.hip).  With a split T axis, whose parts leave fp32
+// tiles in the workspace, a last launch adds those.
 #include "dd_device.hpp"
 #include "dd_tile.hpp"
+#include "dd_gemm.hpp"
 #include "dd_internal.h"
 #include "dd_launch.hpp"
+#include "dd_routes.hpp"
 #include "dd_attn.h"
+
+#include <algorithm>
 
 namespace dd {
 
-struct WgradI8Operands {
-    const int8_t *Q;
-    const float *scales;
-    const uint16_t *dY;
-    uint16_t *dW;
-    long long ldq, ldy, ldw;
-    int T, M, N, tiles_n;
-};
+typedef uint32_t codes16 __attribute__((ext_vector_type(4), aligned(8)));
 
-// One workgroup per 64 x 64 tile, 32 x 32 per wave, 64 tokens a step: both
-// operands row by row (tokens) into LDS, read transposed.
+// XT[m][t] = bf16(scales[t] Q[t][m]), zeros for T <= t < Tp.  One 128 x 128
+// tile per workgroup: rows of codes into LDS as bf16, then its transposing
+// reads, eight tokens of a column per lane.
 __global__ void __launch_bounds__(256)
-wgrad_i8_kernel(WgradI8Operands op)
+restore_kernel(const int8_t *__restrict__ Q, long long ldq, const float *__restrict__ scales,
+               uint16_t *__restrict__ XT, long long Tp, int T, int M)
 {
-    __shared__ __attribute__((aligned(16))) uint16_t xs[64 * 64], ys[64 * 64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, g = lane >> 4;
-    const int e4 = l16 >> 2, c4 = l16 & 3;
-    const int m0 = static_cast<int>(blockIdx.x) / op.tiles_n * 64;
-    const int n0 = static_cast<int>(blockIdx.x) % op.tiles_n * 64;
-    f32x4 acc[2][2] = {};
-    for (int t0 = 0; t0 < op.T; t0 += 64) {
+    // Four sub-tiles of 64 columns x 64 tokens.
+    __shared__ __attribute__((aligned(16))) uint16_t lds[4 * 64 * 64];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const long long t0 = static_cast<long long>(blockIdx.x) * 128;
+    const int m0 = static_cast<int>(blockIdx.y) * 128;
+    const int c = (tid & 7) * 16;
+    u32x4 q[4];
+    float s[4];
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int r = (threadIdx.x >> 3) + 32 * i, c = (threadIdx.x & 7) * 8, t = t0 + r;
-            float x[8] = {};
-            u32x4 y = {0u, 0u, 0u, 0u};
-            if (t < op.T && m0 + c < op.M) {
-                const float s = op.scales[t];
-                const u32x2 u = *reinterpret_cast<const u32x2 *>(op.Q + t * op.ldq + m0 + c);
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    x[e] = s * static_cast<float>(static_cast<int8_t>(u[e >> 2] >> 8 * (e & 3)));
+    for (int i = 0; i < 4; ++i) {
+        const long long t = t0 + (tid >> 3) + 32 * i;
+        const int8_t *p = Q + t * ldq + m0 + c;
+        q[i] = u32x4{0u, 0u, 0u, 0u};
+        s[i] = 0.f;
+        if (t < T) {
+            s[i] = scales[t];
+            if (m0 + c + 16 <= M) {
+                q[i] = *reinterpret_cast<const codes16 *>(p);
+            } else if (m0 + c + 8 <= M) {
+                const u32x2 v = *reinterpret_cast<const u32x2 *>(p);
+                q[i][0] = v[0];
+                q[i][1] = v[1];
             }
-            if (t < op.T && n0 + c < op.N)
-                y = *reinterpret_cast<const u32x4 *>(op.dY + t * op.ldy + n0 + c);
-            *reinterpret_cast<u32x4 *>(xs + tile_off<64>(r, c)) = pack8f(x);
-            *reinterpret_cast<u32x4 *>(ys + tile_off<64>(r, c)) = y;
         }
-        __syncthreads();
-#pragma unroll
-        for (int kk = 0; kk < 2; ++kk) {
-            bf16x8 a[2], b[2];
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const int r = 32 * kk + 8 * g + e4;
-                const int cm = 32 * (wave >> 1) + 16 * i + 4 * c4, cn = 32 * (wave & 1) + 16 * i + 4 * c4;
-                a[i] = join(lds_tr4(xs + tile_off<64>(r, cm)), lds_tr4(xs + tile_off<64>(r + 4, cm)));
-                b[i] = join(lds_tr4(ys + tile_off<64>(r, cn)), lds_tr4(ys + tile_off<64>(r + 4, cn)));
-            }
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-#pragma unroll
-                for (int j = 0; j < 2; ++j)
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b[j], a[i], acc[i][j], 0, 0, 0);
-        }
-        __syncthreads();
     }
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int i = 0; i < 4; ++i) {
+        const int r = (tid >> 3) + 32 * i;  // token of the tile
+        uint16_t *sub = lds + (2 * (r >> 6) + (c >> 6)) * 4096;
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const int m = m0 + 32 * (wave >> 1) + 16 * i + l16;
-            const int n = n0 + 32 * (wave & 1) + 16 * j + 4 * g;
-            const f32x4 v = acc[i][j];
-            if (m < op.M && n < op.N)
-                *reinterpret_cast<bf16x4 *>(op.dW + m * op.ldw + n) = pack4(v[0], v[1], v[2], v[3]);
+        for (int h = 0; h < 2; ++h) {
+            float f[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                f[e] = s[i] * static_cast<float>(static_cast<int8_t>(q[i][2 * h + (e >> 2)] >> 8 * (e & 3)));
+            *reinterpret_cast<u32x4 *>(sub + tile_off<64>(r & 63, (c & 63) + 8 * h)) = pack8f(f);
         }
+    }
+    __syncthreads();
+    // 128 columns x 16 pieces of eight tokens; 16 columns and four pieces per
+    // wave instruction.
+    const int l16 = lane & 15, g = lane >> 4, e4 = l16 >> 2, c4 = l16 & 3;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int blk = wave * 2 + (i & 1), piece = (i >> 1) * 4 + g;  // columns 16 blk ..
+        const uint16_t *sub = lds + (2 * (piece >> 3) + (blk >> 2)) * 4096;
+        const int r = 8 * (piece & 7) + e4, col = 16 * (blk & 3) + 4 * c4;
+        const bf16x8 v =
+            join(lds_tr4(sub + tile_off<64>(r, col)), lds_tr4(sub + tile_off<64>(r + 4, col)));
+        const int m = m0 + 16 * blk + l16;
+        const long long t = t0 + 8 * piece;
+        if (m < M && t < Tp)
+            *reinterpret_cast<bf16x8 *>(XT + m * Tp + t) = v;
+    }
 }
 
-size_t wgrad_i8_workspace_bytes(int, int, int) { return 0; }
+// P: fp32 partial tiles [splits][tiles_m][tiles_n][BM][BN], or NULL.
+struct WgradOperands {
+    const uint16_t *XT, *dY;
+    uint16_t *dW;
+    float *P;
+    long long Tp, ldy, ldw;
+    int T, M, N, k_len, tiles_m, tiles_n, xm;
+};
+
+// Direct loads of a tile's K steps.  XT: 64 columns (rows of XT) of a step are
+// a sub-tile, 128-byte rows in chunks swizzled for row reads; dY: the step's
+// 64 tokens x 64 columns, swizzled for transposing reads.  Columns of XT
+// behind M are the last one again and tokens behind T read as zeros in dY;
+// what columns behind N read is not stored.
+struct WgradLoads {
+    const uint16_t *a;
+    uint64_t b;           // address of dY's rows of the step, columns n0 ..
+    long long b_left;     // bytes from there to the end of dY
+    u32x4 buf;
+    uint32_t va[4], vb;
+    long long b_step;
+
+    template <int NA>
+    __device__ __forceinline__ void init(const WgradOperands &op, int m0, int n0, long long kbeg,
+                                         int wave, int lane)
+    {
+        const int r = 8 * wave + (lane >> 3);
+        a = op.XT + m0 * op.Tp + kbeg;
+#pragma unroll
+        for (int s = 0; s < NA; ++s)
+            va[s] = static_cast<uint32_t>(min(64 * s + r, op.M - 1 - m0) * op.Tp * 2 +
+                                          ((lane & 7) ^ row_swz(r)) * 16);
+        b = reinterpret_cast<uint64_t>(op.dY + kbeg * op.ldy + n0);
+        b_left = ((op.T - 1LL - kbeg) * op.ldy + op.N - n0) * 2;
+        b_step = 64 * op.ldy * 2;
+        vb = static_cast<uint32_t>((r * op.ldy + ((lane & 7) ^ swz<64>(r)) * 8) * 2);
+        buf = buffer_of(reinterpret_cast<const void *>(b), b_left);
+    }
+    __device__ __forceinline__ void next()
+    {
+        a += 64;
+        b += b_step;
+        b_left -= b_step;
+        buf = buffer_of(reinterpret_cast<const void *>(b), b_left);
+    }
+    __device__ __forceinline__ void load_a(int s, uint32_t l) const { dma_b128_off(a, va[s], l); }
+    __device__ __forceinline__ void load_b(int s, uint32_t l) const
+    {
+        dma_b128_buf(buf, vb + 128u * s, l);
+    }
+};
+
+__device__ __forceinline__ f32x4 mfma16w(bf16x8 a, bf16x8 b, f32x4 c)
+{
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+
+// LDS image of the finished tile, as in dd_gemm_i8.hip.
+template <int BN>
+__device__ __forceinline__ int wgrad_off(int r, int c)
+{
+    return r * BN + 4 * ((c >> 2) ^ (2 * (r & 15)));
+}
+
+template <int BM, int BN>
+__device__ __forceinline__ void wgrad_store(const uint16_t *lds, const WgradOperands &op, int m0,
+                                            int n0, int tid)
+{
+    constexpr int CPR = BN / 8;
+#pragma unroll 4
+    for (int it = 0; it < BM * CPR / 512; ++it) {
+        const int idx = it * 512 + tid, r = idx / CPR, c = idx % CPR * 8;
+        const u32x4 v = *reinterpret_cast<const u32x4 *>(lds + wgrad_off<BN>(r, c));
+        if (m0 + r < op.M && n0 + c < op.N)
+            *reinterpret_cast<u32x4 *>(op.dW + (m0 + r) * op.ldw + n0 + c) = v;
+    }
+}
+
+// 256 x 256 tiles, the phases of dd_gemm.hip.
+template <bool SPLIT>
+__global__ void __launch_bounds__(512, 1)
+wgrad_kernel(WgradOperands op)
+{
+    constexpr int SUB = 64 * 64, HALF = 2 * SUB, SIDE = 4 * HALF;  // elements
+    __shared__ __attribute__((aligned(1024))) uint16_t lds[2 * SIDE];
+    const int tid = threadIdx.x;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+    const int l16 = lane & 15, g = lane >> 4;
+    const int wm = wave >> 2, wn = wave & 3;
+    int tm, tn;
+    tile_of(static_cast<int>(blockIdx.x), op.tiles_m, op.tiles_n, op.xm, tm, tn);
+    const int m0 = tm * 256, n0 = tn * 256;
+    const int nkt = op.k_len / 64;
+    WgradLoads at;
+    at.init<4>(op, m0, n0, static_cast<long long>(blockIdx.y) * op.k_len, wave, lane);
+    const uint32_t lds0 = lds_base_sgpr(lds) + 1024u * wave;
+    auto load_a = [&](int h, int S) __attribute__((always_inline)) {
+        const uint32_t l = lds0 + 2u * (2 * h + S) * HALF;
+        at.load_a(2 * h, l);
+        at.load_a(2 * h + 1, l + 2u * SUB);
+    };
+    auto load_b = [&](int h, int S) __attribute__((always_inline)) {
+        const uint32_t l = lds0 + 2u * (SIDE + (2 * h + S) * HALF);
+        at.load_b(2 * h, l);
+        at.load_b(2 * h + 1, l + 2u * SUB);
+    };
+    const int e4 = l16 >> 2, c4 = l16 & 3;
+    const uint16_t *fa[2], *fb[4];
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk)
+        fa[kk] = lds + wm * SUB + 64 * l16 + (((4 * kk + g) ^ row_swz(l16)) << 3);
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        fb[j] = lds + SIDE + (wn >> 1) * SUB +
+                tile_off<64>(8 * g + 4 * (j & 1) + e4, 32 * (wn & 1) + 16 * (j >> 1) + 4 * c4);
+    bf16x8 a0[4][2], a1[4][2], b0[2][2], b1[2][2];
+    auto read_a = [&](bf16x8 (&f)[4][2], int h, int S) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int kk = 0; kk < 2; ++kk)
+                f[i][kk] = lds_row8(fa[kk] + ((2 * h + S) * HALF + 1024 * i));
+    };
+    auto read_b = [&](bf16x8 (&f)[2][2], int h, int S) __attribute__((always_inline)) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int kk = 0; kk < 2; ++kk) {
+                const int o = (2 * h + S) * HALF + 2048 * kk;
+                f[j][kk] = join(lds_tr4(fb[2 * j] + o), lds_tr4(fb[2 * j + 1] + o));
+            }
+    };
+    f32x4 acc[2][2][4][2];  // [A half][B half][i][j]
+#pragma unroll
+    for (int x = 0; x < 4; ++x)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+                acc[x >> 1][x & 1][i][j] = f32x4{};
+    auto multiply = [&](f32x4 (&c)[4][2], const bf16x8 (&a)[4][2],
+                        const bf16x8 (&b)[2][2]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+                    c[i][j] = mfma16w(b[j][kk], a[i][kk], c[i][j]);  // rows n, columns m
+    };
+    auto products = [&](f32x4 (&c)[4][2], const bf16x8 (&a)[4][2],
+                        const bf16x8 (&b)[2][2]) __attribute__((always_inline)) {
+        __builtin_amdgcn_s_setprio(1);
+        multiply(c, a, b);
+        __builtin_amdgcn_s_setprio(0);
+        plain_barrier();
+    };
+    // One K step from stage S.  MODE 0: also starts the loads of the step
+    // after the next one; 1, 2: the last step but one, the last step.
+    auto step = [&](auto stage, auto mode) __attribute__((always_inline)) {
+        constexpr int S = decltype(stage)::value, MODE = decltype(mode)::value;
+        read_b(b0, 0, S);
+        if constexpr (MODE == 0)
+            load_a(0, S);
+        wait_and_barrier<MODE == 0 ? 12 : MODE == 1 ? 10 : 2>();
+        products(acc[0][0], a0, b0);
+        read_b(b1, 1, S);
+        if constexpr (MODE == 0)
+            load_b(0, S);
+        wait_and_barrier<MODE == 0 ? 12 : MODE == 1 ? 8 : 0>();
+        products(acc[0][1], a0, b1);
+        read_a(a1, 1, S);
+        if constexpr (MODE == 0)
+            load_b(1, S);
+        wait_and_barrier<MODE == 0 ? 12 : MODE == 1 ? 6 : 0>();
+        products(acc[1][1], a1, b1);
+        if constexpr (MODE != 2)
+            read_a(a0, 0, 1 - S);
+        if constexpr (MODE == 0) {
+            load_a(1, S);
+            at.next();
+        }
+        wait_and_barrier<MODE == 0 ? 12 : MODE == 1 ? 4 : 0>();
+        products(acc[1][0], a1, b0);
+    };
+    auto load_step = [&](int S) __attribute__((always_inline)) {
+        load_a(0, S);
+        load_b(0, S);
+        load_b(1, S);
+        load_a(1, S);
+        at.next();
+    };
+    if (nkt == 1) {
+        load_step(0);
+        wait_and_barrier<0>();
+        read_a(a0, 0, 0);
+        read_b(b0, 0, 0);
+        multiply(acc[0][0], a0, b0);
+        read_b(b1, 1, 0);
+        multiply(acc[0][1], a0, b1);
+        read_a(a1, 1, 0);
+        multiply(acc[1][1], a1, b1);
+        multiply(acc[1][0], a1, b0);
+    } else {
+        const int s0 = nkt & 1;
+        load_step(s0);
+        load_step(1 - s0);
+        wait_and_barrier<8>();
+        read_a(a0, 0, s0);
+        // Phase 1 refills the half just read: only after a barrier that every
+        // wave reaches with its reads returned.
+        wait_and_barrier<8>();
+        // Waves 4-7 run half a phase behind waves 0-3.
+        if (wm == 1)
+            plain_barrier();
+        for (int kt = 2 - s0; kt < nkt; kt += 2) {
+            if (kt > 1)
+                step(IC<0>{}, IC<0>{});
+            step(IC<1>{}, IC<0>{});
+        }
+        step(IC<0>{}, IC<1>{});
+        step(IC<1>{}, IC<2>{});
+        if (wm == 0)
+            plain_barrier();
+    }
+
+    // Accumulator (ha, hb, i, j), register e: row m = 128 ha + 64 wm + 16 i +
+    // l16, column n = 128 hb + 32 wn + 16 j + 4 g + e of the tile.
+    float *part = op.P + ((static_cast<long long>(blockIdx.y) * op.tiles_m + tm) * op.tiles_n + tn) *
+                             (256 * 256);
+    if constexpr (!SPLIT)
+        __syncthreads();
+#pragma unroll
+    for (int x = 0; x < 16; ++x) {
+        const int ha = x >> 3, i = (x >> 1) & 3, hb = x & 1, r = 128 * ha + 64 * wm + 16 * i + l16;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const int c = 128 * hb + 32 * wn + 16 * j + 4 * g;
+            const f32x4 v = acc[ha][hb][i][j];
+            if constexpr (SPLIT)
+                *reinterpret_cast<f32x4 *>(part + r * 256 + c) = v;
+            else
+                *reinterpret_cast<bf16x4 *>(lds + wgrad_off<256>(r, c)) =
+                    pack4(v[0], v[1], v[2], v[3]);
+        }
+    }
+    if constexpr (!SPLIT) {
+        __syncthreads();
+        wgrad_store<256, 256>(lds, op, m0, n0, tid);
+    }
+}
+
+// 128 x 128 tiles for gradients whose large tiles would leave CUs idle: a
+// phase of 16 products of every wave per K step, four stages of which three
+// are in flight (128 KiB).
+template <bool SPLIT>
+__global__ void __launch_bounds__(512, 1)
+wgrad_small_kernel(WgradOperands op)
+{
+    constexpr int SUB = 64 * 64, STAGE = 4 * SUB, NST = 4;  // elements
+    __shared__ __attribute__((aligned(1024))) uint16_t lds[NST * STAGE];
+    const int tid = threadIdx.x;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+    const int l16 = lane & 15, g = lane >> 4;
+    const int wm = wave >> 2, wn = wave & 3;
+    int tm, tn;
+    tile_of(static_cast<int>(blockIdx.x), op.tiles_m, op.tiles_n, op.xm, tm, tn);
+    const int m0 = tm * 128, n0 = tn * 128;
+    const int nkt = op.k_len / 64;
+    WgradLoads at;
+    at.init<2>(op, m0, n0, static_cast<long long>(blockIdx.y) * op.k_len, wave, lane);
+    const uint32_t lds0 = lds_base_sgpr(lds) + 1024u * wave;
+    auto load_step = [&](int st) __attribute__((always_inline)) {
+        const uint32_t l = lds0 + 2u * STAGE * st;
+        at.load_a(0, l);
+        at.load_a(1, l + 2u * SUB);
+        at.load_b(0, l + 4u * SUB);
+        at.load_b(1, l + 6u * SUB);
+        at.next();
+    };
+    const int e4 = l16 >> 2, c4 = l16 & 3;
+    int fa[2], fb[4];  // element offsets in a stage
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk)
+        fa[kk] = wm * SUB + 64 * l16 + (((4 * kk + g) ^ row_swz(l16)) << 3);
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        fb[j] = (2 + (wn >> 1)) * SUB +
+                tile_off<64>(8 * g + 4 * (j & 1) + e4, 32 * (wn & 1) + 16 * (j >> 1) + 4 * c4);
+    f32x4 acc[4][2];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+            acc[i][j] = f32x4{};
+    const int first = min(nkt, NST - 1);
+    for (int kt = 0; kt < first; ++kt)
+        load_step(kt);
+    if (nkt > NST - 2)
+        wait_and_barrier<4 * (NST - 2)>();
+    else
+        wait_and_barrier<0>();
+    if (wm == 1)
+        plain_barrier();
+    int rs = 0, ws = NST - 1;  // the stages read and refilled by a step
+    for (int kt = 0; kt < nkt; ++kt) {
+        const uint16_t *st = lds + rs * STAGE;
+        bf16x8 a[4][2], b[2][2];
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk) {
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+                b[j][kk] = join(lds_tr4(st + fb[2 * j] + 2048 * kk),
+                                lds_tr4(st + fb[2 * j + 1] + 2048 * kk));
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                a[i][kk] = lds_row8(st + fa[kk] + 1024 * i);
+        }
+        // The stage that the step before has read is refilled; before the
+        // next step starts, its own loads have to be there (the steps after
+        // it may be in flight).
+        const int ahead = nkt - 1 - kt;  // steps after this one
+        if (ahead >= NST - 1) {
+            load_step(ws);
+            wait_and_barrier<4 * (NST - 2)>();
+        } else if (ahead == 2) {
+            wait_and_barrier<4>();
+        } else {
+            wait_and_barrier<0>();
+        }
+        ws = rs;
+        rs = rs + 1 == NST ? 0 : rs + 1;
+        __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+                    acc[i][j] = mfma16w(b[j][kk], a[i][kk], acc[i][j]);  // rows n, columns m
+        __builtin_amdgcn_s_setprio(0);
+        plain_barrier();
+    }
+    if (wm == 0)
+        plain_barrier();
+
+    // Accumulator (i, j), register e: row m = 64 wm + 16 i + l16, column n =
+    // 32 wn + 16 j + 4 g + e of the tile.
+    float *part = op.P + ((static_cast<long long>(blockIdx.y) * op.tiles_m + tm) * op.tiles_n + tn) *
+                             (128 * 128);
+    if constexpr (!SPLIT)
+        __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const int r = 64 * wm + 16 * i + l16, c = 32 * wn + 16 * j + 4 * g;
+            const f32x4 v = acc[i][j];
+            if constexpr (SPLIT)
+                *reinterpret_cast<f32x4 *>(part + r * 128 + c) = v;
+            else
+                *reinterpret_cast<bf16x4 *>(lds + wgrad_off<128>(r, c)) =
+                    pack4(v[0], v[1], v[2], v[3]);
+        }
+    if constexpr (!SPLIT) {
+        __syncthreads();
+        wgrad_store<128, 128>(lds, op, m0, n0, tid);
+    }
+}
+
+// dW = the sum of the partial tiles over the splits, 8 elements per thread.
+template <int EDGE>
+__global__ void __launch_bounds__(256)
+wgrad_reduce_kernel(WgradOperands op, int splits)
+{
+    constexpr int PER = EDGE * EDGE / 8 / 256;  // workgroups per tile
+    const int tile = static_cast<int>(blockIdx.x) / PER;
+    const int v = static_cast<int>(blockIdx.x) % PER * 256 + threadIdx.x;
+    const int m = tile / op.tiles_n * EDGE + v / (EDGE / 8);
+    const int n = tile % op.tiles_n * EDGE + v % (EDGE / 8) * 8;
+    if (m >= op.M || n >= op.N)
+        return;
+    const float *p = op.P + static_cast<long long>(tile) * EDGE * EDGE + v * 8;
+    const long long step = static_cast<long long>(op.tiles_m) * op.tiles_n * EDGE * EDGE;
+    f32x4 s0 = *reinterpret_cast<const f32x4 *>(p), s1 = *reinterpret_cast<const f32x4 *>(p + 4);
+    for (int s = 1; s < splits; ++s) {
+        s0 += *reinterpret_cast<const f32x4 *>(p + s * step);
+        s1 += *reinterpret_cast<const f32x4 *>(p + s * step + 4);
+    }
+    *reinterpret_cast<bf16x8 *>(op.dW + m * op.ldw + n) =
+        join(pack4(s0[0], s0[1], s0[2], s0[3]), pack4(s1[0], s1[1], s1[2], s1[3]));
+}
+
+namespace {
+
+// The workspace's parts: XT, then the partial tiles.
+struct WgradSpace {
+    WgradPlan plan;
+    long long Tp;
+    size_t restored, partials;  // bytes
+};
+
+WgradSpace wgrad_space(int T, int M, int N)
+{
+    WgradSpace w;
+    const WgradPlan &p = w.plan = wgrad_plan(T, M, N, device_cu_count());
+    w.Tp = static_cast<long long>(p.k_len) * p.splits;
+    w.restored = static_cast<size_t>(M) * w.Tp * 2;
+    w.partials = p.splits > 1 ? static_cast<size_t>(p.splits) * p.tiles_m * p.tiles_n * p.edge *
+                                    p.edge * sizeof(float)
+                              : 0;
+    return w;
+}
+
+}  // namespace
+
+size_t wgrad_i8_workspace_bytes(int T, int M, int N)
+{
+    const WgradSpace w = wgrad_space(T, M, N);
+    return w.restored + w.partials;
+}
 
 int launch_wgrad_i8(const WgradI8Args &a)
 {
-    const WgradI8Operands op{static_cast<const int8_t *>(a.Q), a.scales,
-                             static_cast<const uint16_t *>(a.dY), static_cast<uint16_t *>(a.dW),
-                             a.ldq, a.ldy, a.ldw, a.T, a.M, a.N, (a.N + 63) / 64};
-    const dim3 grid(static_cast<unsigned>((a.M + 63) / 64) * op.tiles_n);
-    const hipError_t e =
-        launch_kernel(wgrad_i8_kernel, grid, dim3(256), static_cast<hipStream_t>(a.stream), op);
+    hipStream_t st = static_cast<hipStream_t>(a.stream);
+    const WgradSpace w = wgrad_space(a.T, a.M, a.N);
+    const WgradPlan &p = w.plan;
+    auto *xt = static_cast<uint16_t *>(a.workspace);
+    auto *parts = w.partials ? reinterpret_cast<float *>(static_cast<char *>(a.workspace) + w.restored)
+                             : nullptr;
+    hipError_t e = launch_kernel(restore_kernel,
+                                 dim3(static_cast<unsigned>((w.Tp + 127) / 128),
+                                      static_cast<unsigned>((a.M + 127) / 128)),
+                                 dim3(256), st, static_cast<const int8_t *>(a.Q), a.ldq, a.scales,
+                                 xt, w.Tp, a.T, a.M);
+    if (e != hipSuccess)
+        return DD_ERR_HIP;
+    const WgradOperands op{xt, static_cast<const uint16_t *>(a.dY), static_cast<uint16_t *>(a.dW),
+                           parts, w.Tp, a.ldy, a.ldw, a.T, a.M, a.N, p.k_len, p.tiles_m, p.tiles_n,
+                           tile_rows_step(p.tiles_m, p.tiles_n)};
+    const unsigned tiles = static_cast<unsigned>(p.tiles_m) * static_cast<unsigned>(p.tiles_n);
+    const auto kern = p.edge == 256 ? (parts ? wgrad_kernel<true> : wgrad_kernel<false>)
+                                    : (parts ? wgrad_small_kernel<true> : wgrad_small_kernel<false>);
+    e = launch_kernel(kern, dim3(tiles, static_cast<unsigned>(p.splits)), dim3(512), st, op);
+    if (e != hipSuccess || !parts)
+        return e == hipSuccess ? DD_OK : DD_ERR_HIP;
+    e = p.edge == 256 ? launch_kernel(wgrad_reduce_kernel<256>, dim3(tiles * 32), dim3(256), st, op,
+                                      p.splits)
+                      : launch_kernel(wgrad_reduce_kernel<128>, dim3(tiles * 8), dim3(256), st, op,
+                                      p.splits);
     return e == hipSuccess ? DD_OK : DD_ERR_HIP;
 }
 
