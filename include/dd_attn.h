@@ -331,7 +331,7 @@ size_t dd_rmsnorm_bwd_workspace_bytes(int rows, int d);
  *
  * dd_gemm_i8_wgrad: the weight gradient of a layer y = x W whose input was
  * kept as codes: dW [M][N] = X^T dY with X = bf16(scales Q), Q [T][M] int8,
- * dY [T][N] bf16, fp32 sums.  T >= 1, M and N multiples of 8; strides
+ * dY [T][N] bf16, fp32 sums.  1 <= T <= 2^25 - 64, M and N multiples of 8; strides
  * multiples of 8, ldq and ldy below 2^23; Q 8-byte, dY and dW 16-byte aligned.
  * dW must not overlap the inputs.  workspace: scratch of
  * dd_gemm_i8_wgrad_workspace_bytes(T, M, N) bytes, 16-byte aligned (may be

@@ -187,9 +187,10 @@ int dd_gemm_i8(const int8_t *A, long long lda, const float *sa, const int8_t *B,
 
 namespace {
 
+// T: the restored input's rows have to keep 32-bit offsets too (64 of them).
 bool wgrad_ok(int T, int M, int N)
 {
-    return T >= 1 && M >= 8 && N >= 8 && M % 8 == 0 && N % 8 == 0 && tiles64(M, N) <= kMaxTiles;
+    return T >= 1 && T <= (1 << 25) - 64 && M >= 8 && N >= 8 && M % 8 == 0 && N % 8 == 0 && tiles64(M, N) <= kMaxTiles;
 }
 
 }  // namespace

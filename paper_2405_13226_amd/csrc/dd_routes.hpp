@@ -190,28 +190,56 @@ inline GemmI8Tile gemm_i8_tile(int M, int N, int K, int cus)
                : GemmI8Tile::kLarge;
 }
 
-// How a weight gradient of M x N over T tokens runs: tiles of 256 x 256 or
-// 128 x 128 (`edge`), T in `splits` parts of k_len tokens (a multiple of 64).
+// How a weight gradient of M x N over T tokens runs: on tiles of 256 x 256 or
+// 128 x 128 (`edge`), T in `steps` of 64 tokens.  The first `whole` tiles are a
+// workgroup's each.  The others, fewer than the CUs, are shared out so that
+// every workgroup has `head` steps: one workgroup per tile takes its first
+// `head`, and the rest of them, one tile after the other, is cut into pieces
+// of `head` steps for `tails` further workgroups.  (In parts of equal length
+// 176 tiles of 1024 steps, 2048 x 5632 over 65,536 tokens, would be 2.75
+// rounds of 256 CUs at four parts each, which takes three.)
 struct WgradPlan {
-    int edge, splits, k_len, tiles_m, tiles_n;
+    int edge, tiles_m, tiles_n, whole, steps, head, tails;
+
+    int shared() const { return tiles_m * tiles_n - whole; }
+    int rest() const { return steps - head; }  // of a shared tile
+    // Parts of tiles that one of the `tails` can touch.
+    int most() const { return (head - 1) / std::max(rest(), 1) + 2; }
+    long long partials() const { return head ? shared() + static_cast<long long>(tails) * most() : 0; }
 };
 
 inline WgradPlan wgrad_plan(int T, int M, int N, int cus)
 {
     cus = std::max(cus, 1);
-    const long long steps = (T + 63LL) / 64;
+    const int steps = static_cast<int>((T + 63LL) / 64);
     WgradPlan best{};
     double cost = -1;
     for (const int edge : {256, 128}) {
-        const long long tm = (M + edge - 1LL) / edge, tn = (N + edge - 1LL) / edge;
-        for (int s = 1; s == 1 || (s <= 32 && steps / s >= 8); ++s) {
-            const double c = gemm_cost(static_cast<double>(tm * tn), cus, static_cast<double>(steps), s,
-                                       static_cast<double>(tm * tn) * edge * edge,
-                                       edge == 256 ? GemmPlan::kLarge : GemmPlan::kSmall);
+        const long long tm = (M + edge - 1LL) / edge, tn = (N + edge - 1LL) / edge, tiles = tm * tn;
+        const double step = edge == 256 ? 1.4 : 0.55;  // us, a full chip
+        const double light = edge == 256 ? 1.1 : 0.42;  // us, few workgroups
+        for (const bool share : {false, true}) {
+            const long long over = tiles % cus, full = tiles / cus;
+            WgradPlan p{edge, static_cast<int>(tm), static_cast<int>(tn), static_cast<int>(tiles),
+                        steps, 0, 0};
+            double c;
+            if (share) {
+                // Parts of at least 8 steps: shorter ones are mostly start-up.
+                p.head = static_cast<int>(std::max((over * steps + cus - 1) / cus, 8LL));
+                if (over == 0 || p.head >= steps)
+                    continue;
+                p.whole = static_cast<int>(tiles - over);
+                p.tails = static_cast<int>((over * p.rest() + p.head - 1) / p.head);
+                c = full * (steps * step + 6.0) + p.head * step + 6.0 + 8.0 +
+                    static_cast<double>(over + over + p.tails) * edge * edge * 8.0 / 4.0e6;
+            } else {
+                c = full * (steps * step + 6.0);
+                if (over)
+                    c += steps * (light + (step - light) * over / cus) + 6.0;
+            }
             if (cost < 0 || c < cost) {
                 cost = c;
-                best = WgradPlan{edge, s, static_cast<int>((steps + s - 1) / s * 64),
-                                 static_cast<int>(tm), static_cast<int>(tn)};
+                best = p;
             }
         }
     }

@@ -87,57 +87,104 @@ restore_kernel(const int8_t *__restrict__ Q, long long ldq, const float *__restr
     }
 }
 
-// P: fp32 partial tiles [splits][tiles_m][tiles_n][BM][BN], or NULL.
+// P: fp32 parts of the shared tiles: one per tile for its first `head` steps,
+// then `most` per further workgroup.
 struct WgradOperands {
     const uint16_t *XT, *dY;
     uint16_t *dW;
     float *P;
     long long Tp, ldy, ldw;
-    int T, M, N, k_len, tiles_m, tiles_n, xm;
+    int T, M, N, tiles_m, tiles_n, xm, whole, shared, steps, head, rest, most;
+};
+
+// The parts of tiles that workgroup `id` computes, one after the other: steps
+// `first` .. first + count - 1 of `tile`, stored to part `slot`, or as the
+// result (slot < 0).
+struct WgradParts {
+    int tile, first, count, slot;
+    int at, end;  // in the shared tiles' rests, laid out one after the other
+
+    __device__ __forceinline__ void init(const WgradOperands &op, int id)
+    {
+        at = end = 0;
+        if (id < op.whole) {
+            tile = id;
+            first = 0;
+            count = op.steps;
+            slot = -1;
+        } else if (id < op.whole + op.shared) {
+            tile = id;
+            first = 0;
+            count = op.head;
+            slot = id - op.whole;
+        } else {
+            const int w = id - op.whole - op.shared;
+            at = w * op.head;
+            end = min(at + op.head, op.shared * op.rest);
+            slot = op.shared + w * op.most - 1;
+            next(op);
+        }
+    }
+    __device__ __forceinline__ bool more() const { return at < end; }
+    __device__ __forceinline__ void next(const WgradOperands &op)
+    {
+        const int i = at / op.rest, skip = at - i * op.rest;
+        tile = op.whole + i;
+        first = op.head + skip;
+        count = min(op.rest - skip, end - at);
+        at += count;
+        ++slot;
+    }
 };
 
 // Direct loads of a tile's K steps.  XT: 64 columns (rows of XT) of a step are
 // a sub-tile, 128-byte rows in chunks swizzled for row reads; dY: the step's
-// 64 tokens x 64 columns, swizzled for transposing reads.  Columns of XT
-// behind M are the last one again and tokens behind T read as zeros in dY;
-// what columns behind N read is not stored.
+// 64 tokens x 64 columns, swizzled for transposing reads.  Tokens behind T
+// are zeros in XT and read as zeros in dY; what is read in columns behind M
+// (XT has room for whole tiles) and N is not stored.
 struct WgradLoads {
     const uint16_t *a;
-    uint64_t b;           // address of dY's rows of the step, columns n0 ..
-    long long b_left;     // bytes from there to the end of dY
-    u32x4 buf;
-    uint32_t va[4], vb;
-    long long b_step;
+    u32x4 buf;            // dY from the rows of the step and column n0 on
+    long long b_left;     // its bytes
+    uint32_t va, vb, b_step;
+    long long a_step;     // from sub-tile to sub-tile (elements)
 
-    template <int NA>
     __device__ __forceinline__ void init(const WgradOperands &op, int m0, int n0, long long kbeg,
                                          int wave, int lane)
     {
         const int r = 8 * wave + (lane >> 3);
         a = op.XT + m0 * op.Tp + kbeg;
-#pragma unroll
-        for (int s = 0; s < NA; ++s)
-            va[s] = static_cast<uint32_t>(min(64 * s + r, op.M - 1 - m0) * op.Tp * 2 +
-                                          ((lane & 7) ^ row_swz(r)) * 16);
-        b = reinterpret_cast<uint64_t>(op.dY + kbeg * op.ldy + n0);
+        a_step = 64 * op.Tp;
+        va = static_cast<uint32_t>(r * op.Tp * 2 + ((lane & 7) ^ row_swz(r)) * 16);
         b_left = ((op.T - 1LL - kbeg) * op.ldy + op.N - n0) * 2;
-        b_step = 64 * op.ldy * 2;
+        b_step = static_cast<uint32_t>(64 * op.ldy * 2);
         vb = static_cast<uint32_t>((r * op.ldy + ((lane & 7) ^ swz<64>(r)) * 8) * 2);
-        buf = buffer_of(reinterpret_cast<const void *>(b), b_left);
+        buf = buffer_of(op.dY + kbeg * op.ldy + n0, b_left);
     }
     __device__ __forceinline__ void next()
     {
         a += 64;
-        b += b_step;
         b_left -= b_step;
+        const uint64_t b = (static_cast<uint64_t>(buf[1]) << 32 | buf[0]) + b_step;
         buf = buffer_of(reinterpret_cast<const void *>(b), b_left);
     }
-    __device__ __forceinline__ void load_a(int s, uint32_t l) const { dma_b128_off(a, va[s], l); }
+    __device__ __forceinline__ void load_a(int s, uint32_t l) const
+    {
+        dma_b128_off(a + s * a_step, va, l);
+    }
     __device__ __forceinline__ void load_b(int s, uint32_t l) const
     {
         dma_b128_buf(buf, vb + 128u * s, l);
     }
 };
+
+// The same value, of which the compiler does not know it: what is formed from
+// it stays where it is used, and is not kept in registers around the K loop.
+__device__ __forceinline__ int fresh(int v)
+{
+    asm volatile("" : "+v"(v));
+    return v;
+}
 
 __device__ __forceinline__ f32x4 mfma16w(bf16x8 a, bf16x8 b, f32x4 c)
 {
@@ -165,8 +212,28 @@ __device__ __forceinline__ void wgrad_store(const uint16_t *lds, const WgradOper
     }
 }
 
+// What becomes of a part's accumulators, which `each` hands to a function of
+// (row, column, the values of four columns): an fp32 part, or the result.
+template <int EDGE, typename F>
+__device__ __forceinline__ void finish_part(const WgradOperands &op, const WgradParts &part,
+                                            uint16_t *lds, int m0, int n0, int tid, F each)
+{
+    if (part.slot >= 0) {
+        float *dst = op.P + static_cast<long long>(part.slot) * (EDGE * EDGE);
+        each([&](int r, int c, const f32x4 &v) __attribute__((always_inline)) {
+            *reinterpret_cast<f32x4 *>(dst + r * EDGE + c) = v;
+        });
+    } else {
+        __syncthreads();
+        each([&](int r, int c, const f32x4 &v) __attribute__((always_inline)) {
+            *reinterpret_cast<bf16x4 *>(lds + wgrad_off<EDGE>(r, c)) = pack4(v[0], v[1], v[2], v[3]);
+        });
+        __syncthreads();
+        wgrad_store<EDGE, EDGE>(lds, op, m0, n0, fresh(tid));
+    }
+}
+
 // 256 x 256 tiles, the phases of dd_gemm.hip.
-template <bool SPLIT>
 __global__ void __launch_bounds__(512, 1)
 wgrad_kernel(WgradOperands op)
 {
@@ -176,12 +243,8 @@ wgrad_kernel(WgradOperands op)
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
     const int l16 = lane & 15, g = lane >> 4;
     const int wm = wave >> 2, wn = wave & 3;
-    int tm, tn;
-    tile_of(static_cast<int>(blockIdx.x), op.tiles_m, op.tiles_n, op.xm, tm, tn);
-    const int m0 = tm * 256, n0 = tn * 256;
-    const int nkt = op.k_len / 64;
+    int m0 = 0, n0 = 0;
     WgradLoads at;
-    at.init<4>(op, m0, n0, static_cast<long long>(blockIdx.y) * op.k_len, wave, lane);
     const uint32_t lds0 = lds_base_sgpr(lds) + 1024u * wave;
     auto load_a = [&](int h, int S) __attribute__((always_inline)) {
         const uint32_t l = lds0 + 2u * (2 * h + S) * HALF;
@@ -220,13 +283,6 @@ wgrad_kernel(WgradOperands op)
             }
     };
     f32x4 acc[2][2][4][2];  // [A half][B half][i][j]
-#pragma unroll
-    for (int x = 0; x < 4; ++x)
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int j = 0; j < 2; ++j)
-                acc[x >> 1][x & 1][i][j] = f32x4{};
     auto multiply = [&](f32x4 (&c)[4][2], const bf16x8 (&a)[4][2],
                         const bf16x8 (&b)[2][2]) __attribute__((always_inline)) {
 #pragma unroll
@@ -279,70 +335,81 @@ wgrad_kernel(WgradOperands op)
         load_a(1, S);
         at.next();
     };
-    if (nkt == 1) {
-        load_step(0);
-        wait_and_barrier<0>();
-        read_a(a0, 0, 0);
-        read_b(b0, 0, 0);
-        multiply(acc[0][0], a0, b0);
-        read_b(b1, 1, 0);
-        multiply(acc[0][1], a0, b1);
-        read_a(a1, 1, 0);
-        multiply(acc[1][1], a1, b1);
-        multiply(acc[1][0], a1, b0);
-    } else {
-        const int s0 = nkt & 1;
-        load_step(s0);
-        load_step(1 - s0);
-        wait_and_barrier<8>();
-        read_a(a0, 0, s0);
-        // Phase 1 refills the half just read: only after a barrier that every
-        // wave reaches with its reads returned.
-        wait_and_barrier<8>();
-        // Waves 4-7 run half a phase behind waves 0-3.
-        if (wm == 1)
-            plain_barrier();
-        for (int kt = 2 - s0; kt < nkt; kt += 2) {
-            if (kt > 1)
-                step(IC<0>{}, IC<0>{});
-            step(IC<1>{}, IC<0>{});
+    WgradParts part;
+    part.init(op, static_cast<int>(blockIdx.x));
+    for (;;) {
+        int tm, tn;
+        tile_of(part.tile, op.tiles_m, op.tiles_n, op.xm, tm, tn);
+        m0 = tm * 256;
+        n0 = tn * 256;
+        const int nkt = part.count;
+        at.init(op, m0, n0, part.first * 64LL, wave, fresh(lane));
+#pragma unroll
+        for (int x = 0; x < 4; ++x)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+                    acc[x >> 1][x & 1][i][j] = f32x4{};
+        if (nkt == 1) {
+            load_step(0);
+            wait_and_barrier<0>();
+            read_a(a0, 0, 0);
+            read_b(b0, 0, 0);
+            multiply(acc[0][0], a0, b0);
+            read_b(b1, 1, 0);
+            multiply(acc[0][1], a0, b1);
+            read_a(a1, 1, 0);
+            multiply(acc[1][1], a1, b1);
+            multiply(acc[1][0], a1, b0);
+        } else {
+            const int s0 = nkt & 1;
+            load_step(s0);
+            load_step(1 - s0);
+            wait_and_barrier<8>();
+            read_a(a0, 0, s0);
+            // Phase 1 refills the half just read: only after a barrier that every
+            // wave reaches with its reads returned.
+            wait_and_barrier<8>();
+            // Waves 4-7 run half a phase behind waves 0-3.
+            if (wm == 1)
+                plain_barrier();
+            for (int kt = 2 - s0; kt < nkt; kt += 2) {
+                if (kt > 1)
+                    step(IC<0>{}, IC<0>{});
+                step(IC<1>{}, IC<0>{});
+            }
+            step(IC<0>{}, IC<1>{});
+            step(IC<1>{}, IC<2>{});
+            if (wm == 0)
+                plain_barrier();
         }
-        step(IC<0>{}, IC<1>{});
-        step(IC<1>{}, IC<2>{});
-        if (wm == 0)
-            plain_barrier();
-    }
 
-    // Accumulator (ha, hb, i, j), register e: row m = 128 ha + 64 wm + 16 i +
-    // l16, column n = 128 hb + 32 wn + 16 j + 4 g + e of the tile.
-    float *part = op.P + ((static_cast<long long>(blockIdx.y) * op.tiles_m + tm) * op.tiles_n + tn) *
-                             (256 * 256);
-    if constexpr (!SPLIT)
-        __syncthreads();
+        // Accumulator (ha, hb, i, j), register e: row m = 128 ha + 64 wm + 16 i +
+        // l16, column n = 128 hb + 32 wn + 16 j + 4 g + e of the tile.
+        const int el = fresh(lane), el16 = el & 15, eg = el >> 4;
+        auto finish = [&](auto put) __attribute__((always_inline)) {
 #pragma unroll
-    for (int x = 0; x < 16; ++x) {
-        const int ha = x >> 3, i = (x >> 1) & 3, hb = x & 1, r = 128 * ha + 64 * wm + 16 * i + l16;
+            for (int x = 0; x < 16; ++x) {
+                const int ha = x >> 3, i = (x >> 1) & 3, hb = x & 1;
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const int c = 128 * hb + 32 * wn + 16 * j + 4 * g;
-            const f32x4 v = acc[ha][hb][i][j];
-            if constexpr (SPLIT)
-                *reinterpret_cast<f32x4 *>(part + r * 256 + c) = v;
-            else
-                *reinterpret_cast<bf16x4 *>(lds + wgrad_off<256>(r, c)) =
-                    pack4(v[0], v[1], v[2], v[3]);
-        }
-    }
-    if constexpr (!SPLIT) {
+                for (int j = 0; j < 2; ++j)
+                    put(128 * ha + 64 * wm + 16 * i + el16, 128 * hb + 32 * wn + 16 * j + 4 * eg,
+                        acc[ha][hb][i][j]);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        };
+        finish_part<256>(op, part, lds, m0, n0, tid, finish);
+        if (!part.more())
+            return;
+        part.next(op);
         __syncthreads();
-        wgrad_store<256, 256>(lds, op, m0, n0, tid);
     }
 }
 
 // 128 x 128 tiles for gradients whose large tiles would leave CUs idle: a
 // phase of 16 products of every wave per K step, four stages of which three
 // are in flight (128 KiB).
-template <bool SPLIT>
 __global__ void __launch_bounds__(512, 1)
 wgrad_small_kernel(WgradOperands op)
 {
@@ -352,12 +419,8 @@ wgrad_small_kernel(WgradOperands op)
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
     const int l16 = lane & 15, g = lane >> 4;
     const int wm = wave >> 2, wn = wave & 3;
-    int tm, tn;
-    tile_of(static_cast<int>(blockIdx.x), op.tiles_m, op.tiles_n, op.xm, tm, tn);
-    const int m0 = tm * 128, n0 = tn * 128;
-    const int nkt = op.k_len / 64;
+    int m0 = 0, n0 = 0;
     WgradLoads at;
-    at.init<2>(op, m0, n0, static_cast<long long>(blockIdx.y) * op.k_len, wave, lane);
     const uint32_t lds0 = lds_base_sgpr(lds) + 1024u * wave;
     auto load_step = [&](int st) __attribute__((always_inline)) {
         const uint32_t l = lds0 + 2u * STAGE * st;
@@ -377,128 +440,131 @@ wgrad_small_kernel(WgradOperands op)
         fb[j] = (2 + (wn >> 1)) * SUB +
                 tile_off<64>(8 * g + 4 * (j & 1) + e4, 32 * (wn & 1) + 16 * (j >> 1) + 4 * c4);
     f32x4 acc[4][2];
+    WgradParts part;
+    part.init(op, static_cast<int>(blockIdx.x));
+    for (;;) {
+        int tm, tn;
+        tile_of(part.tile, op.tiles_m, op.tiles_n, op.xm, tm, tn);
+        m0 = tm * 128;
+        n0 = tn * 128;
+        const int nkt = part.count;
+        at.init(op, m0, n0, part.first * 64LL, wave, fresh(lane));
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-            acc[i][j] = f32x4{};
-    const int first = min(nkt, NST - 1);
-    for (int kt = 0; kt < first; ++kt)
-        load_step(kt);
-    if (nkt > NST - 2)
-        wait_and_barrier<4 * (NST - 2)>();
-    else
-        wait_and_barrier<0>();
-    if (wm == 1)
-        plain_barrier();
-    int rs = 0, ws = NST - 1;  // the stages read and refilled by a step
-    for (int kt = 0; kt < nkt; ++kt) {
-        const uint16_t *st = lds + rs * STAGE;
-        bf16x8 a[4][2], b[2][2];
-#pragma unroll
-        for (int kk = 0; kk < 2; ++kk) {
+        for (int i = 0; i < 4; ++i)
 #pragma unroll
             for (int j = 0; j < 2; ++j)
-                b[j][kk] = join(lds_tr4(st + fb[2 * j] + 2048 * kk),
-                                lds_tr4(st + fb[2 * j + 1] + 2048 * kk));
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                a[i][kk] = lds_row8(st + fa[kk] + 1024 * i);
-        }
-        // The stage that the step before has read is refilled; before the
-        // next step starts, its own loads have to be there (the steps after
-        // it may be in flight).
-        const int ahead = nkt - 1 - kt;  // steps after this one
-        if (ahead >= NST - 1) {
-            load_step(ws);
+                acc[i][j] = f32x4{};
+        const int first = min(nkt, NST - 1);
+        for (int kt = 0; kt < first; ++kt)
+            load_step(kt);
+        if (nkt > NST - 2)
             wait_and_barrier<4 * (NST - 2)>();
-        } else if (ahead == 2) {
-            wait_and_barrier<4>();
-        } else {
+        else
             wait_and_barrier<0>();
-        }
-        ws = rs;
-        rs = rs + 1 == NST ? 0 : rs + 1;
-        __builtin_amdgcn_s_setprio(1);
+        if (wm == 1)
+            plain_barrier();
+        int rs = 0, ws = NST - 1;  // the stages read and refilled by a step
+        for (int kt = 0; kt < nkt; ++kt) {
+            const uint16_t *st = lds + rs * STAGE;
+            bf16x8 a[4][2], b[2][2];
 #pragma unroll
-        for (int kk = 0; kk < 2; ++kk)
+            for (int kk = 0; kk < 2; ++kk) {
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+                    b[j][kk] = join(lds_tr4(st + fb[2 * j] + 2048 * kk),
+                                    lds_tr4(st + fb[2 * j + 1] + 2048 * kk));
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    a[i][kk] = lds_row8(st + fa[kk] + 1024 * i);
+            }
+            // The stage that the step before has read is refilled; before the
+            // next step starts, its own loads have to be there (the steps after
+            // it may be in flight).
+            const int ahead = nkt - 1 - kt;  // steps after this one
+            if (ahead >= NST - 1) {
+                load_step(ws);
+                wait_and_barrier<4 * (NST - 2)>();
+            } else if (ahead == 2) {
+                wait_and_barrier<4>();
+            } else {
+                wait_and_barrier<0>();
+            }
+            ws = rs;
+            rs = rs + 1 == NST ? 0 : rs + 1;
+            __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+            for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int j = 0; j < 2; ++j)
+                        acc[i][j] = mfma16w(b[j][kk], a[i][kk], acc[i][j]);  // rows n, columns m
+            __builtin_amdgcn_s_setprio(0);
+            plain_barrier();
+        }
+        if (wm == 0)
+            plain_barrier();
+
+        // Accumulator (i, j), register e: row m = 64 wm + 16 i + l16, column n =
+        // 32 wn + 16 j + 4 g + e of the tile.
+        const int el = fresh(lane), el16 = el & 15, eg = el >> 4;
+        auto finish = [&](auto put) __attribute__((always_inline)) {
 #pragma unroll
             for (int i = 0; i < 4; ++i)
 #pragma unroll
                 for (int j = 0; j < 2; ++j)
-                    acc[i][j] = mfma16w(b[j][kk], a[i][kk], acc[i][j]);  // rows n, columns m
-        __builtin_amdgcn_s_setprio(0);
-        plain_barrier();
-    }
-    if (wm == 0)
-        plain_barrier();
-
-    // Accumulator (i, j), register e: row m = 64 wm + 16 i + l16, column n =
-    // 32 wn + 16 j + 4 g + e of the tile.
-    float *part = op.P + ((static_cast<long long>(blockIdx.y) * op.tiles_m + tm) * op.tiles_n + tn) *
-                             (128 * 128);
-    if constexpr (!SPLIT)
+                    put(64 * wm + 16 * i + el16, 32 * wn + 16 * j + 4 * eg, acc[i][j]);
+        };
+        finish_part<128>(op, part, lds, m0, n0, tid, finish);
+        if (!part.more())
+            return;
+        part.next(op);
         __syncthreads();
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const int r = 64 * wm + 16 * i + l16, c = 32 * wn + 16 * j + 4 * g;
-            const f32x4 v = acc[i][j];
-            if constexpr (SPLIT)
-                *reinterpret_cast<f32x4 *>(part + r * 128 + c) = v;
-            else
-                *reinterpret_cast<bf16x4 *>(lds + wgrad_off<128>(r, c)) =
-                    pack4(v[0], v[1], v[2], v[3]);
-        }
-    if constexpr (!SPLIT) {
-        __syncthreads();
-        wgrad_store<128, 128>(lds, op, m0, n0, tid);
     }
 }
 
-// dW = the sum of the partial tiles over the splits, 8 elements per thread.
+// dW of the shared tiles: the sum of a tile's parts, 8 elements per thread.
 template <int EDGE>
 __global__ void __launch_bounds__(256)
-wgrad_reduce_kernel(WgradOperands op, int splits)
+wgrad_sum_kernel(WgradOperands op)
 {
     constexpr int PER = EDGE * EDGE / 8 / 256;  // workgroups per tile
     const int tile = static_cast<int>(blockIdx.x) / PER;
     const int v = static_cast<int>(blockIdx.x) % PER * 256 + threadIdx.x;
-    const int m = tile / op.tiles_n * EDGE + v / (EDGE / 8);
-    const int n = tile % op.tiles_n * EDGE + v % (EDGE / 8) * 8;
+    int tm, tn;
+    tile_of(op.whole + tile, op.tiles_m, op.tiles_n, op.xm, tm, tn);
+    const int m = tm * EDGE + v / (EDGE / 8), n = tn * EDGE + v % (EDGE / 8) * 8;
     if (m >= op.M || n >= op.N)
         return;
-    const float *p = op.P + static_cast<long long>(tile) * EDGE * EDGE + v * 8;
-    const long long step = static_cast<long long>(op.tiles_m) * op.tiles_n * EDGE * EDGE;
-    f32x4 s0 = *reinterpret_cast<const f32x4 *>(p), s1 = *reinterpret_cast<const f32x4 *>(p + 4);
-    for (int s = 1; s < splits; ++s) {
-        s0 += *reinterpret_cast<const f32x4 *>(p + s * step);
-        s1 += *reinterpret_cast<const f32x4 *>(p + s * step + 4);
-    }
+    f32x4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = s0;
+    auto add = [&](int slot) {
+        const float *p = op.P + static_cast<long long>(slot) * (EDGE * EDGE) + v * 8;
+        s0 += *reinterpret_cast<const f32x4 *>(p);
+        s1 += *reinterpret_cast<const f32x4 *>(p + 4);
+    };
+    add(tile);
+    // The further workgroups that touch this tile, and which of their parts
+    // it is.
+    const int w0 = tile * op.rest / op.head, w1 = ((tile + 1) * op.rest - 1) / op.head;
+    for (int w = w0; w <= w1; ++w)
+        add(op.shared + w * op.most + tile - w * op.head / op.rest);
     *reinterpret_cast<bf16x8 *>(op.dW + m * op.ldw + n) =
         join(pack4(s0[0], s0[1], s0[2], s0[3]), pack4(s1[0], s1[1], s1[2], s1[3]));
 }
 
 namespace {
 
-// The workspace's parts: XT, then the partial tiles.
+// The workspace's parts, in bytes: XT, then the parts of the shared tiles.
 struct WgradSpace {
     WgradPlan plan;
-    long long Tp;
-    size_t restored, partials;  // bytes
+    size_t restored, partials;
 };
 
 WgradSpace wgrad_space(int T, int M, int N)
 {
-    WgradSpace w;
-    const WgradPlan &p = w.plan = wgrad_plan(T, M, N, device_cu_count());
-    w.Tp = static_cast<long long>(p.k_len) * p.splits;
-    w.restored = static_cast<size_t>(M) * w.Tp * 2;
-    w.partials = p.splits > 1 ? static_cast<size_t>(p.splits) * p.tiles_m * p.tiles_n * p.edge *
-                                    p.edge * sizeof(float)
-                              : 0;
-    return w;
+    const WgradPlan p = wgrad_plan(T, M, N, device_cu_count());
+    return WgradSpace{p, static_cast<size_t>(p.tiles_m) * p.edge * p.steps * 128,
+                      static_cast<size_t>(p.partials()) * p.edge * p.edge * sizeof(float)};
 }
 
 }  // namespace
@@ -514,29 +580,27 @@ int launch_wgrad_i8(const WgradI8Args &a)
     hipStream_t st = static_cast<hipStream_t>(a.stream);
     const WgradSpace w = wgrad_space(a.T, a.M, a.N);
     const WgradPlan &p = w.plan;
+    const long long Tp = p.steps * 64LL;
     auto *xt = static_cast<uint16_t *>(a.workspace);
-    auto *parts = w.partials ? reinterpret_cast<float *>(static_cast<char *>(a.workspace) + w.restored)
-                             : nullptr;
+    auto *parts = reinterpret_cast<float *>(static_cast<char *>(a.workspace) + w.restored);
     hipError_t e = launch_kernel(restore_kernel,
-                                 dim3(static_cast<unsigned>((w.Tp + 127) / 128),
+                                 dim3(static_cast<unsigned>((Tp + 127) / 128),
                                       static_cast<unsigned>((a.M + 127) / 128)),
                                  dim3(256), st, static_cast<const int8_t *>(a.Q), a.ldq, a.scales,
-                                 xt, w.Tp, a.T, a.M);
+                                 xt, Tp, a.T, a.M);
     if (e != hipSuccess)
         return DD_ERR_HIP;
+    const int shared = p.head ? p.shared() : 0;
     const WgradOperands op{xt, static_cast<const uint16_t *>(a.dY), static_cast<uint16_t *>(a.dW),
-                           parts, w.Tp, a.ldy, a.ldw, a.T, a.M, a.N, p.k_len, p.tiles_m, p.tiles_n,
-                           tile_rows_step(p.tiles_m, p.tiles_n)};
-    const unsigned tiles = static_cast<unsigned>(p.tiles_m) * static_cast<unsigned>(p.tiles_n);
-    const auto kern = p.edge == 256 ? (parts ? wgrad_kernel<true> : wgrad_kernel<false>)
-                                    : (parts ? wgrad_small_kernel<true> : wgrad_small_kernel<false>);
-    e = launch_kernel(kern, dim3(tiles, static_cast<unsigned>(p.splits)), dim3(512), st, op);
-    if (e != hipSuccess || !parts)
+                           parts, Tp, a.ldy, a.ldw, a.T, a.M, a.N, p.tiles_m, p.tiles_n,
+                           tile_rows_step(p.tiles_m, p.tiles_n), p.whole, shared, p.steps, p.head,
+                           p.rest(), p.most()};
+    const unsigned wgs = static_cast<unsigned>(p.whole) + shared + p.tails;
+    e = launch_kernel(p.edge == 256 ? wgrad_kernel : wgrad_small_kernel, dim3(wgs), dim3(512), st, op);
+    if (e != hipSuccess || !shared)
         return e == hipSuccess ? DD_OK : DD_ERR_HIP;
-    e = p.edge == 256 ? launch_kernel(wgrad_reduce_kernel<256>, dim3(tiles * 32), dim3(256), st, op,
-                                      p.splits)
-                      : launch_kernel(wgrad_reduce_kernel<128>, dim3(tiles * 8), dim3(256), st, op,
-                                      p.splits);
+    e = p.edge == 256 ? launch_kernel(wgrad_sum_kernel<256>, dim3(shared * 32u), dim3(256), st, op)
+                      : launch_kernel(wgrad_sum_kernel<128>, dim3(shared * 8u), dim3(256), st, op);
     return e == hipSuccess ? DD_OK : DD_ERR_HIP;
 }
 

@@ -282,7 +282,8 @@ def test_gemm_int8_scales_that_are_not_finite(cuda):
 
 WGRAD = [(1, 8, 8), (2, 16, 40), (63, 64, 64), (64, 72, 128), (65, 128, 72), (200, 256, 256),
          (129, 264, 520), (1000, 520, 264), (3001, 1040, 1416), (64, 512, 768), (192, 256, 512),
-         (4096, 256, 256), (8200, 512, 264), (300, 2304, 2560), (20000, 136, 200)]
+         (4096, 256, 256), (8200, 512, 264), (300, 2304, 2560), (20000, 136, 200),
+         (8192, 1024, 1416), (4100, 2056, 1000), (700, 4352, 4360), (9000, 1800, 5000)]
 
 
 @pytest.mark.parametrize("T,M,N", WGRAD)

@@ -116,7 +116,7 @@ def test_weight_gradient_refusals(lib):
              M=96, N=128, ws=fake(4), bytes=need)
     for n in ("Q", "scales", "dY", "dW"):
         assert call(lib, "dd_gemm_i8_wgrad", g, **{n: None}) == NULL, n
-    for kw in (dict(T=0), dict(M=0), dict(M=92), dict(N=100), dict(ldq=88), dict(ldy=120),
+    for kw in (dict(T=0), dict(T=1 << 25), dict(M=0), dict(M=92), dict(N=100), dict(ldq=88), dict(ldy=120),
                dict(ldw=120), dict(ldq=1 << 23), dict(ldy=1 << 23)):
         assert call(lib, "dd_gemm_i8_wgrad", g, **kw) == SHAPE, kw
     for kw in (dict(ldq=100), dict(ldy=132), dict(ldw=132), dict(Q=fake(0, 4)), dict(dY=fake(2, 8)),
