@@ -281,10 +281,7 @@ int dd_transpose(const void *X, long long ldx, void *Y, long long ldy, int rows,
  * 0; a row that holds a NaN or an infinity has codes 0 and a NaN scale (all
  * its values are NaN, and no other row's).  rows >= 1, 1 <= d <= 16384, rows
  * * d < 2^40; row strides (elements) at least d; bf16 pointers 2-byte, fp32
- * pointers 4-byte aligned.  Rows of 16-byte aligned pieces (d and the strides
- * multiples of 8, pointers 16-byte, codes 8-byte aligned) run with wide
- * accesses, others element by element.  Outputs must not overlap inputs or
- * each other.
+ * pointers 4-byte aligned.  Outputs must not overlap inputs or each other.
  *
  * dd_quantize    codes and scales (A / 127) of the rows of a bf16 matrix X.
  * dd_dequantize  Y = bf16(scale * q).

@@ -18,6 +18,7 @@ its current stream; matrices without rows or columns give empty results.
 from __future__ import annotations
 
 import ctypes
+import functools
 
 import torch
 
@@ -235,15 +236,20 @@ def swiglu_backward(u, v, dy):
 # rows in 8 bits
 
 
+@functools.lru_cache(maxsize=None)
+def _entry(name):
+    return getattr(lib(), name)
+
+
 def _call(dev, name, *args):
     """Runs an entry point on the current stream of ``dev``."""
-    fn = getattr(lib(), name)
-    if dev.index == torch.cuda.current_device():
-        st = fn(*args, _stream(dev))
+    if dev.index == torch._C._cuda_getDevice():
+        st = _entry(name)(*args, _stream(dev))
     else:
         with torch.cuda.device(dev):
-            st = fn(*args, _stream(dev))
-    check(st, name)
+            st = _entry(name)(*args, _stream(dev))
+    if st:
+        check(st, name)
 
 
 def _on(t, name, dev):
@@ -294,7 +300,7 @@ def _norm_inputs(x, w, residual):
     _on(residual, "residual", dev)
     if residual.shape != x.shape:
         raise ValueError("residual must match x in shape")
-    return dev, torch.empty(x.shape, dtype=torch.bfloat16, device=dev)
+    return dev, torch.empty_like(x)
 
 
 def rms_norm(x, w, residual=None, eps: float = LN_EPS):
@@ -302,7 +308,7 @@ def rms_norm(x, w, residual=None, eps: float = LN_EPS):
     bf16; x itself without one): rstd = 1 / sqrt(mean(h^2) + eps), y = h rstd w."""
     dev, h = _norm_inputs(x, w, residual)
     rows, d = x.shape
-    y = torch.empty((rows, d), dtype=torch.bfloat16, device=dev)
+    y = torch.empty_like(x)
     rstd = torch.empty(rows, dtype=torch.float32, device=dev)
     if y.numel():
         _call(dev, "dd_rmsnorm_fwd", _p(x), _ld(x), _p(residual),
@@ -315,7 +321,7 @@ def rms_norm_int8(x, w, residual=None, eps: float = LN_EPS):
     """(codes, scales, h, rstd): ``rms_norm`` with its output as codes."""
     dev, h = _norm_inputs(x, w, residual)
     rows, d = x.shape
-    codes = torch.empty((rows, d), dtype=torch.int8, device=dev)
+    codes = torch.empty_like(x, dtype=torch.int8)
     scales, rstd = (torch.empty(rows, dtype=torch.float32, device=dev) for _ in range(2))
     if codes.numel():
         _call(dev, "dd_rmsnorm_int8_fwd", _p(x), _ld(x), _p(residual),
@@ -336,10 +342,9 @@ def rms_norm_backward(h, w, rstd, dy, dres=None):
     for t, n in ((dy, "dy"), (dres, "dres")):
         if t is not None or n == "dy":
             _rows(t, n, h.shape, dev)
-    dx = torch.empty((rows, d), dtype=torch.bfloat16, device=dev)
+    dx, dw = torch.empty_like(h), torch.empty_like(w)
     if not dx.numel():
-        return dx, torch.zeros(d, dtype=torch.bfloat16, device=dev)
-    dw = torch.empty(d, dtype=torch.bfloat16, device=dev)
+        return dx, dw.zero_()
     need = lib().dd_rmsnorm_bwd_workspace_bytes(rows, d)
     ws = torch.empty(need, dtype=torch.uint8, device=dev)
     _call(dev, "dd_rmsnorm_bwd", _p(h), _p(w), _p(rstd), _p(dy), _p(dres), _p(dx), _p(dw), rows,
@@ -351,7 +356,7 @@ def quantize(x):
     """(codes, scales) of the rows of a bf16 matrix."""
     _mat(x, "x")
     rows, d = x.shape
-    codes = torch.empty((rows, d), dtype=torch.int8, device=x.device)
+    codes = torch.empty_like(x, dtype=torch.int8)
     scales = torch.empty(rows, dtype=torch.float32, device=x.device)
     if codes.numel():
         _call(x.device, "dd_quantize", _p(x), _ld(x), _p(codes), d, _p(scales), rows, d)

@@ -25,7 +25,10 @@ __device__ __forceinline__ i32x4 mfma_i8(u32x4 a, u32x4 b, i32x4 c)
                                                  __builtin_bit_cast(i32x4, b), c, 0, 0, 0);
 }
 
-// `wide`: the rows of C (and R) are made of 16-byte aligned pieces.
+// Pieces of rows at any bf16 address (the hardware takes unaligned vectors).
+typedef uint32_t piece16 __attribute__((ext_vector_type(4), aligned(2)));
+typedef uint32_t piece8 __attribute__((ext_vector_type(2), aligned(2)));
+
 struct GemmI8Operands {
     const int8_t *A, *B;
     const float *sa, *sb;
@@ -33,7 +36,6 @@ struct GemmI8Operands {
     uint16_t *C;
     long long lda, ldb, ldc;
     int M, N, K, tiles_m, tiles_n, xm;
-    bool wide;
 };
 
 __device__ __forceinline__ float bf16_at(const uint16_t *p)
@@ -52,8 +54,8 @@ __device__ __forceinline__ bf16x4 scaled(const GemmI8Operands &op, i32x4 acc, fl
         c[e] = static_cast<float>(acc[e]) * ra * rb[e];
     if (op.R != nullptr && m < op.M) {
         const uint16_t *r = op.R + m * op.ldc + n;
-        if (op.wide && n + 4 <= op.N) {
-            const bf16x4 v = *reinterpret_cast<const bf16x4 *>(r);
+        if (n + 4 <= op.N) {
+            const bf16x4 v = __builtin_bit_cast(bf16x4, *reinterpret_cast<const piece8 *>(r));
 #pragma unroll
             for (int e = 0; e < 4; ++e)
                 c[e] += static_cast<float>(v[e]);
@@ -89,8 +91,8 @@ __device__ __forceinline__ void store_image(const uint16_t *lds, const GemmI8Ope
         if (m >= op.M || n >= op.N)
             continue;
         uint16_t *p = op.C + m * op.ldc + n;
-        if (op.wide && n + 8 <= op.N) {
-            *reinterpret_cast<u32x4 *>(p) = v;
+        if (n + 8 <= op.N) {
+            *reinterpret_cast<piece16 *>(p) = v;
         } else {
 #pragma unroll
             for (int e = 0; e < 8; ++e)
@@ -496,9 +498,7 @@ int launch_gemm_i8(const GemmI8Args &a)
     hipStream_t st = static_cast<hipStream_t>(a.stream);
     GemmI8Operands op{static_cast<const int8_t *>(a.A), static_cast<const int8_t *>(a.B), a.sa,
                       a.sb, static_cast<const uint16_t *>(a.R), static_cast<uint16_t *>(a.C),
-                      a.lda, a.ldb, a.ldc, a.M, a.N, a.K, 0, 0, 0, false};
-    op.wide = a.ldc % 8 == 0 && reinterpret_cast<uintptr_t>(a.C) % 16 == 0 &&
-              reinterpret_cast<uintptr_t>(a.R) % 16 == 0;
+                      a.lda, a.ldb, a.ldc, a.M, a.N, a.K, 0, 0, 0};
     const GemmI8Tile tile = gemm_i8_tile(a.M, a.N, a.K, device_cu_count());
     if (tile == GemmI8Tile::kFew) {
         const int mb = (a.M + 15) / 16;

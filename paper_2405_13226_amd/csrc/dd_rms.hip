@@ -36,34 +36,39 @@ struct RowThreads {
     static constexpr int WAVES = TPR / 64;  // per row
 };
 
+// Pieces of rows at any element's address (the hardware takes unaligned
+// vectors).
+typedef uint32_t piece16 __attribute__((ext_vector_type(4), aligned(2)));
+typedef uint32_t codes8 __attribute__((ext_vector_type(2), aligned(1)));
+
 // Eight elements from `p`, of which `left` (or more) exist; zeros for the
-// others.  VEC: left is a multiple of 8 and p 16-byte aligned.
-template <bool VEC>
+// others.  WHOLE: left is a multiple of 8.
+template <bool WHOLE>
 __device__ __forceinline__ void load8(const uint16_t *p, int left, float (&f)[8])
 {
-    if constexpr (VEC) {
-        u32x4 u = {0u, 0u, 0u, 0u};
-        if (left > 0)
-            u = *reinterpret_cast<const u32x4 *>(p);
-        unpack8(u, f);
-    } else {
+    u32x4 u = {0u, 0u, 0u, 0u};
+    if (WHOLE ? left > 0 : left >= 8) {
+        u = *reinterpret_cast<const piece16 *>(p);
+    } else if (!WHOLE) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            f[i] = i < left ? __uint_as_float(static_cast<uint32_t>(p[i]) << 16) : 0.f;
+        for (int i = 0; i < 7; ++i)
+            if (i < left)
+                u[i >> 1] |= static_cast<uint32_t>(p[i]) << 16 * (i & 1);
     }
+    unpack8(u, f);
 }
 
-template <bool VEC>
+template <bool WHOLE>
 __device__ __forceinline__ void store8(uint16_t *p, int left, const float (&f)[8])
 {
-    if constexpr (VEC) {
-        if (left > 0)
-            *reinterpret_cast<u32x4 *>(p) = pack8f(f);
-    } else {
+    const u32x4 u = pack8f(f);
+    if (WHOLE ? left > 0 : left >= 8) {
+        *reinterpret_cast<piece16 *>(p) = u;
+    } else if (!WHOLE) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
+        for (int i = 0; i < 7; ++i)
             if (i < left)
-                p[i] = __builtin_bit_cast(uint16_t, static_cast<__bf16>(f[i]));
+                p[i] = static_cast<uint16_t>(u[i >> 1] >> 16 * (i & 1));
     }
 }
 
@@ -136,7 +141,7 @@ struct CodeScale {
 
 __device__ __forceinline__ uint32_t abs_bits(float x) { return __float_as_uint(x) & 0x7fffffffu; }
 
-template <bool VEC>
+template <bool WHOLE>
 __device__ __forceinline__ void store_codes(int8_t *p, int left, const float (&z)[8],
                                             const CodeScale &cs, bool usable)
 {
@@ -144,17 +149,16 @@ __device__ __forceinline__ void store_codes(int8_t *p, int left, const float (&z
 #pragma unroll
     for (int i = 0; i < 8; ++i)
         c[i] = usable ? cs.code(z[i]) : 0;
-    if constexpr (VEC) {
-        u32x2 u;
+    u32x2 u;
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
-            u[i] = (c[4 * i] & 255) | (c[4 * i + 1] & 255) << 8 | (c[4 * i + 2] & 255) << 16 |
-                   static_cast<uint32_t>(c[4 * i + 3]) << 24;
-        if (left > 0)
-            *reinterpret_cast<u32x2 *>(p) = u;
-    } else {
+    for (int i = 0; i < 2; ++i)
+        u[i] = (c[4 * i] & 255) | (c[4 * i + 1] & 255) << 8 | (c[4 * i + 2] & 255) << 16 |
+               static_cast<uint32_t>(c[4 * i + 3]) << 24;
+    if (WHOLE ? left > 0 : left >= 8) {
+        *reinterpret_cast<codes8 *>(p) = u;
+    } else if (!WHOLE) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
+        for (int i = 0; i < 7; ++i)
             if (i < left)
                 p[i] = static_cast<int8_t>(c[i]);
     }
@@ -174,7 +178,7 @@ struct RowOperands {
     float eps;
 };
 
-template <int TPR, int CH, bool VEC, int KIND>
+template <int TPR, int CH, bool WHOLE, int KIND>
 __global__ void __launch_bounds__(RowThreads<TPR>::THREADS)
 row_kernel(RowOperands op)
 {
@@ -189,18 +193,18 @@ row_kernel(RowOperands op)
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
             const int col = (t + TPR * c) * 8;
-            load8<VEC>(op.X + row * op.ldx + col, d - col, v[c]);
+            load8<WHOLE>(op.X + row * op.ldx + col, d - col, v[c]);
         }
         if (KIND != kCodes && op.R != nullptr) {
 #pragma unroll
             for (int c = 0; c < CH; ++c) {
                 const int col = (t + TPR * c) * 8;
                 float r[8];
-                load8<VEC>(op.R + row * op.ldr + col, d - col, r);
+                load8<WHOLE>(op.R + row * op.ldr + col, d - col, r);
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
                     v[c][i] = static_cast<float>(static_cast<__bf16>(v[c][i] + r[i]));
-                store8<VEC>(op.H + row * d + col, d - col, v[c]);
+                store8<WHOLE>(op.H + row * d + col, d - col, v[c]);
             }
         }
         float s = 0.f;
@@ -210,7 +214,7 @@ row_kernel(RowOperands op)
         for (int c = 0; c < CH; ++c) {
             const int col = (t + TPR * c) * 8;
             if constexpr (KIND != kCodes)
-                load8<VEC>(op.W + col, d - col, w[c]);
+                load8<WHOLE>(op.W + col, d - col, w[c]);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 if constexpr (KIND != kCodes)
@@ -236,7 +240,7 @@ row_kernel(RowOperands op)
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
                     y[i] = v[c][i] * rstd * w[c][i];
-                store8<VEC>(op.Y + row * d + col, d - col, y);
+                store8<WHOLE>(op.Y + row * d + col, d - col, y);
             }
         } else {
             const CodeScale cs(m);
@@ -247,14 +251,14 @@ row_kernel(RowOperands op)
 #pragma unroll
             for (int c = 0; c < CH; ++c) {
                 const int col = (t + TPR * c) * 8;
-                store_codes<VEC>(op.Q + row * op.ldq + col, d - col, v[c], cs, cs.usable());
+                store_codes<WHOLE>(op.Q + row * op.ldq + col, d - col, v[c], cs, cs.usable());
             }
         }
     }
 }
 
 // Codes to bf16: one wave per row and 2048 columns, 8 codes per lane and load.
-template <bool VEC>
+template <bool WHOLE>
 __global__ void __launch_bounds__(256)
 dequantize_kernel(const int8_t *__restrict__ Q, long long ldq, const float *__restrict__ scales,
                   uint16_t *__restrict__ Y, long long ldy, int rows, int d)
@@ -269,20 +273,20 @@ dequantize_kernel(const int8_t *__restrict__ Q, long long ldq, const float *__re
             const int col = static_cast<int>(blockIdx.y) * 2048 + (lane + 64 * c) * 8;
             const int left = d - col;
             const int8_t *q = Q + row * ldq + col;
-            float f[8];
-            if constexpr (VEC) {
-                u32x2 u = {0u, 0u};
-                if (left > 0)
-                    u = *reinterpret_cast<const u32x2 *>(q);
+            u32x2 u = {0u, 0u};
+            if (WHOLE ? left > 0 : left >= 8) {
+                u = *reinterpret_cast<const codes8 *>(q);
+            } else if (!WHOLE) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    f[i] = s * static_cast<float>(static_cast<int8_t>(u[i >> 2] >> 8 * (i & 3)));
-            } else {
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    f[i] = i < left ? s * static_cast<float>(q[i]) : 0.f;
+                for (int i = 0; i < 7; ++i)
+                    if (i < left)
+                        u[i >> 2] |= static_cast<uint32_t>(q[i] & 255) << 8 * (i & 3);
             }
-            store8<VEC>(Y + row * ldy + col, left, f);
+            float f[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                f[i] = s * static_cast<float>(static_cast<int8_t>(u[i >> 2] >> 8 * (i & 3)));
+            store8<WHOLE>(Y + row * ldy + col, left, f);
         }
     }
 }
@@ -297,7 +301,7 @@ struct RmsBackOperands {
     int rows, d, per_wg;
 };
 
-template <int TPR, int CH, bool VEC>
+template <int TPR, int CH, bool WHOLE>
 __global__ void __launch_bounds__(RowThreads<TPR>::THREADS)
 rms_bwd_kernel(RmsBackOperands op)
 {
@@ -310,7 +314,7 @@ rms_bwd_kernel(RmsBackOperands op)
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
         const int col = (t + TPR * c) * 8;
-        load8<VEC>(op.W + col, d - col, w[c]);
+        load8<WHOLE>(op.W + col, d - col, w[c]);
 #pragma unroll
         for (int i = 0; i < 8; ++i)
             dw[c][i] = 0.f;
@@ -326,8 +330,8 @@ rms_bwd_kernel(RmsBackOperands op)
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
             const int col = (t + TPR * c) * 8;
-            load8<VEC>(op.H + base + col, d - col, xh[c]);
-            load8<VEC>(op.dY + base + col, d - col, g[c]);
+            load8<WHOLE>(op.H + base + col, d - col, xh[c]);
+            load8<WHOLE>(op.dY + base + col, d - col, g[c]);
         }
 #pragma unroll
         for (int c = 0; c < CH; ++c)
@@ -350,12 +354,12 @@ rms_bwd_kernel(RmsBackOperands op)
                 out[i] = rstd * (g[c][i] - xh[c][i] * mean);
             if (op.dRes != nullptr) {
                 float r[8];
-                load8<VEC>(op.dRes + base + col, d - col, r);
+                load8<WHOLE>(op.dRes + base + col, d - col, r);
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
                     out[i] += r[i];
             }
-            store8<VEC>(op.dX + base + col, d - col, out);
+            store8<WHOLE>(op.dX + base + col, d - col, out);
         }
     }
     float *dst = op.part + static_cast<long long>(blockIdx.x) * d;
@@ -428,14 +432,6 @@ int rms_rows_per_wg(int rows)
     return std::max(per, 8);
 }
 
-bool aligned16(std::initializer_list<const void *> ps)
-{
-    for (const void *p : ps)
-        if (reinterpret_cast<uintptr_t>(p) & 15)
-            return false;
-    return true;
-}
-
 // Threads per row and chunks per thread for rows of d elements.
 struct RowShape {
     int tpr, ch;
@@ -476,15 +472,13 @@ int launch_rows(const RowArgs &a)
                          static_cast<const uint16_t *>(a.w), static_cast<uint16_t *>(a.H),
                          static_cast<uint16_t *>(a.Y),       static_cast<int8_t *>(a.Q),
                          a.scales, a.rstd, a.ldx, a.ldr, a.ldq, a.rows, a.d, a.eps};
-    const bool vec = a.d % 8 == 0 && a.ldx % 8 == 0 && a.ldr % 8 == 0 && a.ldq % 8 == 0 &&
-                     aligned16({a.X, a.R, a.w, a.H, a.Y}) &&
-                     reinterpret_cast<uintptr_t>(a.Q) % 8 == 0;
+    const bool whole = a.d % 8 == 0;
     const hipError_t e = with_shape(row_shape(a.rows, a.d), [&](auto tpr, auto ch) {
         using T = RowThreads<decltype(tpr)::value>;
         constexpr int TPR = decltype(tpr)::value, CH = decltype(ch)::value;
         auto run = [&](auto kind) {
             constexpr int K = decltype(kind)::value;
-            return launch_kernel(vec ? row_kernel<TPR, CH, true, K> : row_kernel<TPR, CH, false, K>,
+            return launch_kernel(whole ? row_kernel<TPR, CH, true, K> : row_kernel<TPR, CH, false, K>,
                                  dim3(grid_of((a.rows + T::ROWS - 1LL) / T::ROWS)),
                                  dim3(T::THREADS), st, op);
         };
@@ -495,11 +489,10 @@ int launch_rows(const RowArgs &a)
 
 int launch_dequantize(const DequantizeArgs &a)
 {
-    const bool vec = a.d % 8 == 0 && a.ldq % 8 == 0 && a.ldy % 8 == 0 && aligned16({a.Y}) &&
-                     reinterpret_cast<uintptr_t>(a.Q) % 8 == 0;
+    const bool whole = a.d % 8 == 0;
     const dim3 grid(grid_of((a.rows + 3LL) / 4), static_cast<unsigned>((a.d + 2047) / 2048));
     const hipError_t e =
-        launch_kernel(vec ? dequantize_kernel<true> : dequantize_kernel<false>, grid, dim3(256),
+        launch_kernel(whole ? dequantize_kernel<true> : dequantize_kernel<false>, grid, dim3(256),
                       static_cast<hipStream_t>(a.stream), static_cast<const int8_t *>(a.Q), a.ldq,
                       a.scales, static_cast<uint16_t *>(a.Y), a.ldy, a.rows, a.d);
     return e == hipSuccess ? DD_OK : DD_ERR_HIP;
@@ -521,10 +514,10 @@ int launch_rmsnorm_bwd(const RmsBackArgs &a)
     const RmsBackOperands op{static_cast<const uint16_t *>(a.H), static_cast<const uint16_t *>(a.w),
                              static_cast<const uint16_t *>(a.dY), static_cast<const uint16_t *>(a.dRes),
                              a.rstd, static_cast<uint16_t *>(a.dX), part, a.rows, a.d, per};
-    const bool vec = a.d % 8 == 0 && aligned16({a.H, a.w, a.dY, a.dRes, a.dX});
+    const bool whole = a.d % 8 == 0;
     hipError_t e = with_shape(row_shape(a.rows, a.d), [&](auto tpr, auto ch) {
         constexpr int TPR = decltype(tpr)::value, CH = decltype(ch)::value;
-        return launch_kernel(vec ? rms_bwd_kernel<TPR, CH, true> : rms_bwd_kernel<TPR, CH, false>,
+        return launch_kernel(whole ? rms_bwd_kernel<TPR, CH, true> : rms_bwd_kernel<TPR, CH, false>,
                              dim3(static_cast<unsigned>(parts)), dim3(RowThreads<TPR>::THREADS), st,
                              op);
     });

@@ -172,7 +172,8 @@ inline GemmPlan gemm_plan(int M, long long N, long long K, bool may_split, int c
 }
 
 // How an int8 product of M x N over K runs: few tokens with the weights
-// straight into registers, or on tiles of 128 x 128 or 256 x 256.
+// straight into registers (64 x 6144 over 2048: 12.0 us, on small tiles 12.3;
+// 33 x 8192 over 6144 23.0 and 28.5), or on tiles of 128 x 128 or 256 x 256.
 enum class GemmI8Tile { kFew, kSmall, kLarge };
 
 inline GemmI8Tile gemm_i8_tile(int M, int N, int K, int cus)
@@ -180,14 +181,18 @@ inline GemmI8Tile gemm_i8_tile(int M, int N, int K, int cus)
     if (M <= 64)
         return GemmI8Tile::kFew;
     cus = std::max(cus, 1);
-    auto rounds = [&](int edge) {
+    // us: rounds of workgroups over the CUs, each a start-up and tail and its
+    // K steps, which a full chip's power makes longer on the large tiles (one
+    // per CU of 16 steps: 32 us, 48 of them 22.5; on small tiles 12.4 to 13.2).
+    auto time = [&](int edge) {
         const double tiles = std::ceil(M / static_cast<double>(edge)) * std::ceil(N / static_cast<double>(edge));
-        return std::ceil(tiles / cus);
+        const double steps = std::ceil(K / 128.0), full = std::floor(tiles / cus), last = tiles / cus - full;
+        auto round = [&](double used) {
+            return edge == 256 ? 8.0 + steps * (0.9 + 0.6 * used) : 5.5 + steps * 0.48;
+        };
+        return full * round(1.0) + (last > 0 ? round(last) : 0.0);
     };
-    const double steps = std::ceil(K / 128.0);
-    return rounds(128) * (steps * 0.5 + 6.0) < rounds(256) * (steps * 1.2 + 6.0)
-               ? GemmI8Tile::kSmall
-               : GemmI8Tile::kLarge;
+    return time(128) < time(256) ? GemmI8Tile::kSmall : GemmI8Tile::kLarge;
 }
 
 // How a weight gradient of M x N over T tokens runs: on tiles of 256 x 256 or
@@ -216,8 +221,14 @@ inline WgradPlan wgrad_plan(int T, int M, int N, int cus)
     double cost = -1;
     for (const int edge : {256, 128}) {
         const long long tm = (M + edge - 1LL) / edge, tn = (N + edge - 1LL) / edge, tiles = tm * tn;
-        const double step = edge == 256 ? 1.4 : 0.55;  // us, a full chip
-        const double light = edge == 256 ? 1.1 : 0.42;  // us, few workgroups
+        // us a step: with few workgroups its latency, with a full chip its
+        // power (2048 x 5632, 16,384 tokens: 176 workgroups of 256 steps
+        // 300 us, 256 of 176 steps 280; 256 x 256, 65,536 tokens, one
+        // workgroup of 1024 steps per tile: 938 us, 542 on 128 x 128 tiles).
+        auto step = [&](double wgs) {
+            const double used = std::min(wgs / cus, 1.0);
+            return edge == 256 ? std::max(1.03, 1.62 * used) : std::max(0.50, 0.58 * used);
+        };
         for (const bool share : {false, true}) {
             const long long over = tiles % cus, full = tiles / cus;
             WgradPlan p{edge, static_cast<int>(tm), static_cast<int>(tn), static_cast<int>(tiles),
@@ -230,12 +241,12 @@ inline WgradPlan wgrad_plan(int T, int M, int N, int cus)
                     continue;
                 p.whole = static_cast<int>(tiles - over);
                 p.tails = static_cast<int>((over * p.rest() + p.head - 1) / p.head);
-                c = full * (steps * step + 6.0) + p.head * step + 6.0 + 8.0 +
-                    static_cast<double>(over + over + p.tails) * edge * edge * 8.0 / 4.0e6;
+                c = full * (steps * step(cus) + 6.0) + p.head * step(over + p.tails) + 6.0 + 6.0 +
+                    static_cast<double>(over + over + p.tails) * edge * edge * 8.0 / 1.0e7;
             } else {
-                c = full * (steps * step + 6.0);
+                c = full * (steps * step(cus) + 6.0);
                 if (over)
-                    c += steps * (light + (step - light) * over / cus) + 6.0;
+                    c += steps * step(over) + 6.0;
             }
             if (cost < 0 || c < cost) {
                 cost = c;
