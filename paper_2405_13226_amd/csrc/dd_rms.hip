@@ -44,7 +44,7 @@ typedef uint32_t codes8 __attribute__((ext_vector_type(2), aligned(1)));
 // Eight elements from `p`, of which `left` (or more) exist; zeros for the
 // others.  WHOLE: left is a multiple of 8.
 template <bool WHOLE>
-__device__ __forceinline__ void load8(const uint16_t *p, int left, float (&f)[8])
+__device__ __forceinline__ u32x4 load8(const uint16_t *p, int left)
 {
     u32x4 u = {0u, 0u, 0u, 0u};
     if (WHOLE ? left > 0 : left >= 8) {
@@ -55,7 +55,13 @@ __device__ __forceinline__ void load8(const uint16_t *p, int left, float (&f)[8]
             if (i < left)
                 u[i >> 1] |= static_cast<uint32_t>(p[i]) << 16 * (i & 1);
     }
-    unpack8(u, f);
+    return u;
+}
+
+template <bool WHOLE>
+__device__ __forceinline__ void load8(const uint16_t *p, int left, float (&f)[8])
+{
+    unpack8(load8<WHOLE>(p, left), f);
 }
 
 template <bool WHOLE>
@@ -291,8 +297,8 @@ dequantize_kernel(const int8_t *__restrict__ Q, long long ldq, const float *__re
     }
 }
 
-// Backward of rms_rows_per_wg rows per workgroup: dx of each, and their column
-// sums of dy xh into row blockIdx.x of an fp32 workspace.
+// Backward of per_wg rows per workgroup: dx of each, and their column sums of
+// dy xh into row blockIdx.x of an fp32 workspace.
 struct RmsBackOperands {
     const uint16_t *H, *W, *dY, *dRes;
     const float *rstd;
@@ -310,11 +316,12 @@ rms_bwd_kernel(RmsBackOperands op)
     // TPR = 64: the four waves' column sums; else the reductions.
     __shared__ float red[T::ROWS > 1 ? T::ROWS * COLS : 4 * T::WAVES];
     const int t = threadIdx.x % TPR, d = op.d;
-    float w[CH][8], dw[CH][8];
+    u32x4 w[CH];
+    float dw[CH][8];
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
         const int col = (t + TPR * c) * 8;
-        load8<WHOLE>(op.W + col, d - col, w[c]);
+        w[c] = load8<WHOLE>(op.W + col, d - col);
 #pragma unroll
         for (int i = 0; i < 8; ++i)
             dw[c][i] = 0.f;
@@ -325,36 +332,50 @@ rms_bwd_kernel(RmsBackOperands op)
     for (int rr = threadIdx.x / TPR; rr < n; rr += T::ROWS, flip ^= 1) {
         const long long row = row0 + rr, base = row * d;
         const float rstd = op.rstd[row];
-        float xh[CH][8], g[CH][8];
+        u32x4 h[CH], dy[CH], res[CH];
         float s = 0.f;
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
             const int col = (t + TPR * c) * 8;
-            load8<WHOLE>(op.H + base + col, d - col, xh[c]);
-            load8<WHOLE>(op.dY + base + col, d - col, g[c]);
+            h[c] = load8<WHOLE>(op.H + base + col, d - col);
+            dy[c] = load8<WHOLE>(op.dY + base + col, d - col);
+        }
+        if (op.dRes != nullptr) {
+#pragma unroll
+            for (int c = 0; c < CH; ++c) {
+                const int col = (t + TPR * c) * 8;
+                res[c] = load8<WHOLE>(op.dRes + base + col, d - col);
+            }
         }
 #pragma unroll
-        for (int c = 0; c < CH; ++c)
+        for (int c = 0; c < CH; ++c) {
+            float x[8], y[8], v[8];
+            unpack8(h[c], x);
+            unpack8(dy[c], y);
+            unpack8(w[c], v);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                xh[c][i] *= rstd;
-                dw[c][i] += g[c][i] * xh[c][i];
-                g[c][i] *= w[c][i];
-                s += g[c][i] * xh[c][i];
+                const float p = y[i] * (x[i] * rstd);
+                dw[c][i] += p;
+                s += p * v[i];
             }
+        }
         uint32_t none = 0;
         row_reduce<TPR>(s, none, red, flip);
         const float mean = s / d;
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
             const int col = (t + TPR * c) * 8;
-            float out[8];
+            float x[8], y[8], v[8], out[8];
+            unpack8(h[c], x);
+            unpack8(dy[c], y);
+            unpack8(w[c], v);
 #pragma unroll
             for (int i = 0; i < 8; ++i)
-                out[i] = rstd * (g[c][i] - xh[c][i] * mean);
+                out[i] = rstd * (y[i] * v[i] - x[i] * rstd * mean);
             if (op.dRes != nullptr) {
                 float r[8];
-                load8<WHOLE>(op.dRes + base + col, d - col, r);
+                unpack8(res[c], r);
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
                     out[i] += r[i];
@@ -421,14 +442,19 @@ rms_columns_kernel(const float *__restrict__ part, int n, int per, int d, float 
 
 namespace {
 
-// Partial rows of the backward that one launch sums; more go through
-// kRmsChunks chunk sums.
+// Rows per workgroup of the backward.  Every workgroup leaves a row of column
+// sums; at most kRmsOneStage of those are summed in one launch, more go through
+// kRmsChunks chunk sums in two.  So one workgroup per CU for few rows, two for
+// many, and four for short rows, of which a workgroup has few in flight.  us
+// with 256 / 512 / 1024 workgroups: 2048 x 1024 7.9 / 8.9 / 8.9, 4096 x 2048 18.7
+// / 19.9 / 22.3, 16,384 x 5632 172.7 / 166.5 / 170.8, 65,536 x 2048 220.5 / 217.3
+// / 217.5, 65,536 x 512 72.7 / 50.2 / 48.4.
 constexpr int kRmsOneStage = 256, kRmsChunks = 32;
 
-int rms_rows_per_wg(int rows)
+int rms_rows_per_wg(int rows, int d)
 {
-    const long long wgs = (rows <= 16384 ? 1 : rows <= 32768 ? 2 : 4) * kRmsOneStage;
-    const int per = static_cast<int>((rows + wgs - 1) / wgs + 3) / 4 * 4;
+    const int wgs = d <= 512 ? 1024 : rows <= 8192 ? 256 : 512;
+    const int per = static_cast<int>((rows + wgs - 1LL) / wgs + 3) / 4 * 4;
     return std::max(per, 8);
 }
 
@@ -500,7 +526,7 @@ int launch_dequantize(const DequantizeArgs &a)
 
 size_t rmsnorm_workspace_bytes(int rows, int d)
 {
-    const int per = rms_rows_per_wg(rows);
+    const int per = rms_rows_per_wg(rows, d);
     const long long parts = (rows + per - 1LL) / per;
     return static_cast<size_t>(parts + kRmsChunks) * d * sizeof(float);
 }
@@ -508,7 +534,7 @@ size_t rmsnorm_workspace_bytes(int rows, int d)
 int launch_rmsnorm_bwd(const RmsBackArgs &a)
 {
     hipStream_t st = static_cast<hipStream_t>(a.stream);
-    const int per = rms_rows_per_wg(a.rows), parts = static_cast<int>((a.rows + per - 1LL) / per);
+    const int per = rms_rows_per_wg(a.rows, a.d), parts = static_cast<int>((a.rows + per - 1LL) / per);
     auto *part = static_cast<float *>(a.workspace);
     auto *dw = static_cast<uint16_t *>(a.dw);
     const RmsBackOperands op{static_cast<const uint16_t *>(a.H), static_cast<const uint16_t *>(a.w),
