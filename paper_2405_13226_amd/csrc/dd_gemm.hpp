@@ -104,4 +104,21 @@ __device__ __forceinline__ void dma_b128_buf(u32x4 buf, uint32_t off, uint32_t l
                  : "m0", "memory");
 }
 
+// The same with 4 bytes per lane.
+__device__ __forceinline__ void dma_b32_buf(u32x4 buf, uint32_t off, uint32_t lds_base)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds"
+                 :
+                 : "s"(lds_base), "v"(off), "s"(buf)
+                 : "m0", "memory");
+}
+
+// The same value, of which the compiler does not know it: what is formed from
+// it stays where it is used, and is not kept in registers around the K loop.
+__device__ __forceinline__ int fresh(int v)
+{
+    asm volatile("" : "+v"(v));
+    return v;
+}
+
 }  // namespace dd

@@ -12,6 +12,8 @@
 #include "dd_routes.hpp"
 #include "dd_attn.h"
 
+#include <algorithm>
+
 namespace dd {
 
 typedef int i32x4 __attribute__((ext_vector_type(4)));
@@ -67,6 +69,29 @@ __device__ __forceinline__ bf16x4 scaled(const GemmI8Operands &op, i32x4 acc, fl
         }
     }
     return pack4(c[0], c[1], c[2], c[3]);
+}
+
+// c += the eight bf16 values of a piece.
+__device__ __forceinline__ void add8(float (&c)[8], const u32x4 &r)
+{
+    float v[8];
+    unpack8(r, v);
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        c[e] += v[e];
+}
+
+// Stores the first `left` (or all) of eight values at element `o` of C, with
+// the residual.
+__device__ __forceinline__ void store_edge(const GemmI8Operands &op, long long o, int left,
+                                           const float (&c)[8])
+{
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        if (e < left) {
+            const float v = op.R != nullptr ? c[e] + bf16_at(op.R + o + e) : c[e];
+            op.C[o + e] = __builtin_bit_cast(uint16_t, static_cast<__bf16>(v));
+        }
 }
 
 // The finished BM x BN tile in LDS, and from there to memory in 16-byte pieces
@@ -139,30 +164,90 @@ struct I8Loads {
 
 // 256 x 256 tiles, K in steps of 128: the loop of the bf16 product (dd_gemm.hip,
 // which has its phases), since an int8 product instruction takes the bytes and
-// the time of a bf16 one with twice the k.
+// the time of a bf16 one with twice the k.  A tile is so half as many steps, and
+// its start and end weigh twice as much: a workgroup walks tiles blockIdx.x,
+// blockIdx.x + gridDim.x, ... as one sequence of steps, the loads running ahead
+// across tiles, and the accumulators go to memory straight from registers.
+struct I8Walk {
+    I8Loads ld;
+    int tile, count;   // of the next step to load: its tile, how many before it
+    int tm, tn, base;  // lane i: the place of the walk's tile base + i
+    u32x4 sa, sb;      // the scales of the tile's rows and columns
+
+    // A tile's place comes from the lanes' table: its divisions, made at every
+    // tile by every wave, were 2 us of it.
+    __device__ __forceinline__ int m0(int n) const
+    {
+        return __builtin_amdgcn_readlane(tm, n - base) * 256;
+    }
+    __device__ __forceinline__ int n0(int n) const
+    {
+        return __builtin_amdgcn_readlane(tn, n - base) * 256;
+    }
+    __device__ __forceinline__ void places(const GemmI8Operands &op, int from, int lane)
+    {
+        base = from;
+        tile_of(static_cast<int>(blockIdx.x) + (from + lane) * static_cast<int>(gridDim.x),
+                op.tiles_m, op.tiles_n, op.xm, tm, tn);
+    }
+    __device__ __forceinline__ void start(const GemmI8Operands &op, int wave, int lane,
+                                          uint32_t scales)
+    {
+        if (tile < op.tiles_m * op.tiles_n) {
+            if (count - base == 64)  // the tile computed is at most three behind
+                places(op, count - 3, lane);
+            const int m = m0(count), n = n0(count);
+            ld.init(op, m, n, wave, lane);
+            sa = buffer_of(op.sa + m, (op.M - m) * 4LL);
+            sb = buffer_of(op.sb + n, (op.N - n) * 4LL);
+        } else {  // nothing left: the loads read zeros
+            ld.k = 0;
+            ld.a[2] = ld.b[2] = sa[2] = sb[2] = 0;
+        }
+        // 256 + 256 scales, 64 per wave, to one of four places in LDS.
+        const uint32_t l = scales + 2048u * (count & 3) + 256u * wave;
+        if (wave < 4)
+            dma_b32_buf(sa, 4u * (64 * wave + lane), l);
+        else
+            dma_b32_buf(sb, 4u * (64 * (wave - 4) + lane), l);
+    }
+    __device__ __forceinline__ void next(const GemmI8Operands &op, int wave, int lane,
+                                         uint32_t scales)
+    {
+        ld.k += 128;
+        if (ld.k >= op.K) {
+            tile += static_cast<int>(gridDim.x);
+            ++count;
+            start(op, wave, lane, scales);
+        }
+    }
+};
+
 __global__ void __launch_bounds__(512, 1)
 gemm_i8_kernel(GemmI8Operands op)
 {
     constexpr int SUB = 64 * 128, HALF = 2 * SUB, SIDE = 4 * HALF;  // bytes
-    __shared__ __attribute__((aligned(1024))) int8_t lds[2 * SIDE];
+    __shared__ __attribute__((aligned(1024))) int8_t lds[2 * SIDE + 4 * 2048];
     const int tid = threadIdx.x;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
     const int l16 = lane & 15, g = lane >> 4;
     const int wm = wave >> 2, wn = wave & 3;
-    int tm, tn;
-    tile_of(static_cast<int>(blockIdx.x), op.tiles_m, op.tiles_n, op.xm, tm, tn);
-    const int m0 = tm * 256, n0 = tn * 256;
-    const int nkt = (op.K + 127) / 128;
-    I8Loads at;
-    at.init(op, m0, n0, wave, lane);
-    const uint32_t lds0 = lds_base_sgpr(lds) + 1024u * wave;
+    const int tiles = op.tiles_m * op.tiles_n, nkt = (op.K + 127) / 128;
+    const uint32_t lds0 = lds_base_sgpr(lds), scales = lds0 + 2 * SIDE;
+    I8Walk at;
+    at.tile = static_cast<int>(blockIdx.x);
+    at.count = 0;
+    at.places(op, 0, lane);
+    at.start(op, wave, lane, scales);
     auto load_a = [&](int h, int S) __attribute__((always_inline)) {
-        at.load_a(2 * h, lds0 + (2 * h + S) * HALF);
-        at.load_a(2 * h + 1, lds0 + (2 * h + S) * HALF + SUB);
+        const uint32_t l = lds0 + 1024u * wave + (2 * h + S) * HALF;
+        at.ld.load_a(2 * h, l);
+        at.ld.load_a(2 * h + 1, l + SUB);
     };
     auto load_b = [&](int h, int S) __attribute__((always_inline)) {
-        at.load_b(2 * h, lds0 + SIDE + (2 * h + S) * HALF);
-        at.load_b(2 * h + 1, lds0 + SIDE + (2 * h + S) * HALF + SUB);
+        const uint32_t l = lds0 + 1024u * wave + SIDE + (2 * h + S) * HALF;
+        at.ld.load_b(2 * h, l);
+        at.ld.load_b(2 * h + 1, l + SUB);
     };
     const int8_t *fa[2], *fb[2];
 #pragma unroll
@@ -187,124 +272,152 @@ gemm_i8_kernel(GemmI8Operands op)
                 f[j][kk] = *reinterpret_cast<const u32x4 *>(fb[kk] + ((2 * h + S) * HALF + 2048 * j));
     };
     i32x4 acc[2][2][4][2];  // [A half][B half][i][j]
-#pragma unroll
-    for (int x = 0; x < 4; ++x)
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int j = 0; j < 2; ++j)
-                acc[x >> 1][x & 1][i][j] = i32x4{};
-    auto multiply = [&](i32x4 (&c)[4][2], const u32x4 (&a)[4][2],
-                        const u32x4 (&b)[2][2]) __attribute__((always_inline)) {
+    // c += b a, or in a tile's first step c = b a.
+    auto products = [&](i32x4 (&c)[4][2], const u32x4 (&a)[4][2], const u32x4 (&b)[2][2],
+                        bool first) __attribute__((always_inline)) {
+        __builtin_amdgcn_s_setprio(1);
 #pragma unroll
         for (int kk = 0; kk < 2; ++kk)
 #pragma unroll
             for (int i = 0; i < 4; ++i)
 #pragma unroll
                 for (int j = 0; j < 2; ++j)
-                    c[i][j] = mfma_i8(b[j][kk], a[i][kk], c[i][j]);  // rows n, columns m
-    };
-    auto products = [&](i32x4 (&c)[4][2], const u32x4 (&a)[4][2],
-                        const u32x4 (&b)[2][2]) __attribute__((always_inline)) {
-        __builtin_amdgcn_s_setprio(1);
-        multiply(c, a, b);
+                    c[i][j] = mfma_i8(b[j][kk], a[i][kk],
+                                      first && kk == 0 ? i32x4{} : c[i][j]);  // rows n, columns m
         __builtin_amdgcn_s_setprio(0);
         plain_barrier();
     };
-    // One K step from stage S.  MODE 0: also starts the loads of the step
-    // after the next one; 1, 2: the last step but one, the last step.
-    auto step = [&](auto stage, auto mode) __attribute__((always_inline)) {
-        constexpr int S = decltype(stage)::value, MODE = decltype(mode)::value;
+    // Six halves of loads (12) stay in flight, as in the bf16 product; in the
+    // six phases after a whole tile's 16 stores, which no load waits for, those
+    // too.  (A tile's scales are one load more: the waits are then one tighter.)
+    bool stored = false;
+    auto wait = [&](bool first) __attribute__((always_inline)) {
+        if (first && stored)
+            wait_and_barrier<28>();
+        else
+            wait_and_barrier<12>();
+    };
+    // One step from stage S, its tile's first (FIRST 2), second (1) or a later
+    // one.
+    auto step = [&](auto stage, auto first) __attribute__((always_inline)) {
+        constexpr int S = decltype(stage)::value, FIRST = decltype(first)::value;
         read_b(b0, 0, S);
-        if constexpr (MODE == 0)
-            load_a(0, S);
-        wait_and_barrier<MODE == 0 ? 12 : MODE == 1 ? 10 : 2>();
-        products(acc[0][0], a0, b0);
+        load_a(0, S);
+        wait(FIRST > 0);
+        products(acc[0][0], a0, b0, FIRST == 2);
         read_b(b1, 1, S);
-        if constexpr (MODE == 0)
-            load_b(0, S);
-        wait_and_barrier<MODE == 0 ? 12 : MODE == 1 ? 8 : 0>();
-        products(acc[0][1], a0, b1);
+        load_b(0, S);
+        wait(FIRST > 0);
+        products(acc[0][1], a0, b1, FIRST == 2);
         read_a(a1, 1, S);
-        if constexpr (MODE == 0)
-            load_b(1, S);
-        wait_and_barrier<MODE == 0 ? 12 : MODE == 1 ? 6 : 0>();
-        products(acc[1][1], a1, b1);
-        if constexpr (MODE != 2)
-            read_a(a0, 0, 1 - S);
-        if constexpr (MODE == 0) {
-            load_a(1, S);
-            at.k += 128;
-        }
-        wait_and_barrier<MODE == 0 ? 12 : MODE == 1 ? 4 : 0>();
-        products(acc[1][0], a1, b0);
+        load_b(1, S);
+        wait(FIRST > 1);
+        products(acc[1][1], a1, b1, FIRST == 2);
+        read_a(a0, 0, 1 - S);  // of the next step
+        load_a(1, S);
+        at.next(op, wave, lane, scales);
+        wait(FIRST > 1);
+        products(acc[1][0], a1, b0, FIRST == 2);
     };
     auto load_step = [&](int S) __attribute__((always_inline)) {
         load_a(0, S);
         load_b(0, S);
         load_b(1, S);
         load_a(1, S);
-        at.k += 128;
+        at.next(op, wave, lane, scales);
     };
-    if (nkt == 1) {
-        load_step(0);
-        wait_and_barrier<0>();
-        read_a(a0, 0, 0);
-        read_b(b0, 0, 0);
-        multiply(acc[0][0], a0, b0);
-        read_b(b1, 1, 0);
-        multiply(acc[0][1], a0, b1);
-        read_a(a1, 1, 0);
-        multiply(acc[1][1], a1, b1);
-        multiply(acc[1][0], a1, b0);
-    } else {
-        const int s0 = nkt & 1;
-        load_step(s0);
-        load_step(1 - s0);
-        wait_and_barrier<8>();
-        read_a(a0, 0, s0);
-        // Phase 1 refills the half just read: only after a barrier that every
-        // wave reaches with its reads returned.
-        wait_and_barrier<8>();
-        // Waves 4-7 run half a phase behind waves 0-3.
-        if (wm == 1)
-            plain_barrier();
-        for (int kt = 2 - s0; kt < nkt; kt += 2) {
-            if (kt > 1)
-                step(IC<0>{}, IC<0>{});
-            step(IC<1>{}, IC<0>{});
+    load_step(0);
+    load_step(1);
+    wait_and_barrier<8>();
+    read_a(a0, 0, 0);
+    // Phase 1 refills the half just read: only after a barrier that every wave
+    // reaches with its reads returned.
+    wait_and_barrier<8>();
+    // Waves 4-7 run half a phase behind waves 0-3.
+    if (wm == 1)
+        plain_barrier();
+    int tile = static_cast<int>(blockIdx.x), done = 0;
+    // A tile whose first step is in stage S; with an odd number of steps the
+    // next tile's is in the other.
+    auto whole_tile = [&](auto stage) __attribute__((always_inline)) {
+        constexpr int S = decltype(stage)::value;
+        step(IC<S>{}, IC<2>{});
+        if (nkt > 1) {
+            step(IC<1 - S>{}, IC<1>{});
+            for (int kt = 2; kt + 1 < nkt; kt += 2) {
+                step(IC<S>{}, IC<0>{});
+                step(IC<1 - S>{}, IC<0>{});
+            }
+            if (nkt & 1)
+                step(IC<S>{}, IC<0>{});
         }
-        step(IC<0>{}, IC<1>{});
-        step(IC<1>{}, IC<2>{});
-        if (wm == 0)
-            plain_barrier();
-    }
-
-    // Accumulator (ha, hb, i, j), register e: row m = 128 ha + 64 wm + 16 i +
-    // l16, column n = 128 hb + 32 wn + 16 j + 4 g + e of the tile.
-    float rb[2][2][4];
+        // Accumulator (ha, hb, i, j), register e: row m = 128 ha + 64 wm + 16 i
+        // + l16, column n = 128 hb + 32 wn + 16 j + 4 g + e of the tile.  The
+        // lanes of neighbouring g exchange halves of j = 0 and j = 1, after
+        // which a lane holds the eight columns from 16 (g % 2) + 8 (g / 2) on.
+        const int m0 = at.m0(done), n0 = at.n0(done);
+        const bool whole = m0 + 256 <= op.M && n0 + 256 <= op.N;
+        const float *sc = reinterpret_cast<const float *>(lds + 2 * SIDE + 2048 * (done & 3));
+        const int el = fresh(lane), row = 64 * wm + (el & 15);
+        const int col = 32 * wn + 16 * ((el >> 4) & 1) + 8 * (el >> 5);
 #pragma unroll
-    for (int hb = 0; hb < 2; ++hb)
+        for (int hb = 0; hb < 2; ++hb) {
+            const int n = n0 + 128 * hb + col;
+            // Of the lane's first row; from there 32 bits (ldc < 2^23).
+            const long long at0 = (m0 + row) * op.ldc + n;
+            const uint32_t ld = fresh(static_cast<int>(op.ldc));
+            float rb[8];
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
+            for (int e = 0; e < 8; ++e)
+                rb[e] = sc[256 + 128 * hb + col + e];
+            // The residual's pieces first, together: a wait for one also waits
+            // for what is in flight.
+            u32x4 res[8];
+            if (op.R != nullptr) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                rb[hb][j][e] = op.sb[min(n0 + 128 * hb + 32 * wn + 16 * j + 4 * g + e, op.N - 1)];
-    __syncthreads();
-    uint16_t *image = reinterpret_cast<uint16_t *>(lds);
+                for (int x = 0; x < 8; ++x) {
+                    const int r = 128 * (x >> 2) + 16 * (x & 3), m = m0 + r + row;
+                    res[x] = u32x4{0u, 0u, 0u, 0u};
+                    if (whole || (m < op.M && n + 8 <= op.N))
+                        res[x] = *reinterpret_cast<const piece16 *>(op.R + at0 + r * ld);
+                }
+            }
 #pragma unroll
-    for (int x = 0; x < 8; ++x) {
-        const int ha = x >> 2, i = x & 3, r = 128 * ha + 64 * wm + 16 * i + l16;
-        const float ra = op.sa[min(m0 + r, op.M - 1)];
+            for (int x = 0; x < 8; ++x) {
+                const int ha = x >> 2, i = x & 3, r = 128 * ha + 16 * i, m = m0 + r + row;
+                const float ra = sc[r + row];
+                float c[8];
 #pragma unroll
-        for (int y = 0; y < 4; ++y) {
-            const int hb = y >> 1, j = y & 1, c = 128 * hb + 32 * wn + 16 * j + 4 * g;
-            *reinterpret_cast<bf16x4 *>(image + image_off<256>(r, c)) =
-                scaled(op, acc[ha][hb][i][j], ra, rb[hb][j], m0 + r, n0 + c);
+                for (int e = 0; e < 4; ++e) {
+                    const auto p = __builtin_amdgcn_permlane16_swap(acc[ha][hb][i][0][e],
+                                                                    acc[ha][hb][i][1][e], false, false);
+                    c[e] = static_cast<float>(static_cast<int>(p[0])) * ra * rb[e];
+                    c[e + 4] = static_cast<float>(static_cast<int>(p[1])) * ra * rb[e + 4];
+                }
+                const long long o = at0 + r * ld;
+                if (whole || (m < op.M && n + 8 <= op.N)) {
+                    if (op.R != nullptr)
+                        add8(c, res[x]);
+                    *reinterpret_cast<piece16 *>(op.C + o) = pack8f(c);
+                } else if (m < op.M) {
+                    store_edge(op, o, op.N - n, c);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
         }
+        stored = whole;
+        tile += static_cast<int>(gridDim.x);
+        ++done;
+    };
+    while (tile < tiles) {
+        whole_tile(IC<0>{});
+        if ((nkt & 1) && tile < tiles)
+            whole_tile(IC<1>{});
     }
-    __syncthreads();
-    store_image<256, 256>(image, op, m0, n0, tid);
+    if (wm == 0)
+        plain_barrier();
+    // The loads behind the last tile still write to this workgroup's LDS.
+    wait_vmem();
 }
 
 // 128 x 128 tiles for products whose large tiles would leave CUs idle: eight
@@ -499,7 +612,9 @@ int launch_gemm_i8(const GemmI8Args &a)
     GemmI8Operands op{static_cast<const int8_t *>(a.A), static_cast<const int8_t *>(a.B), a.sa,
                       a.sb, static_cast<const uint16_t *>(a.R), static_cast<uint16_t *>(a.C),
                       a.lda, a.ldb, a.ldc, a.M, a.N, a.K, 0, 0, 0};
-    const GemmI8Tile tile = gemm_i8_tile(a.M, a.N, a.K, device_cu_count());
+    GemmI8Tile tile = gemm_i8_tile(a.M, a.N, a.K, device_cu_count());
+    if (tile == GemmI8Tile::kLarge && a.ldc >= 1 << 23)  // its offsets in a tile of C
+        tile = GemmI8Tile::kSmall;
     if (tile == GemmI8Tile::kFew) {
         const int mb = (a.M + 15) / 16;
         const bool two = a.N > 16 * 1024;
@@ -518,8 +633,13 @@ int launch_gemm_i8(const GemmI8Args &a)
     op.tiles_n = (a.N + edge - 1) / edge;
     op.xm = tile_rows_step(op.tiles_m, op.tiles_n);
     const dim3 grid(static_cast<unsigned>(op.tiles_m) * static_cast<unsigned>(op.tiles_n));
-    const hipError_t e = launch_kernel(
-        tile == GemmI8Tile::kLarge ? gemm_i8_kernel : gemm_i8_small_kernel, grid, dim3(512), st, op);
+    // The large tiles' workgroups, one per CU, walk them; a multiple of the
+    // XCDs, so that each keeps its XCD's tiles (tile_of).
+    const unsigned cus = static_cast<unsigned>(std::max(device_cu_count() / kXcds * kXcds, kXcds));
+    const hipError_t e =
+        tile == GemmI8Tile::kLarge
+            ? launch_kernel(gemm_i8_kernel, dim3(std::min(grid.x, cus)), dim3(512), st, op)
+            : launch_kernel(gemm_i8_small_kernel, grid, dim3(512), st, op);
     return e == hipSuccess ? DD_OK : DD_ERR_HIP;
 }
 

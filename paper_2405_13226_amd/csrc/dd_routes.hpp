@@ -181,16 +181,20 @@ inline GemmI8Tile gemm_i8_tile(int M, int N, int K, int cus)
     if (M <= 64)
         return GemmI8Tile::kFew;
     cus = std::max(cus, 1);
-    // us: rounds of workgroups over the CUs, each a start-up and tail and its
-    // K steps, which a full chip's power makes longer on the large tiles (one
-    // per CU of 16 steps: 32 us, 48 of them 22.5; on small tiles 12.4 to 13.2).
+    // us: rounds of tiles over the CUs, each its own start and end and its K
+    // steps, which a full chip's power makes longer on the large tiles (16
+    // steps, one tile on each of 256 CUs 32 us, 16 of them 24; 22 rounds 640).
+    // Those pay more for a launch, and for storing parts of tiles (1531 x 5001
+    // over 1040: 26.6 us, on small tiles 20.4; 2048 x 6144 over 2048: 29.4 and
+    // 40.7).
     auto time = [&](int edge) {
         const double tiles = std::ceil(M / static_cast<double>(edge)) * std::ceil(N / static_cast<double>(edge));
         const double steps = std::ceil(K / 128.0), full = std::floor(tiles / cus), last = tiles / cus - full;
         auto round = [&](double used) {
-            return edge == 256 ? 8.0 + steps * (0.9 + 0.6 * used) : 5.5 + steps * 0.48;
+            return edge == 256 ? 6.5 + steps * (0.9 + 0.55 * used) : 5.5 + steps * 0.48;
         };
-        return full * round(1.0) + (last > 0 ? round(last) : 0.0);
+        const double launch = edge == 256 ? 3.0 + (M % 256 || N % 256 ? 6.0 : 0.0) : 0.0;
+        return launch + full * round(1.0) + (last > 0 ? round(last) : 0.0);
     };
     return time(128) < time(256) ? GemmI8Tile::kSmall : GemmI8Tile::kLarge;
 }

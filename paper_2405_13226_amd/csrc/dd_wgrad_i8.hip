@@ -178,14 +178,6 @@ struct WgradLoads {
     }
 };
 
-// The same value, of which the compiler does not know it: what is formed from
-// it stays where it is used, and is not kept in registers around the K loop.
-__device__ __forceinline__ int fresh(int v)
-{
-    asm volatile("" : "+v"(v));
-    return v;
-}
-
 __device__ __forceinline__ f32x4 mfma16w(bf16x8 a, bf16x8 b, f32x4 c)
 {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);

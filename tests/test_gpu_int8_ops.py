@@ -25,6 +25,7 @@ import torch
 from paper_2405_13226_amd import block_ops as ops
 
 import int8_oracle as O
+import int8_routes as routes
 from int8_oracle import bf16, f64
 from parity import log, rel_l2
 
@@ -232,6 +233,42 @@ def test_gemm_int8(cuda, M, N, K, residual):
     check_product(q, s, p, t, r, c)
 
 
+# The large tiles' workgroups walk several tiles as one sequence of steps: one
+# step a tile to several, odd counts (whose tiles start in alternating stages),
+# whole and ragged tiles, with and without stores that waits must pass over.
+@pytest.mark.parametrize("residual", [False, True])
+@pytest.mark.parametrize("K", [16, 128, 144, 272, 400, 528, 640, 1040])
+@pytest.mark.parametrize("M,N", [(5120, 8192), (4400, 8193)])
+def test_gemm_int8_several_tiles_a_workgroup(cuda, M, N, K, residual):
+    assert routes.product(M, N, K) == "large"
+    q, s = random_codes(M, K, M + K, cuda, full=True)
+    p, t = random_codes(N, K, N + K + 1, cuda, full=True)
+    r = bf16((M, N), 9, 3.0).to(cuda) if residual else None
+    c = ops.gemm_int8(q, s, p, t, residual=r)
+    rows = np.unique(np.r_[np.random.default_rng(0).choice(M, 200, replace=False), 0, 255, 256,
+                           M - 1])
+    check_product(q[rows], s[rows], p, t, None if r is None else r[rows], c[rows])
+
+
+def test_gemm_int8_more_tiles_a_workgroup_than_lanes(cuda):
+    M, N, K = 65536, 16650, 48
+    assert routes.product(M, N, K) == "large" and 256 * ((N + 255) // 256) > 64 * routes.CUS
+    q, s = random_codes(M, K, 1, cuda)
+    p, t = random_codes(N, K, 2, cuda)
+    c = ops.gemm_int8(q, s, p, t)
+    rows = np.unique(np.r_[np.arange(0, M, 509), M - 1])
+    check_product(q[rows], s[rows], p, t, None, c[rows])
+
+
+@pytest.mark.parametrize("M,N,K,form", [(64, 300, 80, "few"), (65, 300, 80, "small"),
+                                        (1531, 777, 640, "small"), (2048, 6144, 2048, "large")])
+def test_products_reach_every_form(cuda, M, N, K, form):
+    assert routes.product(M, N, K) == form
+    q, s = random_codes(M, K, 3, cuda)
+    p, t = random_codes(N, K, 4, cuda)
+    check_product(q, s, p, t, None, ops.gemm_int8(q, s, p, t))
+
+
 def test_gemm_int8_extreme_codes_sum_exactly(cuda):
     # all codes -128: the longest sum is 131056 * 2^14, just below 2^31
     for M, N in ((1, 20), (70, 70)):
@@ -297,6 +334,23 @@ def test_gemm_int8_wgrad(cuda, T, M, N):
     mag = np.abs(x).T @ np.abs(f64(dy))
     close(f64(dw), ref, B * np.abs(ref) + T * U * mag, "dw")
     assert rel_l2(f64(dw), ref) <= 3e-3
+
+
+@pytest.mark.parametrize("T,M,N,edge,shared", [
+    (1000, 520, 264, 128, False), (4096, 1024, 1024, 128, True), (16384, 2048, 2048, 256, True),
+    (1024, 4096, 4096, 256, False), (2048, 4200, 4360, 256, True)])
+def test_weight_gradients_reach_every_form(cuda, T, M, N, edge, shared):
+    form = routes.wgrad(T, M, N)
+    assert form["edge"] == edge and (form["shared"] > 0) == shared, form
+    q, s = random_codes(T, M, 5, cuda)
+    dy = bf16((T, N), 6).to(cuda)
+    dw = f64(ops.gemm_int8_wgrad(q, s, dy))
+    x = f64(ops.dequantize(q, s))
+    rows = np.unique(np.r_[np.random.default_rng(0).choice(M, 100, replace=False), 0, M - 1])
+    ref = x[:, rows].T @ f64(dy)
+    mag = np.abs(x[:, rows]).T @ np.abs(f64(dy))
+    close(dw[rows], ref, B * np.abs(ref) + T * U * mag, "dw")
+    assert rel_l2(dw[rows], ref) <= 3e-3
 
 
 @pytest.mark.parametrize("T,M,N", [(100, 40, 72), (500, 264, 264)])

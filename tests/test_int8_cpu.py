@@ -9,6 +9,7 @@ import torch
 from paper_2405_13226_amd import _lib, block_ops as ops
 
 import int8_oracle as O
+import int8_routes as routes
 
 OK, NULL, SHAPE, HEADDIM, DOCLENS, WORKSPACE, ALIGN, ALIAS = range(8)
 
@@ -146,6 +147,58 @@ def test_wrappers_refuse_what_is_not_on_a_gpu_or_of_another_type():
               lambda: ops.gemm_int8(q, s, q, s), lambda: ops.gemm_int8_wgrad(q, s, x)):
         with pytest.raises(ValueError):
             f()
+
+
+def parts_of(plan, wg):
+    """The (tile, first step, steps, slot) that a workgroup computes."""
+    if wg < plan["whole"]:
+        return [(wg, 0, plan["steps"], -1)]
+    i = wg - plan["whole"]
+    if i < plan["shared"]:
+        return [(wg, 0, plan["head"], i)]
+    w, rest = i - plan["shared"], plan["steps"] - plan["head"]
+    at, end, out = w * plan["head"], min((w + 1) * plan["head"], plan["shared"] * rest), []
+    while at < end:
+        tile, skip = divmod(at, rest)
+        n = min(rest - skip, end - at)
+        out.append((plan["whole"] + tile, plan["head"] + skip, n,
+                    plan["shared"] + w * plan["most"] + len(out)))
+        at += n
+    return out
+
+
+@pytest.mark.parametrize("T,M,N", [(65536, 2048, 5632), (3001, 1040, 1416), (65536, 256, 256),
+                                   (4096, 1024, 1024), (16384, 1024, 2816), (700, 4352, 4360),
+                                   (65536, 4096, 8192), (200000, 264, 520), (9000, 1800, 5000),
+                                   (1, 8, 8), (33554368, 8, 8)])
+def test_weight_gradient_plans_cover_every_step_once(T, M, N):
+    p = routes.wgrad(T, M, N)
+    assert p["tiles"] == p["whole"] + p["shared"]
+    covered, slots = {}, set()
+    for wg in range(p["whole"] + p["shared"] + p["tails"]):
+        parts = parts_of(p, wg)
+        assert parts and len(parts) <= p["most"]
+        assert sum(n for _, _, n, _ in parts) <= max(p["head"], p["steps"])
+        for tile, first, n, slot in parts:
+            assert n > 0 and first + n <= p["steps"]
+            covered.setdefault(tile, []).append((first, n))
+            assert slot < 0 or slot not in slots
+            slots.add(slot)
+            # and where the last launch looks for it
+            rest = p["steps"] - p["head"]
+            if slot >= p["shared"]:
+                w, i = wg - p["whole"] - p["shared"], tile - p["whole"]
+                assert i * rest // p["head"] <= w <= ((i + 1) * rest - 1) // p["head"]
+                assert slot == p["shared"] + w * p["most"] + i - w * p["head"] // rest
+    assert sorted(covered) == list(range(p["tiles"]))
+    for parts in covered.values():
+        at = 0
+        for first, n in sorted(parts):
+            assert first == at
+            at += n
+        assert at == p["steps"]
+    # a shared tile's workgroups are resident together with the others
+    assert p["shared"] + p["tails"] <= routes.CUS
 
 
 def test_oracle_codes_take_ties_to_even():
