@@ -326,21 +326,22 @@ size_t dd_rmsnorm_bwd_workspace_bytes(int rows, int d);
  * multiples of 16 below 2^23, A and B 16-byte aligned.  C must not overlap
  * the other inputs.
  *
- * dd_gemm_i8_wgrad: the weight gradient of a layer y = x W whose input was
- * kept as codes: dW [M][N] = X^T dY with X = bf16(scales Q), Q [T][M] int8,
- * dY [T][N] bf16, fp32 sums.  1 <= T <= 2^25 - 64, M and N multiples of 8; strides
- * multiples of 8, ldq and ldy below 2^23; Q 8-byte, dY and dW 16-byte aligned.
- * dW must not overlap the inputs.  workspace: scratch of
- * dd_gemm_i8_wgrad_workspace_bytes(T, M, N) bytes, 16-byte aligned (may be
- * NULL where that is 0).
+ * dd_gemm_i8_wgrad: the weight gradients of n (1 to 3) layers y = x W that
+ * share their input, kept as codes: dW[i] [M][N] = X^T dY[i] with X =
+ * bf16(scales Q), Q [T][M] int8, dY[i] [T][N] bf16, fp32 sums in a fixed order.
+ * 1 <= T <= 2^25 - 64, M and N multiples of 8; strides multiples of 8, ldq and
+ * ldy below 2^23; Q 8-byte, dY[i] and dW[i] 16-byte aligned.  The dW[i] may be
+ * column slices of one matrix, and must not overlap each other otherwise, nor
+ * the inputs.  workspace: scratch of dd_gemm_i8_wgrad_workspace_bytes(T, M, N,
+ * n) bytes, 16-byte aligned; it holds X in bf16.
  */
 int dd_gemm_i8(const int8_t *A, long long lda, const float *sa, const int8_t *B, long long ldb,
                const float *sb, const void *R, void *C, long long ldc, int M, int N, int K,
                void *stream);
-int dd_gemm_i8_wgrad(const int8_t *Q, long long ldq, const float *scales, const void *dY,
-                     long long ldy, void *dW, long long ldw, int T, int M, int N, void *workspace,
-                     size_t workspace_bytes, void *stream);
-size_t dd_gemm_i8_wgrad_workspace_bytes(int T, int M, int N); /* 0: none needed, or invalid */
+int dd_gemm_i8_wgrad(const int8_t *Q, long long ldq, const float *scales, const void *const *dY,
+                     long long ldy, void *const *dW, long long ldw, int n, int T, int M, int N,
+                     void *workspace, size_t workspace_bytes, void *stream);
+size_t dd_gemm_i8_wgrad_workspace_bytes(int T, int M, int N, int n); /* 0: invalid */
 
 /* Workspace bytes dd_attn_bwd needs for this shape (0 for an invalid shape). */
 size_t dd_attn_bwd_workspace_bytes(int B, int L, int H, int D);

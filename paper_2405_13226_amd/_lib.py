@@ -51,9 +51,9 @@ SIGNATURES = {
                                       _P]),
     "dd_rmsnorm_bwd_workspace_bytes": (ctypes.c_size_t, [_I, _I]),
     "dd_gemm_i8": (ctypes.c_int, [_P, _L, _P, _P, _L, _P, _P, _P, _L, _I, _I, _I, _P]),
-    "dd_gemm_i8_wgrad": (ctypes.c_int, [_P, _L, _P, _P, _L, _P, _L, _I, _I, _I, _P,
+    "dd_gemm_i8_wgrad": (ctypes.c_int, [_P, _L, _P, _P, _L, _P, _L, _I, _I, _I, _I, _P,
                                         ctypes.c_size_t, _P]),
-    "dd_gemm_i8_wgrad_workspace_bytes": (ctypes.c_size_t, [_I, _I, _I]),
+    "dd_gemm_i8_wgrad_workspace_bytes": (ctypes.c_size_t, [_I, _I, _I, _I]),
     "dd_doclens_check": (ctypes.c_int, [_P, _I, ctypes.c_longlong]),
     "dd_status_str": (ctypes.c_char_p, [_I]),
     "dd_prof_enable": (ctypes.c_int, [_I]),

@@ -419,28 +419,42 @@ def gemm_int8_wgrad(codes, scales, dy, out=None):
     """``dequantize(codes, scales).T @ dy``: the weight gradient [M, N] of a
     linear layer from its input, kept as codes [T, M], and the gradient dy
     [T, N] of its output; M and N multiples of 8."""
+    return gemm_int8_wgrad_group(codes, scales, [dy], None if out is None else [out])[0]
+
+
+def gemm_int8_wgrad_group(codes, scales, dys, outs=None):
+    """``gemm_int8_wgrad`` of layers that share their input: one result for
+    each of dys (one to three of one shape and row stride), in one launch."""
     _code_matrix(codes, "codes")
-    dev, (T, M) = codes.device, codes.shape
+    dev, (T, M), n = codes.device, codes.shape, len(dys)
     _vec(scales, "scales", T, torch.float32, dev)
-    _mat(dy, "dy")
-    _on(dy, "dy", dev)
-    N = dy.shape[1]
-    if dy.shape[0] != T:
-        raise ValueError(f"codes have {T} rows, dy has {dy.shape[0]}")
+    if not 1 <= n <= 3:
+        raise ValueError(f"need one to three gradients (got {n})")
+    for dy in dys:
+        _mat(dy, "dy")
+        _on(dy, "dy", dev)
+        if dy.shape != dys[0].shape or _ld(dy) != _ld(dys[0]):
+            raise ValueError("the dy matrices must agree in shape and row stride")
+    N = dys[0].shape[1]
+    if dys[0].shape[0] != T:
+        raise ValueError(f"codes have {T} rows, dy has {dys[0].shape[0]}")
     if M % 8 or N % 8:
         raise ValueError(f"the columns of codes and dy must be multiples of 8 (got {M} and {N})")
-    if out is None:
-        out = torch.empty((M, N), dtype=torch.bfloat16, device=dev)
+    if outs is None:
+        outs = [torch.empty((M, N), dtype=torch.bfloat16, device=dev) for _ in dys]
     else:
-        _mat(out, "out")
-        _on(out, "out", dev)
-        if out.shape != (M, N):
-            raise ValueError(f"out has shape {tuple(out.shape)}, expected {(M, N)}")
+        if len(outs) != n:
+            raise ValueError(f"need {n} outputs of shape {(M, N)}")
+        for out in outs:
+            _mat(out, "out")
+            _on(out, "out", dev)
+            if out.shape != (M, N) or _ld(out) != _ld(outs[0]):
+                raise ValueError(f"need {n} outputs of shape {(M, N)} and one row stride")
     if not T:
-        return out.zero_()
-    if out.numel():
-        need = lib().dd_gemm_i8_wgrad_workspace_bytes(T, M, N)
-        ws = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
-        _call(dev, "dd_gemm_i8_wgrad", _p(codes), _ld(codes), _p(scales), _p(dy), _ld(dy),
-              _p(out), _ld(out), T, M, N, _p(ws), need)
-    return out
+        return [out.zero_() for out in outs]
+    if M and N:
+        need = lib().dd_gemm_i8_wgrad_workspace_bytes(T, M, N, n)
+        ws = torch.empty(need, dtype=torch.uint8, device=dev)
+        _call(dev, "dd_gemm_i8_wgrad", _p(codes), _ld(codes), _p(scales), _array(dys),
+              _ld(dys[0]), _array(outs), _ld(outs[0]), n, T, M, N, _p(ws), need)
+    return outs

@@ -188,44 +188,72 @@ int dd_gemm_i8(const int8_t *A, long long lda, const float *sa, const int8_t *B,
 namespace {
 
 // T: the restored input's rows have to keep 32-bit offsets too (64 of them).
-bool wgrad_ok(int T, int M, int N)
+bool wgrad_ok(int T, int M, int N, int n)
 {
-    return T >= 1 && T <= (1 << 25) - 64 && M >= 8 && N >= 8 && M % 8 == 0 && N % 8 == 0 && tiles64(M, N) <= kMaxTiles;
+    return n >= 1 && n <= 3 && T >= 1 && T <= (1 << 25) - 64 && M >= 8 && N >= 8 && M % 8 == 0 &&
+           N % 8 == 0 && n * tiles64(M, N) <= kMaxTiles;
 }
 
 }  // namespace
 
-size_t dd_gemm_i8_wgrad_workspace_bytes(int T, int M, int N)
+size_t dd_gemm_i8_wgrad_workspace_bytes(int T, int M, int N, int n)
 {
-    return wgrad_ok(T, M, N) ? dd::wgrad_i8_workspace_bytes(T, M, N) : 0;
+    return wgrad_ok(T, M, N, n) ? dd::wgrad_i8_workspace_bytes(T, M, N, n) : 0;
 }
 
-int dd_gemm_i8_wgrad(const int8_t *Q, long long ldq, const float *scales, const void *dY,
-                     long long ldy, void *dW, long long ldw, int T, int M, int N, void *workspace,
-                     size_t workspace_bytes, void *stream)
+int dd_gemm_i8_wgrad(const int8_t *Q, long long ldq, const float *scales, const void *const *dY,
+                     long long ldy, void *const *dW, long long ldw, int n, int T, int M, int N,
+                     void *workspace, size_t workspace_bytes, void *stream)
 {
     if (!Q || !scales || !dY || !dW)
         return DD_ERR_NULL;
-    if (!wgrad_ok(T, M, N) || ldq < M || ldy < N || ldw < N || ldq >= kMaxStride ||
+    if (!wgrad_ok(T, M, N, n) || ldq < M || ldy < N || ldw < N || ldq >= kMaxStride ||
         ldy >= kMaxStride)
         return DD_ERR_SHAPE;
-    if (ldq % 8 || ldy % 8 || ldw % 8 || !aligned(Q, 8) || !aligned_all({dY, dW}, 16) ||
-        !aligned(scales, 4))
+    for (int i = 0; i < n; ++i)
+        if (!dY[i] || !dW[i])
+            return DD_ERR_NULL;
+    if (ldq % 8 || ldy % 8 || ldw % 8 || !aligned(Q, 8) || !aligned(scales, 4))
         return DD_ERR_ALIGN;
-    const size_t need = dd::wgrad_i8_workspace_bytes(T, M, N);
+    for (int i = 0; i < n; ++i)
+        if (!aligned_all({dY[i], dW[i]}, 16))
+            return DD_ERR_ALIGN;
+    const size_t need = dd::wgrad_i8_workspace_bytes(T, M, N, n);
     if (need && (!workspace || workspace_bytes < need))
         return DD_ERR_WORKSPACE;
     if (need && !aligned(workspace, 16))
         return DD_ERR_ALIGN;
-    const int st = check_apart({range_of(Q, matrix_bytes(T, M, ldq, 1)),
-                                range_of(scales, static_cast<size_t>(T) * 4),
-                                range_of(dY, matrix_bytes(T, N, ldy, 2))},
-                               {range_of(dW, matrix_bytes(M, N, ldw, 2)),
-                                range_of(workspace, need)});
+    const Range q = range_of(Q, matrix_bytes(T, M, ldq, 1)),
+                sc = range_of(scales, static_cast<size_t>(T) * 4), ws = range_of(workspace, need);
+    const size_t wb = matrix_bytes(M, N, ldw, 2);
+    int st = check_apart({q, sc}, {ws});
+    for (int i = 0; i < n && st == DD_OK; ++i) {
+        const Range w = range_of(dW[i], wb), y = range_of(dY[i], matrix_bytes(T, N, ldy, 2));
+        st = check_apart({q, sc, ws}, {w});
+        if (st == DD_OK)
+            st = check_apart({y}, {ws});
+        for (int j = 0; j < n && st == DD_OK; ++j) {
+            const Range v = range_of(dW[j], wb);
+            if (overlaps(v, y))
+                st = DD_ERR_ALIAS;
+            // Outputs may be column slices of one matrix: they are apart if
+            // their columns are.
+            if (j < i && overlaps(v, w)) {
+                const long long shift =
+                    static_cast<long long>(w.lo < v.lo ? v.lo - w.lo : w.lo - v.lo) / 2 % ldw;
+                if (shift < N || shift + N > ldw)
+                    st = DD_ERR_ALIAS;
+            }
+        }
+    }
     if (st != DD_OK)
         return st;
-    return dd::launch_wgrad_i8(
-        dd::WgradI8Args{Q, dY, scales, dW, workspace, ldq, ldy, ldw, T, M, N, stream});
+    dd::WgradI8Args a{Q, {}, scales, {}, workspace, ldq, ldy, ldw, n, T, M, N, stream};
+    for (int i = 0; i < n; ++i) {
+        a.dY[i] = dY[i];
+        a.dW[i] = dW[i];
+    }
+    return dd::launch_wgrad_i8(a);
 }
 
 }  // extern "C"

@@ -172,17 +172,17 @@ struct GemmI8Args {
 };
 int launch_gemm_i8(const GemmI8Args &a);
 
-// dW [M][N] = X^T dY with X = bf16(scales Q), Q [T][M] int8, dY [T][N] bf16
-// (dd_wgrad_i8.hip).
+// dW[i] [M][N] = X^T dY[i], i < n, with X = bf16(scales Q), Q [T][M] int8,
+// dY[i] [T][N] bf16 (dd_wgrad_i8.hip).
 struct WgradI8Args {
-    const void *Q, *dY;
+    const void *Q, *dY[3];
     const float *scales;
-    void *dW, *workspace;
+    void *dW[3], *workspace;
     long long ldq, ldy, ldw;
-    int T, M, N;
+    int n, T, M, N;
     void *stream;
 };
-size_t wgrad_i8_workspace_bytes(int T, int M, int N);
+size_t wgrad_i8_workspace_bytes(int T, int M, int N, int n);
 int launch_wgrad_i8(const WgradI8Args &a);
 
 // Both return a dd_status value (DD_OK or DD_ERR_HIP).

@@ -199,8 +199,8 @@ inline GemmI8Tile gemm_i8_tile(int M, int N, int K, int cus)
     return time(128) < time(256) ? GemmI8Tile::kSmall : GemmI8Tile::kLarge;
 }
 
-// How a weight gradient of M x N over T tokens runs: on tiles of 256 x 256 or
-// 128 x 128 (`edge`), T in `steps` of 64 tokens.  The first `whole` tiles are a
+// How `n` weight gradients of M x N over T tokens run: on tiles of 256 x 256 or
+// 128 x 128 (`edge`; tiles_n of all n), T in `steps` of 64 tokens.  The first `whole` tiles are a
 // workgroup's each.  The others, fewer than the CUs, are shared out so that
 // every workgroup has `head` steps: one workgroup per tile takes its first
 // `head`, and the rest of them, one tile after the other, is cut into pieces
@@ -217,14 +217,14 @@ struct WgradPlan {
     long long partials() const { return head ? shared() + static_cast<long long>(tails) * most() : 0; }
 };
 
-inline WgradPlan wgrad_plan(int T, int M, int N, int cus)
+inline WgradPlan wgrad_plan(int T, int M, int N, int n, int cus)
 {
     cus = std::max(cus, 1);
     const int steps = static_cast<int>((T + 63LL) / 64);
     WgradPlan best{};
     double cost = -1;
     for (const int edge : {256, 128}) {
-        const long long tm = (M + edge - 1LL) / edge, tn = (N + edge - 1LL) / edge, tiles = tm * tn;
+        const long long tm = (M + edge - 1LL) / edge, tn = (N + edge - 1LL) / edge * n, tiles = tm * tn;
         // us a step: with few workgroups its latency, with a full chip its
         // power (2048 x 5632, 16,384 tokens: 176 workgroups of 256 steps
         // 300 us, 256 of 176 steps 280; 256 x 256, 65,536 tokens, one

@@ -1,5 +1,6 @@
 // dd_wgrad_i8.hip -- the weight gradient of a linear layer whose input was kept
-// in 8 bits:  dW[m, n] = sum over t of X[t, m] dY[t, n],  X = bf16(scales Q).
+// in 8 bits:  dW[m, n] = sum over t of X[t, m] dY[t, n],  X = bf16(scales Q);
+// up to three dY at once (projections that share their input).
 //
 // The restored input is bf16, as the activation that was saved; the products
 // are bf16 matrix-core products with fp32 sums.  Any T, M and N (M and N
@@ -87,15 +88,38 @@ restore_kernel(const int8_t *__restrict__ Q, long long ldq, const float *__restr
     }
 }
 
-// P: fp32 parts of the shared tiles: one per tile for its first `head` steps,
-// then `most` per further workgroup.
+// dW[i] = X^T dY[i] for up to three dY.  Their tiles are one grid of tiles_m x
+// tiles_n, `cols` columns of it each.  P: fp32 parts of the shared tiles: one
+// per tile for its first `head` steps, then `most` per further workgroup.
 struct WgradOperands {
-    const uint16_t *XT, *dY;
-    uint16_t *dW;
+    const uint16_t *XT, *dY[3];
+    uint16_t *dW[3];
     float *P;
     long long Tp, ldy, ldw;
-    int T, M, N, tiles_m, tiles_n, xm, whole, shared, steps, head, rest, most;
+    int T, M, N, tiles_m, tiles_n, cols, xm, whole, shared, steps, head, rest, most;
 };
+
+// Where a tile is: its gradient and its first row and column in that.
+struct WgradPlace {
+    int i, m0, n0;
+};
+
+template <int EDGE>
+__device__ __forceinline__ WgradPlace wgrad_place(const WgradOperands &op, int tile)
+{
+    int tm, tn;
+    tile_of(tile, op.tiles_m, op.tiles_n, op.xm, tm, tn);
+    const int i = (tn >= op.cols) + (tn >= 2 * op.cols);
+    return WgradPlace{i, tm * EDGE, (tn - i * op.cols) * EDGE};
+}
+
+// One of three pointers; an array in the kernel's arguments that is indexed
+// at run time would be copied to memory.
+template <typename P>
+__device__ __forceinline__ P pick3(P const (&p)[3], int i)
+{
+    return i == 0 ? p[0] : i == 1 ? p[1] : p[2];
+}
 
 // The parts of tiles that workgroup `id` computes, one after the other: steps
 // `first` .. first + count - 1 of `tile`, stored to part `slot`, or as the
@@ -149,17 +173,17 @@ struct WgradLoads {
     uint32_t va, vb, b_step;
     long long a_step;     // from sub-tile to sub-tile (elements)
 
-    __device__ __forceinline__ void init(const WgradOperands &op, int m0, int n0, long long kbeg,
+    __device__ __forceinline__ void init(const WgradOperands &op, const WgradPlace &p, long long kbeg,
                                          int wave, int lane)
     {
         const int r = 8 * wave + (lane >> 3);
-        a = op.XT + m0 * op.Tp + kbeg;
+        a = op.XT + p.m0 * op.Tp + kbeg;
         a_step = 64 * op.Tp;
         va = static_cast<uint32_t>(r * op.Tp * 2 + ((lane & 7) ^ row_swz(r)) * 16);
-        b_left = ((op.T - 1LL - kbeg) * op.ldy + op.N - n0) * 2;
+        b_left = ((op.T - 1LL - kbeg) * op.ldy + op.N - p.n0) * 2;
         b_step = static_cast<uint32_t>(64 * op.ldy * 2);
         vb = static_cast<uint32_t>((r * op.ldy + ((lane & 7) ^ swz<64>(r)) * 8) * 2);
-        buf = buffer_of(op.dY + kbeg * op.ldy + n0, b_left);
+        buf = buffer_of(pick3(op.dY, p.i) + kbeg * op.ldy + p.n0, b_left);
     }
     __device__ __forceinline__ void next()
     {
@@ -191,16 +215,17 @@ __device__ __forceinline__ int wgrad_off(int r, int c)
 }
 
 template <int BM, int BN>
-__device__ __forceinline__ void wgrad_store(const uint16_t *lds, const WgradOperands &op, int m0,
-                                            int n0, int tid)
+__device__ __forceinline__ void wgrad_store(const uint16_t *lds, const WgradOperands &op,
+                                            const WgradPlace &p, int tid)
 {
     constexpr int CPR = BN / 8;
+    uint16_t *dW = pick3(op.dW, p.i);
 #pragma unroll 4
     for (int it = 0; it < BM * CPR / 512; ++it) {
         const int idx = it * 512 + tid, r = idx / CPR, c = idx % CPR * 8;
         const u32x4 v = *reinterpret_cast<const u32x4 *>(lds + wgrad_off<BN>(r, c));
-        if (m0 + r < op.M && n0 + c < op.N)
-            *reinterpret_cast<u32x4 *>(op.dW + (m0 + r) * op.ldw + n0 + c) = v;
+        if (p.m0 + r < op.M && p.n0 + c < op.N)
+            *reinterpret_cast<u32x4 *>(dW + (p.m0 + r) * op.ldw + p.n0 + c) = v;
     }
 }
 
@@ -208,7 +233,8 @@ __device__ __forceinline__ void wgrad_store(const uint16_t *lds, const WgradOper
 // (row, column, the values of four columns): an fp32 part, or the result.
 template <int EDGE, typename F>
 __device__ __forceinline__ void finish_part(const WgradOperands &op, const WgradParts &part,
-                                            uint16_t *lds, int m0, int n0, int tid, F each)
+                                            uint16_t *lds, const WgradPlace &place, int tid,
+                                            F each)
 {
     if (part.slot >= 0) {
         float *dst = op.P + static_cast<long long>(part.slot) * (EDGE * EDGE);
@@ -221,7 +247,7 @@ __device__ __forceinline__ void finish_part(const WgradOperands &op, const Wgrad
             *reinterpret_cast<bf16x4 *>(lds + wgrad_off<EDGE>(r, c)) = pack4(v[0], v[1], v[2], v[3]);
         });
         __syncthreads();
-        wgrad_store<EDGE, EDGE>(lds, op, m0, n0, fresh(tid));
+        wgrad_store<EDGE, EDGE>(lds, op, place, fresh(tid));
     }
 }
 
@@ -235,7 +261,6 @@ wgrad_kernel(WgradOperands op)
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
     const int l16 = lane & 15, g = lane >> 4;
     const int wm = wave >> 2, wn = wave & 3;
-    int m0 = 0, n0 = 0;
     WgradLoads at;
     const uint32_t lds0 = lds_base_sgpr(lds) + 1024u * wave;
     auto load_a = [&](int h, int S) __attribute__((always_inline)) {
@@ -330,12 +355,9 @@ wgrad_kernel(WgradOperands op)
     WgradParts part;
     part.init(op, static_cast<int>(blockIdx.x));
     for (;;) {
-        int tm, tn;
-        tile_of(part.tile, op.tiles_m, op.tiles_n, op.xm, tm, tn);
-        m0 = tm * 256;
-        n0 = tn * 256;
+        const WgradPlace place = wgrad_place<256>(op, part.tile);
         const int nkt = part.count;
-        at.init(op, m0, n0, part.first * 64LL, wave, fresh(lane));
+        at.init(op, place, part.first * 64LL, wave, fresh(lane));
 #pragma unroll
         for (int x = 0; x < 4; ++x)
 #pragma unroll
@@ -391,7 +413,7 @@ wgrad_kernel(WgradOperands op)
                 __builtin_amdgcn_sched_barrier(0);
             }
         };
-        finish_part<256>(op, part, lds, m0, n0, tid, finish);
+        finish_part<256>(op, part, lds, place, tid, finish);
         if (!part.more())
             return;
         part.next(op);
@@ -411,7 +433,6 @@ wgrad_small_kernel(WgradOperands op)
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
     const int l16 = lane & 15, g = lane >> 4;
     const int wm = wave >> 2, wn = wave & 3;
-    int m0 = 0, n0 = 0;
     WgradLoads at;
     const uint32_t lds0 = lds_base_sgpr(lds) + 1024u * wave;
     auto load_step = [&](int st) __attribute__((always_inline)) {
@@ -435,12 +456,9 @@ wgrad_small_kernel(WgradOperands op)
     WgradParts part;
     part.init(op, static_cast<int>(blockIdx.x));
     for (;;) {
-        int tm, tn;
-        tile_of(part.tile, op.tiles_m, op.tiles_n, op.xm, tm, tn);
-        m0 = tm * 128;
-        n0 = tn * 128;
+        const WgradPlace place = wgrad_place<128>(op, part.tile);
         const int nkt = part.count;
-        at.init(op, m0, n0, part.first * 64LL, wave, fresh(lane));
+        at.init(op, place, part.first * 64LL, wave, fresh(lane));
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -507,7 +525,7 @@ wgrad_small_kernel(WgradOperands op)
                 for (int j = 0; j < 2; ++j)
                     put(64 * wm + 16 * i + el16, 32 * wn + 16 * j + 4 * eg, acc[i][j]);
         };
-        finish_part<128>(op, part, lds, m0, n0, tid, finish);
+        finish_part<128>(op, part, lds, place, tid, finish);
         if (!part.more())
             return;
         part.next(op);
@@ -523,9 +541,8 @@ wgrad_sum_kernel(WgradOperands op)
     constexpr int PER = EDGE * EDGE / 8 / 256;  // workgroups per tile
     const int tile = static_cast<int>(blockIdx.x) / PER;
     const int v = static_cast<int>(blockIdx.x) % PER * 256 + threadIdx.x;
-    int tm, tn;
-    tile_of(op.whole + tile, op.tiles_m, op.tiles_n, op.xm, tm, tn);
-    const int m = tm * EDGE + v / (EDGE / 8), n = tn * EDGE + v % (EDGE / 8) * 8;
+    const WgradPlace place = wgrad_place<EDGE>(op, op.whole + tile);
+    const int m = place.m0 + v / (EDGE / 8), n = place.n0 + v % (EDGE / 8) * 8;
     if (m >= op.M || n >= op.N)
         return;
     f32x4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = s0;
@@ -540,7 +557,7 @@ wgrad_sum_kernel(WgradOperands op)
     const int w0 = tile * op.rest / op.head, w1 = ((tile + 1) * op.rest - 1) / op.head;
     for (int w = w0; w <= w1; ++w)
         add(op.shared + w * op.most + tile - w * op.head / op.rest);
-    *reinterpret_cast<bf16x8 *>(op.dW + m * op.ldw + n) =
+    *reinterpret_cast<bf16x8 *>(pick3(op.dW, place.i) + m * op.ldw + n) =
         join(pack4(s0[0], s0[1], s0[2], s0[3]), pack4(s1[0], s1[1], s1[2], s1[3]));
 }
 
@@ -552,25 +569,25 @@ struct WgradSpace {
     size_t restored, partials;
 };
 
-WgradSpace wgrad_space(int T, int M, int N)
+WgradSpace wgrad_space(int T, int M, int N, int n)
 {
-    const WgradPlan p = wgrad_plan(T, M, N, device_cu_count());
+    const WgradPlan p = wgrad_plan(T, M, N, n, device_cu_count());
     return WgradSpace{p, static_cast<size_t>(p.tiles_m) * p.edge * p.steps * 128,
                       static_cast<size_t>(p.partials()) * p.edge * p.edge * sizeof(float)};
 }
 
 }  // namespace
 
-size_t wgrad_i8_workspace_bytes(int T, int M, int N)
+size_t wgrad_i8_workspace_bytes(int T, int M, int N, int n)
 {
-    const WgradSpace w = wgrad_space(T, M, N);
+    const WgradSpace w = wgrad_space(T, M, N, n);
     return w.restored + w.partials;
 }
 
 int launch_wgrad_i8(const WgradI8Args &a)
 {
     hipStream_t st = static_cast<hipStream_t>(a.stream);
-    const WgradSpace w = wgrad_space(a.T, a.M, a.N);
+    const WgradSpace w = wgrad_space(a.T, a.M, a.N, a.n);
     const WgradPlan &p = w.plan;
     const long long Tp = p.steps * 64LL;
     auto *xt = static_cast<uint16_t *>(a.workspace);
@@ -583,10 +600,29 @@ int launch_wgrad_i8(const WgradI8Args &a)
     if (e != hipSuccess)
         return DD_ERR_HIP;
     const int shared = p.head ? p.shared() : 0;
-    const WgradOperands op{xt, static_cast<const uint16_t *>(a.dY), static_cast<uint16_t *>(a.dW),
-                           parts, Tp, a.ldy, a.ldw, a.T, a.M, a.N, p.tiles_m, p.tiles_n,
-                           tile_rows_step(p.tiles_m, p.tiles_n), p.whole, shared, p.steps, p.head,
-                           p.rest(), p.most()};
+    WgradOperands op{};
+    op.XT = xt;
+    for (int i = 0; i < a.n; ++i) {
+        op.dY[i] = static_cast<const uint16_t *>(a.dY[i]);
+        op.dW[i] = static_cast<uint16_t *>(a.dW[i]);
+    }
+    op.P = parts;
+    op.Tp = Tp;
+    op.ldy = a.ldy;
+    op.ldw = a.ldw;
+    op.T = a.T;
+    op.M = a.M;
+    op.N = a.N;
+    op.tiles_m = p.tiles_m;
+    op.tiles_n = p.tiles_n;
+    op.cols = p.tiles_n / a.n;
+    op.xm = tile_rows_step(p.tiles_m, p.tiles_n);
+    op.whole = p.whole;
+    op.shared = shared;
+    op.steps = p.steps;
+    op.head = p.head;
+    op.rest = p.rest();
+    op.most = p.most();
     const unsigned wgs = static_cast<unsigned>(p.whole) + shared + p.tails;
     e = launch_kernel(p.edge == 256 ? wgrad_kernel : wgrad_small_kernel, dim3(wgs), dim3(512), st, op);
     if (e != hipSuccess || !shared)

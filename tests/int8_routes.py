@@ -13,8 +13,8 @@ SRC = """
 #include "dd_routes.hpp"
 extern "C" {
 int product(int M, int N, int K, int cus) { return static_cast<int>(dd::gemm_i8_tile(M, N, K, cus)); }
-void wgrad(int T, int M, int N, int cus, int *out) {
-    const dd::WgradPlan p = dd::wgrad_plan(T, M, N, cus);
+void wgrad(int T, int M, int N, int n, int cus, int *out) {
+    const dd::WgradPlan p = dd::wgrad_plan(T, M, N, n, cus);
     out[0] = p.edge; out[1] = p.whole; out[2] = p.head ? p.shared() : 0; out[3] = p.steps;
     out[4] = p.head; out[5] = p.tails; out[6] = p.most(); out[7] = p.tiles_m * p.tiles_n;
 }
@@ -37,9 +37,9 @@ def product(M, N, K):
     return ("few", "small", "large")[_lib().product(M, N, K, CUS)]
 
 
-def wgrad(T, M, N):
-    """How a weight gradient runs: edge, whole, shared, steps, head, tails,
+def wgrad(T, M, N, n=1):
+    """How n weight gradients run: edge, whole, shared, steps, head, tails,
     most, tiles."""
     out = (ctypes.c_int * 8)()
-    _lib().wgrad(T, M, N, CUS, out)
+    _lib().wgrad(T, M, N, n, CUS, out)
     return dict(zip(("edge", "whole", "shared", "steps", "head", "tails", "most", "tiles"), out))

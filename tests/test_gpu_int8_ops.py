@@ -367,6 +367,25 @@ def test_gemm_int8_wgrad_strided(cuda, T, M, N):
     assert (out[keep] == 5.0).all()
 
 
+@pytest.mark.parametrize("n", [1, 2, 3])
+@pytest.mark.parametrize("T,M,N", [(100, 40, 72), (2000, 520, 264), (4096, 1024, 1024),
+                                   (2048, 2048, 2816)])
+def test_gemm_int8_wgrad_group(cuda, T, M, N, n):
+    # gradients of one input together, into column slices of one matrix
+    q, s = random_codes(T, M, T, cuda)
+    dys = [bf16((T, N), 10 + i).to(cuda) for i in range(n)]
+    dw = torch.full((M, n * N), 5.0, dtype=torch.bfloat16, device=cuda)
+    columns = [dw[:, i * N:(i + 1) * N] for i in range(n)]
+    assert ops.gemm_int8_wgrad_group(q, s, dys, outs=columns) is columns
+    x = f64(ops.dequantize(q, s))
+    for i in range(n):
+        ref = x.T @ f64(dys[i])
+        close(f64(columns[i]), ref, B * np.abs(ref) + T * U * (np.abs(x).T @ np.abs(f64(dys[i]))),
+              i)
+    for a, b in zip(ops.gemm_int8_wgrad_group(q, s, dys), columns):
+        assert torch.equal(a, b)
+
+
 def test_gemm_int8_wgrad_rows_behind_the_last_token(cuda):
     # what lies behind the last token is not read into the sums
     T, M, N = 70, 264, 520

@@ -1,0 +1,121 @@
+"""The OpenLM block with 8-bit activation checkpoints, against the float64
+block oracle and against the same block with bf16 ones.
+
+A code is off by at most half a step s = A / 127 of its row, evenly spread:
+s / sqrt(12) rms.  Rows of a few hundred normal values have A of 3 to 4
+deviations, so the norms' outputs and the gate's products are off by 0.7 to
+0.9% of their deviation, and the gated value, a product of two, whose A is 6
+to 12 deviations, by 1.4 to 2.7%.  The errors are independent of the gradients
+they are multiplied with, so a weight gradient is off by the share that its
+input is; the gate's gradients get it from three restored values (the gate
+twice).  Added in squares to the bf16 block's 2e-2 (tests/test_gpu_layer.py)
+that is at most 3.4e-2: the bound is 4e-2.
+"""
+import pytest
+import torch
+
+import synth
+from oracle import layer as OL
+from paper_2405_13226_amd import dd
+from paper_2405_13226_amd.layer import OpenLMBlock
+
+from parity import log, rel_l2, to_dev, to_f64
+
+pytestmark = pytest.mark.gpu
+RTOL = 4e-2
+
+
+def blocks(d, H, hidden, cuda):
+    made = [OpenLMBlock(d, H, hidden, 10000.0, device=cuda, seed=3,
+                        init_scale=0.1 * (256 / d) ** 0.5, checkpoint_bits=bits)
+            for bits in (16, 8)]
+    with torch.no_grad():  # non-trivial norm parameters
+        for n in ("ln1_w", "ln2_w", "ln1_b", "ln2_b"):
+            g = torch.randn(d, device=cuda).to(torch.bfloat16) * 0.2
+            for blk in made:
+                getattr(blk, n).add_(g)
+    return made
+
+
+def step(blk, x0, dy, cu=None, doc_pos=False):
+    blk.zero_grad(set_to_none=True)
+    x = x0.clone().requires_grad_(True)
+    y = blk(x, cu, doc_pos)
+    y.backward(dy)
+    return y.detach(), {"x": x.grad, **{n: p.grad for n, p in blk.weights().items()}}
+
+
+@pytest.mark.parametrize("B,L,d,H,hidden,docs", [(2, 256, 512, 4, 768, False),
+                                                 (2, 256, 512, 8, 1280, True)])
+def test_block_with_8_bit_checkpoints(cuda, B, L, d, H, hidden, docs):
+    log(f"8-bit checkpoints B={B} L={L} d={d} hidden={hidden} docs={docs}")
+    cu = dd.chunk_doclens(synth.lognormal_doc_lengths(4, total_tokens=B * L, median=80, sigma=1.0),
+                          B * L) if docs else None
+    full, short = blocks(d, H, hidden, cuda)
+    x0 = to_dev(synth.normal_bf16((B, L, d), 1, 21), cuda)
+    dy = to_dev(synth.normal_bf16((B, L, d), 1, 22), cuda)
+    w = {n: to_f64(p.detach()) for n, p in short.weights().items()}
+    _, ref = OL.block_fwd_bwd(to_f64(x0), w, to_f64(dy), H, 10000.0, cu, docs)
+    y16, g16 = step(full, x0, dy, cu, docs)
+    y8, g8 = step(short, x0, dy, cu, docs)
+    assert torch.equal(y8, y16)
+    err = {n: rel_l2(to_f64(g8[n]), ref[n]) for n in g8}
+    log("  " + "  ".join(f"{n}={v:.3g}" for n, v in err.items()))
+    assert max(err.values()) <= RTOL, err
+    # the attention's output is kept in bf16 and only its gradient differs
+    assert rel_l2(to_f64(g8["w_o"]), to_f64(g16["w_o"])) <= RTOL
+    # a second pass on new values gives new gradients, and the same inputs the
+    # same ones
+    step(short, x0.flip(0), dy, cu, docs)
+    _, again = step(short, x0, dy, cu, docs)
+    for n in g8:
+        assert torch.equal(again[n], g8[n]), n
+
+
+def test_8_bit_checkpoints_keep_fewer_bytes(cuda):
+    B, L, d, H, hidden = 4, 1024, 1024, 16, 2816
+    kept = {}
+    x = to_dev(synth.normal_bf16((B, L, d), 1, 21), cuda).requires_grad_(True)
+    for blk in blocks(d, H, hidden, cuda):
+        sizes = []
+
+        def pack(t):
+            sizes.append(t.numel() * t.element_size())
+            return t
+
+        with torch.autograd.graph.saved_tensors_hooks(pack, lambda t: t):
+            blk(x)
+        kept[blk.checkpoint_bits] = sum(sizes)
+    # a byte for each value of five activations, less a scale for each token
+    assert kept[16] - kept[8] == B * L * (2 * d + 3 * hidden - 5 * 4), kept
+
+
+def test_block_in_a_captured_graph(cuda):
+    # forward and backward of the block with 8-bit checkpoints, replayed
+    blk = blocks(512, 4, 768, cuda)[1]
+    x = to_dev(synth.normal_bf16((2, 256, 512), 1, 21), cuda).requires_grad_(True)
+    dy = to_dev(synth.normal_bf16((2, 256, 512), 1, 22), cuda)
+    params = [x] + [p for _, p in sorted(blk.weights().items())]
+
+    def run():
+        y = blk(x)
+        return (y.detach(),) + torch.autograd.grad(y, params, dy)
+
+    side = torch.cuda.Stream(cuda)
+    side.wait_stream(torch.cuda.current_stream(cuda))
+    with torch.cuda.stream(side):
+        ref = [t.clone() for t in run()]
+    torch.cuda.current_stream(cuda).wait_stream(side)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        out = run()
+    for rep in range(3):
+        for t in out:
+            t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        for i, (a, b) in enumerate(zip(out, ref)):
+            assert torch.equal(a, b), (rep, i)
+        torch.randn(1 << 20, device=cuda).sum()
+        torch.cuda.synchronize()

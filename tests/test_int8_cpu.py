@@ -109,31 +109,40 @@ def test_product_refusals(lib):
         assert call(lib, "dd_gemm_i8", g, **kw) == ALIAS, kw
 
 
+def pointers(*ps):
+    return (ctypes.c_void_p * len(ps))(*(p.value if p is not None else None for p in ps))
+
+
 def test_weight_gradient_refusals(lib):
-    need = lib.dd_gemm_i8_wgrad_workspace_bytes(64, 96, 128)
-    assert lib.dd_gemm_i8_wgrad_workspace_bytes(0, 96, 128) == 0
-    assert lib.dd_gemm_i8_wgrad_workspace_bytes(64, 92, 128) == 0
-    g = dict(Q=fake(0), ldq=96, scales=fake(1), dY=fake(2), ldy=128, dW=fake(3), ldw=128, T=64,
-             M=96, N=128, ws=fake(4), bytes=need)
+    sizes = lib.dd_gemm_i8_wgrad_workspace_bytes
+    need = sizes(64, 96, 128, 2)
+    assert need > 64 * 96 * 2
+    for bad in ((0, 96, 128, 1), (1 << 25, 96, 128, 1), (64, 92, 128, 1), (64, 96, 124, 1),
+                (64, 96, 128, 0), (64, 96, 128, 4)):
+        assert sizes(*bad) == 0, bad
+    g = dict(Q=fake(0), ldq=96, scales=fake(1), dY=pointers(fake(2), fake(3)), ldy=128,
+             dW=pointers(fake(4), fake(5)), ldw=128, n=2, T=64, M=96, N=128, ws=fake(6),
+             bytes=need)
     for n in ("Q", "scales", "dY", "dW"):
         assert call(lib, "dd_gemm_i8_wgrad", g, **{n: None}) == NULL, n
-    for kw in (dict(T=0), dict(T=1 << 25), dict(M=0), dict(M=92), dict(N=100), dict(ldq=88), dict(ldy=120),
-               dict(ldw=120), dict(ldq=1 << 23), dict(ldy=1 << 23)):
+    assert call(lib, "dd_gemm_i8_wgrad", g, dY=pointers(fake(2), None)) == NULL
+    assert call(lib, "dd_gemm_i8_wgrad", g, dW=pointers(None, fake(5))) == NULL
+    for kw in (dict(T=0), dict(T=1 << 25), dict(M=0), dict(M=92), dict(N=100), dict(n=0),
+               dict(n=4), dict(ldq=88), dict(ldy=120), dict(ldw=120), dict(ldq=1 << 23),
+               dict(ldy=1 << 23)):
         assert call(lib, "dd_gemm_i8_wgrad", g, **kw) == SHAPE, kw
-    for kw in (dict(ldq=100), dict(ldy=132), dict(ldw=132), dict(Q=fake(0, 4)), dict(dY=fake(2, 8)),
-               dict(dW=fake(3, 8)), dict(scales=fake(1, 1))):
+    for kw in (dict(ldq=100), dict(ldy=132), dict(ldw=132), dict(Q=fake(0, 4)),
+               dict(dY=pointers(fake(2, 8), fake(3))), dict(dW=pointers(fake(4), fake(5, 8))),
+               dict(scales=fake(1, 1)), dict(ws=fake(6, 8))):
         assert call(lib, "dd_gemm_i8_wgrad", g, **kw) == ALIGN, kw
-    for kw in (dict(dW=fake(0)), dict(dW=fake(1, 64)), dict(dW=fake(2, 16))):
+    for kw in (dict(bytes=need - 1), dict(ws=None)):
+        assert call(lib, "dd_gemm_i8_wgrad", g, **kw) == WORKSPACE, kw
+    for kw in (dict(dW=pointers(fake(4), fake(0))), dict(dW=pointers(fake(1, 64), fake(5))),
+               dict(dW=pointers(fake(4), fake(2, 16))), dict(dW=pointers(fake(4), fake(4, 32))),
+               dict(ws=fake(0, 16)), dict(ws=fake(3, 32)), dict(ws=fake(5, 16)),
+               # column slices of one matrix that overlap
+               dict(ldw=256, dW=pointers(fake(4), fake(4, 240)))):
         assert call(lib, "dd_gemm_i8_wgrad", g, **kw) == ALIAS, kw
-    # a product whose T axis is split needs its scratch
-    T, M, N = 65536, 256, 256
-    need = lib.dd_gemm_i8_wgrad_workspace_bytes(T, M, N)
-    if need:
-        g.update(T=T, M=M, N=N, ldq=M, ldy=N, ldw=N)
-        assert call(lib, "dd_gemm_i8_wgrad", g, bytes=need - 1) == WORKSPACE
-        assert call(lib, "dd_gemm_i8_wgrad", g, ws=None) == WORKSPACE
-        assert call(lib, "dd_gemm_i8_wgrad", g, ws=fake(4, 8), bytes=need) == ALIGN
-        assert call(lib, "dd_gemm_i8_wgrad", g, ws=fake(3, 16), bytes=need) == ALIAS
 
 
 def test_wrappers_refuse_what_is_not_on_a_gpu_or_of_another_type():
@@ -144,7 +153,8 @@ def test_wrappers_refuse_what_is_not_on_a_gpu_or_of_another_type():
               lambda: ops.rms_norm(x[0], w), lambda: ops.rms_norm_backward(x, w, s, x),
               lambda: ops.quantize(x), lambda: ops.quantize([1.0]),
               lambda: ops.dequantize(q, s), lambda: ops.dequantize(x, s),
-              lambda: ops.gemm_int8(q, s, q, s), lambda: ops.gemm_int8_wgrad(q, s, x)):
+              lambda: ops.gemm_int8(q, s, q, s), lambda: ops.gemm_int8_wgrad(q, s, x),
+              lambda: ops.gemm_int8_wgrad_group(q, s, [x, x])):
         with pytest.raises(ValueError):
             f()
 
@@ -167,21 +177,22 @@ def parts_of(plan, wg):
     return out
 
 
+@pytest.mark.parametrize("n", [1, 2, 3])
 @pytest.mark.parametrize("T,M,N", [(65536, 2048, 5632), (3001, 1040, 1416), (65536, 256, 256),
                                    (4096, 1024, 1024), (16384, 1024, 2816), (700, 4352, 4360),
                                    (65536, 4096, 8192), (200000, 264, 520), (9000, 1800, 5000),
                                    (1, 8, 8), (33554368, 8, 8)])
-def test_weight_gradient_plans_cover_every_step_once(T, M, N):
-    p = routes.wgrad(T, M, N)
-    assert p["tiles"] == p["whole"] + p["shared"]
+def test_weight_gradient_plans_cover_every_step_once(T, M, N, n):
+    p = routes.wgrad(T, M, N, n)
+    assert p["tiles"] == p["whole"] + p["shared"] and p["tiles"] % n == 0
     covered, slots = {}, set()
     for wg in range(p["whole"] + p["shared"] + p["tails"]):
         parts = parts_of(p, wg)
         assert parts and len(parts) <= p["most"]
-        assert sum(n for _, _, n, _ in parts) <= max(p["head"], p["steps"])
-        for tile, first, n, slot in parts:
-            assert n > 0 and first + n <= p["steps"]
-            covered.setdefault(tile, []).append((first, n))
+        assert sum(k for _, _, k, _ in parts) <= max(p["head"], p["steps"])
+        for tile, first, k, slot in parts:
+            assert k > 0 and first + k <= p["steps"]
+            covered.setdefault(tile, []).append((first, k))
             assert slot < 0 or slot not in slots
             slots.add(slot)
             # and where the last launch looks for it
@@ -193,9 +204,9 @@ def test_weight_gradient_plans_cover_every_step_once(T, M, N):
     assert sorted(covered) == list(range(p["tiles"]))
     for parts in covered.values():
         at = 0
-        for first, n in sorted(parts):
+        for first, k in sorted(parts):
             assert first == at
-            at += n
+            at += k
         assert at == p["steps"]
     # a shared tile's workgroups are resident together with the others
     assert p["shared"] + p["tails"] <= routes.CUS
@@ -206,3 +217,10 @@ def test_oracle_codes_take_ties_to_even():
     q, top = O.codes(z)
     assert q.tolist() == [[127, 0, 2, -2, 0], [0] * 5, [0] * 5]
     assert top[0] == 254.0 and top[1] == 0.0
+
+
+def test_block_refuses_other_checkpoint_widths():
+    from paper_2405_13226_amd.layer import OpenLMBlock
+    with pytest.raises(ValueError):
+        OpenLMBlock(512, 8, 768, device="cpu", checkpoint_bits=4)
+    assert OpenLMBlock(512, 8, 768, device="cpu").checkpoint_bits == 16
