@@ -252,14 +252,24 @@ def _call(dev, name, *args):
         check(st, name)
 
 
-def _on(t, name, dev):
-    if t.device != dev:
-        raise ValueError(f"{name} is on {t.device}, not on {dev}")
-
-
-def _ld(t):
-    """Row stride; of a single row, whose stride is never used, its length."""
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+def _dims(t, name, dtype, dev=None):
+    """(rows, columns, row stride) of a matrix of this type with unit column
+    stride on ``dev`` (any GPU if None).  A single row's stride, which is
+    never used, is its length.  (Called some times per call of a few
+    microseconds: one look at everything, and the reasons only on failure.)"""
+    if isinstance(t, torch.Tensor) and t.dtype is dtype and t.dim() == 2:
+        (rows, cols), (ld, one) = t.shape, t.stride()
+        where = t.device
+        if one == 1 and (where == dev if dev is not None else where.type == "cuda"):
+            return rows, cols, ld if rows > 1 else cols
+    if not isinstance(t, torch.Tensor) or t.dim() != 2:
+        raise ValueError(f"{name} must be a 2-D tensor")
+    if t.device.type != "cuda" or t.dtype is not dtype:
+        kind = "bf16" if dtype is torch.bfloat16 else "int8"
+        raise ValueError(f"{name} must be a {kind} GPU tensor")
+    if t.stride(1) != 1:
+        raise ValueError(f"{name} must have unit column stride")
+    raise ValueError(f"{name} is on {t.device}, not on {dev}")
 
 
 def _vec(t, name, n, dtype, dev):
@@ -269,83 +279,79 @@ def _vec(t, name, n, dtype, dev):
     raise ValueError(f"{name} must be a contiguous {dtype} tensor of {n} elements on {dev}")
 
 
-def _code_matrix(t, name, dev=None):
-    if not isinstance(t, torch.Tensor) or t.dim() != 2:
-        raise ValueError(f"{name} must be a 2-D tensor")
-    if t.dtype is not torch.int8 or not t.is_cuda:
-        raise ValueError(f"{name} must be an int8 GPU tensor")
-    if t.stride(1) != 1:
-        raise ValueError(f"{name} must have unit column stride")
-    if dev is not None:
-        _on(t, name, dev)
-
-
 def _rows(t, name, shape, dev):
-    """A contiguous bf16 matrix of this shape on ``dev``."""
-    _mat(t, name)
-    _on(t, name, dev)
-    if t.shape != shape:
-        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
-    if not t.is_contiguous():
+    """Checks a contiguous bf16 matrix of this shape on ``dev``."""
+    rows, cols, ld = _dims(t, name, torch.bfloat16, dev)
+    if (rows, cols) != shape:
+        raise ValueError(f"{name} has shape {(rows, cols)}, expected {shape}")
+    if ld != cols:
         raise ValueError(f"{name} must be contiguous")
 
 
+def _result(out, rows, cols, dev, name="out"):
+    """(``out`` or a new bf16 matrix, its row stride)."""
+    if out is None:
+        return torch.empty((rows, cols), dtype=torch.bfloat16, device=dev), cols
+    r, c, ld = _dims(out, name, torch.bfloat16, dev)
+    if (r, c) != (rows, cols):
+        raise ValueError(f"{name} has shape {(r, c)}, expected {(rows, cols)}")
+    return out, ld
+
+
 def _norm_inputs(x, w, residual):
-    _mat(x, "x")
-    dev = x.device
-    _vec(w, "w", x.shape[1], torch.bfloat16, dev)
+    """(rows, columns, x's row stride, the residual's, x + residual to be)."""
+    rows, d, ldx = _dims(x, "x", torch.bfloat16)
+    _vec(w, "w", d, torch.bfloat16, x.device)
     if residual is None:
-        return dev, None
-    _mat(residual, "residual")
-    _on(residual, "residual", dev)
-    if residual.shape != x.shape:
+        return rows, d, ldx, 0, None
+    r, c, ldr = _dims(residual, "residual", torch.bfloat16, x.device)
+    if (r, c) != (rows, d):
         raise ValueError("residual must match x in shape")
-    return dev, torch.empty_like(x)
+    return rows, d, ldx, ldr, torch.empty_like(x)
 
 
 def rms_norm(x, w, residual=None, eps: float = LN_EPS):
     """(y, h, rstd) of RMSNorm over the rows of h = x + residual (rounded to
     bf16; x itself without one): rstd = 1 / sqrt(mean(h^2) + eps), y = h rstd w."""
-    dev, h = _norm_inputs(x, w, residual)
-    rows, d = x.shape
+    rows, d, ldx, ldr, h = _norm_inputs(x, w, residual)
+    dev = x.device
     y = torch.empty_like(x)
     rstd = torch.empty(rows, dtype=torch.float32, device=dev)
-    if y.numel():
-        _call(dev, "dd_rmsnorm_fwd", _p(x), _ld(x), _p(residual),
-              0 if residual is None else _ld(residual), _p(w), _p(h), _p(y), _p(rstd), rows, d,
-              eps)
+    if rows and d:
+        _call(dev, "dd_rmsnorm_fwd", _p(x), ldx, _p(residual), ldr, _p(w), _p(h), _p(y),
+              _p(rstd), rows, d, eps)
     return y, x if h is None else h, rstd
 
 
 def rms_norm_int8(x, w, residual=None, eps: float = LN_EPS):
     """(codes, scales, h, rstd): ``rms_norm`` with its output as codes."""
-    dev, h = _norm_inputs(x, w, residual)
-    rows, d = x.shape
+    rows, d, ldx, ldr, h = _norm_inputs(x, w, residual)
+    dev = x.device
     codes = torch.empty_like(x, dtype=torch.int8)
-    scales, rstd = (torch.empty(rows, dtype=torch.float32, device=dev) for _ in range(2))
-    if codes.numel():
-        _call(dev, "dd_rmsnorm_int8_fwd", _p(x), _ld(x), _p(residual),
-              0 if residual is None else _ld(residual), _p(w), _p(h), _p(codes), d, _p(scales),
-              _p(rstd), rows, d, eps)
+    scales = torch.empty(rows, dtype=torch.float32, device=dev)
+    rstd = torch.empty_like(scales)
+    if rows and d:
+        _call(dev, "dd_rmsnorm_int8_fwd", _p(x), ldx, _p(residual), ldr, _p(w), _p(h), _p(codes),
+              d, _p(scales), _p(rstd), rows, d, eps)
     return codes, scales, x if h is None else h, rstd
 
 
 def rms_norm_backward(h, w, rstd, dy, dres=None):
     """(dx, dw) of either norm for the gradient dy of its output; dx is the
     gradient of x and of the residual, ``dres`` (optional, the gradient of h
-    from its other uses) is added to it."""
-    _mat(h, "h")
-    dev, (rows, d) = h.device, h.shape
-    _rows(h, "h", h.shape, dev)
+    from its other uses) is added to it.  Contiguous matrices."""
+    rows, d, _ = _dims(h, "h", torch.bfloat16)
+    dev = h.device
+    _rows(h, "h", (rows, d), dev)
     _vec(w, "w", d, torch.bfloat16, dev)
     _vec(rstd, "rstd", rows, torch.float32, dev)
-    for t, n in ((dy, "dy"), (dres, "dres")):
-        if t is not None or n == "dy":
-            _rows(t, n, h.shape, dev)
+    _rows(dy, "dy", (rows, d), dev)
+    if dres is not None:
+        _rows(dres, "dres", (rows, d), dev)
     dx, dw = torch.empty_like(h), torch.empty_like(w)
-    if not dx.numel():
+    if not (rows and d):
         return dx, dw.zero_()
-    need = lib().dd_rmsnorm_bwd_workspace_bytes(rows, d)
+    need = _entry("dd_rmsnorm_bwd_workspace_bytes")(rows, d)
     ws = torch.empty(need, dtype=torch.uint8, device=dev)
     _call(dev, "dd_rmsnorm_bwd", _p(h), _p(w), _p(rstd), _p(dy), _p(dres), _p(dx), _p(dw), rows,
           d, _p(ws), need)
@@ -354,29 +360,22 @@ def rms_norm_backward(h, w, rstd, dy, dres=None):
 
 def quantize(x):
     """(codes, scales) of the rows of a bf16 matrix."""
-    _mat(x, "x")
-    rows, d = x.shape
+    rows, d, ldx = _dims(x, "x", torch.bfloat16)
     codes = torch.empty_like(x, dtype=torch.int8)
     scales = torch.empty(rows, dtype=torch.float32, device=x.device)
-    if codes.numel():
-        _call(x.device, "dd_quantize", _p(x), _ld(x), _p(codes), d, _p(scales), rows, d)
+    if rows and d:
+        _call(x.device, "dd_quantize", _p(x), ldx, _p(codes), d, _p(scales), rows, d)
     return codes, scales
 
 
 def dequantize(codes, scales, out=None):
     """The bf16 values of codes (into ``out`` if given)."""
-    _code_matrix(codes, "codes")
-    dev, (rows, d) = codes.device, codes.shape
+    rows, d, ldq = _dims(codes, "codes", torch.int8)
+    dev = codes.device
     _vec(scales, "scales", rows, torch.float32, dev)
-    if out is None:
-        out = torch.empty((rows, d), dtype=torch.bfloat16, device=dev)
-    else:
-        _mat(out, "out")
-        _on(out, "out", dev)
-        if out.shape != codes.shape:
-            raise ValueError(f"out has shape {tuple(out.shape)}, expected {(rows, d)}")
-    if codes.numel():
-        _call(dev, "dd_dequantize", _p(codes), _ld(codes), _p(scales), _p(out), _ld(out), rows, d)
+    out, ldy = _result(out, rows, d, dev)
+    if rows and d:
+        _call(dev, "dd_dequantize", _p(codes), ldq, _p(scales), _p(out), ldy, rows, d)
     return out
 
 
@@ -387,31 +386,21 @@ def gemm_int8(a, a_scales, b, b_scales, residual=None, out=None):
 
     The sums are exact, scaled in fp32 and rounded once.  ``out`` (optional)
     receives the result and may be ``residual`` itself."""
-    _code_matrix(a, "a")
-    dev, (M, K) = a.device, a.shape
-    _code_matrix(b, "b", dev)
-    N = b.shape[0]
-    if b.shape[1] != K:
-        raise ValueError(f"inner dimensions differ: {K} vs {b.shape[1]}")
+    M, K, lda = _dims(a, "a", torch.int8)
+    dev = a.device
+    N, Kb, ldb = _dims(b, "b", torch.int8, dev)
+    if Kb != K:
+        raise ValueError(f"inner dimensions differ: {K} vs {Kb}")
     if K % 16 or not 0 < K < 1 << 17:
         raise ValueError(f"the inner dimension must be a multiple of 16 below 2^17 (got {K})")
     _vec(a_scales, "a_scales", M, torch.float32, dev)
     _vec(b_scales, "b_scales", N, torch.float32, dev)
-    if out is None:
-        out = torch.empty((M, N), dtype=torch.bfloat16, device=dev)
-    else:
-        _mat(out, "out")
-        _on(out, "out", dev)
-        if out.shape != (M, N):
-            raise ValueError(f"out has shape {tuple(out.shape)}, expected {(M, N)}")
-    if residual is not None:
-        _mat(residual, "residual")
-        _on(residual, "residual", dev)
-        if residual.shape != (M, N) or _ld(residual) != _ld(out):
-            raise ValueError("residual must match out in shape and row stride")
-    if out.numel():
-        _call(dev, "dd_gemm_i8", _p(a), _ld(a), _p(a_scales), _p(b), _ld(b), _p(b_scales),
-              _p(residual), _p(out), _ld(out), M, N, K)
+    out, ldc = _result(out, M, N, dev)
+    if residual is not None and _dims(residual, "residual", torch.bfloat16, dev) != (M, N, ldc):
+        raise ValueError("residual must match out in shape and row stride")
+    if M and N:
+        _call(dev, "dd_gemm_i8", _p(a), lda, _p(a_scales), _p(b), ldb, _p(b_scales), _p(residual),
+              _p(out), ldc, M, N, K)
     return out
 
 
@@ -425,36 +414,32 @@ def gemm_int8_wgrad(codes, scales, dy, out=None):
 def gemm_int8_wgrad_group(codes, scales, dys, outs=None):
     """``gemm_int8_wgrad`` of layers that share their input: one result for
     each of dys (one to three of one shape and row stride), in one launch."""
-    _code_matrix(codes, "codes")
-    dev, (T, M), n = codes.device, codes.shape, len(dys)
+    T, M, ldq = _dims(codes, "codes", torch.int8)
+    dev, n = codes.device, len(dys)
     _vec(scales, "scales", T, torch.float32, dev)
     if not 1 <= n <= 3:
         raise ValueError(f"need one to three gradients (got {n})")
-    for dy in dys:
-        _mat(dy, "dy")
-        _on(dy, "dy", dev)
-        if dy.shape != dys[0].shape or _ld(dy) != _ld(dys[0]):
-            raise ValueError("the dy matrices must agree in shape and row stride")
-    N = dys[0].shape[1]
-    if dys[0].shape[0] != T:
-        raise ValueError(f"codes have {T} rows, dy has {dys[0].shape[0]}")
+    shapes = [_dims(dy, "dy", torch.bfloat16, dev) for dy in dys]
+    Ty, N, ldy = shapes[0]
+    if any(s != shapes[0] for s in shapes):
+        raise ValueError("the dy matrices must agree in shape and row stride")
+    if Ty != T:
+        raise ValueError(f"codes have {T} rows, dy has {Ty}")
     if M % 8 or N % 8:
         raise ValueError(f"the columns of codes and dy must be multiples of 8 (got {M} and {N})")
     if outs is None:
-        outs = [torch.empty((M, N), dtype=torch.bfloat16, device=dev) for _ in dys]
-    else:
-        if len(outs) != n:
-            raise ValueError(f"need {n} outputs of shape {(M, N)}")
-        for out in outs:
-            _mat(out, "out")
-            _on(out, "out", dev)
-            if out.shape != (M, N) or _ld(out) != _ld(outs[0]):
-                raise ValueError(f"need {n} outputs of shape {(M, N)} and one row stride")
+        outs = [None] * n
+    elif len(outs) != n:
+        raise ValueError(f"need {n} outputs of shape {(M, N)}")
+    results = [_result(out, M, N, dev) for out in outs]
+    outs, ldw = [out for out, _ in results], results[0][1]
+    if any(ld != ldw for _, ld in results):
+        raise ValueError("the outputs must agree in row stride")
     if not T:
         return [out.zero_() for out in outs]
     if M and N:
-        need = lib().dd_gemm_i8_wgrad_workspace_bytes(T, M, N, n)
+        need = _entry("dd_gemm_i8_wgrad_workspace_bytes")(T, M, N, n)
         ws = torch.empty(need, dtype=torch.uint8, device=dev)
-        _call(dev, "dd_gemm_i8_wgrad", _p(codes), _ld(codes), _p(scales), _array(dys),
-              _ld(dys[0]), _array(outs), _ld(outs[0]), n, T, M, N, _p(ws), need)
+        _call(dev, "dd_gemm_i8_wgrad", _p(codes), ldq, _p(scales), _array(dys), ldy, _array(outs),
+              ldw, n, T, M, N, _p(ws), need)
     return outs

@@ -108,13 +108,14 @@ __device__ __forceinline__ void row_reduce(float &s, uint32_t &m, float *red, in
     }
 }
 
-// How a row's codes are formed from its largest magnitude: z is multiplied by
-// a power of two that keeps every step below normal and finite (1 for ordinary
-// rows), then by 127 / A.  A row of zeros has codes and scale 0; one that
-// holds a NaN or an infinity has codes 0 and a NaN scale, so that all its
-// values are NaN.
+// How a row's codes are formed from its largest magnitude.  z is first
+// multiplied by `fit`, a power of two that keeps every step below normal and
+// finite (1 for ordinary rows).  A row of zeros has codes and scale 0; one
+// that holds a NaN or an infinity has codes 0 (`keep`) and a NaN scale, so
+// that all its values are NaN.
 struct CodeScale {
     float fit, amax, inv, scale;
+    uint32_t keep;
 
     __device__ __forceinline__ explicit CodeScale(uint32_t amax_bits)
     {
@@ -123,50 +124,67 @@ struct CodeScale {
         amax = a * fit;
         inv = 127.0f / amax;
         scale = a / 127.0f;
+        keep = ~0u;
         if (amax_bits == 0 || amax_bits >= 0x7f800000u) {
-            fit = inv = 0.0f;
-            amax = 1.0f;
+            fit = amax = 1.0f;
+            inv = 0.0f;
+            keep = 0u;
             scale = amax_bits == 0 ? 0.0f : __uint_as_float(0x7fc00000u);
         }
     }
-    __device__ __forceinline__ bool usable() const { return inv != 0.0f; }
-    // The nearest integer to 127 z / amax, ties to even, exactly: the rounded
-    // product of the reciprocal is at most one off, and 127 z - q amax is
-    // exact in fp32 (z and amax have 16 significant bits at most, q and 127
-    // seven), so it tells which side of the border z is on.
-    __device__ __forceinline__ int code(float z) const
+    // The codes of eight values, a byte each.  z inv is off by less than 127
+    // 2^-23 (two roundings), so the integer nearest to it is the one nearest to
+    // 127 z / A unless it is further than 1/2 - 2^-14 from it; then 127 z - q
+    // amax, which is exact in fp32 (z and amax have at most 16 significant
+    // bits, q and 127 seven), tells the side.  Adding 1.5 2^23 rounds to an
+    // integer, ties to even, and leaves its low byte in the bits.
+    __device__ __forceinline__ u32x2 codes(const float (&z)[8]) const
     {
-        z *= fit;
-        float q = rintf(z * inv);
-        const float r = fmaf(-q, amax, 127.0f * z), r2 = 2.0f * fabsf(r);
-        const int qi = static_cast<int>(q);
-        const bool step = r2 > amax || (r2 == amax && (qi & 1));
-        return qi + (step ? (r > 0.f ? 1 : -1) : 0);
+        constexpr float kRound = 12582912.0f;
+        float t[8], worst = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float v = z[i] * inv;
+            t[i] = v + kRound;
+            worst = fmaxf(worst, fabsf(v - (t[i] - kRound)));
+        }
+        if (worst > 0.5f - 0x1p-14f) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float q = t[i] - kRound;
+                const float r = fmaf(-q, amax, 127.0f * z[i]), r2 = 2.0f * fabsf(r);
+                if (r2 > amax || (r2 == amax && (__float_as_uint(t[i]) & 1)))
+                    t[i] += r > 0.f ? 1.0f : -1.0f;
+            }
+        }
+        u32x2 u;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            uint32_t b[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                b[e] = __float_as_uint(t[4 * i + e]);
+            // Bytes 0-3 of a permutation's selector are its second operand's.
+            u[i] = __builtin_amdgcn_perm(__builtin_amdgcn_perm(b[3], b[2], 0x0c0c0400u),
+                                         __builtin_amdgcn_perm(b[1], b[0], 0x0c0c0400u),
+                                         0x05040100u);
+        }
+        return u;
     }
 };
 
 __device__ __forceinline__ uint32_t abs_bits(float x) { return __float_as_uint(x) & 0x7fffffffu; }
 
 template <bool WHOLE>
-__device__ __forceinline__ void store_codes(int8_t *p, int left, const float (&z)[8],
-                                            const CodeScale &cs, bool usable)
+__device__ __forceinline__ void store_codes(int8_t *p, int left, const u32x2 &u)
 {
-    int c[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-        c[i] = usable ? cs.code(z[i]) : 0;
-    u32x2 u;
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-        u[i] = (c[4 * i] & 255) | (c[4 * i + 1] & 255) << 8 | (c[4 * i + 2] & 255) << 16 |
-               static_cast<uint32_t>(c[4 * i + 3]) << 24;
     if (WHOLE ? left > 0 : left >= 8) {
         *reinterpret_cast<codes8 *>(p) = u;
     } else if (!WHOLE) {
 #pragma unroll
         for (int i = 0; i < 7; ++i)
             if (i < left)
-                p[i] = static_cast<int8_t>(c[i]);
+                p[i] = static_cast<int8_t>(u[i >> 2] >> 8 * (i & 3));
     }
 }
 
@@ -251,13 +269,20 @@ row_kernel(RowOperands op)
         } else {
             const CodeScale cs(m);
             if (t == 0)
-                op.scales[row] = KIND == kCodes ? cs.scale
-                                 : cs.usable()  ? __uint_as_float(m) * rstd / 127.0f
-                                                : cs.scale;
+                op.scales[row] =
+                    KIND == kNormCodes && cs.keep ? __uint_as_float(m) * rstd / 127.0f : cs.scale;
+            if (cs.fit != 1.0f) {
+#pragma unroll
+                for (int c = 0; c < CH; ++c)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        v[c][i] *= cs.fit;
+            }
 #pragma unroll
             for (int c = 0; c < CH; ++c) {
                 const int col = (t + TPR * c) * 8;
-                store_codes<WHOLE>(op.Q + row * op.ldq + col, d - col, v[c], cs, cs.usable());
+                const u32x2 u = cs.codes(v[c]);
+                store_codes<WHOLE>(op.Q + row * op.ldq + col, d - col, u32x2{u[0] & cs.keep, u[1] & cs.keep});
             }
         }
     }
