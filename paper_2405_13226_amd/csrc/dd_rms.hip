@@ -26,14 +26,15 @@ namespace {
 
 enum RowKind { kNorm, kNormCodes, kCodes };
 
-// Row `row` of a matrix belongs to TPR threads of a workgroup: one wave (four
-// rows per workgroup), or a whole workgroup of 256 or 1024 threads.  Thread t
-// holds the 8-element chunks t, t + TPR, ... of it, CH of them.
+// Row `row` of a matrix belongs to TPR threads of a workgroup: a wave or a part
+// of one (several rows per workgroup of 256 threads), or a whole workgroup of
+// 256 or 1024.  Thread t holds the 8-element chunks t, t + TPR, ... of it, CH of
+// them.
 template <int TPR>
 struct RowThreads {
-    static constexpr int THREADS = TPR == 64 ? 256 : TPR;
+    static constexpr int THREADS = TPR <= 64 ? 256 : TPR;
     static constexpr int ROWS = THREADS / TPR;
-    static constexpr int WAVES = TPR / 64;  // per row
+    static constexpr int WAVES = TPR <= 64 ? 1 : TPR / 64;  // per row
 };
 
 // Pieces of rows at any element's address (the hardware takes unaligned
@@ -86,7 +87,7 @@ __device__ __forceinline__ void row_reduce(float &s, uint32_t &m, float *red, in
 {
     constexpr int W = RowThreads<TPR>::WAVES;
 #pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) {
+    for (int o = TPR < 64 ? TPR / 2 : 32; o >= 1; o >>= 1) {
         s += __shfl_xor(s, o);
         m = max(m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), o)));
     }
@@ -202,8 +203,10 @@ struct RowOperands {
     float eps;
 };
 
+// Six waves per SIMD for a wave's rows: the norm's codes of rows of 2048 take
+// 172 us a 65,536-token step instead of 185 with four (its registers else).
 template <int TPR, int CH, bool WHOLE, int KIND>
-__global__ void __launch_bounds__(RowThreads<TPR>::THREADS)
+__global__ void __launch_bounds__(RowThreads<TPR>::THREADS, TPR <= 64 ? 6 : 1)
 row_kernel(RowOperands op)
 {
     using T = RowThreads<TPR>;
@@ -288,20 +291,22 @@ row_kernel(RowOperands op)
     }
 }
 
-// Codes to bf16: one wave per row and 2048 columns, 8 codes per lane and load.
-template <bool WHOLE>
+// Codes to bf16, 8 per lane and load: TPR threads (a wave or less) per row and
+// 32 TPR columns.
+template <int TPR, bool WHOLE>
 __global__ void __launch_bounds__(256)
 dequantize_kernel(const int8_t *__restrict__ Q, long long ldq, const float *__restrict__ scales,
                   uint16_t *__restrict__ Y, long long ldy, int rows, int d)
 {
-    const int lane = threadIdx.x & 63;
-    const int step = static_cast<int>(gridDim.x) * 4;
-    for (long long row = static_cast<long long>(blockIdx.x) * 4 + (threadIdx.x >> 6); row < rows;
-         row += step) {
+    using T = RowThreads<TPR>;
+    const int t = threadIdx.x % TPR;
+    const int step = static_cast<int>(gridDim.x) * T::ROWS;
+    for (long long row = static_cast<long long>(blockIdx.x) * T::ROWS + threadIdx.x / TPR;
+         row < rows; row += step) {
         const float s = scales[row];
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
-            const int col = static_cast<int>(blockIdx.y) * 2048 + (lane + 64 * c) * 8;
+            const int col = (static_cast<int>(blockIdx.y) * 4 * TPR + t + TPR * c) * 8;
             const int left = d - col;
             const int8_t *q = Q + row * ldq + col;
             u32x2 u = {0u, 0u};
@@ -338,7 +343,7 @@ rms_bwd_kernel(RmsBackOperands op)
 {
     using T = RowThreads<TPR>;
     constexpr int COLS = TPR * CH * 8;
-    // TPR = 64: the four waves' column sums; else the reductions.
+    // Several rows at once: each one's column sums; else the reductions.
     __shared__ float red[T::ROWS > 1 ? T::ROWS * COLS : 4 * T::WAVES];
     const int t = threadIdx.x % TPR, d = op.d;
     u32x4 w[CH];
@@ -483,14 +488,20 @@ int rms_rows_per_wg(int rows, int d)
     return std::max(per, 8);
 }
 
-// Threads per row and chunks per thread for rows of d elements.
+// Threads per row and chunks per thread for rows of d elements: a wave or less
+// where that holds the row (65,536 rows of 64: 20.0 us with a wave each), a
+// workgroup for longer rows and for few of them, whose latency counts.
 struct RowShape {
     int tpr, ch;
 };
 
 RowShape row_shape(int rows, int d)
 {
-    const int tpr = d <= 2048 && (rows >= 512 || d <= 512) ? 64 : d <= 8192 ? 256 : 1024;
+    const int tpr = d <= 128                              ? 16
+                    : d <= 256                            ? 32
+                    : d <= 512 || (d <= 2048 && rows >= 512) ? 64
+                    : d <= 8192                           ? 256
+                                                          : 1024;
     return RowShape{tpr, (d + 8 * tpr - 1) / (8 * tpr)};
 }
 
@@ -498,6 +509,10 @@ RowShape row_shape(int rows, int d)
 template <typename F>
 auto with_shape(RowShape s, F f)
 {
+    if (s.tpr == 16)
+        return f(IC<16>{}, IC<1>{});
+    if (s.tpr == 32)
+        return f(IC<32>{}, IC<1>{});
     if (s.tpr == 64)
         return s.ch == 1   ? f(IC<64>{}, IC<1>{})
                : s.ch == 2 ? f(IC<64>{}, IC<2>{})
@@ -541,11 +556,16 @@ int launch_rows(const RowArgs &a)
 int launch_dequantize(const DequantizeArgs &a)
 {
     const bool whole = a.d % 8 == 0;
-    const dim3 grid(grid_of((a.rows + 3LL) / 4), static_cast<unsigned>((a.d + 2047) / 2048));
-    const hipError_t e =
-        launch_kernel(whole ? dequantize_kernel<true> : dequantize_kernel<false>, grid, dim3(256),
-                      static_cast<hipStream_t>(a.stream), static_cast<const int8_t *>(a.Q), a.ldq,
-                      a.scales, static_cast<uint16_t *>(a.Y), a.ldy, a.rows, a.d);
+    auto run = [&](auto tpr) {
+        constexpr int TPR = decltype(tpr)::value, ROWS = RowThreads<TPR>::ROWS;
+        const dim3 grid(grid_of((a.rows + ROWS - 1LL) / ROWS),
+                        static_cast<unsigned>((a.d + 32 * TPR - 1) / (32 * TPR)));
+        return launch_kernel(whole ? dequantize_kernel<TPR, true> : dequantize_kernel<TPR, false>,
+                             grid, dim3(256), static_cast<hipStream_t>(a.stream),
+                             static_cast<const int8_t *>(a.Q), a.ldq, a.scales,
+                             static_cast<uint16_t *>(a.Y), a.ldy, a.rows, a.d);
+    };
+    const hipError_t e = a.d <= 512 ? run(IC<16>{}) : run(IC<64>{});
     return e == hipSuccess ? DD_OK : DD_ERR_HIP;
 }
 

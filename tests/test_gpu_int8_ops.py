@@ -33,9 +33,10 @@ pytestmark = pytest.mark.gpu
 U, B = 2.0 ** -24, 2.0 ** -8
 EPS = 1e-5
 
-# every form of a row: one wave of 1-4 chunks per lane, a workgroup of 256
-# with 1-4, one of 1024; whole and ragged, one row to several workgroups
-ROWS = [(1, 1), (3, 7), (2, 8), (1, 64), (5, 100), (9, 512), (2, 520), (1, 2048), (700, 2048),
+# every form of a row: a quarter or half of a wave, one wave of 1-4 chunks per
+# lane, a workgroup of 256 with 1-4, one of 1024; whole and ragged, one row to
+# several workgroups
+ROWS = [(1, 1), (50, 128), (33, 129), (41, 250), (19, 256), (3, 7), (2, 8), (1, 64), (5, 100), (9, 512), (2, 520), (1, 2048), (700, 2048),
         (601, 1416), (513, 1000), (3, 1021), (515, 1029), (2, 2056), (7, 4100), (3, 5632),
         (2, 8192), (2, 8200), (3, 10001), (2, 16384)]
 
