@@ -200,21 +200,28 @@ inline GemmI8Tile gemm_i8_tile(int M, int N, int K, int cus)
 }
 
 // How `n` weight gradients of M x N over T tokens run: on tiles of 256 x 256 or
-// 128 x 128 (`edge`; tiles_n of all n), T in `steps` of 64 tokens.  The first `whole` tiles are a
-// workgroup's each.  The others, fewer than the CUs, are shared out so that
-// every workgroup has `head` steps: one workgroup per tile takes its first
-// `head`, and the rest of them, one tile after the other, is cut into pieces
-// of `head` steps for `tails` further workgroups.  (In parts of equal length
-// 176 tiles of 1024 steps, 2048 x 5632 over 65,536 tokens, would be 2.75
-// rounds of 256 CUs at four parts each, which takes three.)
+// 128 x 128 (`edge`; tiles_n of all n), T in `steps` of 64 tokens.  The first
+// `whole` tiles are a workgroup's each.  The others, fewer than the CUs, are
+// shared out so that every workgroup has `head` steps: `heads` workgroups per
+// tile take its first parts, and the rest of the tiles, one after the other,
+// is cut into pieces for `tails` further workgroups.  (In parts of equal length
+// 176 tiles of 1024 steps, 2048 x 5632 over 65,536 tokens, would be 2.75 rounds
+// of 256 CUs at four parts each, which takes three.)  The heads of all tiles
+// read the same tokens at the same time, the tails do not: 44 tiles of 1024
+// steps with one head each and the rest in pieces took 478 us, as five heads
+// and pieces 421.
 struct WgradPlan {
-    int edge, tiles_m, tiles_n, whole, steps, head, tails;
+    int edge, tiles_m, tiles_n, whole, steps, heads, head, tails;
 
     int shared() const { return tiles_m * tiles_n - whole; }
-    int rest() const { return steps - head; }  // of a shared tile
+    int rest() const { return std::max(steps - heads * head, 0); }  // of a shared tile
     // Parts of tiles that one of the `tails` can touch.
     int most() const { return (head - 1) / std::max(rest(), 1) + 2; }
-    long long partials() const { return head ? shared() + static_cast<long long>(tails) * most() : 0; }
+    long long partials() const
+    {
+        return heads ? static_cast<long long>(heads) * shared() + static_cast<long long>(tails) * most()
+                     : 0;
+    }
 };
 
 inline WgradPlan wgrad_plan(int T, int M, int N, int n, int cus)
@@ -223,40 +230,52 @@ inline WgradPlan wgrad_plan(int T, int M, int N, int n, int cus)
     const int steps = static_cast<int>((T + 63LL) / 64);
     WgradPlan best{};
     double cost = -1;
+    auto consider = [&](const WgradPlan &p, double c) {
+        if (cost < 0 || c < cost) {
+            cost = c;
+            best = p;
+        }
+    };
     for (const int edge : {256, 128}) {
         const long long tm = (M + edge - 1LL) / edge, tn = (N + edge - 1LL) / edge * n, tiles = tm * tn;
         // us a step: with few workgroups its latency, with a full chip its
-        // power (2048 x 5632, 16,384 tokens: 176 workgroups of 256 steps
-        // 300 us, 256 of 176 steps 280; 256 x 256, 65,536 tokens, one
-        // workgroup of 1024 steps per tile: 938 us, 542 on 128 x 128 tiles).
+        // power (2048 x 5632, 65,536 tokens: 176 workgroups of 1024 steps
+        // 1235 us, 256 of 704 steps 1154; 256 x 256, one workgroup of 1024
+        // steps per tile: 938 us, 542 on 128 x 128 tiles).
         auto step = [&](double wgs) {
             const double used = std::min(wgs / cus, 1.0);
-            return edge == 256 ? std::max(1.03, 1.62 * used) : std::max(0.50, 0.58 * used);
+            return edge == 256 ? std::max(1.03, 0.35 + 1.24 * used) : std::max(0.50, 0.58 * used);
         };
-        for (const bool share : {false, true}) {
-            const long long over = tiles % cus, full = tiles / cus;
-            WgradPlan p{edge, static_cast<int>(tm), static_cast<int>(tn), static_cast<int>(tiles),
-                        steps, 0, 0};
-            double c;
-            if (share) {
-                // Parts of at least 8 steps: shorter ones are mostly start-up.
-                p.head = static_cast<int>(std::max((over * steps + cus - 1) / cus, 8LL));
-                if (over == 0 || p.head >= steps)
-                    continue;
-                p.whole = static_cast<int>(tiles - over);
+        const long long over = tiles % cus, full = tiles / cus;
+        const double whole = full * (steps * step(cus) + 6.0);
+        WgradPlan p{edge, static_cast<int>(tm), static_cast<int>(tn), static_cast<int>(tiles), steps,
+                    0, 0, 0};
+        consider(p, over ? whole + steps * step(over) + 6.0 : whole);
+        // Shared: with as many heads as there are CUs for, or one; of equal
+        // parts, or with the rest in pieces.  Parts of at least 8 steps: shorter
+        // ones are mostly start-up, 2.5 us of every part.  (3001 x 1040 x 1416:
+        // two equal heads 34 us, two and pieces of 7 steps 38.)
+        if (over == 0 || steps < 16)
+            continue;
+        p.whole = static_cast<int>(tiles - over);
+        for (const long long most : {cus / over, 1LL})
+            for (const bool pieces : {false, true}) {
+                p.heads = static_cast<int>(std::min<long long>(most, steps / 8));
+                p.head = pieces ? static_cast<int>(std::max((over * steps + cus - 1) / cus, 8LL))
+                                : (steps + p.heads - 1) / p.heads;
+                p.heads = std::min(p.heads, (steps + p.head - 1) / p.head);  // each has steps
                 p.tails = static_cast<int>((over * p.rest() + p.head - 1) / p.head);
-                c = full * (steps * step(cus) + 6.0) + p.head * step(over + p.tails) + 6.0 + 6.0 +
-                    static_cast<double>(over + over + p.tails) * edge * edge * 8.0 / 1.0e7;
-            } else {
-                c = full * (steps * step(cus) + 6.0);
-                if (over)
-                    c += steps * step(over) + 6.0;
+                const long long parts = over * p.heads + p.tails;
+                if (parts > cus || p.head >= steps)
+                    continue;
+                const int starts = p.tails ? (p.head + p.rest() - 1) / p.rest() : 0;
+                // The tiles' first parts share what they read, the pieces do not.
+                const double traffic = (static_cast<double>(p.heads) * p.head * (tm + tn) +
+                                        2.0 * over * p.rest()) * edge * 128.0 / 6.0e6;
+                consider(p, whole + std::max(p.head * step(parts), traffic) + 12.0 + 2.5 * starts +
+                                static_cast<double>(parts + (p.tails ? over : 0)) * edge * edge *
+                                    8.0 / 1.0e7);
             }
-            if (cost < 0 || c < cost) {
-                cost = c;
-                best = p;
-            }
-        }
     }
     return best;
 }

@@ -89,14 +89,15 @@ restore_kernel(const int8_t *__restrict__ Q, long long ldq, const float *__restr
 }
 
 // dW[i] = X^T dY[i] for up to three dY.  Their tiles are one grid of tiles_m x
-// tiles_n, `cols` columns of it each.  P: fp32 parts of the shared tiles: one
-// per tile for its first `head` steps, then `most` per further workgroup.
+// tiles_n, `cols` columns of it each.  P: fp32 parts of the shared tiles (of
+// WgradPlan): `firsts` = heads x shared, one of each tile's first `head` steps,
+// one of its next and so on, then `most` for each of the tails.
 struct WgradOperands {
     const uint16_t *XT, *dY[3];
     uint16_t *dW[3];
     float *P;
     long long Tp, ldy, ldw;
-    int T, M, N, tiles_m, tiles_n, cols, xm, whole, shared, steps, head, rest, most;
+    int T, M, N, tiles_m, tiles_n, cols, xm, whole, shared, firsts, steps, head, rest, most;
 };
 
 // Where a tile is: its gradient and its first row and column in that.
@@ -136,16 +137,17 @@ struct WgradParts {
             first = 0;
             count = op.steps;
             slot = -1;
-        } else if (id < op.whole + op.shared) {
-            tile = id;
-            first = 0;
-            count = op.head;
+        } else if (id < op.whole + op.firsts) {
             slot = id - op.whole;
+            const int j = slot / op.shared;
+            tile = id - j * op.shared;
+            first = j * op.head;
+            count = min(op.head, op.steps - first);
         } else {
-            const int w = id - op.whole - op.shared;
+            const int w = id - op.whole - op.firsts;
             at = w * op.head;
             end = min(at + op.head, op.shared * op.rest);
-            slot = op.shared + w * op.most - 1;
+            slot = op.firsts + w * op.most - 1;
             next(op);
         }
     }
@@ -154,7 +156,7 @@ struct WgradParts {
     {
         const int i = at / op.rest, skip = at - i * op.rest;
         tile = op.whole + i;
-        first = op.head + skip;
+        first = op.steps - op.rest + skip;
         count = min(op.rest - skip, end - at);
         at += count;
         ++slot;
@@ -551,12 +553,14 @@ wgrad_sum_kernel(WgradOperands op)
         s0 += *reinterpret_cast<const f32x4 *>(p);
         s1 += *reinterpret_cast<const f32x4 *>(p + 4);
     };
-    add(tile);
-    // The further workgroups that touch this tile, and which of their parts
-    // it is.
-    const int w0 = tile * op.rest / op.head, w1 = ((tile + 1) * op.rest - 1) / op.head;
-    for (int w = w0; w <= w1; ++w)
-        add(op.shared + w * op.most + tile - w * op.head / op.rest);
+    for (int slot = tile; slot < op.firsts; slot += op.shared)
+        add(slot);
+    // The tails that touch this tile, and which of their parts it is.
+    if (op.rest > 0) {
+        const int w0 = tile * op.rest / op.head, w1 = ((tile + 1) * op.rest - 1) / op.head;
+        for (int w = w0; w <= w1; ++w)
+            add(op.firsts + w * op.most + tile - w * op.head / op.rest);
+    }
     *reinterpret_cast<bf16x8 *>(pick3(op.dW, place.i) + m * op.ldw + n) =
         join(pack4(s0[0], s0[1], s0[2], s0[3]), pack4(s1[0], s1[1], s1[2], s1[3]));
 }
@@ -599,7 +603,7 @@ int launch_wgrad_i8(const WgradI8Args &a)
                                  xt, Tp, a.T, a.M);
     if (e != hipSuccess)
         return DD_ERR_HIP;
-    const int shared = p.head ? p.shared() : 0;
+    const int shared = p.heads ? p.shared() : 0;
     WgradOperands op{};
     op.XT = xt;
     for (int i = 0; i < a.n; ++i) {
@@ -619,11 +623,12 @@ int launch_wgrad_i8(const WgradI8Args &a)
     op.xm = tile_rows_step(p.tiles_m, p.tiles_n);
     op.whole = p.whole;
     op.shared = shared;
+    op.firsts = p.heads * shared;
     op.steps = p.steps;
     op.head = p.head;
     op.rest = p.rest();
     op.most = p.most();
-    const unsigned wgs = static_cast<unsigned>(p.whole) + shared + p.tails;
+    const unsigned wgs = static_cast<unsigned>(p.whole + op.firsts + p.tails);
     e = launch_kernel(p.edge == 256 ? wgrad_kernel : wgrad_small_kernel, dim3(wgs), dim3(512), st, op);
     if (e != hipSuccess || !shared)
         return e == hipSuccess ? DD_OK : DD_ERR_HIP;

@@ -15,8 +15,9 @@ extern "C" {
 int product(int M, int N, int K, int cus) { return static_cast<int>(dd::gemm_i8_tile(M, N, K, cus)); }
 void wgrad(int T, int M, int N, int n, int cus, int *out) {
     const dd::WgradPlan p = dd::wgrad_plan(T, M, N, n, cus);
-    out[0] = p.edge; out[1] = p.whole; out[2] = p.head ? p.shared() : 0; out[3] = p.steps;
+    out[0] = p.edge; out[1] = p.whole; out[2] = p.heads ? p.shared() : 0; out[3] = p.steps;
     out[4] = p.head; out[5] = p.tails; out[6] = p.most(); out[7] = p.tiles_m * p.tiles_n;
+    out[8] = p.heads; out[9] = p.rest();
 }
 }
 """
@@ -39,7 +40,8 @@ def product(M, N, K):
 
 def wgrad(T, M, N, n=1):
     """How n weight gradients run: edge, whole, shared, steps, head, tails,
-    most, tiles."""
-    out = (ctypes.c_int * 8)()
+    most, tiles, heads, rest."""
+    out = (ctypes.c_int * 10)()
     _lib().wgrad(T, M, N, n, CUS, out)
-    return dict(zip(("edge", "whole", "shared", "steps", "head", "tails", "most", "tiles"), out))
+    return dict(zip(("edge", "whole", "shared", "steps", "head", "tails", "most", "tiles",
+                     "heads", "rest"), out))

@@ -163,16 +163,18 @@ def parts_of(plan, wg):
     """The (tile, first step, steps, slot) that a workgroup computes."""
     if wg < plan["whole"]:
         return [(wg, 0, plan["steps"], -1)]
-    i = wg - plan["whole"]
-    if i < plan["shared"]:
-        return [(wg, 0, plan["head"], i)]
-    w, rest = i - plan["shared"], plan["steps"] - plan["head"]
+    i, rest, firsts = wg - plan["whole"], plan["rest"], plan["heads"] * plan["shared"]
+    if i < firsts:
+        j, tile = divmod(i, plan["shared"])
+        first = j * plan["head"]
+        return [(plan["whole"] + tile, first, min(plan["head"], plan["steps"] - first), i)]
+    w = i - firsts
     at, end, out = w * plan["head"], min((w + 1) * plan["head"], plan["shared"] * rest), []
     while at < end:
         tile, skip = divmod(at, rest)
         n = min(rest - skip, end - at)
-        out.append((plan["whole"] + tile, plan["head"] + skip, n,
-                    plan["shared"] + w * plan["most"] + len(out)))
+        out.append((plan["whole"] + tile, plan["steps"] - rest + skip, n,
+                    firsts + w * plan["most"] + len(out)))
         at += n
     return out
 
@@ -181,12 +183,16 @@ def parts_of(plan, wg):
 @pytest.mark.parametrize("T,M,N", [(65536, 2048, 5632), (3001, 1040, 1416), (65536, 256, 256),
                                    (4096, 1024, 1024), (16384, 1024, 2816), (700, 4352, 4360),
                                    (65536, 4096, 8192), (200000, 264, 520), (9000, 1800, 5000),
-                                   (1, 8, 8), (33554368, 8, 8)])
+                                   (1, 8, 8), (33554368, 8, 8), (65536, 1024, 2816),
+                                   (5000, 1100, 2700), (1200, 640, 640), (2100, 300, 300),
+                                   (32832, 256, 256), (20000, 136, 200), (65600, 512, 512),
+                                   (60047, 8, 8)])
 def test_weight_gradient_plans_cover_every_step_once(T, M, N, n):
     p = routes.wgrad(T, M, N, n)
     assert p["tiles"] == p["whole"] + p["shared"] and p["tiles"] % n == 0
     covered, slots = {}, set()
-    for wg in range(p["whole"] + p["shared"] + p["tails"]):
+    firsts = p["heads"] * p["shared"]
+    for wg in range(p["whole"] + firsts + p["tails"]):
         parts = parts_of(p, wg)
         assert parts and len(parts) <= p["most"]
         assert sum(k for _, _, k, _ in parts) <= max(p["head"], p["steps"])
@@ -196,11 +202,11 @@ def test_weight_gradient_plans_cover_every_step_once(T, M, N, n):
             assert slot < 0 or slot not in slots
             slots.add(slot)
             # and where the last launch looks for it
-            rest = p["steps"] - p["head"]
-            if slot >= p["shared"]:
-                w, i = wg - p["whole"] - p["shared"], tile - p["whole"]
+            rest = p["rest"]
+            if slot >= firsts:
+                w, i = wg - p["whole"] - firsts, tile - p["whole"]
                 assert i * rest // p["head"] <= w <= ((i + 1) * rest - 1) // p["head"]
-                assert slot == p["shared"] + w * p["most"] + i - w * p["head"] // rest
+                assert slot == firsts + w * p["most"] + i - w * p["head"] // rest
     assert sorted(covered) == list(range(p["tiles"]))
     for parts in covered.values():
         at = 0
@@ -209,7 +215,7 @@ def test_weight_gradient_plans_cover_every_step_once(T, M, N, n):
             at += k
         assert at == p["steps"]
     # a shared tile's workgroups are resident together with the others
-    assert p["shared"] + p["tails"] <= routes.CUS
+    assert firsts + p["tails"] <= routes.CUS
 
 
 def test_oracle_codes_take_ties_to_even():
