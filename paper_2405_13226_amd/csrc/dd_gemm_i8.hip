@@ -29,7 +29,6 @@ __device__ __forceinline__ i32x4 mfma_i8(u32x4 a, u32x4 b, i32x4 c)
 
 // Pieces of rows at any bf16 address (the hardware takes unaligned vectors).
 typedef uint32_t piece16 __attribute__((ext_vector_type(4), aligned(2)));
-typedef uint32_t piece8 __attribute__((ext_vector_type(2), aligned(2)));
 
 struct GemmI8Operands {
     const int8_t *A, *B;
@@ -45,30 +44,18 @@ __device__ __forceinline__ float bf16_at(const uint16_t *p)
     return __uint_as_float(static_cast<uint32_t>(*p) << 16);
 }
 
-// sa sb acc + R of row m, columns n .. n + 3, in bf16 (junk where they do not
-// exist).  ra: sa of the row, rb: sb of the columns.
-__device__ __forceinline__ bf16x4 scaled(const GemmI8Operands &op, i32x4 acc, float ra,
-                                         const float (&rb)[4], int m, int n)
+// Two accumulators' (j = 0 and 1 of a row block) scaled values of eight
+// neighbouring columns: the lanes of neighbouring g exchange halves, after
+// which a lane holds the columns from 16 (g % 2) + 8 (g / 2) on.
+__device__ __forceinline__ void scale8(i32x4 a0, i32x4 a1, float ra, const float (&rb)[8],
+                                       float (&c)[8])
 {
-    float c[4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
-        c[e] = static_cast<float>(acc[e]) * ra * rb[e];
-    if (op.R != nullptr && m < op.M) {
-        const uint16_t *r = op.R + m * op.ldc + n;
-        if (n + 4 <= op.N) {
-            const bf16x4 v = __builtin_bit_cast(bf16x4, *reinterpret_cast<const piece8 *>(r));
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                c[e] += static_cast<float>(v[e]);
-        } else {
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (n + e < op.N)
-                    c[e] += bf16_at(r + e);
-        }
+    for (int e = 0; e < 4; ++e) {
+        const auto p = __builtin_amdgcn_permlane16_swap(a0[e], a1[e], false, false);
+        c[e] = static_cast<float>(static_cast<int>(p[0])) * ra * rb[e];
+        c[e + 4] = static_cast<float>(static_cast<int>(p[1])) * ra * rb[e + 4];
     }
-    return pack4(c[0], c[1], c[2], c[3]);
 }
 
 // c += the eight bf16 values of a piece.
@@ -92,39 +79,6 @@ __device__ __forceinline__ void store_edge(const GemmI8Operands &op, long long o
             const float v = op.R != nullptr ? c[e] + bf16_at(op.R + o + e) : c[e];
             op.C[o + e] = __builtin_bit_cast(uint16_t, static_cast<__bf16>(v));
         }
-}
-
-// The finished BM x BN tile in LDS, and from there to memory in 16-byte pieces
-// of rows.  A row's 4-element group x sits at x ^ (2 (r mod 16)), which keeps
-// the two groups of a piece adjacent and spreads one write instruction's 16
-// rows over the LDS banks.
-template <int BN>
-__device__ __forceinline__ int image_off(int r, int c)
-{
-    return r * BN + 4 * ((c >> 2) ^ (2 * (r & 15)));
-}
-
-template <int BM, int BN>
-__device__ __forceinline__ void store_image(const uint16_t *lds, const GemmI8Operands &op, int m0,
-                                            int n0, int tid)
-{
-    constexpr int CPR = BN / 8;
-#pragma unroll 4
-    for (int it = 0; it < BM * CPR / 512; ++it) {
-        const int idx = it * 512 + tid, r = idx / CPR, c = idx % CPR * 8, m = m0 + r, n = n0 + c;
-        const u32x4 v = *reinterpret_cast<const u32x4 *>(lds + image_off<BN>(r, c));
-        if (m >= op.M || n >= op.N)
-            continue;
-        uint16_t *p = op.C + m * op.ldc + n;
-        if (n + 8 <= op.N) {
-            *reinterpret_cast<piece16 *>(p) = v;
-        } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (n + e < op.N)
-                    p[e] = static_cast<uint16_t>(v[e >> 1] >> 16 * (e & 1));
-        }
-    }
 }
 
 // The direct loads of both operands of a tile.  Every 64 rows x 128 bytes of
@@ -352,9 +306,8 @@ gemm_i8_kernel(GemmI8Operands op)
                 step(IC<S>{}, IC<0>{});
         }
         // Accumulator (ha, hb, i, j), register e: row m = 128 ha + 64 wm + 16 i
-        // + l16, column n = 128 hb + 32 wn + 16 j + 4 g + e of the tile.  The
-        // lanes of neighbouring g exchange halves of j = 0 and j = 1, after
-        // which a lane holds the eight columns from 16 (g % 2) + 8 (g / 2) on.
+        // + l16, column n = 128 hb + 32 wn + 16 j + 4 g + e of the tile; eight
+        // neighbouring columns per lane by scale8.
         const int m0 = at.m0(done), n0 = at.n0(done);
         const bool whole = m0 + 256 <= op.M && n0 + 256 <= op.N;
         const float *sc = reinterpret_cast<const float *>(lds + 2 * SIDE + 2048 * (done & 3));
@@ -387,13 +340,7 @@ gemm_i8_kernel(GemmI8Operands op)
                 const int ha = x >> 2, i = x & 3, r = 128 * ha + 16 * i, m = m0 + r + row;
                 const float ra = sc[r + row];
                 float c[8];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const auto p = __builtin_amdgcn_permlane16_swap(acc[ha][hb][i][0][e],
-                                                                    acc[ha][hb][i][1][e], false, false);
-                    c[e] = static_cast<float>(static_cast<int>(p[0])) * ra * rb[e];
-                    c[e + 4] = static_cast<float>(static_cast<int>(p[1])) * ra * rb[e + 4];
-                }
+                scale8(acc[ha][hb][i][0], acc[ha][hb][i][1], ra, rb, c);
                 const long long o = at0 + r * ld;
                 if (whole || (m < op.M && n + 8 <= op.N)) {
                     if (op.R != nullptr)
@@ -420,14 +367,18 @@ gemm_i8_kernel(GemmI8Operands op)
     wait_vmem();
 }
 
-// 128 x 128 tiles for products whose large tiles would leave CUs idle: eight
-// waves in two groups that run half a phase apart, a phase of 16 products of
-// every wave per K step of 128, four stages in LDS of which three are in
-// flight (128 KiB).
-__global__ void __launch_bounds__(512, 1)
+// 128 x 128 tiles, two workgroups per CU (80 KiB each), whose starts and ends
+// the other one's products fill.  K in steps of 64, five stages of which four
+// are in flight; eight waves, 64 x 32 each, one barrier a step.  What the end
+// needs is loaded before the loop.  (One workgroup per CU, four stages of 128
+// and two wave groups half a phase apart, with the tile's image through LDS:
+// 16,384 x 500 over 512 14.7 us, here 12.1; 65,536 x 512 over 512 51.2 and
+// 34.9; 4096 x 2048 over 2048 with a residual 32.2 and 27.7; at one tile per CU
+// or fewer the same within 8%.)
+__global__ void __launch_bounds__(512, 4)
 gemm_i8_small_kernel(GemmI8Operands op)
 {
-    constexpr int SUB = 64 * 128, STAGE = 4 * SUB, NST = 4;  // bytes
+    constexpr int SIDE = 128 * 64, STAGE = 2 * SIDE, NST = 5;  // bytes
     __shared__ __attribute__((aligned(1024))) int8_t lds[NST * STAGE];
     const int tid = threadIdx.x;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
@@ -436,100 +387,88 @@ gemm_i8_small_kernel(GemmI8Operands op)
     int tm, tn;
     tile_of(static_cast<int>(blockIdx.x), op.tiles_m, op.tiles_n, op.xm, tm, tn);
     const int m0 = tm * 128, n0 = tn * 128;
-    const int nkt = (op.K + 127) / 128;
-    I8Loads at;
-    at.init(op, m0, n0, wave, lane);
+    const int nkt = (op.K + 63) / 64;
+
+    // A wave loads 16 rows of 64 bytes of each side.  Chunk x of row r sits at
+    // x ^ (-(r / 4) mod 4): the 16 lanes that the LDS serves together (rows r,
+    // r + 12 of chunk x, r + 4, r + 8 of chunk x + 1, r < 4, and so on) then read
+    // all banks.
+    const int swz = -(lane >> 4) & 3;
+    const int kx = ((lane & 3) ^ swz) * 16;
+    const u32x4 ba = buffer_of(op.A + m0 * op.lda, (op.M - 1LL - m0) * op.lda + op.K);
+    const u32x4 bb = buffer_of(op.B + n0 * op.ldb, (op.N - 1LL - n0) * op.ldb + op.K);
+    const uint32_t va = static_cast<uint32_t>((16 * wave + (lane >> 2)) * op.lda + kx);
+    const uint32_t vb = static_cast<uint32_t>((16 * wave + (lane >> 2)) * op.ldb + kx);
     const uint32_t lds0 = lds_base_sgpr(lds) + 1024u * wave;
-    auto load_step = [&](int st) __attribute__((always_inline)) {
-        at.load_a(0, lds0 + STAGE * st);
-        at.load_a(1, lds0 + STAGE * st + SUB);
-        at.load_b(0, lds0 + STAGE * st + 2 * SUB);
-        at.load_b(1, lds0 + STAGE * st + 3 * SUB);
-        at.k += 128;
+    auto load = [&](int kt, int st) __attribute__((always_inline)) {
+        const int k = kt * 64;
+        dma_b128_buf(ba, kx + k < op.K ? va + k : kBufferEnd, lds0 + STAGE * st);
+        dma_b128_buf(bb, kx + k < op.K ? vb + k : kBufferEnd, lds0 + STAGE * st + SIDE);
     };
-    int fa[2], fb[2];  // byte offsets in a stage
+    const int x = (g ^ (-(l16 >> 2) & 3)) * 16;
+    const int fa = (64 * wm + l16) * 64 + x, fb = SIDE + (32 * wn + l16) * 64 + x;
+
+    // The lane's rows and columns in the end (gemm_i8_kernel).
+    const int row = m0 + 64 * wm + l16, n = n0 + 32 * wn + 16 * (g & 1) + 8 * (g >> 1);
+    float ra[4], rb[8];
+    u32x4 res[4];
 #pragma unroll
-    for (int kk = 0; kk < 2; ++kk) {
-        const int x = ((4 * kk + g) ^ row_swz(l16)) * 16;
-        fa[kk] = wm * SUB + 128 * l16 + x;
-        fb[kk] = (2 + (wn >> 1)) * SUB + 128 * (32 * (wn & 1) + l16) + x;
+    for (int e = 0; e < 8; ++e)
+        rb[e] = op.sb[min(n + e, op.N - 1)];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int m = row + 16 * i;
+        ra[i] = op.sa[min(m, op.M - 1)];
+        res[i] = u32x4{0u, 0u, 0u, 0u};
+        if (op.R != nullptr && m < op.M && n + 8 <= op.N)
+            res[i] = *reinterpret_cast<const piece16 *>(op.R + m * op.ldc + n);
     }
+
     i32x4 acc[4][2];
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
         for (int j = 0; j < 2; ++j)
             acc[i][j] = i32x4{};
-    const int first = min(nkt, NST - 1);
-    for (int kt = 0; kt < first; ++kt)
-        load_step(kt);
-    if (nkt > NST - 2)
-        wait_and_barrier<4 * (NST - 2)>();
-    else
-        wait_and_barrier<0>();
-    if (wm == 1)
-        plain_barrier();
+    for (int kt = 0; kt < NST - 1; ++kt)
+        load(kt, kt);  // (behind K: zeros)
     int rs = 0, ws = NST - 1;  // the stages read and refilled by a step
     for (int kt = 0; kt < nkt; ++kt) {
+        // This step's loads are there, and every wave has read the stage of the
+        // step before.
+        wait_and_barrier<2 * (NST - 2)>();
+        load(kt + NST - 1, ws);
         const int8_t *st = lds + rs * STAGE;
-        u32x4 a[4][2], b[2][2];
+        u32x4 a[4], b[2];
 #pragma unroll
-        for (int kk = 0; kk < 2; ++kk) {
+        for (int j = 0; j < 2; ++j)
+            b[j] = *reinterpret_cast<const u32x4 *>(st + fb + 1024 * j);
 #pragma unroll
-            for (int j = 0; j < 2; ++j)
-                b[j][kk] = *reinterpret_cast<const u32x4 *>(st + fb[kk] + 2048 * j);
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                a[i][kk] = *reinterpret_cast<const u32x4 *>(st + fa[kk] + 2048 * i);
-        }
-        // The stage that the step before has read is refilled; before the
-        // next step starts, its own loads have to be there (the steps after
-        // it may be in flight).
-        const int ahead = nkt - 1 - kt;  // steps after this one
-        if (ahead >= NST - 1) {
-            load_step(ws);
-            wait_and_barrier<4 * (NST - 2)>();
-        } else if (ahead == 2) {
-            wait_and_barrier<4>();
-        } else {
-            wait_and_barrier<0>();
-        }
+        for (int i = 0; i < 4; ++i)
+            a[i] = *reinterpret_cast<const u32x4 *>(st + fa + 1024 * i);
         ws = rs;
         rs = rs + 1 == NST ? 0 : rs + 1;
-        __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-        for (int kk = 0; kk < 2; ++kk)
+        for (int i = 0; i < 4; ++i)
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int j = 0; j < 2; ++j)
-                    acc[i][j] = mfma_i8(b[j][kk], a[i][kk], acc[i][j]);  // rows n, columns m
-        __builtin_amdgcn_s_setprio(0);
-        plain_barrier();
+            for (int j = 0; j < 2; ++j)
+                acc[i][j] = mfma_i8(b[j], a[i], acc[i][j]);  // rows n, columns m
     }
-    if (wm == 0)
-        plain_barrier();
-
-    // Accumulator (i, j), register e: row m = 64 wm + 16 i + l16, column n =
-    // 32 wn + 16 j + 4 g + e of the tile.
-    __syncthreads();
-    uint16_t *image = reinterpret_cast<uint16_t *>(lds);
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-        const int c = 32 * wn + 16 * j + 4 * g;
-        float rb[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-            rb[e] = op.sb[min(n0 + c + e, op.N - 1)];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int r = 64 * wm + 16 * i + l16;
-            *reinterpret_cast<bf16x4 *>(image + image_off<128>(r, c)) =
-                scaled(op, acc[i][j], op.sa[min(m0 + r, op.M - 1)], rb, m0 + r, n0 + c);
+    for (int i = 0; i < 4; ++i) {
+        const int m = row + 16 * i;
+        float c[8];
+        scale8(acc[i][0], acc[i][1], ra[i], rb, c);
+        const long long o = m * op.ldc + n;
+        if (m < op.M && n + 8 <= op.N) {
+            add8(c, res[i]);
+            *reinterpret_cast<piece16 *>(op.C + o) = pack8f(c);
+        } else if (m < op.M) {
+            store_edge(op, o, op.N - n, c);
         }
     }
-    __syncthreads();
-    store_image<128, 128>(image, op, m0, n0, tid);
+    // The loads behind the last step still write to this workgroup's LDS.
+    wait_vmem();
 }
 
 // At most 64 tokens: the weights are read once, straight into registers, 16

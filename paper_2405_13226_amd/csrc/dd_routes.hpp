@@ -172,31 +172,39 @@ inline GemmPlan gemm_plan(int M, long long N, long long K, bool may_split, int c
 }
 
 // How an int8 product of M x N over K runs: few tokens with the weights
-// straight into registers (64 x 6144 over 2048: 12.0 us, on small tiles 12.3;
-// 33 x 8192 over 6144 23.0 and 28.5), or on tiles of 128 x 128 or 256 x 256.
+// straight into registers, or on tiles of 128 x 128 or 256 x 256.
 enum class GemmI8Tile { kFew, kSmall, kLarge };
 
 inline GemmI8Tile gemm_i8_tile(int M, int N, int K, int cus)
 {
-    if (M <= 64)
-        return GemmI8Tile::kFew;
     cus = std::max(cus, 1);
-    // us: rounds of tiles over the CUs, each its own start and end and its K
-    // steps, which a full chip's power makes longer on the large tiles (16
-    // steps, one tile on each of 256 CUs 32 us, 16 of them 24; 22 rounds 640).
-    // Those pay more for a launch, and for storing parts of tiles (1531 x 5001
-    // over 1040: 26.6 us, on small tiles 20.4; 2048 x 6144 over 2048: 29.4 and
-    // 40.7).
-    auto time = [&](int edge) {
-        const double tiles = std::ceil(M / static_cast<double>(edge)) * std::ceil(N / static_cast<double>(edge));
-        const double steps = std::ceil(K / 128.0), full = std::floor(tiles / cus), last = tiles / cus - full;
-        auto round = [&](double used) {
-            return edge == 256 ? 6.5 + steps * (0.9 + 0.55 * used) : 5.5 + steps * 0.48;
-        };
-        const double launch = edge == 256 ? 3.0 + (M % 256 || N % 256 ? 6.0 : 0.0) : 0.0;
-        return launch + full * round(1.0) + (last > 0 ? round(last) : 0.0);
+    const double steps = std::ceil(K / 128.0);
+    auto tiles = [&](int edge) {
+        return std::ceil(M / static_cast<double>(edge)) * std::ceil(N / static_cast<double>(edge)) / cus;
     };
-    return time(128) < time(256) ? GemmI8Tile::kSmall : GemmI8Tile::kLarge;
+    // us.  Small tiles, of which a CU has two at once: a third one starts when
+    // the first is done.  One to four per CU of 16 steps 14.3, 26.0, 37.4, 47.3;
+    // 352 and 384 on 256 CUs 21.9 and 21.2; 2048 of 4 steps 34.9.
+    const double s = tiles(128), rounds = std::max(1.0, std::min(std::ceil(s), s + 0.25));
+    const double small = 3.0 + rounds * (1.7 + steps * 0.62);
+    // Large ones: each its own start and end and its K steps, which a full
+    // chip's power makes longer (16 steps, one tile on each of 256 CUs 32, 16 of
+    // them 24; 22 rounds 610), and what it takes to store parts of tiles (8192
+    // x 700 over 1008 23.4, small 15.5; 1500 x 5632 over 2048 27.6 and 34.0).
+    auto round = [&](double used) { return 6.5 + steps * (0.9 + 0.55 * used); };
+    const double l = tiles(256), full = std::floor(l);
+    const double large = 3.0 + (N % 256 ? 6.0 : 0.0) + full * round(1.0) +
+                         (l > full ? round(l - full) : 0.0);
+    if (M <= 64) {
+        // The weights once, and the tokens again for every 16 or 32 rows of
+        // them, from L2 (6144 x 2048 for 1, 20 and 64 tokens 4.3, 6.9 and 12.1,
+        // on small tiles 12; 50,432 x 2048 18.1, 26.0 and 46.1, 20 to 22).
+        const double again = std::ceil(N / (N > 16384 ? 32.0 : 16.0)) * M * K;
+        const double few = 2.3 + K / 1365.0 + static_cast<double>(N) * K / 5.8e6 + again / 1.0e7;
+        if (few < std::min(small, large))
+            return GemmI8Tile::kFew;
+    }
+    return small < large ? GemmI8Tile::kSmall : GemmI8Tile::kLarge;
 }
 
 // How `n` weight gradients of M x N over T tokens run: on tiles of 256 x 256 or

@@ -238,17 +238,27 @@ def test_gemm_int8(cuda, M, N, K, residual):
 # step a tile to several, odd counts (whose tiles start in alternating stages),
 # whole and ragged tiles, with and without stores that waits must pass over.
 @pytest.mark.parametrize("residual", [False, True])
-@pytest.mark.parametrize("K", [16, 128, 144, 272, 400, 528, 640, 1040])
-@pytest.mark.parametrize("M,N", [(5120, 8192), (4400, 8193)])
+@pytest.mark.parametrize("K", [16, 128, 144, 272, 400, 640, 1040])
+@pytest.mark.parametrize("M,N", [(16384, 12288), (16400, 12289)])
 def test_gemm_int8_several_tiles_a_workgroup(cuda, M, N, K, residual):
     assert routes.product(M, N, K) == "large"
     q, s = random_codes(M, K, M + K, cuda, full=True)
     p, t = random_codes(N, K, N + K + 1, cuda, full=True)
-    r = bf16((M, N), 9, 3.0).to(cuda) if residual else None
+    gen = torch.Generator(device=cuda).manual_seed(K)
+    r = torch.randn((M, N), generator=gen, device=cuda).to(torch.bfloat16) if residual else None
     c = ops.gemm_int8(q, s, p, t, residual=r)
-    rows = np.unique(np.r_[np.random.default_rng(0).choice(M, 200, replace=False), 0, 255, 256,
+    rows = np.unique(np.r_[np.random.default_rng(0).choice(M, 100, replace=False), 0, 255, 256,
                            M - 1])
     check_product(q[rows], s[rows], p, t, None if r is None else r[rows], c[rows])
+    # every other element against the small tiles, whose sums are the same
+    for m in range(0, M, 2100):
+        assert routes.product(min(2100, M - m), 4000, K) == "small"
+        for n in range(0, N, 4000):
+            part = ops.gemm_int8(q[m:m + 2100], s[m:m + 2100].contiguous(), p[n:n + 4000],
+                                 t[n:n + 4000].contiguous(),
+                                 residual=None if r is None else
+                                 r[m:m + 2100, n:n + 4000].contiguous())
+            assert torch.equal(c[m:m + 2100, n:n + 4000], part)
 
 
 def test_gemm_int8_more_tiles_a_workgroup_than_lanes(cuda):
@@ -262,7 +272,7 @@ def test_gemm_int8_more_tiles_a_workgroup_than_lanes(cuda):
 
 
 @pytest.mark.parametrize("M,N,K,form", [(64, 300, 80, "few"), (65, 300, 80, "small"),
-                                        (1531, 777, 640, "small"), (2048, 6144, 2048, "large")])
+                                        (1531, 777, 640, "small"), (2048, 6144, 2048, "large"), (9000, 6152, 912, "large")])
 def test_products_reach_every_form(cuda, M, N, K, form):
     assert routes.product(M, N, K) == form
     q, s = random_codes(M, K, 3, cuda)
