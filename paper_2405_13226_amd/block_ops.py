@@ -13,7 +13,7 @@ values are scales[r] * codes[r].  ``quantize`` forms them (the nearest codes
 to 127 x / max |x| of each row, ties to even) and so does ``rms_norm_int8``;
 ``gemm_int8`` multiplies two of them, ``gemm_int8_wgrad`` takes one as the
 kept input of a linear layer.  Their calls run on the tensors' device, on
-its current stream; matrices without rows or columns give empty results.
+its current stream; matrices without rows give empty results.
 """
 from __future__ import annotations
 
@@ -252,6 +252,14 @@ def _call(dev, name, *args):
         check(st, name)
 
 
+def _need(dev, name, *sizes):
+    """Workspace bytes of a call on ``dev`` (its CUs are counted)."""
+    if dev.index == torch._C._cuda_getDevice():
+        return _entry(name)(*sizes)
+    with torch.cuda.device(dev):
+        return _entry(name)(*sizes)
+
+
 def _dims(t, name, dtype, dev=None):
     """(rows, columns, row stride) of a matrix of this type with unit column
     stride on ``dev`` (any GPU if None).  A single row's stride, which is
@@ -301,6 +309,8 @@ def _result(out, rows, cols, dev, name="out"):
 def _norm_inputs(x, w, residual):
     """(rows, columns, x's row stride, the residual's, x + residual to be)."""
     rows, d, ldx = _dims(x, "x", torch.bfloat16)
+    if not d:
+        raise ValueError("the rows of x are empty")
     _vec(w, "w", d, torch.bfloat16, x.device)
     if residual is None:
         return rows, d, ldx, 0, None
@@ -317,7 +327,7 @@ def rms_norm(x, w, residual=None, eps: float = LN_EPS):
     dev = x.device
     y = torch.empty_like(x)
     rstd = torch.empty(rows, dtype=torch.float32, device=dev)
-    if rows and d:
+    if rows:
         _call(dev, "dd_rmsnorm_fwd", _p(x), ldx, _p(residual), ldr, _p(w), _p(h), _p(y),
               _p(rstd), rows, d, eps)
     return y, x if h is None else h, rstd
@@ -330,7 +340,7 @@ def rms_norm_int8(x, w, residual=None, eps: float = LN_EPS):
     codes = torch.empty_like(x, dtype=torch.int8)
     scales = torch.empty(rows, dtype=torch.float32, device=dev)
     rstd = torch.empty_like(scales)
-    if rows and d:
+    if rows:
         _call(dev, "dd_rmsnorm_int8_fwd", _p(x), ldx, _p(residual), ldr, _p(w), _p(h), _p(codes),
               d, _p(scales), _p(rstd), rows, d, eps)
     return codes, scales, x if h is None else h, rstd
@@ -351,7 +361,7 @@ def rms_norm_backward(h, w, rstd, dy, dres=None):
     dx, dw = torch.empty_like(h), torch.empty_like(w)
     if not (rows and d):
         return dx, dw.zero_()
-    need = _entry("dd_rmsnorm_bwd_workspace_bytes")(rows, d)
+    need = _need(dev, "dd_rmsnorm_bwd_workspace_bytes", rows, d)
     ws = torch.empty(need, dtype=torch.uint8, device=dev)
     _call(dev, "dd_rmsnorm_bwd", _p(h), _p(w), _p(rstd), _p(dy), _p(dres), _p(dx), _p(dw), rows,
           d, _p(ws), need)
@@ -363,7 +373,9 @@ def quantize(x):
     rows, d, ldx = _dims(x, "x", torch.bfloat16)
     codes = torch.empty_like(x, dtype=torch.int8)
     scales = torch.empty(rows, dtype=torch.float32, device=x.device)
-    if rows and d:
+    if not d:
+        return codes, scales.zero_()
+    if rows:
         _call(x.device, "dd_quantize", _p(x), ldx, _p(codes), d, _p(scales), rows, d)
     return codes, scales
 
@@ -438,7 +450,7 @@ def gemm_int8_wgrad_group(codes, scales, dys, outs=None):
     if not T:
         return [out.zero_() for out in outs]
     if M and N:
-        need = _entry("dd_gemm_i8_wgrad_workspace_bytes")(T, M, N, n)
+        need = _need(dev, "dd_gemm_i8_wgrad_workspace_bytes", T, M, N, n)
         ws = torch.empty(need, dtype=torch.uint8, device=dev)
         _call(dev, "dd_gemm_i8_wgrad", _p(codes), ldq, _p(scales), _array(dys), ldy, _array(outs),
               ldw, n, T, M, N, _p(ws), need)

@@ -18,11 +18,13 @@ fp32 rounding, 2^-8 the bf16 one, both relative to the value):
 * weight gradients: 2^-8 and T u of the magnitudes (a sum of T products), and
   relative L2 <= 3e-3 (the rounding of the result alone: 1.7e-3).
 """
+import ctypes
+
 import numpy as np
 import pytest
 import torch
 
-from paper_2405_13226_amd import block_ops as ops
+from paper_2405_13226_amd import _lib, block_ops as ops
 
 import int8_oracle as O
 import int8_routes as routes
@@ -36,8 +38,8 @@ EPS = 1e-5
 # every form of a row: a quarter or half of a wave, one wave of 1-4 chunks per
 # lane, a workgroup of 256 with 1-4, one of 1024; whole and ragged, one row to
 # several workgroups
-ROWS = [(1, 1), (50, 128), (33, 129), (41, 250), (19, 256), (3, 7), (2, 8), (1, 64), (5, 100), (9, 512), (2, 520), (1, 2048), (700, 2048),
-        (601, 1416), (513, 1000), (3, 1021), (515, 1029), (2, 2056), (7, 4100), (3, 5632),
+ROWS = [(1, 1), (50, 128), (33, 129), (41, 250), (19, 256), (3, 7), (2, 8), (1, 64), (5, 100),
+        (9, 512), (2, 520), (1, 2048), (700, 2048), (601, 1416), (513, 1000), (3, 1021), (515, 1029), (2, 2056), (7, 4100), (3, 5632),
         (2, 8192), (2, 8200), (3, 10001), (2, 16384)]
 
 
@@ -408,6 +410,41 @@ def test_gemm_int8_wgrad_rows_behind_the_last_token(cuda):
     assert torch.equal(ops.gemm_int8_wgrad(q[:T], s[:T].contiguous(), dy[:T]), want)
 
 
+def test_offsets_past_32_bits(cuda):
+    # 2.3e9 elements: the last rows are those of a matrix of their own
+    rows, d = 280_000, 8192
+    assert rows * d > 2 ** 31
+    x = torch.empty((rows, d), dtype=torch.bfloat16, device=cuda)
+    tail = bf16((64, d), 1).to(cuda)
+    x.zero_()
+    x[-64:] = tail
+    w = (1 + 0.1 * bf16((d,), 2).float()).to(torch.bfloat16).to(cuda)
+    q, s = ops.quantize(x)
+    q1, s1 = ops.quantize(tail)
+    assert torch.equal(q[-64:], q1) and torch.equal(s[-64:], s1) and not s[:-64].any()
+    assert torch.equal(ops.dequantize(q, s)[-64:], ops.dequantize(q1, s1))
+    dw = ops.gemm_int8_wgrad(q, s, torch.ones((rows, 8), dtype=torch.bfloat16, device=cuda))
+    ref = f64(ops.dequantize(q1, s1)).sum(0)
+    mag = np.abs(f64(ops.dequantize(q1, s1))).sum(0)
+    close(f64(dw)[:, 0], ref, B * np.abs(ref) + 64 * U * mag, "dw")
+    del q
+    for a, b in zip(ops.rms_norm(x, w, residual=x), ops.rms_norm(tail, w, residual=tail)):
+        assert torch.equal(a[-64:], b)
+    r = torch.ones(rows, device=cuda)
+    dx, _ = ops.rms_norm_backward(x, w, r, x)
+    assert torch.equal(dx[-64:], ops.rms_norm_backward(tail, w, r[:64].contiguous(), tail)[0])
+
+
+@pytest.mark.parametrize("M,N", [(70_000, 32_768), (8_400_000, 264)])
+def test_products_past_32_bits(cuda, M, N):
+    assert M * N > 2 ** 31
+    q, s = random_codes(M, 32, 1, cuda)
+    p, t = random_codes(N, 32, 2, cuda)
+    c = ops.gemm_int8(q, s, p, t)
+    rows = np.r_[0:8, M // 2:M // 2 + 8, M - 8:M]
+    check_product(q[rows], s[rows], p, t, None, c[rows])
+
+
 def test_empty_matrices(cuda):
     e = lambda *s, t=torch.bfloat16: torch.empty(s, dtype=t, device=cuda)
     y, h, rstd = ops.rms_norm(e(0, 64), e(64))
@@ -419,6 +456,8 @@ def test_empty_matrices(cuda):
     assert ops.dequantize(q, s).shape == (0, 64)
     b, sb = ops.quantize(e(32, 64).zero_())
     assert ops.gemm_int8(q, s, b, sb).shape == (0, 32)
+    q0, s0 = ops.quantize(e(4, 0))
+    assert q0.shape == (4, 0) and not s0.any()
     dw = ops.gemm_int8_wgrad(q, s, e(0, 16))
     assert dw.shape == (64, 16) and not dw.any()
     assert ops.gemm_int8_wgrad(b[:, :0].contiguous(), sb, e(32, 16)).shape == (0, 16)
@@ -514,3 +553,78 @@ def test_graph_replay_matches_eager(cuda, T, d, n):
             assert torch.equal(a, b), (rep, i)
         layer_step(*other)
         torch.cuda.synchronize()
+
+
+class Guarded:
+    """A tensor of this shape inside a buffer with bands of a pattern around it."""
+
+    def __init__(self, shape, dtype, dev):
+        n = int(np.prod(shape)) * torch.empty(0, dtype=dtype).element_size()
+        self.raw = torch.full((4096 + n + 4096,), 0xA5, dtype=torch.uint8, device=dev)
+        self.t = self.raw[4096:4096 + n].view(dtype).view(shape)
+        self.p = ctypes.c_void_p(self.t.data_ptr())
+
+    def intact(self):
+        n = self.raw.numel()
+        return bool((self.raw[:4096] == 0xA5).all() and (self.raw[n - 4096:] == 0xA5).all())
+
+
+def at(t):
+    return ctypes.c_void_p(t.data_ptr())
+
+
+@pytest.mark.parametrize("rows,d", [(7, 1), (33, 100), (19, 256), (5, 1021), (700, 1032), (3, 8200)])
+def test_row_outputs_stay_inside_their_buffers(cuda, rows, d):
+    lib, st = _lib.lib(), ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+    G = lambda *shape, dtype=torch.bfloat16: Guarded(shape, dtype, cuda)
+    x, r, dy = (bf16((rows, d), i).to(cuda) for i in range(3))
+    w = bf16((d,), 4).to(cuda)
+    f32, i8 = torch.float32, torch.int8
+    h, y, rstd = G(rows, d), G(rows, d), G(rows, dtype=f32)
+    assert lib.dd_rmsnorm_fwd(at(x), d, at(r), d, at(w), h.p, y.p, rstd.p, rows, d, 1e-5, st) == 0
+    h8, q, s, rstd8 = G(rows, d), G(rows, d, dtype=i8), G(rows, dtype=f32), G(rows, dtype=f32)
+    assert lib.dd_rmsnorm_int8_fwd(at(x), d, at(r), d, at(w), h8.p, q.p, d, s.p, rstd8.p, rows, d,
+                                   1e-5, st) == 0
+    need = lib.dd_rmsnorm_bwd_workspace_bytes(rows, d)
+    dx, dw, ws = G(rows, d), G(d), G(need, dtype=torch.uint8)
+    assert lib.dd_rmsnorm_bwd(h.p, at(w), rstd.p, at(dy), at(r), dx.p, dw.p, rows, d, ws.p, need,
+                              st) == 0
+    q2, s2, v = G(rows, d, dtype=i8), G(rows, dtype=f32), G(rows, d)
+    assert lib.dd_quantize(at(x), d, q2.p, d, s2.p, rows, d, st) == 0
+    assert lib.dd_dequantize(q2.p, d, s2.p, v.p, d, rows, d, st) == 0
+    torch.cuda.synchronize()
+    for i, g in enumerate((h, y, rstd, h8, q, s, rstd8, dx, dw, ws, q2, s2, v)):
+        assert g.intact(), i
+    assert torch.equal(h.t, h8.t) and torch.isfinite(dx.t.float()).all()
+
+
+@pytest.mark.parametrize("M,N,K", [(1, 1, 16), (33, 77, 48), (130, 257, 80), (2300, 2601, 144),
+                                   (9001, 6153, 912)])
+def test_products_stay_inside_their_buffers(cuda, M, N, K):
+    lib, st = _lib.lib(), ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+    q, s = random_codes(M, K, 1, cuda)
+    p, t = random_codes(N, K, 2, cuda)
+    c = Guarded((M, N), torch.bfloat16, cuda)
+    assert lib.dd_gemm_i8(at(q), K, at(s), at(p), K, at(t), None, c.p, N, M, N, K, st) == 0
+    torch.cuda.synchronize()
+    assert c.intact() and torch.isfinite(c.t.float()).all()
+
+
+@pytest.mark.parametrize("T,M,N,n", [(1, 8, 8, 1), (70, 136, 264, 2), (1300, 264, 136, 3),
+                                     (5000, 1096, 2704, 1), (20000, 136, 200, 1),
+                                     (9000, 1032, 2824, 1)])
+def test_weight_gradients_stay_inside_their_buffers(cuda, T, M, N, n):
+    lib, st = _lib.lib(), ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+    q, s = random_codes(T, M, 1, cuda)
+    dys = [bf16((T, N), 2 + i).to(cuda) for i in range(n)]
+    need = lib.dd_gemm_i8_wgrad_workspace_bytes(T, M, N, n)
+    dws = [Guarded((M, N), torch.bfloat16, cuda) for _ in range(n)]
+    ws = Guarded((need,), torch.uint8, cuda)
+    ptrs = lambda ps: (ctypes.c_void_p * n)(*ps)
+    assert lib.dd_gemm_i8_wgrad(at(q), M, at(s), ptrs([y.data_ptr() for y in dys]), N,
+                                ptrs([w.t.data_ptr() for w in dws]), N, n, T, M, N, ws.p, need,
+                                st) == 0
+    torch.cuda.synchronize()
+    assert ws.intact()
+    for w, y in zip(dws, dys):
+        assert w.intact() and torch.equal(w.t, ops.gemm_int8_wgrad_group(q, s, dys)[dws.index(w)])
