@@ -554,12 +554,16 @@ int launch_gemm_i8(const GemmI8Args &a)
     GemmI8Tile tile = gemm_i8_tile(a.M, a.N, a.K, device_cu_count());
     if (tile == GemmI8Tile::kLarge && a.ldc >= 1 << 23)  // its offsets in a tile of C
         tile = GemmI8Tile::kSmall;
+    // Weight rows per workgroup of few tokens; a dispatch holds fewer than 2^32
+    // work-items.
+    const bool two = a.N > 16 * 1024;
+    const int cols = two ? 32 : 16;
+    if (tile == GemmI8Tile::kFew && (a.N + cols - 1LL) / cols >= 1 << 23)
+        tile = GemmI8Tile::kSmall;
     if (tile == GemmI8Tile::kFew) {
         const int mb = (a.M + 15) / 16;
-        const bool two = a.N > 16 * 1024;
         auto run = [&](auto m) {
             constexpr int MB = decltype(m)::value;
-            const int cols = two ? 32 : 16;
             return launch_kernel(two ? gemm_i8_few_kernel<MB, 2> : gemm_i8_few_kernel<MB, 1>,
                                  dim3(static_cast<unsigned>((a.N + cols - 1) / cols)), dim3(512),
                                  st, op);

@@ -445,6 +445,16 @@ def test_products_past_32_bits(cuda, M, N):
     check_product(q[rows], s[rows], p, t, None, c[rows])
 
 
+def test_product_of_one_token_with_more_channels_than_a_grid_of_few_tokens_holds(cuda):
+    N = 32 * (1 << 23) + 40
+    p = torch.ones((N, 16), dtype=torch.int8, device=cuda)
+    p[-1], p[0] = 2, 3
+    q = torch.ones((1, 16), dtype=torch.int8, device=cuda)
+    one = torch.ones(1, device=cuda)
+    c = ops.gemm_int8(q, one, p, torch.ones(N, device=cuda))
+    assert c[0, 0] == 48 and c[0, -1] == 32 and bool((c[0, 1:-1] == 16).all())
+
+
 def test_empty_matrices(cuda):
     e = lambda *s, t=torch.bfloat16: torch.empty(s, dtype=t, device=cuda)
     y, h, rstd = ops.rms_norm(e(0, 64), e(64))
