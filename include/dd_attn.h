@@ -329,7 +329,7 @@ size_t dd_rmsnorm_bwd_workspace_bytes(int rows, int d);
  * dd_gemm_i8_wgrad: the weight gradients of n (1 to 3) layers y = x W that
  * share their input, kept as codes: dW[i] [M][N] = X^T dY[i] with X =
  * bf16(scales Q), Q [T][M] int8, dY[i] [T][N] bf16, fp32 sums in a fixed order.
- * 1 <= T <= 2^25 - 64, M and N multiples of 8; strides multiples of 8, ldq and
+ * 1 <= T <= 2^25 - 64, M and N multiples of 8, M at most 2^23 - 128; strides multiples of 8, ldq and
  * ldy below 2^23; Q 8-byte, dY[i] and dW[i] 16-byte aligned.  The dW[i] may be
  * column slices of one matrix, and must not overlap each other otherwise, nor
  * the inputs.  workspace: scratch of dd_gemm_i8_wgrad_workspace_bytes(T, M, N,

@@ -188,10 +188,11 @@ int dd_gemm_i8(const int8_t *A, long long lda, const float *sa, const int8_t *B,
 namespace {
 
 // T: the restored input's rows have to keep 32-bit offsets too (64 of them).
+// M: a grid over its parts of 128 in y, fewer than 2^16.
 bool wgrad_ok(int T, int M, int N, int n)
 {
     return n >= 1 && n <= 3 && T >= 1 && T <= (1 << 25) - 64 && M >= 8 && N >= 8 && M % 8 == 0 &&
-           N % 8 == 0 && n * tiles64(M, N) <= kMaxTiles;
+           M <= (1 << 23) - 128 && N % 8 == 0 && n * tiles64(M, N) <= kMaxTiles;
 }
 
 }  // namespace

@@ -145,6 +145,12 @@ def test_weight_gradient_refusals(lib):
         assert call(lib, "dd_gemm_i8_wgrad", g, **kw) == ALIAS, kw
 
 
+@pytest.mark.parametrize("M, ok", [((1 << 23) - 128, True), ((1 << 23) - 120, False),
+                                  ((1 << 23) - 8, False)])
+def test_weight_gradient_has_fewer_than_2_16_parts_of_its_rows(lib, M, ok):
+    assert (lib.dd_gemm_i8_wgrad_workspace_bytes(1, M, 8, 1) > 0) == ok
+
+
 def test_wrappers_refuse_what_is_not_on_a_gpu_or_of_another_type():
     x = torch.zeros(4, 32, dtype=torch.bfloat16)
     q, s = torch.zeros(4, 32, dtype=torch.int8), torch.zeros(4)
