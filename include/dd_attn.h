@@ -291,7 +291,8 @@ int dd_transpose(const void *X, long long ldx, void *Y, long long ldy, int rows,
  *                Y = H rstd w, w bf16 [d].  H and Y contiguous, eps finite
  *                and > 0.
  * dd_rmsnorm_int8_fwd  the same with the output as codes of the rows of
- *                H w and scales A rstd / 127.
+ *                H w and scales A rstd / 127.  (The sum of squares is fp32: a
+ *                row whose sum passes 3.4e38 has rstd 0 and gives zeros.)
  * dd_rmsnorm_bwd its backward (of either form; codes pass the gradient
  *                straight through) for the upstream gradient dY: dX is the
  *                gradient of X and of R alike, plus dRes (optional: the

@@ -455,6 +455,20 @@ def test_product_of_one_token_with_more_channels_than_a_grid_of_few_tokens_holds
     assert c[0, 0] == 48 and c[0, -1] == 32 and bool((c[0, 1:-1] == 16).all())
 
 
+@pytest.mark.parametrize("d", [8, 2048])
+def test_norm_of_a_row_whose_squares_overflow_fp32_is_zero(cuda, d):
+    x = torch.ones((3, d), dtype=torch.bfloat16, device=cuda)
+    x[1] = 2e19  # its square alone is 4e38, past fp32
+    w = torch.ones(d, dtype=torch.bfloat16, device=cuda)
+    y, h, rstd = ops.rms_norm(x, w)
+    assert rstd[1] == 0 and not y[1].any() and torch.equal(h, x)
+    assert bool((y[0] == 1).all()) and bool((y[2] == 1).all())
+    q, s, _, rstd = ops.rms_norm_int8(x, w)
+    assert rstd[1] == 0 and s[1] == 0 and not ops.dequantize(q, s)[1].any()
+    dx, dw = ops.rms_norm_backward(x, w, rstd, torch.ones_like(x))
+    assert not dx[1].any() and bool(dw.isfinite().all())
+
+
 def test_empty_matrices(cuda):
     e = lambda *s, t=torch.bfloat16: torch.empty(s, dtype=t, device=cuda)
     y, h, rstd = ops.rms_norm(e(0, 64), e(64))
