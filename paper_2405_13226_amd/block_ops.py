@@ -13,7 +13,8 @@ values are scales[r] * codes[r].  ``quantize`` forms them (the nearest codes
 to 127 x / max |x| of each row, ties to even) and so does ``rms_norm_int8``;
 ``gemm_int8`` multiplies two of them, ``gemm_int8_wgrad`` takes one as the
 kept input of a linear layer.  Their calls run on the tensors' device, on
-its current stream; matrices without rows give empty results.
+its current stream; matrices without rows give empty results.  Rows have at
+most 16384 elements (products: see there).
 """
 from __future__ import annotations
 

@@ -85,8 +85,9 @@ const char *dd_status_str(int status)
     case DD_OK: return "ok";
     case DD_ERR_NULL: return "a required pointer is NULL";
     case DD_ERR_SHAPE:
-        return "invalid shape: need B, L, H >= 1, B*L*H < 2^31, H*D < 2^23, "
-               "B*H*ceil(L/128) <= 2^23 - 8 and a RoPE base that is finite and > 0";
+        return "invalid shape: attention needs B, L, H >= 1, B*L*H < 2^31, H*D < 2^23, "
+               "B*H*ceil(L/128) <= 2^23 - 8 and a RoPE base that is finite and > 0; the other "
+               "calls' conditions are in dd_attn.h";
     case DD_ERR_HEADDIM: return "unsupported head dimension: D must be 64 or 128";
     case DD_ERR_DOCLENS: return "invalid cu_doclens / n_docs";
     case DD_ERR_WORKSPACE: return "backward workspace missing or too small";
