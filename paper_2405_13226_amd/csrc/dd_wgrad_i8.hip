@@ -9,8 +9,14 @@
 // Two launches, or three.  The first restores X, transposed: XT [M][T] in the
 // workspace, T padded with zeros to whole K steps.  The product then reads XT
 // along its rows and dY, as it is stored, transposed, with the loop of the
-// bf16 product (dd_gemm.hip).  With a split T axis, whose parts leave fp32
-// tiles in the workspace, a last launch adds those.
+// bf16 product (dd_gemm.hip).  Tiles that several workgroups share (WgradPlan)
+// leave fp32 parts in the workspace, which a last launch adds in a fixed order.
+//
+// 65,536 tokens, 2048 x 5632, us: restoring 69-78 (5.2-5.8 TB/s), product
+// 1056-1159 (1,300-1,430 TFLOP/s; pipes 81% busy at 1.64 GHz: power), sum 21-22;
+// in all 1193-1292, dd_gemm from bf16 activations 1187-1293.  Converting the codes
+// inside the product's loop would save the restoring, but costs its LDS, which
+// moves 256 KiB a step of 2,400 clocks, another 48 KiB.
 #include "dd_device.hpp"
 #include "dd_tile.hpp"
 #include "dd_gemm.hpp"
@@ -27,7 +33,7 @@ typedef uint32_t codes16 __attribute__((ext_vector_type(4), aligned(8)));
 
 // XT[m][t] = bf16(scales[t] Q[t][m]), zeros for T <= t < Tp.  One 128 x 128
 // tile per workgroup: rows of codes into LDS as bf16, then its transposing
-// reads, eight tokens of a column per lane.
+// reads, eight tokens of a column per lane.  Bound by HBM.
 __global__ void __launch_bounds__(256)
 restore_kernel(const int8_t *__restrict__ Q, long long ldq, const float *__restrict__ scales,
                uint16_t *__restrict__ XT, long long Tp, int T, int M)
@@ -209,7 +215,7 @@ __device__ __forceinline__ f32x4 mfma16w(bf16x8 a, bf16x8 b, f32x4 c)
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }
 
-// LDS image of the finished tile, as in dd_gemm_i8.hip.
+// Element offset of (row r, column c) in the LDS image of the finished tile.
 template <int BN>
 __device__ __forceinline__ int wgrad_off(int r, int c)
 {
