@@ -579,6 +579,63 @@ def test_graph_replay_matches_eager(cuda, T, d, n):
         torch.cuda.synchronize()
 
 
+def test_two_streams_at_once(cuda):
+    # Equal sizes, other values: what one call left where the other reads shows.
+    cases = [layer_inputs(2048, 1024, 2816, cuda), layer_inputs(2048, 1024, 2816, cuda)]
+    cases[1][0] = cases[1][0] * 3
+    ref = [[t.clone() for t in layer_step(*c)] for c in cases]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(cuda) for _ in cases]
+    out = [[], []]
+    for _ in range(4):
+        for i, st in enumerate(streams):
+            with torch.cuda.stream(st):
+                out[i].append(layer_step(*cases[i]))
+    torch.cuda.synchronize()
+    for i in range(2):
+        for step in out[i]:
+            for a, b in zip(step, ref[i]):
+                assert torch.equal(a, b), i
+
+
+def test_two_graphs_at_once(cuda):
+    cases = [layer_inputs(2048, 1024, 2816, cuda), layer_inputs(2048, 1024, 2816, cuda)]
+    cases[1][0] = cases[1][0] * 3
+    ref = [[t.clone() for t in layer_step(*c)] for c in cases]
+    torch.cuda.synchronize()
+    graphs, outs = [], []
+    streams = [torch.cuda.Stream(cuda) for _ in cases]
+    for c, st in zip(cases, streams):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=st):
+            outs.append(layer_step(*c))
+        graphs.append(g)
+    for rep in range(3):
+        for g, st in zip(graphs, streams):
+            with torch.cuda.stream(st):
+                g.replay()
+        torch.cuda.synchronize()
+        for i in range(2):
+            for a, b in zip(outs[i], ref[i]):
+                assert torch.equal(a, b), (rep, i)
+                a.zero_()
+        torch.cuda.synchronize()
+
+
+def test_the_same_tensor_twice(cuda):
+    q, s = ops.quantize(bf16((300, 512), 5).to(cuda))
+    assert torch.equal(ops.gemm_int8(q, s, q, s),
+                       ops.gemm_int8(q, s, q.clone(), s.clone()))
+    dy = bf16((300, 264), 6).to(cuda)
+    one = ops.gemm_int8_wgrad_group(q, s, [dy, dy.clone(), dy.clone()])
+    for a, b in zip(ops.gemm_int8_wgrad_group(q, s, [dy, dy, dy]), one):
+        assert torch.equal(a, b)
+    x = bf16((40, 512), 7).to(cuda)
+    w = torch.ones(512, dtype=torch.bfloat16, device=cuda)
+    for a, b in zip(ops.rms_norm(x, w, residual=x), ops.rms_norm(x, w, residual=x.clone())):
+        assert torch.equal(a, b)
+
+
 class Guarded:
     """A tensor of this shape inside a buffer with bands of a pattern around it."""
 
