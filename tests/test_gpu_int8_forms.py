@@ -1,0 +1,91 @@
+"""Forms of the 8-bit products and weight gradients that only some sizes take:
+each test names the form (int8_routes) and fails where its sizes no longer
+reach it.
+
+Tolerances as in test_gpu_int8_ops.py: the rounding of the result (2^-8) and
+T (weight gradient) or 4 (product) times 2^-24 of the magnitudes.  T 2^-24
+bounds any order of the sum and is wide for long ones, so each tile's sampled
+elements are also held to a relative L2 error of 3e-3: the rounding of the
+result is 1.7e-3 and the sum's own error, which walks at random, below 1e-4;
+a step left out of a few hundred would be 5e-2.
+"""
+import ctypes
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2405_13226_amd import _lib, block_ops as ops
+
+import int8_routes as routes
+from parity import log
+from test_gpu_int8_ops import B, U, Guarded, at, random_codes
+
+pytestmark = pytest.mark.gpu
+
+
+def gradient(T, N, seed, dev):
+    gen = torch.Generator(device=dev).manual_seed(seed)
+    return torch.randn((T, N), generator=gen, device=dev).to(torch.bfloat16)
+
+
+def check_gradient(q, s, dy, dw, edge):
+    """dw against float64 on the first, the last and two other rows of every
+    row of tiles, at every column."""
+    T, M = q.shape
+    rng = np.random.default_rng(T + M)
+    rows = np.unique(np.concatenate(
+        [np.r_[m, min(m + edge, M) - 1, rng.integers(m, min(m + edge, M), 2)]
+         for m in range(0, M, edge)]))
+    rows_d = torch.from_numpy(rows).to(q.device)
+    x = (q[:, rows_d].float() * s[:, None]).to(torch.bfloat16).double().t().contiguous()
+    ref, mag = x @ dy.double(), x.abs() @ dy.double().abs()
+    got = dw[rows_d].double()
+    assert bool(got.isfinite().all())
+    off = (got - ref).abs() - (B * ref.abs() + T * U * mag)
+    assert float(off.max()) <= 0, (float(off.max()), int((off > 0).sum()))
+    for m in range(0, M, edge):
+        mine = torch.from_numpy((rows >= m) & (rows < m + edge)).to(q.device)
+        for n in range(0, dy.shape[1], edge):
+            g, r = got[mine, n:n + edge], ref[mine, n:n + edge]
+            # a few numbers at a matrix's edge have no average rounding
+            if r.numel() >= 128:
+                assert float((g - r).norm() / r.norm()) <= 3e-3, (m, n)
+
+
+# The first steps of shared tiles by equal parts, the rest of all of them in
+# pieces that workgroups take one after the other.
+@pytest.mark.parametrize("T,M,N,n,edge,heads,whole", [
+    (4710, 2736, 5944, 1, 256, 1, True), (20012, 4272, 5832, 1, 256, 1, True),
+    (16384, 1024, 2816, 2, 256, 2, False), (11504, 320, 3592, 1, 128, 2, False)])
+def test_weight_gradients_with_the_rest_in_pieces(cuda, T, M, N, n, edge, heads, whole):
+    log(f"wgrad pieces T={T} M={M} N={N} n={n}")
+    form = routes.wgrad(T, M, N, n)
+    assert form["tails"] > 0 and form["rest"] > 0, form
+    assert (form["edge"], form["heads"], form["whole"] > 0) == (edge, heads, whole), form
+    q, s = random_codes(T, M, T + M, cuda)
+    dys = [gradient(T, N, N + i, cuda) for i in range(n)]
+    dw = torch.empty((M, n * N), dtype=torch.bfloat16, device=cuda)
+    columns = [dw[:, i * N:(i + 1) * N] for i in range(n)]
+    ops.gemm_int8_wgrad_group(q, s, dys, outs=columns)
+    for dy, c in zip(dys, columns):
+        check_gradient(q, s, dy, c, edge)
+    again = ops.gemm_int8_wgrad_group(q, s, dys)
+    for a, c in zip(again, columns):
+        assert torch.equal(a, c)
+
+
+def test_weight_gradient_in_pieces_stays_inside_its_buffers(cuda):
+    T, M, N = 11504, 320, 3592
+    assert routes.wgrad(T, M, N)["tails"] > 0
+    lib, st = _lib.lib(), ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+    q, s = random_codes(T, M, 1, cuda)
+    dy = gradient(T, N, 2, cuda)
+    need = lib.dd_gemm_i8_wgrad_workspace_bytes(T, M, N, 1)
+    dw, ws = Guarded((M, N), torch.bfloat16, cuda), Guarded((need,), torch.uint8, cuda)
+    ptrs = lambda t: (ctypes.c_void_p * 1)(t.data_ptr())
+    assert lib.dd_gemm_i8_wgrad(at(q), M, at(s), ptrs(dy), N, ptrs(dw.t), N, 1, T, M, N, ws.p,
+                                need, st) == 0
+    torch.cuda.synchronize()
+    assert ws.intact() and dw.intact()
+    assert torch.equal(dw.t, ops.gemm_int8_wgrad(q, s, dy))
