@@ -89,3 +89,24 @@ def test_weight_gradient_in_pieces_stays_inside_its_buffers(cuda):
     torch.cuda.synchronize()
     assert ws.intact() and dw.intact()
     assert torch.equal(dw.t, ops.gemm_int8_wgrad(q, s, dy))
+
+
+# T of at most 64 tokens in 256 x 256 tiles: one step, without the loop; then
+# two, which is the loop's start and end alone.
+@pytest.mark.parametrize("T,M,N,n,steps", [
+    (1, 3584, 1792, 1, 1), (45, 3584, 1792, 1, 1), (64, 2032, 2200, 1, 1), (1, 2032, 2200, 1, 1),
+    (50, 2048, 2048, 3, 1), (64, 1280, 1280, 3, 1), (65, 2032, 2200, 1, 2),
+    (100, 3584, 1792, 1, 2), (128, 2032, 2200, 1, 2)])
+def test_weight_gradients_of_one_and_two_steps_in_large_tiles(cuda, T, M, N, n, steps):
+    log(f"wgrad large tiles T={T} M={M} N={N} n={n}")
+    form = routes.wgrad(T, M, N, n)
+    assert form["edge"] == 256 and form["steps"] == steps, form
+    # what lies behind the last token is not read into the sums
+    q, s = random_codes(T + 40, M, T + M, cuda)
+    dys = [gradient(T + 40, N, N + i, cuda) for i in range(n)]
+    for dy in dys:
+        dy[T:] = float("nan")
+    s[T:] = float("inf")
+    q, s, dys = q[:T], s[:T], [dy[:T] for dy in dys]
+    for dy, dw in zip(dys, ops.gemm_int8_wgrad_group(q, s, dys)):
+        check_gradient(q, s, dy, dw, 256)
