@@ -110,3 +110,33 @@ def test_weight_gradients_of_one_and_two_steps_in_large_tiles(cuda, T, M, N, n, 
     q, s, dys = q[:T], s[:T], [dy[:T] for dy in dys]
     for dy, dw in zip(dys, ops.gemm_int8_wgrad_group(q, s, dys)):
         check_gradient(q, s, dy, dw, 256)
+
+
+def check_product(q, s, p, t, r, c):
+    """c against float64, every element (the sums of codes are exact in it)."""
+    ref = (q.double() @ p.double().t()) * torch.outer(s.double(), t.double())
+    mag = ref.abs()
+    if r is not None:
+        ref, mag = ref + r.double(), mag + r.double().abs()
+    off = (c.double() - ref).abs() - (B * ref.abs() + 4 * U * mag)
+    assert bool(c.isfinite().all()) and float(off.max()) <= 0, float(off.max())
+
+
+# Few tokens and more than 16,384 channels: 32 of them a workgroup, two blocks
+# of 16; one, two and four blocks of tokens.
+@pytest.mark.parametrize("residual", [False, True])
+@pytest.mark.parametrize("M,N,K", [
+    (M, N, K) for M in (1, 17, 33, 64) for N in (16385, 20001) for K in (16, 1040, 2048)
+    if (M, N, K) not in ((33, 20001, 2048), (64, 16385, 2048), (64, 20001, 1040),
+                         (64, 20001, 2048))])  # which go to tiles
+def test_few_tokens_with_many_channels(cuda, M, N, K, residual):
+    log(f"gemm_int8 few M={M} N={N} K={K} residual={residual}")
+    assert routes.product(M, N, K) == "few" and N > 16384
+    q, s = random_codes(M, K, M + K, cuda, full=True)
+    p, t = random_codes(N, K, N + K + 1, cuda, full=True)
+    r = gradient(M, N, 9, cuda) if residual else None
+    out = Guarded((M, N), torch.bfloat16, cuda)
+    ops.gemm_int8(q, s, p, t, residual=r, out=out.t)
+    torch.cuda.synchronize()
+    assert out.intact()
+    check_product(q, s, p, t, r, out.t)
