@@ -140,3 +140,26 @@ def test_few_tokens_with_many_channels(cuda, M, N, K, residual):
     torch.cuda.synchronize()
     assert out.intact()
     check_product(q, s, p, t, r, out.t)
+
+
+# The large tiles with the residual in the output itself, rows of any
+# alignment, whole and ragged tiles, several tiles a workgroup.
+@pytest.mark.parametrize("off", [0, 1, 8])
+@pytest.mark.parametrize("M,N,K", [(9000, 6152, 912), (16384, 12288, 144)])
+def test_large_tiles_add_to_their_output_in_place(cuda, M, N, K, off):
+    log(f"gemm_int8 in place M={M} N={N} K={K} off={off}")
+    assert routes.product(M, N, K) == "large"
+    q, s = random_codes(M, K, 1, cuda)
+    p, t = random_codes(N, K, 2, cuda)
+    r = gradient(M, N, 3, cuda)
+    want = ops.gemm_int8(q, s, p, t, residual=r)
+    wide = torch.full((M + 2, N + 24), 5.0, dtype=torch.bfloat16, device=cuda)
+    into = wide[1:-1, off:off + N]
+    into.copy_(r)
+    ops.gemm_int8(q, s, p, t, residual=into, out=into)
+    assert torch.equal(into, want)
+    keep = torch.ones_like(wide, dtype=torch.bool)
+    keep[1:-1, off:off + N] = False
+    assert bool((wide[keep] == 5.0).all())
+    check_product(q[:512], s[:512], p, t, r[:512], into[:512])
+    check_product(q[-300:], s[-300:], p, t, r[-300:], into[-300:])
