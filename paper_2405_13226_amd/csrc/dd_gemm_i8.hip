@@ -146,7 +146,8 @@ struct I8Walk {
     __device__ __forceinline__ void places(const GemmI8Operands &op, int from, int lane)
     {
         base = from;
-        tile_of(static_cast<int>(blockIdx.x) + (from + lane) * static_cast<int>(gridDim.x),
+        tile_of(walk_tile(static_cast<int>(blockIdx.x), from + lane, static_cast<int>(gridDim.x),
+                          op.tiles_m * op.tiles_n),
                 op.tiles_m, op.tiles_n, op.xm, tm, tn);
     }
     __device__ __forceinline__ void start(const GemmI8Operands &op, int wave, int lane,

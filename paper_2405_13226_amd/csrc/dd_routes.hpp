@@ -207,6 +207,14 @@ inline GemmI8Tile gemm_i8_tile(int M, int N, int K, int cus)
     return small < large ? GemmI8Tile::kSmall : GemmI8Tile::kLarge;
 }
 
+// Tile `i` of workgroup `wg`'s walk through `tiles` tiles: wg, wg + grid, ...  Behind
+// the last one it is the last one: a place formed from an id that no tile has
+// (tile_of) would be a division by zero.
+constexpr int walk_tile(int wg, int i, int grid, int tiles)
+{
+    return std::min(wg + i * grid, tiles - 1);
+}
+
 // How `n` weight gradients of M x N over T tokens run: on tiles of 256 x 256 or
 // 128 x 128 (`edge`; tiles_n of all n), T in `steps` of 64 tokens.  The first
 // `whole` tiles are a workgroup's each.  The others, fewer than the CUs, are

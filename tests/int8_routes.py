@@ -19,6 +19,7 @@ void wgrad(int T, int M, int N, int n, int cus, int *out) {
     out[4] = p.head; out[5] = p.tails; out[6] = p.most(); out[7] = p.tiles_m * p.tiles_n;
     out[8] = p.heads; out[9] = p.rest();
 }
+int walk(int wg, int i, int grid, int tiles) { return dd::walk_tile(wg, i, grid, tiles); }
 }
 """
 
@@ -45,3 +46,8 @@ def wgrad(T, M, N, n=1):
     _lib().wgrad(T, M, N, n, CUS, out)
     return dict(zip(("edge", "whole", "shared", "steps", "head", "tails", "most", "tiles",
                      "heads", "rest"), out))
+
+
+def walk(wg, i, grid, tiles):
+    """Tile i of a workgroup's walk, as the lanes that hold its place see it."""
+    return _lib().walk(wg, i, grid, tiles)
