@@ -62,7 +62,7 @@ class _BlockFunction(torch.autograd.Function):
         u1, u3, g = ops.gemm_swiglu(m, w_1, w_3)
         y = ops.gemm(g, w_2, residual=h)
         kept = (a, m, u1, u3, g)
-        if bits == 8:
+        if bits == 8 and any(ctx.needs_input_grad):
             kept = [t for act in kept for t in ops.quantize(act)]
         ctx.save_for_backward(x, ln1_w, w_qkv, w_o, ln2_w, w_1, w_3, w_2, mean1, rstd1, qr, kr, v,
                               o, lse, h, mean2, rstd2, *kept)
@@ -144,10 +144,12 @@ class OpenLMBlock(torch.nn.Module):
     def forward(self, x, cu_doclens=None, doc_positions: bool = False):
         B, L, d = x.shape
         docs = _doclens(cu_doclens, B, L, x.device)
+        # without a backward nothing is kept, so no codes are formed
+        bits = self.checkpoint_bits if torch.is_grad_enabled() else 16
         y = _BlockFunction.apply(x.reshape(B * L, d), self.ln1_w, self.ln1_b, self.w_qkv,
                                  self.w_o, self.ln2_w, self.ln2_b, self.w_1, self.w_3, self.w_2,
                                  (B, L, self.H, self.D), self.rope_base, docs, doc_positions,
-                                 self.checkpoint_bits)
+                                 bits)
         return y.view(B, L, d)
 
     def gemm_flops(self, tokens: int) -> int:

@@ -119,3 +119,25 @@ def test_block_in_a_captured_graph(cuda):
             assert torch.equal(a, b), (rep, i)
         torch.randn(1 << 20, device=cuda).sum()
         torch.cuda.synchronize()
+
+
+def test_8_bit_checkpoints_form_no_codes_without_a_backward(cuda, monkeypatch):
+    from paper_2405_13226_amd import layer
+    made = []
+    quantize = layer.ops.quantize
+    monkeypatch.setattr(layer.ops, "quantize", lambda t: (made.append(t.shape), quantize(t))[1])
+    blk = blocks(512, 4, 768, cuda)[1]
+    x = to_dev(synth.normal_bf16((2, 256, 512), 1, 21), cuda)
+    y = blk(x)
+    assert len(made) == 5
+    made.clear()
+    with torch.no_grad():
+        assert torch.equal(blk(x), y)
+    with torch.inference_mode():
+        assert torch.equal(blk(x), y)
+    blk.requires_grad_(False)
+    assert torch.equal(blk(x), y)
+    assert not made, made
+    # a gradient of the input alone still needs them
+    blk(x.clone().requires_grad_(True)).sum().backward()
+    assert len(made) == 5
