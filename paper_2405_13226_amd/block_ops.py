@@ -27,6 +27,7 @@ from ._lib import check, lib
 from .attention import _ptr as _p, _stream
 
 LN_EPS = 1e-5
+MAX_ROW = 16384  # elements of a row that RMSNorm takes or that is held as codes
 
 
 def _mat(t, name):

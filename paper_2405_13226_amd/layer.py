@@ -117,6 +117,9 @@ class OpenLMBlock(torch.nn.Module):
             raise ValueError("d must be a multiple of H")
         if checkpoint_bits not in (8, 16):
             raise ValueError(f"checkpoint_bits must be 8 or 16 (got {checkpoint_bits})")
+        if checkpoint_bits == 8 and hidden > ops.MAX_ROW:
+            raise ValueError(f"checkpoint_bits=8 takes a width of at most {ops.MAX_ROW} "
+                             f"(got {hidden})")
         self.checkpoint_bits = checkpoint_bits
         self.d, self.H, self.D, self.hidden = d, H, d // H, hidden
         self.rope_base = rope_base

@@ -248,3 +248,11 @@ def test_walks_of_large_tiles_hold_no_tile_behind_the_last(tiles):
         for i in range(n, n + 64):
             assert 0 <= routes.walk(wg, i, grid, tiles) < tiles, (wg, i)
     assert sorted(seen) == list(range(tiles))
+
+
+def test_block_refuses_a_width_without_codes():
+    from paper_2405_13226_amd.layer import OpenLMBlock
+    with pytest.raises(ValueError, match="16384"):
+        OpenLMBlock(512, 8, 16640, device="meta", checkpoint_bits=8)
+    assert OpenLMBlock(512, 8, 16384, device="meta", checkpoint_bits=8).hidden == 16384
+    assert OpenLMBlock(512, 8, 16640, device="meta").hidden == 16640
