@@ -270,7 +270,8 @@ def _dims(t, name, dtype, dev=None):
     if isinstance(t, torch.Tensor) and t.dtype is dtype and t.dim() == 2:
         (rows, cols), (ld, one) = t.shape, t.stride()
         where = t.device
-        if one == 1 and (where == dev if dev is not None else where.type == "cuda"):
+        if (one == 1 and not (rows | cols) >> 31  # int in the C ABI
+                and (where == dev if dev is not None else where.type == "cuda")):
             return rows, cols, ld if rows > 1 else cols
     if not isinstance(t, torch.Tensor) or t.dim() != 2:
         raise ValueError(f"{name} must be a 2-D tensor")
@@ -279,6 +280,8 @@ def _dims(t, name, dtype, dev=None):
         raise ValueError(f"{name} must be a {kind} GPU tensor")
     if t.stride(1) != 1:
         raise ValueError(f"{name} must have unit column stride")
+    if max(t.shape) >> 31:
+        raise ValueError(f"{name} has 2^31 rows or columns or more: {tuple(t.shape)}")
     raise ValueError(f"{name} is on {t.device}, not on {dev}")
 
 

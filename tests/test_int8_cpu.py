@@ -256,3 +256,18 @@ def test_block_refuses_a_width_without_codes():
         OpenLMBlock(512, 8, 16640, device="meta", checkpoint_bits=8)
     assert OpenLMBlock(512, 8, 16384, device="meta", checkpoint_bits=8).hidden == 16384
     assert OpenLMBlock(512, 8, 16640, device="meta").hidden == 16640
+
+
+@pytest.mark.parametrize("rows,cols", [((1 << 32) + 8, 1), (1 << 31, 1), (1, 1 << 31),
+                                       (2, (1 << 32) + 16)])
+def test_wrappers_refuse_sizes_past_31_bits(rows, cols):
+    # (they would reach the C ABI without their upper bits)
+    from torch._subclasses.fake_tensor import FakeTensorMode
+    with FakeTensorMode():
+        x = torch.empty((rows, cols), dtype=torch.bfloat16, device="cuda:0")
+        q = torch.empty((rows, cols), dtype=torch.int8, device="cuda:0")
+        for t, dtype in ((x, torch.bfloat16), (q, torch.int8)):
+            with pytest.raises(ValueError, match="2\\^31"):
+                ops._dims(t, "x", dtype)
+        ok = torch.empty(((1 << 31) - 1, 1), dtype=torch.bfloat16, device="cuda:0")
+        assert ops._dims(ok, "x", torch.bfloat16) == ((1 << 31) - 1, 1, 1)
