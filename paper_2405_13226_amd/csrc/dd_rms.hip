@@ -8,7 +8,8 @@
 //            q = the integer nearest to 127 z / A (ties to even) and one fp32
 //            scale; the row's values are scale q.
 // For the norm's codes z = h w: rstd cancels out of the codes, so they need no
-// sum over the row, and h w is exact in fp32 (two 8-bit significands).  The
+// sum over the row, and h w is exact in fp32 (two 8-bit significands) unless it
+// leaves fp32's range: rows with A outside 2^-60 .. 2^60 take it in fp64.  The
 // scale is A rstd / 127.
 //
 // Backward, with xh = h rstd and g = dy w:
@@ -207,10 +208,77 @@ struct RowOperands {
     float eps;
 };
 
+// Element i of h w in fp64, which holds every product of two bf16 numbers: 16
+// significant bits, so that the high word alone tells a magnitude.
+__device__ __forceinline__ double product_at(const RowOperands &op, long long row, int i)
+{
+    auto at = [](const uint16_t *p) { return __uint_as_float(static_cast<uint32_t>(*p) << 16); };
+    float h = at(op.X + row * op.ldx + i);
+    if (op.R != nullptr)
+        h = static_cast<float>(static_cast<__bf16>(h + at(op.R + row * op.ldr + i)));
+    return static_cast<double>(h) * at(op.W + i);
+}
+
+// The codes and the scale of a row of the norm whose largest magnitude A by its
+// fp32 products is 0, below 2^-60, above 2^60 or not finite.  Zeros are looked up
+// as such; else A and the codes come from products in fp64, an element at a time:
+// the integer nearest to a quotient of two numbers of at most 23 bits, which fp64
+// does not round onto a border.  (In the other rows a product that has lost bits,
+// below 2^-126, has code 0 either way.)  65,536 rows of 2048: zeros 133 us,
+// extreme values 544, ordinary rows 167.
+template <int TPR>
+__device__ __forceinline__ void extreme_row(const RowOperands &op, long long row, float rstd,
+                                            int t, float *red, int &flip)
+{
+    // Nothing is shared with the ordinary rows' way, whose registers it would take.
+    asm volatile("" : "+v"(t), "+v"(row));
+    const int d = op.d;
+    int8_t *q = op.Q + row * op.ldq;
+    float none = 0.f;
+    uint32_t m = 0;
+    if (d >= 8) {
+#pragma unroll 1
+        for (int i = 8 * t; i < d; i += 8 * TPR) {
+            const int col = min(i, d - 8);
+            u32x4 u = *reinterpret_cast<const piece16 *>(op.X + row * op.ldx + col);
+            if (op.R != nullptr)
+                u |= *reinterpret_cast<const piece16 *>(op.R + row * op.ldr + col);
+            m |= (u[0] | u[1] | u[2] | u[3]) & 0x7fff7fffu;
+        }
+        flip ^= 1;
+        row_reduce<TPR>(none, m, red, flip);
+        if (m == 0) {
+            for (int i = 8 * t; i < d; i += 8 * TPR)
+                *reinterpret_cast<codes8 *>(q + min(i, d - 8)) = u32x2{0u, 0u};
+            if (t == 0)
+                op.scales[row] = 0.0f;
+            return;
+        }
+        m = 0;
+    }
+#pragma unroll 1
+    for (int i = t; i < d; i += TPR)
+        m = max(m, static_cast<uint32_t>(__double2hiint(product_at(op, row, i))) & 0x7fffffffu);
+    flip ^= 1;
+    row_reduce<TPR>(none, m, red, flip);
+    const bool values = m != 0 && m < 0x7ff00000u;
+    const double amax = __hiloint2double(static_cast<int>(m), 0);
+    if (t == 0)
+        op.scales[row] = values   ? static_cast<float>(amax * rstd / 127.0)
+                         : m == 0 ? 0.0f
+                                  : __uint_as_float(0x7fc00000u);
+#pragma unroll 1
+    for (int i = t; i < d; i += TPR)
+        q[i] = values ? static_cast<int8_t>(__double2int_rn(127.0 * product_at(op, row, i) / amax))
+                      : 0;
+}
+
 // Six waves per SIMD for a wave's rows: the norm's codes of rows of 2048 take
 // 172 us a 65,536-token step instead of 185 with four (its registers else).
+// Eight for rows of 1024 threads: two workgroups per CU (8192 x 16,384, codes,
+// 165 us; with one 196).
 template <int TPR, int CH, bool WHOLE, int KIND>
-__global__ void __launch_bounds__(RowThreads<TPR>::THREADS, TPR <= 64 ? 6 : 1)
+__global__ void __launch_bounds__(RowThreads<TPR>::THREADS, TPR <= 64 ? 6 : TPR == 1024 ? 8 : 1)
 row_kernel(RowOperands op)
 {
     using T = RowThreads<TPR>;
@@ -274,10 +342,16 @@ row_kernel(RowOperands op)
                 store8<WHOLE>(op.Y + row * d + col, d - col, y);
             }
         } else {
+            if constexpr (KIND == kNormCodes) {
+                if (m < __float_as_uint(0x1p-60f) || m > __float_as_uint(0x1p60f)) {
+                    extreme_row<TPR>(op, row, rstd, t, red, flip);
+                    continue;
+                }
+            }
             const CodeScale cs(m);
             if (t == 0)
                 op.scales[row] =
-                    KIND == kNormCodes && cs.keep ? __uint_as_float(m) * rstd / 127.0f : cs.scale;
+                    KIND == kNormCodes ? __uint_as_float(m) * rstd / 127.0f : cs.scale;
             if (cs.fit != 1.0f) {
 #pragma unroll
                 for (int c = 0; c < CH; ++c)

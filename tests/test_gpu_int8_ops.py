@@ -709,3 +709,64 @@ def test_weight_gradients_stay_inside_their_buffers(cuda, T, M, N, n):
     assert ws.intact()
     for w, y in zip(dws, dys):
         assert w.intact() and torch.equal(w.t, ops.gemm_int8_wgrad_group(q, s, dys)[dws.index(w)])
+
+
+def extreme_rows(d, seed):
+    """Rows of every magnitude that bf16 has, one of zeros, two not finite."""
+    x = torch.stack([bf16((d,), seed + i).double() * 2.0 ** e
+                     for i, e in enumerate((-128, -100, -62, -30, 0, 30, 60, 100, 125))])
+    x = x.clamp(-3e38, 3e38).to(torch.bfloat16)
+    bad = torch.stack([x[4].clone(), x[0].clone(), torch.zeros_like(x[0])])
+    bad[0, d // 2], bad[1, d - 1] = float("nan"), float("inf")
+    return torch.cat([x, bad])
+
+
+@pytest.mark.parametrize("weight", [-126, -70, 0, 65, 120, "mixed"])
+@pytest.mark.parametrize("residual", [False, True])
+@pytest.mark.parametrize("d", [7, 250, 1416, 2056, 8200])
+def test_norm_codes_whose_products_leave_fp32(cuda, d, residual, weight):
+    # h w passes 3.4e38 or loses bits below 2^-126: its codes are the nearest
+    # ones all the same, and its scale has rstd's magnitude back
+    x = extreme_rows(d, d)
+    r = extreme_rows(d, d + 50) if residual else None
+    w = bf16((d,), 3).double()
+    w = w * (2.0 ** torch.linspace(-120, 120, d).double() if weight == "mixed" else 2.0 ** weight)
+    w = w.clamp(-3e38, 3e38).to(torch.bfloat16)
+    h = x if r is None else O.add(x, r)
+    q, s, hg, rstd = ops.rms_norm_int8(x.to(cuda), w.to(cuda),
+                                       residual=None if r is None else r.to(cuda), eps=EPS)
+    bad = ~torch.isfinite(h.float()).all(1).numpy()
+    assert bad.sum() >= 2
+    q, s, rstd = q.cpu().numpy(), s.double().cpu().numpy(), rstd.double().cpu().numpy()
+    want, top = O.codes(f64(h) * f64(w))
+    assert np.isnan(s[bad]).all() and not q[bad].any()
+    good = ~bad
+    ref = O.rstd(f64(h)[good], EPS)
+    over = (f64(h)[good] ** 2).sum(1) > 3.4e38  # documented: such rows give zeros
+    assert over.any() and (s[good][over] == 0).all() and (rstd[good][over] == 0).all()
+    assert np.array_equal(q[good], want[good])
+    scale = np.where(over, 0, top[good] * ref / 127)
+    assert (scale < 3.4e38).all()
+    # 2^-150: half a step of an fp32 scale below 2^-126
+    assert (np.abs(s[good] - scale) <= 36 * U * scale + 2.0 ** -150).all()
+
+
+def test_norm_codes_of_extreme_rows_among_others_of_a_workgroup(cuda):
+    # more rows than the grid has workgroups: a workgroup's second row reuses
+    # what its first one reduced through
+    rows, d, grid = (1 << 20) + 512, 2056, 1 << 20
+    x = torch.ones((rows, d), dtype=torch.bfloat16, device=cuda)
+    block = bf16((512, d), 1).to(cuda)
+    x[:512], x[grid:] = block, block.flip(0)
+    w = (1 + 0.1 * bf16((d,), 2).float()).to(torch.bfloat16).to(cuda)
+    x[0:512:3] *= 2.0 ** -100
+    x[1:512:3] = 0
+    x[grid + 1::2] *= 2.0 ** -110
+    q, s, _, rstd = ops.rms_norm_int8(x, w)
+    for part in (slice(0, 512), slice(grid, rows)):
+        for a, b in zip(ops.rms_norm_int8(x[part].contiguous(), w), (q[part], s[part], x[part],
+                                                                     rstd[part])):
+            assert torch.equal(a, b)
+        want, _ = O.codes(f64(x[part]) * f64(w))
+        assert np.array_equal(q[part].cpu().numpy(), want)
+    assert torch.equal(s[512:grid].min(), s[512:grid].max())
