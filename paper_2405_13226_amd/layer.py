@@ -52,18 +52,30 @@ class _BlockFunction(torch.autograd.Function):
                 docs, doc_pos, bits):
         B, L, H, D = shape
         d = H * D
+        codes = bits == 8 and any(ctx.needs_input_grad)
+        kept = []
+
+        def keep(act):  # the last use of an activation: its codes take its place
+            kept.extend(ops.quantize(act) if codes else (act,))
+
         a, mean1, rstd1 = ops.layer_norm(x, ln1_w, ln1_b, LN_EPS)
         q, k, v = ops.gemm_group(a, [w_qkv[:, i * d:(i + 1) * d] for i in range(3)])
+        keep(a)
+        del a
         o, lse, qr, kr = forward_rope(q.view(B, L, H, D), k.view(B, L, H, D),
                                       v.view(B, L, H, D), base, True, docs, doc_pos)
         o2 = o.view(B * L, d)
         h = ops.gemm(o2, w_o, residual=x)
         m, mean2, rstd2 = ops.layer_norm(h, ln2_w, ln2_b, LN_EPS)
         u1, u3, g = ops.gemm_swiglu(m, w_1, w_3)
+        keep(m)
+        del m
+        keep(u1)
+        del u1
+        keep(u3)
+        del u3
         y = ops.gemm(g, w_2, residual=h)
-        kept = (a, m, u1, u3, g)
-        if bits == 8 and any(ctx.needs_input_grad):
-            kept = [t for act in kept for t in ops.quantize(act)]
+        keep(g)
         ctx.save_for_backward(x, ln1_w, w_qkv, w_o, ln2_w, w_1, w_3, w_2, mean1, rstd1, qr, kr, v,
                               o, lse, h, mean2, rstd2, *kept)
         ctx.cfg = (shape, base, docs, doc_pos, bits)
@@ -78,7 +90,6 @@ class _BlockFunction(torch.autograd.Function):
         dy = dy.contiguous()
         if bits == 8:
             a, m, u1, u3, g = zip(kept[::2], kept[1::2])
-            u1, u3 = ops.dequantize(*u1), ops.dequantize(*u3)
 
             def weight_grads(act, dys, outs=None):
                 return ops.gemm_int8_wgrad_group(*act, dys, outs=outs)
@@ -87,11 +98,16 @@ class _BlockFunction(torch.autograd.Function):
 
             def weight_grads(act, dys, outs=None):
                 return ops.gemm_group(act, dys, trans_a=True, outs=outs)
-        # MLP: y = h + swiglu(m W1, m W3) W2
-        du1, du3 = ops.gemm_swiglu_backward(dy, w_2, u1, u3)
+        # MLP: y = h + swiglu(m W1, m W3) W2 (each restored activation only as
+        # long as it is read: the weight gradients hold one too)
         dw_2, = weight_grads(g, [dy])
+        if bits == 8:
+            u1, u3 = ops.dequantize(*u1), ops.dequantize(*u3)
+        du1, du3 = ops.gemm_swiglu_backward(dy, w_2, u1, u3)
+        del u1, u3
         dm = ops.gemm_sum([du1, du3], [w_1, w_3], trans_b=True)
         dw_1, dw_3 = weight_grads(m, [du1, du3])
+        del du1, du3
         dh, dln2_w, dln2_b = ops.layer_norm_backward(h, ln2_w, mean2, rstd2, dm, dres=dy)
         # attention: h = x + attn(RoPE(q), RoPE(k), v) Wo
         do = ops.gemm(dh, w_o, trans_b=True)

@@ -141,3 +141,33 @@ def test_8_bit_checkpoints_form_no_codes_without_a_backward(cuda, monkeypatch):
     # a gradient of the input alone still needs them
     blk(x.clone().requires_grad_(True)).sum().backward()
     assert len(made) == 5
+
+
+def test_8_bit_checkpoints_need_less_memory_at_their_peak(cuda):
+    # not only between the passes: in the forward an activation and its codes
+    # exist together only while they are formed, in the backward a restored one
+    # as long as it is read
+    B, L, d, H, hidden = 4, 1024, 1024, 16, 2816
+    x = to_dev(synth.normal_bf16((B, L, d), 1, 21), cuda).requires_grad_(True)
+    dy = to_dev(synth.normal_bf16((B, L, d), 1, 22), cuda)
+    peaks = {}
+    for blk in blocks(d, H, hidden, cuda):
+        for again in range(2):  # the first pass also fills the allocator's cache
+            blk.zero_grad(set_to_none=True)
+            x.grad = None
+            torch.cuda.synchronize()
+            base = torch.cuda.memory_allocated()
+            torch.cuda.reset_peak_memory_stats()
+            y = blk(x)
+            forward = torch.cuda.max_memory_allocated() - base
+            held = torch.cuda.memory_allocated() - base
+            torch.cuda.reset_peak_memory_stats()
+            y.backward(dy)
+            peaks[blk.checkpoint_bits] = (forward, held, torch.cuda.max_memory_allocated() - base)
+            del y
+    log(f"forward, held, backward: {peaks}, a token's: "
+        f"{ {b: [n // (B * L) for n in p] for b, p in peaks.items()} }")
+    # (u1, u3 and g are formed by one launch: their bf16 values and the codes of
+    # the two activations before them are the forward's peak)
+    for short, full in zip(peaks[8], peaks[16]):
+        assert short < full, peaks
