@@ -171,3 +171,23 @@ def test_8_bit_checkpoints_need_less_memory_at_their_peak(cuda):
     # the two activations before them are the forward's peak)
     for short, full in zip(peaks[8], peaks[16]):
         assert short < full, peaks
+
+
+def test_1b_block_with_8_bit_checkpoints(cuda):
+    # d = 2048, hidden 5632: the gated value's largest of 5632 is up to 14
+    # deviations, a code's error then 3.2% of one (14 / 127 / sqrt(12)); with
+    # the bf16 block's 2e-2 in squares 3.8e-2
+    B, L, d, H, hidden = 1, 512, 2048, 16, 5632
+    log(f"8-bit checkpoints B={B} L={L} d={d} hidden={hidden}")
+    full, short = blocks(d, H, hidden, cuda)
+    x0 = to_dev(synth.normal_bf16((B, L, d), 1, 21), cuda)
+    dy = to_dev(synth.normal_bf16((B, L, d), 1, 22), cuda)
+    w = {n: to_f64(p.detach()) for n, p in short.weights().items()}
+    _, ref = OL.block_fwd_bwd(to_f64(x0), w, to_f64(dy), H, 10000.0, None, False)
+    y16, g16 = step(full, x0, dy)
+    y8, g8 = step(short, x0, dy)
+    assert torch.equal(y8, y16)
+    for g in (g8, g16):
+        err = {n: rel_l2(to_f64(g[n]), ref[n]) for n in g}
+        log("  " + "  ".join(f"{n}={v:.3g}" for n, v in err.items()))
+        assert max(err.values()) <= RTOL, err
