@@ -291,8 +291,9 @@ int dd_transpose(const void *X, long long ldx, void *Y, long long ldy, int rows,
  *                Y = H rstd w, w bf16 [d].  H and Y contiguous, eps finite
  *                and > 0.
  * dd_rmsnorm_int8_fwd  the same with the output as codes of the rows of
- *                H w and scales A rstd / 127.  (The sum of squares is fp32: a
- *                row whose sum passes 3.4e38 has rstd 0 and gives zeros.)
+ *                H w, of any magnitude, and scales A rstd / 127.  (The sum of
+ *                squares is fp32: a row whose sum passes 3.4e38 has rstd 0 and
+ *                gives zeros.)
  * dd_rmsnorm_bwd its backward (of either form; codes pass the gradient
  *                straight through) for the upstream gradient dY: dX is the
  *                gradient of X and of R alike, plus dRes (optional: the
@@ -321,7 +322,8 @@ size_t dd_rmsnorm_bwd_workspace_bytes(int rows, int d);
  * dd_gemm_i8: C[m, n] = bf16(sa[m] sb[n] sum_k A[m, k] B[n, k] (+ R[m, n])),
  * A [M][K] and B [N][K] int8 with row strides lda and ldb, an fp32 scale per
  * row of each (per token, per output channel); the sum is exact in int32, the
- * rest fp32 with one rounding.  R: NULL, or a bf16 [M][N] matrix of row
+ * rest fp32 with one rounding: sum x sa[m] first, which has to stay finite
+ * (sa below 1.5e29 always does).  R: NULL, or a bf16 [M][N] matrix of row
  * stride ldc, which may be C itself.  Any M and N >= 1 (together at most
  * 2^23 - 1 tiles of 64 x 64), K a multiple of 16 below 2^17; lda and ldb
  * multiples of 16 below 2^23, A and B 16-byte aligned.  C must not overlap

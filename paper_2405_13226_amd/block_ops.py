@@ -402,7 +402,8 @@ def gemm_int8(a, a_scales, b, b_scales, residual=None, out=None):
     as ``quantize(W.T.contiguous())``), K a multiple of 16 below 2^17.
 
     The sums are exact, scaled in fp32 and rounded once.  ``out`` (optional)
-    receives the result and may be ``residual`` itself."""
+    receives the result and may be ``residual`` itself.  (``quantize`` forms
+    codes of K up to 16384; longer rows are a caller's own.)"""
     M, K, lda = _dims(a, "a", torch.int8)
     dev = a.device
     N, Kb, ldb = _dims(b, "b", torch.int8, dev)

@@ -122,9 +122,10 @@ struct I8Loads {
 // its start and end weigh twice as much: a workgroup walks tiles blockIdx.x,
 // blockIdx.x + gridDim.x, ... as one sequence of steps, the loads running ahead
 // across tiles, and the accumulators go to memory straight from registers.
-// 65,536 x 5632 over 2048: 638-709 us back to back (2,130-2,370 TOPS; a process's
-// first calls are the slow ones), 601-620 between other work; 8192^3 373-386
-// (2,850-2,950).
+// 65,536 x 5632 over 2048: 601-625 us (2,420-2,515 TOPS), in a process's first
+// calls up to 709; 8192^3 373-386 (2,850-2,950).  With a residual 65,536 x 2048
+// over 2048 292-389 and 30,000 x 5000 over 1008, whose rows of 10,000 bytes end
+// inside a tile, 275-328 (by the profiler, 50 calls).
 // The matrix pipes are busy 61% of the time at 2.0 GHz; without the stores 620 us
 // where the whole took 667.
 struct I8Walk {

@@ -15,9 +15,10 @@
 // Backward, with xh = h rstd and g = dy w:
 //            dx = rstd (g - xh mean(g xh)) (+ dres),  dw = sum over rows dy xh.
 //
-// 65,536 x 2048, us (TB/s; a plain copy's rate is 4.8): norm with a residual
-// 186-190 (5.7), with codes 171-174 (5.5), backward 215-217 (5.0), quantizing 74
-// (5.4), dequantizing 70 (5.8).  One row of 2048: 2.6, 3.5 with codes.
+// 65,536 x 2048, us (TB/s; a plain copy's rate is 4.8): norm with a residual 188
+// (5.7), with codes 167-172 (5.6), backward 215-217 (5.0), quantizing 75 call after
+// call (5.4) and 65 after other kernels (6.2), dequantizing 70 (5.8).  One row of
+// 2048: 2.3, 2.8 with codes.
 #include "dd_device.hpp"
 #include "dd_internal.h"
 #include "dd_launch.hpp"

@@ -12,11 +12,15 @@
 // bf16 product (dd_gemm.hip).  Tiles that several workgroups share (WgradPlan)
 // leave fp32 parts in the workspace, which a last launch adds in a fixed order.
 //
-// 65,536 tokens, 2048 x 5632, us: restoring 69-78 (5.2-5.8 TB/s), product
-// 1056-1159 (1,300-1,430 TFLOP/s; pipes 81% busy at 1.64 GHz: power), sum 21-22;
-// in all 1193-1292, dd_gemm from bf16 activations 1187-1293.  Converting the codes
-// inside the product's loop would save the restoring, but costs its LDS, which
-// moves 256 KiB a step of 2,400 clocks, another 48 KiB.
+// 65,536 tokens, 2048 x 5632, us: a call 1183 (1,278 TFLOP/s; median, in turn with
+// dd_gemm from bf16 activations, 1256; forming the codes, 75, is not in it).  Its
+// kernels under the profiler, mean and least of 50: restoring 76 and 70 (5.8 TB/s),
+// product 1151 and 1070, sum 22 and 21.  Power bounds the product: pipes 81-84%
+// busy at 1.4-1.65 GHz.  What its uneven tiles cost beside that: 256 whole ones
+// (2048 x 8192) keep the pipes 90% busy and read 3.2 GB from behind L2, these 176
+// with their pieces 6.5-6.8.  Converting the codes inside the loop, which would save
+// the restoring, has not been built: counted, it moves 48 KiB more through an LDS
+// that moves 256 a step of 2,400 clocks.
 #include "dd_device.hpp"
 #include "dd_tile.hpp"
 #include "dd_gemm.hpp"

@@ -24,7 +24,9 @@ token budget.
 With ``checkpoint_bits=8`` the block keeps five of its activations between
 forward and backward as int8 codes with a scale per token instead of bf16: the
 outputs of the norms, the two gate products and the gated value (of the 1B
-block's 66.6 KB a token 45.6 are left).  The forward is the same; the backward
+block's 66.6 KB a token 45.6 are left; with what the passes themselves need,
+91 of 101 at the peak).  A step of 65,536 tokens takes 4 to 7% longer for it.
+Without a backward no codes are formed.  The forward is the same; the backward
 forms the weight gradients from the codes and the gate's gradient from the
 restored values, so gradients carry the codes' rounding, at most half a step
 of a token's largest value / 127.  The width of the SwiGLU is then at most
