@@ -770,3 +770,32 @@ def test_norm_codes_of_extreme_rows_among_others_of_a_workgroup(cuda):
         want, _ = O.codes(f64(x[part]) * f64(w))
         assert np.array_equal(q[part].cpu().numpy(), want)
     assert torch.equal(s[512:grid].min(), s[512:grid].max())
+
+
+@pytest.mark.parametrize("d", [7, 100, 256, 1021, 2048, 4104, 10001])
+def test_norm_codes_of_zero_and_extreme_rows_in_wider_matrices(cuda, d):
+    # rows inside wider ones on all sides: what is beside them stays as it was
+    lib, st = _lib.lib(), ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+    x, r = extreme_rows(d, 1), extreme_rows(d, 60)
+    x[3], r[3] = 0, 0
+    x[5], r[5] = bf16((d,), 9), -bf16((d,), 9)  # a sum of zeros
+    rows, wide = x.shape[0], d + 24
+    w = (1 + 0.1 * bf16((d,), 2).float()).to(torch.bfloat16).to(cuda)
+    xw, rw = (torch.full((rows, wide), 3.0, dtype=torch.bfloat16, device=cuda) for _ in range(2))
+    xw[:, 5:5 + d], rw[:, 1:1 + d] = x.to(cuda), r.to(cuda)
+    q = torch.full((rows + 2, wide), 77, dtype=torch.int8, device=cuda)
+    h, s, rstd = (Guarded(shape, t, cuda) for shape, t in (((rows, d), torch.bfloat16),
+                                                           ((rows,), torch.float32),
+                                                           ((rows,), torch.float32)))
+    into = q[1:-1, 3:3 + d]
+    assert lib.dd_rmsnorm_int8_fwd(at(xw[:, 5:]), wide, at(rw[:, 1:]), wide, at(w), h.p, at(into),
+                                   wide, s.p, rstd.p, rows, d, 1e-5, st) == 0
+    torch.cuda.synchronize()
+    keep = torch.ones_like(q, dtype=torch.bool)
+    keep[1:-1, 3:3 + d] = False
+    assert bool((q[keep] == 77).all()) and all(g.intact() for g in (h, s, rstd))
+    sums = O.add(x, r)
+    want, top = O.codes(f64(sums) * f64(w))
+    assert np.array_equal(into.cpu().numpy(), want)
+    assert s.t[3] == 0 and s.t[5] == 0 and not top[[3, 5]].any()
+    assert bool(torch.isnan(s.t.cpu()[~np.isfinite(top)]).all())
