@@ -238,7 +238,7 @@ def test_block_refuses_other_checkpoint_widths():
     assert OpenLMBlock(512, 8, 768, device="cpu").checkpoint_bits == 16
 
 
-@pytest.mark.parametrize("tiles", [1, 3, 255, 256, 257, 2000, 3072, 16896, 66000])
+@pytest.mark.parametrize("tiles", [1, 3, 255, 256, 257, 2000, 3008, 16896, 66000])
 def test_walks_of_large_tiles_hold_no_tile_behind_the_last(tiles):
     # a wave's lanes hold the next 64 tiles of its workgroup's walk
     grid, seen = min(tiles, routes.CUS), []
