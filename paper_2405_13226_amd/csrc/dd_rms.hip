@@ -229,15 +229,14 @@ __device__ __forceinline__ double product_at(const RowOperands &op, long long ro
 // extreme values 544, ordinary rows 167.
 template <int TPR>
 __device__ __forceinline__ void extreme_row(const RowOperands &op, long long row, float rstd,
-                                            int t, float *red, int &flip)
+                                            int t, uint32_t m, float *red, int &flip)
 {
     // Nothing is shared with the ordinary rows' way, whose registers it would take.
     asm volatile("" : "+v"(t), "+v"(row));
     const int d = op.d;
     int8_t *q = op.Q + row * op.ldq;
     float none = 0.f;
-    uint32_t m = 0;
-    if (d >= 8) {
+    if (m == 0 && d >= 8) {
 #pragma unroll 1
         for (int i = 8 * t; i < d; i += 8 * TPR) {
             const int col = min(i, d - 8);
@@ -255,8 +254,8 @@ __device__ __forceinline__ void extreme_row(const RowOperands &op, long long row
                 op.scales[row] = 0.0f;
             return;
         }
-        m = 0;
     }
+    m = 0;
 #pragma unroll 1
     for (int i = t; i < d; i += TPR)
         m = max(m, static_cast<uint32_t>(__double2hiint(product_at(op, row, i))) & 0x7fffffffu);
@@ -345,7 +344,7 @@ row_kernel(RowOperands op)
         } else {
             if constexpr (KIND == kNormCodes) {
                 if (m < __float_as_uint(0x1p-60f) || m > __float_as_uint(0x1p60f)) {
-                    extreme_row<TPR>(op, row, rstd, t, red, flip);
+                    extreme_row<TPR>(op, row, rstd, t, m, red, flip);
                     continue;
                 }
             }

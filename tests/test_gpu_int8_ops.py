@@ -799,3 +799,14 @@ def test_norm_codes_of_zero_and_extreme_rows_in_wider_matrices(cuda, d):
     assert np.array_equal(into.cpu().numpy(), want)
     assert s.t[3] == 0 and s.t[5] == 0 and not top[[3, 5]].any()
     assert bool(torch.isnan(s.t.cpu()[~np.isfinite(top)]).all())
+
+
+@pytest.mark.parametrize("value", [float("inf"), -float("inf"), float("nan")])
+@pytest.mark.parametrize("d", [7, 256, 1021, 2048, 4104])
+def test_norm_codes_of_zeros_under_a_weight_that_is_not_finite(cuda, d, value):
+    # 0 inf is no number, in a row of zeros too
+    x = extreme_rows(d, 1)
+    w = torch.ones(d, dtype=torch.bfloat16)
+    w[d // 3] = value
+    q, s, _, _ = ops.rms_norm_int8(x.to(cuda), w.to(cuda))
+    assert bool(torch.isnan(s).all()) and not q.any()
