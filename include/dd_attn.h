@@ -75,7 +75,8 @@ typedef enum {
     DD_ERR_ALIGN = 6,     /* a tensor pointer is not 16-byte aligned (LSE: 4)  */
     DD_ERR_ALIAS = 7,     /* an output overlaps an input or another output     */
     DD_ERR_HIP = 8,       /* the HIP runtime rejected a launch                 */
-    DD_ERR_SCRATCH = 9    /* dd_attn_bwd_noalloc: shape exceeds its scratch    */
+    DD_ERR_SCRATCH = 9,   /* dd_attn_bwd_noalloc: shape exceeds its scratch    */
+    DD_ERR_CACHE = 10     /* dd_cache_check: lengths, offsets or pages         */
 } dd_status;
 
 /*
@@ -345,6 +346,108 @@ int dd_gemm_i8_wgrad(const int8_t *Q, long long ldq, const float *scales, const 
                      long long ldy, void *const *dW, long long ldw, int n, int T, int M, int N,
                      void *workspace, size_t workspace_bytes, void *stream);
 size_t dd_gemm_i8_wgrad_workspace_bytes(int T, int M, int N, int n); /* 0: invalid */
+
+/*
+ * A paged cache of keys and values, for generation and for texts scored in
+ * pieces.  Pages: bf16 [pages][Hkv][page][D], the slots of one head of a page
+ * contiguous; `page` a power of two in 16 .. 1024.  table int32 [B][per] names
+ * each sequence's pages in order: slot j of sequence b is row j % page of page
+ * table[b][j / page].  A call takes a ragged chunk of new tokens: rows
+ * cu_new[b] .. cu_new[b + 1] - 1 of its tensors (cu_new int32 [B + 1], from 0
+ * on, at most T) are sequence b's, which has lens[b] (int32) slots in use before
+ * the call; its new token i gets slot lens[b] + i.  A sequence may have no new
+ * tokens, and no slots; rows from cu_new[B] to T belong to none and are left as
+ * they were, in every output.
+ *
+ * D in {64, 128}, Hkv divides H (H / Hkv heads share a key head), T <= 2^23,
+ * T * H <= 2^26, H * D < 2^23, B * Hkv <= 65535, per * page < 2^30.  Row
+ * strides (ldq, ldk, ldv: elements between tokens, at least H D or Hkv D, the
+ * heads of a token contiguous) multiples of 8; bf16 pointers 16-byte, others
+ * 4-byte aligned.  Outputs must not overlap inputs or each other unless said.
+ *
+ * table, lens, cu_new (and start, seen) are device memory and not validated;
+ * callers check host copies with dd_cache_check: offsets in order, slots within
+ * the table, every page in use named once.  Malformed contents cannot make a
+ * kernel access memory out of bounds, but results are then unspecified; a token
+ * without a slot, or whose page the cache does not have, is not written.
+ *
+ * dd_cache_append  V's rows, and K's rotated at their positions with rope_base
+ *                  (bit-identical to dd_rope; 0: as they are), into their slots;
+ *                  Q's rotated rows to Qrot (contiguous [T][H][D]; Q and Qrot
+ *                  NULL: keys only; Qrot may be Q where ldq is H D).  Token i
+ *                  has position start[b] + i (start NULL: its slot).  positions
+ *                  (NULL, or int32 [B][Hkv][per * page]) receives it per slot.
+ * dd_cache_attn_fwd  O [T][H][D] bf16 and LSE [T][H] fp32 of attention (scale
+ *                  1/sqrt(D)) of Q's rows over the cache, whose slots hold the
+ *                  chunk's own tokens already: new token i sees the slots up to
+ *                  lens[b] + i.  What the others hold leaves no trace.  With W_in
+ *                  and W_out (fp32 [B][Hkv][per * page], one may be the other):
+ *                  W_out = (W_in, or 0 for the chunk's own slots) + the sum of the
+ *                  attention probabilities of the slot over the chunk's tokens and
+ *                  the heads that share the key head, for the slots in use; the
+ *                  rest is left as it was.  Sums in a fixed order.  workspace:
+ *                  dd_cache_attn_workspace_bytes(...) bytes, 16-byte aligned.
+ * dd_cache_evict   per sequence and key head, the `budget` slots of most weight
+ *                  stay: first those whose position is at least seen[b] - recent
+ *                  (recent <= budget), then by W_in (a NaN counts least), equal
+ *                  ones by the lowest slot.  The n-th slot below the budget that
+ *                  does not stay receives key, value, weight and position of the
+ *                  n-th slot behind it that does: slots are in no order after it,
+ *                  which attention does not depend on.  lens_out = min(lens,
+ *                  budget); a sequence with no more slots keeps all of them.
+ *                  W_out and P_out (positions) hold lens_out slots, the rest is
+ *                  left as it was; W_out may be W_in, P_out P_in, lens_out lens.
+ *                  workspace: dd_cache_evict_workspace_bytes(...) bytes.
+ */
+int dd_cache_append(const void *Q, long long ldq, const void *K, long long ldk, const void *V,
+                    long long ldv, void *Qrot, void *Kp, void *Vp, int32_t *positions,
+                    const int32_t *table, const int32_t *lens, const int32_t *start,
+                    const int32_t *cu_new, int T, int B, int H, int Hkv, int D, int pages, int page,
+                    int per, float rope_base, void *stream);
+int dd_cache_attn_fwd(const void *Q, long long ldq, const void *Kp, const void *Vp,
+                      const int32_t *table, const int32_t *lens, const int32_t *cu_new, void *O,
+                      float *LSE, const float *W_in, float *W_out, int T, int B, int H, int Hkv,
+                      int D, int pages, int page, int per, void *workspace, size_t workspace_bytes,
+                      void *stream);
+size_t dd_cache_attn_workspace_bytes(int T, int B, int H, int Hkv, int D, int page, int per);
+int dd_cache_evict(void *Kp, void *Vp, const int32_t *table, const int32_t *lens, const float *W_in,
+                   const int32_t *P_in, const int32_t *seen, float *W_out, int32_t *P_out,
+                   int32_t *lens_out, int B, int Hkv, int D, int pages, int page, int per,
+                   int budget, int recent, void *workspace, size_t workspace_bytes, void *stream);
+size_t dd_cache_evict_workspace_bytes(int B, int Hkv, int D, int page, int per, int budget);
+int dd_cache_check(const int32_t *host_table, const int32_t *host_lens, const int32_t *host_cu_new,
+                   int T, int B, int pages, int page, int per); /* cu_new NULL: no new tokens */
+
+/*
+ * Log probabilities of given tokens.  X: logits [rows][V], bf16 (f32 = 0) or
+ * fp32 (f32 = 1), row stride ldx >= V, any alignment of their type; targets
+ * int64 [rows], a negative one is ignored (log probability and its gradient 0),
+ * one of V or more gives NaN.  1 <= rows <= 2^23, 1 <= V <= 2^30, rows *
+ * ceil(V / 8192) < 2^24, top <= min(V, 64).  fp32 throughout; sums in a fixed
+ * order.
+ *
+ * dd_logprobs_fwd  lse = log sum_j e^x_j, logp = x_t - lse, entropy = - sum_j p_j
+ *                  log p_j (-inf logits have p = 0 and add nothing), and the `top`
+ *                  largest logits' log probabilities (fp32 [rows][top]) and ids
+ *                  (int64), in order, equal ones by the lowest id.  A row that
+ *                  holds a NaN or +inf has NaN lse, logp and entropy, and a NaN
+ *                  counts least among the alternatives; a row of -inf alone has
+ *                  lse -inf, the others NaN.  workspace:
+ *                  dd_logprobs_workspace_bytes(rows, V, top) bytes, 8-byte
+ *                  aligned.
+ * dd_logprobs_bwd  the gradient of sum(g_logp logp + g_entropy entropy + g_lse
+ *                  lse) (each gradient fp32 [rows] or NULL): dX_j = p_j (g_lse -
+ *                  g_logp - g_entropy (log p_j + entropy)) + g_logp [j = t], of
+ *                  X's type, rounded once; lse and entropy from the forward.  dX
+ *                  may be X (with lddx = ldx).
+ */
+int dd_logprobs_fwd(const void *X, long long ldx, int f32, const int64_t *targets, float *logp,
+                    float *entropy, float *lse, float *top_logp, int64_t *top_ids, int rows, int V,
+                    int top, void *workspace, size_t workspace_bytes, void *stream);
+size_t dd_logprobs_workspace_bytes(int rows, int V, int top);
+int dd_logprobs_bwd(const void *X, long long ldx, int f32, const int64_t *targets, const float *lse,
+                    const float *entropy, const float *g_logp, const float *g_entropy,
+                    const float *g_lse, void *dX, long long lddx, int rows, int V, void *stream);
 
 /* Workspace bytes dd_attn_bwd needs for this shape (0 for an invalid shape). */
 size_t dd_attn_bwd_workspace_bytes(int B, int L, int H, int D);

@@ -12,8 +12,13 @@ include/dd_attn.h.
 from ._lib import DDError, LibraryMissing, lib  # noqa: F401
 from .attention import (DDAttnFunction, DocLens, attention, backward,  # noqa: F401
                         backward_rope, forward, forward_rope, rope, workspace_bytes)
+from .cache import (PagedCache, cache_append, cache_attention, cache_evict,  # noqa: F401
+                    check_cache)
+from .loss import logprobs, logprobs_backward, token_logprobs  # noqa: F401
 from . import dd  # noqa: F401
 
 __all__ = ["forward", "backward", "attention", "DDAttnFunction", "DocLens",
+           "PagedCache", "cache_append", "cache_attention", "cache_evict", "check_cache",
+           "logprobs", "logprobs_backward", "token_logprobs",
            "rope", "forward_rope", "backward_rope",
            "workspace_bytes", "lib", "DDError", "LibraryMissing", "dd"]

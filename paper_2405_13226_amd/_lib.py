@@ -54,6 +54,16 @@ SIGNATURES = {
     "dd_gemm_i8_wgrad": (ctypes.c_int, [_P, _L, _P, _P, _L, _P, _L, _I, _I, _I, _I, _P,
                                         ctypes.c_size_t, _P]),
     "dd_gemm_i8_wgrad_workspace_bytes": (ctypes.c_size_t, [_I, _I, _I, _I]),
+    "dd_cache_append": (ctypes.c_int, [_P, _L, _P, _L, _P, _L, _P, _P, _P, _P, _P, _P, _P, _P,
+                                       *[_I] * 8, ctypes.c_float, _P]),
+    "dd_cache_attn_fwd": (ctypes.c_int, [_P, _L, *[_P] * 9, *[_I] * 8, _P, ctypes.c_size_t, _P]),
+    "dd_cache_attn_workspace_bytes": (ctypes.c_size_t, [_I] * 7),
+    "dd_cache_evict": (ctypes.c_int, [*[_P] * 10, *[_I] * 8, _P, ctypes.c_size_t, _P]),
+    "dd_cache_evict_workspace_bytes": (ctypes.c_size_t, [_I] * 6),
+    "dd_cache_check": (ctypes.c_int, [_P, _P, _P, *[_I] * 5]),
+    "dd_logprobs_fwd": (ctypes.c_int, [_P, _L, _I, *[_P] * 6, _I, _I, _I, _P, ctypes.c_size_t, _P]),
+    "dd_logprobs_workspace_bytes": (ctypes.c_size_t, [_I] * 3),
+    "dd_logprobs_bwd": (ctypes.c_int, [_P, _L, _I, *[_P] * 7, _L, _I, _I, _P]),
     "dd_doclens_check": (ctypes.c_int, [_P, _I, ctypes.c_longlong]),
     "dd_status_str": (ctypes.c_char_p, [_I]),
     "dd_prof_enable": (ctypes.c_int, [_I]),
@@ -94,7 +104,7 @@ def prof_launches():
 STATUS = {
     0: "DD_OK", 1: "DD_ERR_NULL", 2: "DD_ERR_SHAPE", 3: "DD_ERR_HEADDIM",
     4: "DD_ERR_DOCLENS", 5: "DD_ERR_WORKSPACE", 6: "DD_ERR_ALIGN", 7: "DD_ERR_ALIAS",
-    8: "DD_ERR_HIP", 9: "DD_ERR_SCRATCH",
+    8: "DD_ERR_HIP", 9: "DD_ERR_SCRATCH", 10: "DD_ERR_CACHE",
 }
 
 _lib = None

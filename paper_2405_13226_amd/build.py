@@ -23,7 +23,8 @@ LIB = os.path.join(PKG, "libdd_attn.so")
 ARCH = "gfx950"
 HIP_SOURCES = ["dd_fwd.hip", "dd_bwd.hip", "dd_dkdv.hip", "dd_bwd_short.hip", "dd_prof.hip",
                "dd_rope.hip", "dd_noalloc.hip", "dd_gemm.hip", "dd_block.hip", "dd_rms.hip",
-               "dd_gemm_i8.hip", "dd_wgrad_i8.hip"]
+               "dd_gemm_i8.hip", "dd_wgrad_i8.hip", "dd_cache.hip", "dd_cache_attn.hip",
+               "dd_logprobs.hip"]
 # Extra flags per source.  The D = 128 dK/dV kernel, the one-kernel
 # short-row backward and the GEMM are scheduled for instruction-level
 # parallelism (measured: dK/dV ~6% faster at L = 8192, neutral at L = 256;
@@ -33,7 +34,7 @@ HIP_SOURCES = ["dd_fwd.hip", "dd_bwd.hip", "dd_dkdv.hip", "dd_bwd_short.hip", "d
 _ILP = ["-mllvm", "-amdgpu-sched-strategy=max-ilp"]
 HIP_SOURCE_FLAGS = {"dd_dkdv.hip": _ILP, "dd_bwd_short.hip": _ILP, "dd_gemm.hip": _ILP,
                     "dd_gemm_i8.hip": _ILP, "dd_wgrad_i8.hip": _ILP}
-CXX_SOURCES = ["dd_api.cpp", "dd_api8.cpp"]
+CXX_SOURCES = ["dd_api.cpp", "dd_api8.cpp", "dd_api_cache.cpp"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 # Packed fp32 VALU forms are disabled for all device code.
 HIP_FLAGS = ["-O3", "-std=c++17", f"--offload-arch={ARCH}", "-fPIC",

@@ -90,13 +90,15 @@ const char *dd_status_str(int status)
                "calls' conditions are in dd_attn.h";
     case DD_ERR_HEADDIM: return "unsupported head dimension: D must be 64 or 128";
     case DD_ERR_DOCLENS: return "invalid cu_doclens / n_docs";
-    case DD_ERR_WORKSPACE: return "backward workspace missing or too small";
+    case DD_ERR_WORKSPACE: return "workspace missing or too small";
     case DD_ERR_ALIGN: return "misaligned pointer: tensors need 16-byte alignment";
     case DD_ERR_ALIAS: return "an output buffer overlaps another buffer";
     case DD_ERR_HIP: return "HIP launch failed";
     case DD_ERR_SCRATCH:
         return "shape needs more than the 16 MiB device scratch of dd_attn_bwd_noalloc "
                "(B*H*L <= 2^21); call dd_attn_bwd with a workspace";
+    case DD_ERR_CACHE:
+        return "invalid cache: lengths, cu_new offsets or pages (out of range or named twice)";
     default: return "unknown status";
     }
 }

@@ -1,0 +1,324 @@
+// dd_cache.hip -- writing and thinning out a paged cache (dd_cache.hpp).
+//
+// Append: a ragged chunk's keys and values into their slots, keys (and the
+// chunk's queries) rotated at their positions (dd_rope.hpp: bit-identical to a
+// dd_rope pass at these positions).  One workgroup per token: thread t holds
+// the 8-element chunk t % (D/8) of its heads, so an angle is formed once per
+// token and thread.  Bytes only: each row is read and written once.
+//
+// Eviction: per sequence and key head, the `budget` slots of most weight stay
+// (slots of the last `recent` positions before all others; equal ones by the
+// lowest slot).  Attention does not depend on the order of the slots, keys
+// carry their rotation, and every kept slot is older than any later token, so
+// nothing is shifted: the n-th evicted slot below the budget receives the n-th
+// kept slot behind it.  Sources and targets are disjoint, so rows move in any
+// order, and no more of them than the result needs.
+//   select: one workgroup per (sequence, head) finds the weight of rank
+//           `budget` by three histograms of 11, 11 and 10 bits of the ordered
+//           weights, then lists holes and survivors in slot order
+//   move:   the listed rows
+#include "dd_cache.hpp"
+#include "dd_internal.h"
+#include "dd_launch.hpp"
+#include "dd_rope.hpp"
+#include "dd_attn.h"
+
+#include <algorithm>
+
+namespace dd {
+
+namespace {
+
+struct AppendRows {
+    const uint16_t *Q, *K, *V;
+    uint16_t *Qrot, *Kp, *Vp;
+    int32_t *P;
+    const int32_t *start;
+    long long ldq, ldk, ldv;
+    int H;
+};
+
+template <int D, bool ROPE>
+__global__ void __launch_bounds__(256)
+append_kernel(AppendRows a, CacheView c, RopeEpi rt)
+{
+    constexpr int CG = D / 8, ROWS = 256 / CG;
+    const int t = static_cast<int>(blockIdx.x);
+    const int cg = threadIdx.x % CG, r0 = threadIdx.x / CG;
+    const int b = cache_seq_of(c, t);
+    const CacheSeq s = cache_seq(c, b);
+    const int i = t - s.row0;
+    if (i < 0 || i >= s.n)  // behind the last sequence
+        return;
+    const int slot = s.len + i;
+    const int pos = (a.start ? a.start[b] : s.len) + i;
+    const int id = slot < c.slots() ? cache_page(c, b, slot) : -1;
+
+    float sn[4], cs[4];
+    if constexpr (ROPE) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            rope_sincos(rope_theta_j(rt, cg * 4 + e), pos, sn[e], cs[e]);
+    }
+    auto rotated = [&](u32x4 u) __attribute__((always_inline)) {
+        if constexpr (ROPE) {
+            float f[8];
+            unpack8(u, f);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                rope_pair<false>(f[2 * e], f[2 * e + 1], sn[e], cs[e]);
+            u = pack8f(f);
+        }
+        return u;
+    };
+    if (a.Q != nullptr) {
+        const uint16_t *q = a.Q + t * a.ldq + cg * 8;
+        uint16_t *y = a.Qrot + static_cast<long long>(t) * a.H * D + cg * 8;
+        for (int h = r0; h < a.H; h += ROWS)
+            *reinterpret_cast<u32x4 *>(y + h * D) =
+                rotated(*reinterpret_cast<const u32x4 *>(q + h * D));
+    }
+    if (id < 0)
+        return;
+    const uint16_t *k = a.K + t * a.ldk + cg * 8, *v = a.V + t * a.ldv + cg * 8;
+    for (int h = r0; h < c.Hkv; h += ROWS) {
+        const long long at = cache_row(c, id, h, slot) * D + cg * 8;
+        const u32x4 kh = *reinterpret_cast<const u32x4 *>(k + h * D);
+        const u32x4 vh = *reinterpret_cast<const u32x4 *>(v + h * D);
+        *reinterpret_cast<u32x4 *>(a.Kp + at) = rotated(kh);
+        *reinterpret_cast<u32x4 *>(a.Vp + at) = vh;
+        if (a.P != nullptr && cg == 0)
+            a.P[(static_cast<long long>(b) * c.Hkv + h) * c.slots() + slot] = pos;
+    }
+}
+
+template <int D>
+int launch_append_d(const CacheAppendArgs &a)
+{
+    const AppendRows r{static_cast<const uint16_t *>(a.Q), static_cast<const uint16_t *>(a.K),
+                       static_cast<const uint16_t *>(a.V), static_cast<uint16_t *>(a.Qrot),
+                       static_cast<uint16_t *>(a.Kp), static_cast<uint16_t *>(a.Vp), a.P, a.start,
+                       a.ldq, a.ldk, a.ldv, a.H};
+    const CacheView c{a.c.table, a.c.lens, a.c.cu_new, a.c.T, a.c.B, a.c.Hkv, a.c.pages,
+                      a.c.shift, a.c.per};
+    const bool rope = a.rope_base > 0.0;
+    const hipError_t e = launch_kernel(
+        rope ? append_kernel<D, true> : append_kernel<D, false>, dim3(static_cast<unsigned>(a.c.T)),
+        dim3(256), static_cast<hipStream_t>(a.stream), r, c,
+        rope ? rope_epi(a.rope_base, D) : RopeEpi{});
+    return e == hipSuccess ? DD_OK : DD_ERR_HIP;
+}
+
+// ---------------------------------------------------------------------------
+
+struct EvictRows {
+    const float *W;
+    const int32_t *P, *seen;
+    float *Wout;
+    int32_t *Pout, *lens_out;
+    int32_t *count;     // [B * Hkv] rows to move
+    int32_t *to, *from; // [B * Hkv][list] their targets and sources
+    uint16_t *Kp, *Vp;
+    int budget, recent, list;
+};
+
+constexpr int kSelectThreads = 1024;
+
+// Weights in order as unsigned numbers: a NaN below all, the slots that stay
+// in any case above all.
+__device__ __forceinline__ uint32_t weight_key(float w, bool stays)
+{
+    const uint32_t u = __float_as_uint(w + 0.0f);  // -0 as 0
+    const uint32_t k = u >> 31 ? ~u : u | 0x80000000u;
+    return stays ? 0xffffffffu : w != w ? 0u : k;
+}
+
+// Exclusive prefix sum of x over the workgroup's threads, and its total.
+__device__ __forceinline__ uint32_t block_prefix(uint32_t x, uint32_t *waves, uint32_t &total)
+{
+    constexpr int NW = kSelectThreads / 64;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    uint32_t s = x;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const uint32_t y = __shfl_up(static_cast<int>(s), o);
+        s += lane >= o ? y : 0u;
+    }
+    __syncthreads();  // `waves` of the call before have been read
+    if (lane == 63)
+        waves[wave] = s;
+    __syncthreads();
+    uint32_t before = 0, all = 0;
+#pragma unroll
+    for (int i = 0; i < NW; ++i) {
+        const uint32_t w = waves[i];
+        before += i < wave ? w : 0u;
+        all += w;
+    }
+    total = all;
+    return before + s - x;
+}
+
+__global__ void __launch_bounds__(kSelectThreads)
+select_kernel(EvictRows a, CacheView c)
+{
+    __shared__ uint32_t hist[2048];
+    __shared__ uint32_t waves[kSelectThreads / 64];
+    __shared__ uint32_t found[2];
+    const int bh = static_cast<int>(blockIdx.x), b = bh / c.Hkv, tid = threadIdx.x;
+    const int n = min(max(c.lens[b], 0), c.slots());
+    const long long base = static_cast<long long>(bh) * c.slots();
+    const float *W = a.W + base;
+    const int32_t *P = a.P + base;
+    float *Wout = a.Wout + base;
+    int32_t *Pout = a.Pout + base;
+    if (n <= a.budget) {
+        if (tid == 0)
+            a.count[bh] = 0;
+        if (Wout != W || Pout != P)
+            for (int j = tid; j < n; j += kSelectThreads) {
+                Wout[j] = W[j];
+                Pout[j] = P[j];
+            }
+        return;
+    }
+    const long long first = static_cast<long long>(a.seen[b]) - a.recent;
+    auto key_of = [&](int j) __attribute__((always_inline)) {
+        return weight_key(W[j], P[j] >= first);
+    };
+
+    // The key of rank `budget` (counted from the largest), from its leading
+    // bits on, and how many keys equal to it stay.
+    uint32_t prefix = 0, need = static_cast<uint32_t>(a.budget);
+    for (int part = 0; part < 3; ++part) {
+        const int low = part == 0 ? 21 : part == 1 ? 10 : 0, bits = part == 2 ? 10 : 11;
+        const uint32_t mask = (1u << bits) - 1;
+        for (int i = tid; i < 2048; i += kSelectThreads)
+            hist[i] = 0;
+        __syncthreads();
+        for (int j = tid; j < n; j += kSelectThreads) {
+            const uint32_t k = key_of(j);
+            if (part == 0 || k >> (low + bits) == prefix)
+                atomicAdd(&hist[(k >> low) & mask], 1u);
+        }
+        __syncthreads();
+        // bins from the largest key down, two per thread
+        const int i0 = 2047 - 2 * tid;
+        const uint32_t h0 = hist[i0], h1 = hist[i0 - 1];
+        uint32_t all;
+        const uint32_t above = block_prefix(h0 + h1, waves, all);
+        if (above < need && need <= above + h0) {
+            found[0] = i0;
+            found[1] = need - above;
+        } else if (above + h0 < need && need <= above + h0 + h1) {
+            found[0] = i0 - 1;
+            found[1] = need - above - h0;
+        }
+        __syncthreads();
+        prefix = prefix << bits | found[0];
+        need = found[1];
+        __syncthreads();
+    }
+
+    // Holes and survivors in slot order.
+    int32_t *to = a.to + static_cast<long long>(bh) * a.list;
+    int32_t *from = a.from + static_cast<long long>(bh) * a.list;
+    uint32_t equal = 0, holes = 0, extra = 0;  // so far
+    for (int j0 = 0; j0 < n; j0 += kSelectThreads) {
+        const int j = j0 + tid;
+        const bool in = j < n;
+        const uint32_t k = in ? key_of(j) : 0u;
+        const bool eq = in && k == prefix;
+        uint32_t all;
+        const uint32_t before = equal + block_prefix(eq ? 1u : 0u, waves, all);
+        equal += all;
+        const bool keep = in && (k > prefix || (eq && before < need));
+        const bool hole = in && !keep && j < a.budget, moved = keep && j >= a.budget;
+        // holes and moved rows of a step: below 2^16 of each
+        const uint32_t place = block_prefix((hole ? 1u : 0u) | (moved ? 1u << 16 : 0u), waves, all);
+        if (hole)
+            to[holes + (place & 0xffffu)] = j;
+        if (moved)
+            from[extra + (place >> 16)] = j;
+        holes += all & 0xffffu;
+        extra += all >> 16;
+        if (keep && j < a.budget && (Wout != W || Pout != P)) {
+            Wout[j] = W[j];
+            Pout[j] = P[j];
+        }
+    }
+    if (tid == 0)
+        a.count[bh] = static_cast<int>(holes);
+}
+
+template <int D>
+__global__ void __launch_bounds__(256) move_kernel(EvictRows a, CacheView c)
+{
+    constexpr int CG = D / 8, ROWS = 256 / CG;
+    const int bh = static_cast<int>(blockIdx.y), b = bh / c.Hkv, h = bh % c.Hkv;
+    if (blockIdx.x == 0 && h == 0 && threadIdx.x == 0)
+        a.lens_out[b] = min(min(max(c.lens[b], 0), c.slots()), a.budget);
+    const int n = a.count[bh], cg = threadIdx.x % CG;
+    const long long base = static_cast<long long>(bh) * c.slots();
+    const int32_t *to = a.to + static_cast<long long>(bh) * a.list;
+    const int32_t *from = a.from + static_cast<long long>(bh) * a.list;
+    for (int r = static_cast<int>(blockIdx.x) * ROWS + threadIdx.x / CG; r < n;
+         r += static_cast<int>(gridDim.x) * ROWS) {
+        const int d = to[r], s = from[r];
+        const int pd = cache_page(c, b, d), ps = cache_page(c, b, s);
+        if (pd >= 0 && ps >= 0) {
+            const long long rd = cache_row(c, pd, h, d) * D + cg * 8;
+            const long long rs = cache_row(c, ps, h, s) * D + cg * 8;
+            const u32x4 k = *reinterpret_cast<const u32x4 *>(a.Kp + rs);
+            const u32x4 v = *reinterpret_cast<const u32x4 *>(a.Vp + rs);
+            *reinterpret_cast<u32x4 *>(a.Kp + rd) = k;
+            *reinterpret_cast<u32x4 *>(a.Vp + rd) = v;
+        }
+        if (cg == 0) {
+            a.Wout[base + d] = a.W[base + s];
+            a.Pout[base + d] = a.P[base + s];
+        }
+    }
+}
+
+// Entries of a list: holes lie below the budget, survivors behind it.
+int evict_list(const CacheShape &c, int budget)
+{
+    return std::max(std::min(budget, (c.per << c.shift) - budget), 0);
+}
+
+}  // namespace
+
+int launch_cache_append(const CacheAppendArgs &a)
+{
+    return a.c.D == 64 ? launch_append_d<64>(a) : launch_append_d<128>(a);
+}
+
+size_t cache_evict_workspace_bytes(const CacheShape &c, int budget)
+{
+    return static_cast<size_t>(c.B) * c.Hkv * (1 + 2 * static_cast<size_t>(evict_list(c, budget))) *
+           sizeof(int32_t);
+}
+
+int launch_cache_evict(const CacheEvictArgs &a)
+{
+    const CacheView c{a.c.table, a.c.lens, nullptr, 0, a.c.B, a.c.Hkv, a.c.pages, a.c.shift,
+                      a.c.per};
+    const int bh = a.c.B * a.c.Hkv, list = evict_list(a.c, a.budget);
+    int32_t *ws = static_cast<int32_t *>(a.workspace);
+    const EvictRows r{a.W, a.P, a.seen, a.Wout, a.Pout, a.lens_out, ws, ws + bh,
+                      ws + bh + static_cast<size_t>(bh) * list, static_cast<uint16_t *>(a.Kp),
+                      static_cast<uint16_t *>(a.Vp), a.budget, a.recent, list};
+    hipStream_t st = static_cast<hipStream_t>(a.stream);
+    hipError_t e = launch_kernel(select_kernel, dim3(static_cast<unsigned>(bh)),
+                                 dim3(kSelectThreads), st, r, c);
+    if (e != hipSuccess)
+        return DD_ERR_HIP;
+    const int rows = 256 / (a.c.D / 8);
+    const unsigned parts = static_cast<unsigned>(std::clamp((list + 4 * rows - 1) / (4 * rows), 1, 64));
+    e = launch_kernel(a.c.D == 64 ? move_kernel<64> : move_kernel<128>,
+                      dim3(parts, static_cast<unsigned>(bh)), dim3(256), st, r, c);
+    return e == hipSuccess ? DD_OK : DD_ERR_HIP;
+}
+
+}  // namespace dd

@@ -1,0 +1,635 @@
+// dd_cache_attn.hip -- attention of a ragged chunk of new tokens over a paged
+// cache (dd_cache.hpp), and the attention weight of each cached slot.
+//
+//   O[t, h]   = sum_j p_j V_j,  p = softmax over j <= len + i of q K_j / sqrt(D)
+//   W[b, g, j] += sum of p_j over the sequence's new tokens and the heads that
+//               share key head g
+//
+// A sequence's rows for one key head are its new tokens times the G = H / Hkv
+// heads that share it, token-major: row r is token r / G, head r % G.  A wave
+// holds 32 rows as matrix-core B operands and keeps a running maximum and sum
+// (log2 domain, fp32); S^T = K Q^T puts a row in a lane column, P^T stays in
+// registers as the B operand of O^T += V^T P^T.  Two kernels differ in who
+// reads the keys:
+//
+//   tile_kernel  many rows: four waves (128 rows) share 64-key tiles,
+//                double-buffered in LDS
+//   few_kernel   few rows (generation): every wave walks key tiles of its own
+//                (32 keys, its own LDS stages, no barrier), the waves' sums are
+//                joined through LDS at the end
+//
+// Either splits the keys over workgroups where there are too few rows to fill
+// the chip; join_kernel adds the parts.  Tiles arrive by direct global->LDS
+// loads; one load instruction covers rows of one page (pages hold at least 16
+// slots), whose number is a scalar load.
+//
+// Slots behind a sequence's last are never read (a tile's rows are clamped to
+// it).  A slot that a row may not see leaves no trace in it, whatever it
+// holds: its score is replaced, and where a boundary tile holds a value that
+// is not finite its keys are added one by one, each only to the rows that see
+// it (zero times infinity would not be zero).
+#include "dd_cache.hpp"
+#include "dd_internal.h"
+#include "dd_launch.hpp"
+#include "dd_tile.hpp"
+#include "dd_attn.h"
+
+#include <algorithm>
+#include <cmath>
+
+namespace dd {
+
+namespace {
+
+typedef uint16_t u16x8 __attribute__((ext_vector_type(8)));
+
+// Rescaling of the accumulator is skipped until the running maximum has grown
+// by this many log2 units (probabilities stay below 2^8).
+constexpr float kSlack = 8.0f;
+
+struct AttnRows {
+    const uint16_t *Q, *K, *V;
+    uint16_t *O;
+    float *LSE;
+    float *part_o, *part_lse;  // [splits][T * H][D], [splits][T * H] (log2), splits > 1
+    long long ldq;
+    int H, G, tiles, splits;
+    float scale_log2;
+};
+
+template <int N>
+__device__ __forceinline__ void wait_vm()
+{
+    asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory");
+}
+
+// One tile of NB x 32 keys for the wave's 32 rows.  MASKED: the lane's row sees
+// the tile's keys 0 .. hi_r only (boundary tiles).
+template <int D, int NB, bool MASKED>
+__device__ __forceinline__ void
+attend_tile(const uint16_t *kt, const uint16_t *vt, const bf16x8 (&qf)[D / 16],
+            const int (&koff)[D / 16], const int (&voff)[D / 32][2], int hi_r, int g,
+            float scale_log2, f32x16 (&acc)[D / 32], float &m_i, float &l_i)
+{
+    constexpr int KK = D / 16, DB = D / 32;
+    f32x16 s[NB];
+#pragma unroll
+    for (int kb = 0; kb < NB; ++kb) {
+        s[kb] = f32x16{};
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk)
+            s[kb] = mfma32(lds_row8(kt + kb * 32 * D + koff[kk]), qf[kk], s[kb]);
+    }
+    if constexpr (MASKED) {
+#pragma unroll
+        for (int kb = 0; kb < NB; ++kb)
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                s[kb][r] = kb * 32 + 8 * (r >> 2) + (r & 3) <= hi_r - 4 * g ? s[kb][r] : -INFINITY;
+    }
+    float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+    for (int kb = 0; kb < NB; ++kb)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+            m4[r & 3] = fmaxf(m4[r & 3], s[kb][r]);
+    const float mc = halves_max(fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]))) * scale_log2;
+    if (__any(mc > m_i + kSlack)) {
+        const float m_new = fmaxf(m_i, mc);
+        const float alpha = fast_exp2(m_i - (m_new == -INFINITY ? 0.f : m_new));
+        l_i *= alpha;
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+            acc[db] *= alpha;
+        m_i = m_new;
+    }
+    const float neg_m = m_i == -INFINITY ? 0.f : -m_i;
+    float psum = 0.f;
+#pragma unroll
+    for (int kb = 0; kb < NB; ++kb)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            const float p = fast_exp2(fmaf(s[kb][r], scale_log2, neg_m));
+            s[kb][r] = p;
+            psum += p;
+        }
+    l_i += psum;
+
+    bf16x8 pb[NB][2];
+#pragma unroll
+    for (int kb = 0; kb < NB; ++kb)
+#pragma unroll
+        for (int t2 = 0; t2 < 2; ++t2)
+            pb[kb][t2] = pack8(s[kb], 8 * t2);
+    auto value = [&](int kb, int t2, int db) __attribute__((always_inline)) {
+        const uint16_t *vr = vt + (kb * 32 + 16 * t2) * D;
+        return join(lds_tr4(vr + voff[db][0]), lds_tr4(vr + voff[db][1]));
+    };
+    if constexpr (MASKED) {
+        u16x8 top = {};
+#pragma unroll
+        for (int kb = 0; kb < NB; ++kb)
+#pragma unroll
+            for (int t2 = 0; t2 < 2; ++t2)
+#pragma unroll
+                for (int db = 0; db < DB; ++db) {
+                    const u32x4 a = __builtin_bit_cast(u32x4, value(kb, t2, db)) & 0x7fff7fffu;
+                    top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x8, a));
+                }
+        if (__any(__builtin_reduce_max(top) >= 0x7f80)) {
+#pragma unroll
+            for (int kb = 0; kb < NB; ++kb)
+#pragma unroll
+                for (int t2 = 0; t2 < 2; ++t2)
+#pragma unroll 1
+                    for (int x = 0; x < 16; ++x) {
+                        // slot e of half gx: key 16 t2 + 8 (e / 4) + 4 gx + e % 4
+                        const int gx = x >> 3, e = x & 7;
+                        const bool sees =
+                            kb * 32 + 16 * t2 + 8 * (e >> 2) + 4 * gx + (e & 3) <= hi_r;
+                        const uint32_t half = gx == g ? (e & 1 ? 0xffff0000u : 0xffffu) : 0u;
+#pragma unroll
+                        for (int db = 0; db < DB; ++db) {
+                            u32x4 a = __builtin_bit_cast(u32x4, value(kb, t2, db));
+#pragma unroll
+                            for (int w = 0; w < 4; ++w)
+                                a[w] &= w == e >> 1 ? half : 0u;
+                            const f32x16 one = mfma32(as_bf16x8(a), pb[kb][t2], f32x16{});
+#pragma unroll
+                            for (int r = 0; r < 16; ++r)
+                                acc[db][r] += sees ? one[r] : 0.f;
+                        }
+                    }
+            return;
+        }
+    }
+#pragma unroll
+    for (int kb = 0; kb < NB; ++kb)
+#pragma unroll
+        for (int t2 = 0; t2 < 2; ++t2)
+#pragma unroll
+            for (int db = 0; db < DB; ++db)
+                acc[db] = mfma32(value(kb, t2, db), pb[kb][t2], acc[db]);
+}
+
+// A work item: BM rows of one sequence and key head, and the part of the key
+// tiles (of BN keys) that it takes.
+struct AttnItem {
+    CacheSeq s;
+    int b, h, row, rows;  // first row, rows of the sequence
+    int t0, t1;           // key tiles [t0, t1)
+    int split;
+};
+
+// The sequences' row tiles lie one after the other: those of sequence b start
+// at cu[b] G / BM + b, which leaves room for each of its parts of BM rows.
+template <int BM, int BN>
+__device__ __forceinline__ bool attn_item(const CacheView &c, const AttnRows &a, AttnItem &it)
+{
+    int j;
+    block_slice(static_cast<int>(blockIdx.x), a.tiles * a.splits, c.Hkv, it.h, j);
+    if (it.h >= c.Hkv || j >= a.tiles * a.splits)
+        return false;
+    it.split = j % a.splits;
+    const int tile = a.tiles - 1 - j / a.splits;  // a sequence's last rows see the most keys
+    auto first = [&](int b) __attribute__((always_inline)) {
+        return static_cast<int>(static_cast<long long>(cache_cu(c, b)) * a.G / BM) + b;
+    };
+    int lo = 0, hi = c.B - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (first(mid) <= tile)
+            lo = mid;
+        else
+            hi = mid - 1;
+    }
+    it.b = lo;
+    it.s = cache_seq(c, lo);
+    it.rows = it.s.n * a.G;
+    it.row = (tile - first(lo)) * BM;
+    if (it.row < 0 || it.row >= it.rows)
+        return false;
+    const int last = min(it.row + BM, it.rows) - 1;
+    const int keys = min(it.s.len + last / a.G + 1, it.s.total);
+    const int tiles = (keys + BN - 1) / BN;
+    it.t0 = static_cast<int>(static_cast<long long>(tiles) * it.split / a.splits);
+    it.t1 = static_cast<int>(static_cast<long long>(tiles) * (it.split + 1) / a.splits);
+    return true;
+}
+
+// Direct loads of one tile of ROWS slots from slot j0 on, shared by NW waves.
+// RPI rows per instruction lie in one page.
+template <int D, int ROWS, int NW>
+struct PagedTile {
+    static constexpr int CPR = D / 8, RPI = 64 / CPR, PER = ROWS / RPI / NW;
+
+    static __device__ __forceinline__ void issue(const CacheView &c, const uint16_t *X, uint16_t *lds,
+                                                 const AttnItem &it, int j0, int wave, int lane)
+    {
+        const int w = NW == 1 ? 0 : __builtin_amdgcn_readfirstlane(wave);
+        const uint32_t slot0 = lds_base_sgpr(lds) + 1024u * static_cast<uint32_t>(w);
+        typedef const __attribute__((address_space(4))) int32_t *scalar_ptr;
+        const scalar_ptr table =
+            (scalar_ptr)(c.table + static_cast<long long>(it.b) * c.per);
+        const int lr = lane / CPR;
+        const int end = it.s.total - 1;
+#pragma unroll
+        for (int k = 0; k < PER; ++k) {
+            const int r0 = (w + NW * k) * RPI;  // row of the tile
+            // an instruction behind the last slot reads the last slot's rows
+            const int first = __builtin_amdgcn_readfirstlane(min(j0 + r0, end & -RPI));
+            const uint32_t id = min(static_cast<uint32_t>(table[first >> c.shift]),
+                                    static_cast<uint32_t>(c.pages - 1));
+            const uint16_t *base = X + cache_row(c, static_cast<int>(id), it.h, first) * D;
+            const int row = min(lr, end - first);
+            const int x = (lane % CPR) ^ swz<D>(r0 + lr);
+            dma_b128_off(base, static_cast<uint32_t>((row * D + x * 8) * 2), slot0 + 1024u * NW * k);
+        }
+    }
+};
+
+// The wave's 32 rows from `row` on: its query fragments, and the last slot the
+// lane's row sees.  Rows behind the last read the last one's.
+template <int D>
+__device__ __forceinline__ void load_rows(const CacheView &c, const AttnRows &a, const AttnItem &it,
+                                          int row, int l32, int g, bf16x8 (&qf)[D / 16], int &hi,
+                                          long long &out)
+{
+    const int r = min(row + l32, it.rows - 1), i = r / a.G, h = it.h * a.G + r - i * a.G;
+    hi = min(it.s.len + i, it.s.total - 1);
+    out = static_cast<long long>(it.s.row0 + i) * a.H + h;
+    const uint16_t *src = a.Q + (it.s.row0 + i) * a.ldq + h * D + g * 8;
+#pragma unroll
+    for (int kk = 0; kk < D / 16; ++kk)
+        qf[kk] = as_bf16x8(*reinterpret_cast<const u32x4 *>(src + kk * 16));
+}
+
+template <int D>
+__device__ __forceinline__ void tile_offsets(int lane, int (&koff)[D / 16], int (&voff)[D / 32][2])
+{
+    const int l32 = lane & 31, g = lane >> 5;
+#pragma unroll
+    for (int kk = 0; kk < D / 16; ++kk)
+        koff[kk] = tile_off<D>(l32, kk * 16 + g * 8);
+    const int q = lane >> 4, e = (lane & 15) >> 2, x = lane & 3;
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+        for (int hh = 0; hh < 2; ++hh)
+            voff[db][hh] = tile_off<D>(8 * hh + 4 * g + e, db * 32 + 16 * (q & 1) + 4 * x);
+}
+
+// O and the LSE of the lane's row (`ok`: it has one), or a split's part.
+template <int D>
+__device__ __forceinline__ void store_rows(const CacheView &c, const AttnRows &a, int split,
+                                           long long out, bool ok, int g, const f32x16 (&acc)[D / 32],
+                                           float m_i, float l_i)
+{
+    const float l = halves_sum(l_i);
+    if (a.splits == 1) {
+        const float inv = 1.0f / l;
+#pragma unroll
+        for (int db = 0; db < D / 32; ++db)
+            store_block_bf16(a.O + out * D + db * 32, acc[db], inv, g, ok);
+        if (ok && g == 0)
+            a.LSE[out] = (m_i + log2f(l)) * kLn2;
+        return;
+    }
+    const long long at = static_cast<long long>(split) * c.T * a.H + out;
+    const float inv = l == 0.f ? 0.f : 1.0f / l;  // no key in this part
+    if (!ok)
+        return;
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+        for (int rg = 0; rg < 4; ++rg) {
+            f32x4 v;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                v[e] = acc[db][4 * rg + e] * inv;
+            *reinterpret_cast<f32x4 *>(a.part_o + at * D + db * 32 + 8 * rg + 4 * g) = v;
+        }
+    if (g == 0)
+        a.part_lse[at] = m_i + log2f(l);
+}
+
+template <int D>
+__global__ void __launch_bounds__(256, 2) tile_kernel(AttnRows a, CacheView c)
+{
+    constexpr int BM = 128, BN = 64, TILE = BN * D, KK = D / 16, DB = D / 32;
+    __shared__ __attribute__((aligned(1024))) uint16_t lds[4 * TILE];
+    AttnItem it;
+    if (!attn_item<BM, BN>(c, a, it))
+        return;
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, l32 = lane & 31, g = lane >> 5;
+    const int row = it.row + wave * 32;
+    const bool on = __builtin_amdgcn_readfirstlane(row < it.rows);
+
+    bf16x8 qf[KK];
+    int hi;
+    long long out;
+    load_rows<D>(c, a, it, row, l32, g, qf, hi, out);
+    const int hi_first = __builtin_amdgcn_readlane(hi, 0), hi_last = __builtin_amdgcn_readlane(hi, 31);
+    int koff[KK], voff[DB][2];
+    tile_offsets<D>(lane, koff, voff);
+    f32x16 acc[DB];
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+        acc[db] = f32x16{};
+    float m_i = -INFINITY, l_i = 0.f;
+
+    auto issue = [&](int t, uint16_t *stage) __attribute__((always_inline)) {
+        PagedTile<D, BN, 4>::issue(c, a.K, stage, it, t * BN, wave, lane);
+        PagedTile<D, BN, 4>::issue(c, a.V, stage + TILE, it, t * BN, wave, lane);
+    };
+    auto step = [&](int t, auto bufc) __attribute__((always_inline)) {
+        constexpr int BUF = decltype(bufc)::value;
+        const uint16_t *kt = lds + BUF * 2 * TILE;
+        if (t + 1 < it.t1)
+            issue(t + 1, lds + (1 - BUF) * 2 * TILE);
+        const int j0 = t * BN;
+        if (on && j0 <= hi_last) {
+            if (j0 + BN - 1 <= hi_first)
+                attend_tile<D, 2, false>(kt, kt + TILE, qf, koff, voff, 0, g, a.scale_log2, acc, m_i,
+                                         l_i);
+            else
+                attend_tile<D, 2, true>(kt, kt + TILE, qf, koff, voff, hi - j0, g, a.scale_log2, acc,
+                                        m_i, l_i);
+        }
+        wait_vmem();
+        __syncthreads();
+    };
+    if (it.t0 < it.t1)
+        issue(it.t0, lds);
+    wait_vmem();
+    __syncthreads();
+    for (int t = it.t0; t < it.t1; t += 2) {
+        step(t, IC<0>{});
+        if (t + 1 < it.t1)
+            step(t + 1, IC<1>{});
+    }
+    if (on)
+        store_rows<D>(c, a, it.split, out, row + l32 < it.rows, g, acc, m_i, l_i);
+}
+
+template <int D>
+__global__ void __launch_bounds__(256) few_kernel(AttnRows a, CacheView c)
+{
+    constexpr int BN = 32, TILE = BN * D, KK = D / 16, DB = D / 32;
+    constexpr int LOADS = 2 * PagedTile<D, BN, 1>::PER;  // of a tile's K and V
+    __shared__ __attribute__((aligned(1024))) uint16_t lds[4 * 4 * TILE];
+    AttnItem it;
+    if (!attn_item<32, BN>(c, a, it))
+        return;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63, l32 = lane & 31, g = lane >> 5;
+    uint16_t *const mine = lds + wave * 4 * TILE;
+
+    int t = it.t0 + wave;
+    auto issue = [&](int tile, int buf) __attribute__((always_inline)) {
+        uint16_t *stage = mine + buf * 2 * TILE;
+        PagedTile<D, BN, 1>::issue(c, a.K, stage, it, tile * BN, 0, lane);
+        PagedTile<D, BN, 1>::issue(c, a.V, stage + TILE, it, tile * BN, 0, lane);
+    };
+    if (t < it.t1)
+        issue(t, 0);
+    if (t + 4 < it.t1)
+        issue(t + 4, 1);
+
+    bf16x8 qf[KK];
+    int hi;
+    long long out;
+    load_rows<D>(c, a, it, it.row, l32, g, qf, hi, out);
+    const int hi_first = __builtin_amdgcn_readlane(hi, 0);
+    int koff[KK], voff[DB][2];
+    tile_offsets<D>(lane, koff, voff);
+    f32x16 acc[DB];
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+        acc[db] = f32x16{};
+    float m_i = -INFINITY, l_i = 0.f;
+
+    int buf = 0;
+    for (; t < it.t1; t += 4, buf ^= 1) {
+        if (t + 4 < it.t1)
+            wait_vm<LOADS>();
+        else
+            wait_vm<0>();
+        const uint16_t *kt = mine + buf * 2 * TILE;
+        const int j0 = t * BN;
+        if (j0 + BN - 1 <= hi_first)
+            attend_tile<D, 1, false>(kt, kt + TILE, qf, koff, voff, 0, g, a.scale_log2, acc, m_i,
+                                     l_i);
+        else
+            attend_tile<D, 1, true>(kt, kt + TILE, qf, koff, voff, hi - j0, g, a.scale_log2, acc,
+                                    m_i, l_i);
+        if (t + 8 < it.t1) {
+            // the stage's last reads have returned before it is filled again
+            asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
+            issue(t + 8, buf);
+        }
+    }
+
+    // Waves 1 to 3 hand over through LDS (every wave is done with its stages).
+    constexpr int NS = 1 + 4 * DB;
+    float *x = reinterpret_cast<float *>(lds) + lane * 4;
+    __syncthreads();
+    if (wave > 0) {
+        float *y = x + (wave - 1) * NS * 256;
+        *reinterpret_cast<f32x4 *>(y) = f32x4{m_i, l_i, 0.f, 0.f};
+#pragma unroll
+        for (int r = 0; r < 4 * DB; ++r) {
+            f32x4 v;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                v[e] = acc[r >> 2][4 * (r & 3) + e];
+            *reinterpret_cast<f32x4 *>(y + (r + 1) * 256) = v;
+        }
+    }
+    __syncthreads();
+    if (wave > 0)
+        return;
+#pragma unroll 1
+    for (int o = 0; o < 3; ++o) {
+        const float *y = x + o * NS * 256;
+        const f32x4 ml = *reinterpret_cast<const f32x4 *>(y);
+        const float m = fmaxf(m_i, ml[0]), ref = m == -INFINITY ? 0.f : m;
+        const float a0 = fast_exp2(m_i - ref), a1 = fast_exp2(ml[0] - ref);
+        m_i = m;
+        l_i = l_i * a0 + ml[1] * a1;
+#pragma unroll
+        for (int r = 0; r < 4 * DB; ++r) {
+            const f32x4 v = *reinterpret_cast<const f32x4 *>(y + (r + 1) * 256);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                acc[r >> 2][4 * (r & 3) + e] = acc[r >> 2][4 * (r & 3) + e] * a0 + v[e] * a1;
+        }
+    }
+    store_rows<D>(c, a, it.split, out, it.row + l32 < it.rows, g, acc, m_i, l_i);
+}
+
+// A row's parts on a common maximum: D / 4 lanes per row.
+template <int D>
+__global__ void __launch_bounds__(256) join_kernel(AttnRows a, CacheView c)
+{
+    constexpr int LANES = D / 4, ROWS = 256 / LANES;
+    const long long n = static_cast<long long>(c.T) * a.H;
+    const long long row = static_cast<long long>(blockIdx.x) * ROWS + threadIdx.x / LANES;
+    const int x = threadIdx.x % LANES;
+    if (row < static_cast<long long>(cache_cu(c, 0)) * a.H ||
+        row >= static_cast<long long>(cache_cu(c, c.B)) * a.H)
+        return;
+    float m = -INFINITY;
+    for (int s = 0; s < a.splits; ++s)
+        m = fmaxf(m, a.part_lse[s * n + row]);
+    const float ref = m == -INFINITY ? 0.f : m;
+    float l = 0.f;
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+    for (int s = 0; s < a.splits; ++s) {
+        const float w = fast_exp2(a.part_lse[s * n + row] - ref);
+        l += w;
+        o += w * *reinterpret_cast<const f32x4 *>(a.part_o + (s * n + row) * D + 4 * x);
+    }
+    const float inv = 1.0f / l;
+    const bf16x4 y = pack4(o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
+    *reinterpret_cast<u32x2 *>(a.O + row * D + 4 * x) = __builtin_bit_cast(u32x2, y);
+    if (x == 0)
+        a.LSE[row] = (m + log2f(l)) * kLn2;
+}
+
+// ---------------------------------------------------------------------------
+
+struct WeightRows {
+    const uint16_t *Q, *K;
+    const float *LSE, *W;
+    float *Wout;
+    long long ldq;
+    int H, G;
+    float scale_log2;
+};
+
+// The weights of 128 slots of one key head, 32 per wave: S = Q K^T puts a slot
+// in a lane column, so a slot's sum stays in its lane; the sequence's rows pass
+// 32 at a time.
+template <int D>
+__global__ void __launch_bounds__(256) weights_kernel(WeightRows a, CacheView c)
+{
+    constexpr int KK = D / 16;
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, l32 = lane & 31, g = lane >> 5;
+    const int b = static_cast<int>(blockIdx.y) / c.Hkv, h = static_cast<int>(blockIdx.y) % c.Hkv;
+    const CacheSeq s = cache_seq(c, b);
+    const int key0 = (static_cast<int>(blockIdx.x) * 4 + wave) * 32, key = key0 + l32;
+    if (key0 >= s.total)
+        return;
+    const bool live = key < s.total;
+    const int at = min(key, s.total - 1);
+    const int id = max(cache_page(c, b, at), 0);
+    const uint16_t *kp = a.K + cache_row(c, id, h, at) * D + g * 8;
+    bf16x8 kf[KK];
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk)
+        kf[kk] = as_bf16x8(*reinterpret_cast<const u32x4 *>(kp + kk * 16));
+
+    const int rows = s.n * a.G;
+    // the first row that sees the lane's slot, and the wave's first slot
+    const int sees = static_cast<int>(min(static_cast<long long>(max(key - s.len, 0)) * a.G,
+                                          static_cast<long long>(rows)));
+    const int begin = __builtin_amdgcn_readlane(sees, 0), all = wave_max(sees);
+    float sum = 0.f;
+    for (int r0 = begin & ~31; r0 < rows; r0 += 32) {
+        const int r = min(r0 + l32, rows - 1), i = r / a.G, hq = h * a.G + r - i * a.G;
+        const uint16_t *q = a.Q + (s.row0 + i) * a.ldq + hq * D + g * 8;
+        const float lse2 = a.LSE[static_cast<long long>(s.row0 + i) * a.H + hq] * kLog2e;
+        f32x16 p = f32x16{};
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk)
+            p = mfma32(as_bf16x8(*reinterpret_cast<const u32x4 *>(q + kk * 16)), kf[kk], p);
+        const bool whole = r0 >= all && r0 + 32 <= rows;
+#pragma unroll
+        for (int x = 0; x < 16; ++x) {
+            const int rr = 8 * (x >> 2) + 4 * g + (x & 3);
+            const float w = fast_exp2(fmaf(p[x], a.scale_log2, -__shfl(lse2, rr)));
+            sum += whole || (r0 + rr >= sees && r0 + rr < rows) ? w : 0.f;
+        }
+    }
+    sum = halves_sum(sum);
+    if (live && g == 0) {
+        const long long w = (static_cast<long long>(b) * c.Hkv + h) * c.slots() + key;
+        a.Wout[w] = (key < s.len ? a.W[w] : 0.f) + sum;
+    }
+}
+
+CacheView view(const CacheShape &c)
+{
+    return CacheView{c.table, c.lens, c.cu_new, c.T, c.B, c.Hkv, c.pages, c.shift, c.per};
+}
+
+// How a call runs: by what the host knows of it (rows, sequences, slots).
+struct AttnPlan {
+    bool few;
+    int tiles, splits;
+};
+
+AttnPlan attn_plan(const CacheShape &c, int H)
+{
+    AttnPlan p;
+    const long long rows = static_cast<long long>(c.T) * (H / c.Hkv);
+    p.few = rows <= 64LL * c.B;
+    const int bm = p.few ? 32 : 128;
+    p.tiles = static_cast<int>(rows / bm) + c.B;
+    // workgroups with work in them, if the rows are spread evenly
+    const long long each = (rows + c.B - 1) / c.B;
+    const long long work = std::min<long long>(c.B, c.T) * ((each + bm - 1) / bm) * c.Hkv;
+    const long long slots = static_cast<long long>(c.per) << c.shift;
+    const long long most = std::max(1LL, slots / (p.few ? 256 : 512));
+    p.splits = static_cast<int>(std::clamp((p.few ? 1024 : 512) / work, 1LL, std::min(most, 64LL)));
+    return p;
+}
+
+template <int D>
+int launch_attn_d(const CacheAttnArgs &a)
+{
+    const AttnPlan p = attn_plan(a.c, a.H);
+    const CacheView c = view(a.c);
+    const size_t rows = static_cast<size_t>(a.c.T) * a.H;
+    float *ws = static_cast<float *>(a.workspace);
+    const float scale_log2 = kLog2e / std::sqrt(static_cast<float>(D));
+    const AttnRows r{static_cast<const uint16_t *>(a.Q), static_cast<const uint16_t *>(a.Kp),
+                     static_cast<const uint16_t *>(a.Vp), static_cast<uint16_t *>(a.O), a.LSE, ws,
+                     ws ? ws + p.splits * rows * D : nullptr, a.ldq, a.H, a.H / a.c.Hkv, p.tiles,
+                     p.splits, scale_log2};
+    hipStream_t st = static_cast<hipStream_t>(a.stream);
+    const long long items = static_cast<long long>(p.tiles) * p.splits * a.c.Hkv;
+    const unsigned grid = static_cast<unsigned>((items + kXcds - 1) / kXcds * kXcds);
+    hipError_t e = launch_kernel(p.few ? few_kernel<D> : tile_kernel<D>, dim3(grid), dim3(256), st, r,
+                                 c);
+    if (e == hipSuccess && p.splits > 1) {
+        constexpr int ROWS = 256 / (D / 4);
+        e = launch_kernel(join_kernel<D>, dim3(static_cast<unsigned>((rows + ROWS - 1) / ROWS)),
+                          dim3(256), st, r, c);
+    }
+    if (e == hipSuccess && a.Wout) {
+        const WeightRows w{r.Q, r.K, a.LSE, a.W, a.Wout, a.ldq, a.H, r.G, scale_log2};
+        e = launch_kernel(weights_kernel<D>,
+                          dim3(static_cast<unsigned>((c.slots() + 127) / 128),
+                               static_cast<unsigned>(a.c.B * a.c.Hkv)),
+                          dim3(256), st, w, c);
+    }
+    return e == hipSuccess ? DD_OK : DD_ERR_HIP;
+}
+
+}  // namespace
+
+size_t cache_attn_workspace_bytes(const CacheShape &c, int H)
+{
+    const AttnPlan p = attn_plan(c, H);
+    return p.splits == 1 ? 0
+                         : p.splits * static_cast<size_t>(c.T) * H * (c.D + 1) * sizeof(float);
+}
+
+int launch_cache_attn(const CacheAttnArgs &a)
+{
+    return a.c.D == 64 ? launch_attn_d<64>(a) : launch_attn_d<128>(a);
+}
+
+}  // namespace dd

@@ -185,6 +185,83 @@ struct WgradI8Args {
 size_t wgrad_i8_workspace_bytes(int T, int M, int N, int n);
 int launch_wgrad_i8(const WgradI8Args &a);
 
+// A paged cache (dd_cache.hpp) and a call's ragged chunk: pages of 1 << shift
+// slots, `per` of them per sequence in table [B][per].
+struct CacheShape {
+    const int32_t *table, *lens, *cu_new;
+    int T, B, Hkv, D, pages, shift, per;
+};
+
+// Q (optional) rotated to Qrot, K rotated and V into their slots (dd_cache.hip).
+struct CacheAppendArgs {
+    CacheShape c;
+    const void *Q, *K, *V;
+    void *Qrot, *Kp, *Vp;
+    int32_t *P;            // optional [B][Hkv][slots]
+    const int32_t *start;  // optional [B]
+    long long ldq, ldk, ldv;
+    int H;
+    double rope_base;  // 0: no rotation
+    void *stream;
+};
+int launch_cache_append(const CacheAppendArgs &a);
+
+// Attention of the chunk over the cache; W, Wout: [B][Hkv][slots] or NULL
+// (dd_cache_attn.hip).
+struct CacheAttnArgs {
+    CacheShape c;
+    const void *Q, *Kp, *Vp;
+    void *O;
+    float *LSE;
+    const float *W;
+    float *Wout;
+    long long ldq;
+    int H;
+    void *workspace, *stream;
+};
+size_t cache_attn_workspace_bytes(const CacheShape &c, int H);
+int launch_cache_attn(const CacheAttnArgs &a);
+
+// The `budget` slots of most weight stay (dd_cache.hip).
+struct CacheEvictArgs {
+    CacheShape c;
+    void *Kp, *Vp;
+    const float *W;
+    const int32_t *P, *seen;
+    float *Wout;
+    int32_t *Pout, *lens_out;
+    int budget, recent;
+    void *workspace, *stream;
+};
+size_t cache_evict_workspace_bytes(const CacheShape &c, int budget);
+int launch_cache_evict(const CacheEvictArgs &a);
+
+// Log probabilities of given tokens (dd_logprobs.hip); X and dX bf16 or fp32.
+struct LogprobArgs {
+    const void *X;
+    const int64_t *targets;
+    float *logp, *entropy, *lse, *top_logp;
+    int64_t *top_ids;
+    long long ldx;
+    int rows, V, top;
+    bool f32;
+    void *workspace, *stream;
+};
+size_t logprobs_workspace_bytes(int rows, int V, int top);
+int launch_logprobs(const LogprobArgs &a);
+
+struct LogprobBackArgs {
+    const void *X;
+    const int64_t *targets;
+    const float *lse, *entropy, *g_logp, *g_entropy, *g_lse;  // gradients optional
+    void *dX;
+    long long ldx, lddx;
+    int rows, V;
+    bool f32;
+    void *stream;
+};
+int launch_logprobs_bwd(const LogprobBackArgs &a);
+
 // Both return a dd_status value (DD_OK or DD_ERR_HIP).
 int launch_fwd(const FwdArgs &a);
 int launch_bwd(const BwdArgs &a);

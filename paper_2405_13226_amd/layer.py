@@ -173,6 +173,29 @@ class OpenLMBlock(torch.nn.Module):
                                  bits)
         return y.view(B, L, d)
 
+    @torch.no_grad()
+    def extend(self, x, cache, news):
+        """The block on a ragged chunk of new tokens: x [tokens, d] holds news[b]
+        rows of sequence b, one after the other; ``cache`` (a PagedCache of H
+        heads of d / H) receives their keys and values and holds what they
+        attend to.  Forward only."""
+        T, d = x.shape
+        rows = -(-T // 256) * 256  # the products take whole tiles of rows
+        if not T:
+            return x.clone()
+        xp = x.new_zeros((rows, d))
+        xp[:T] = x
+        a, _, _ = ops.layer_norm(xp, self.ln1_w, self.ln1_b, LN_EPS)
+        q, k, v = (t.view(rows, self.H, self.D) for t in
+                   ops.gemm_group(a, [self.w_qkv[:, i * d:(i + 1) * d] for i in range(3)]))
+        # (rows behind the chunk's last keep their zeros)
+        o, _ = cache.extend(q, k, v, news, self.rope_base, out=torch.zeros_like(q),
+                            lse=torch.empty((rows, self.H), dtype=torch.float32, device=x.device))
+        h = ops.gemm(o.view(rows, d), self.w_o, residual=xp)
+        m, _, _ = ops.layer_norm(h, self.ln2_w, self.ln2_b, LN_EPS)
+        _, _, g = ops.gemm_swiglu(m, self.w_1, self.w_3)
+        return ops.gemm(g, self.w_2, residual=h)[:T]
+
     def gemm_flops(self, tokens: int) -> int:
         """Forward FLOPs of the projections and the MLP (backward: twice this)."""
         d, h = self.d, self.hidden

@@ -1,0 +1,112 @@
+"""Log probabilities of given tokens from a model's logits, with the entropy
+and the most likely alternatives, and their gradient: what a loss is made of
+and what a text is scored with.
+
+Argument marshalling only, as in ``attention.py``; the kernels are behind
+dd_logprobs_fwd and dd_logprobs_bwd of include/dd_attn.h.
+
+Logits are [rows, V] in bf16 or fp32 with unit column stride (the columns of a
+wider, padded matrix are fine), targets int64 [rows]; a negative target is
+ignored.  Statistics are fp32.
+"""
+from __future__ import annotations
+
+import torch
+
+from .attention import _ptr as _p
+from .block_ops import _call, _need, _vec
+
+MAX_TOP = 64
+
+
+def _logits(t, name, dev=None):
+    """(rows, V, row stride, whether fp32)."""
+    if not isinstance(t, torch.Tensor) or t.dim() != 2:
+        raise ValueError(f"{name} must be a 2-D tensor")
+    if t.dtype not in (torch.bfloat16, torch.float32) or not t.is_cuda:
+        raise ValueError(f"{name} must be a bf16 or fp32 GPU tensor")
+    if dev is not None and t.device != dev:
+        raise ValueError(f"{name} is on {t.device}, not on {dev}")
+    rows, V = t.shape
+    if V < 1:
+        raise ValueError(f"the rows of {name} are empty")
+    if V > 1 and t.stride(1) != 1:
+        raise ValueError(f"{name} must have unit column stride")
+    return rows, V, t.stride(0) if rows > 1 else V, t.dtype is torch.float32
+
+
+def logprobs(logits, targets, top: int = 0):
+    """(logp, entropy, lse) of each row, fp32: the target's log probability, the
+    entropy, and the log of the sum of exponentials; with ``top`` also the log
+    probabilities (fp32 [rows, top]) and ids (int64) of the most likely tokens,
+    in order, equal ones by the lowest id."""
+    rows, V, ldx, f32 = _logits(logits, "logits")
+    dev = logits.device
+    _vec(targets, "targets", rows, torch.int64, dev)
+    if not 0 <= top <= min(V, MAX_TOP):
+        raise ValueError(f"top must be at most {min(V, MAX_TOP)} (got {top})")
+    logp, entropy, lse = (torch.empty(rows, dtype=torch.float32, device=dev) for _ in range(3))
+    best = ids = None
+    if top:
+        best = torch.empty((rows, top), dtype=torch.float32, device=dev)
+        ids = torch.empty((rows, top), dtype=torch.int64, device=dev)
+    if rows:
+        need = _need(dev, "dd_logprobs_workspace_bytes", rows, V, top)
+        ws = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
+        _call(dev, "dd_logprobs_fwd", _p(logits), ldx, f32, _p(targets), _p(logp), _p(entropy),
+              _p(lse), _p(best), _p(ids), rows, V, top, _p(ws), need)
+    return (logp, entropy, lse, best, ids) if top else (logp, entropy, lse)
+
+
+def logprobs_backward(logits, targets, lse, entropy, g_logp=None, g_entropy=None, g_lse=None,
+                      out=None):
+    """The gradient of the logits for the gradients of ``logprobs``' results
+    (fp32 [rows], each optional), of their type; ``out`` (optional) receives it
+    and may be the logits themselves."""
+    rows, V, ldx, f32 = _logits(logits, "logits")
+    dev = logits.device
+    _vec(targets, "targets", rows, torch.int64, dev)
+    for t, name in ((lse, "lse"), (entropy, "entropy"), (g_logp, "g_logp"),
+                    (g_entropy, "g_entropy"), (g_lse, "g_lse")):
+        if t is not None or name in ("lse", "entropy"):
+            _vec(t, name, rows, torch.float32, dev)
+    if out is None:
+        out = torch.empty((rows, V), dtype=logits.dtype, device=dev)
+    r, c, ldd, same = _logits(out, "out", dev)
+    if (r, c, same) != (rows, V, f32):
+        raise ValueError(f"out must be a {logits.dtype} tensor of shape {(rows, V)}")
+    if rows:
+        _call(dev, "dd_logprobs_bwd", _p(logits), ldx, f32, _p(targets), _p(lse), _p(entropy),
+              _p(g_logp), _p(g_entropy), _p(g_lse), _p(out), ldd, rows, V)
+    return out
+
+
+class LogProbFunction(torch.autograd.Function):
+    """Autograd wrapper: the forward keeps the logits and each row's lse and
+    entropy; alternatives carry no gradient."""
+
+    @staticmethod
+    def forward(ctx, logits, targets, top):
+        res = logprobs(logits, targets, top)
+        ctx.save_for_backward(logits, targets, res[2], res[1])
+        ctx.set_materialize_grads(False)
+        ctx.mark_non_differentiable(*res[3:])
+        return res
+
+    @staticmethod
+    def backward(ctx, g_logp, g_entropy, g_lse, *_):
+        logits, targets, lse, entropy = ctx.saved_tensors
+        if g_logp is None and g_entropy is None and g_lse is None:
+            return None, None, None
+        grads = [None if g is None else g.contiguous() for g in (g_logp, g_entropy, g_lse)]
+        return logprobs_backward(logits, targets, lse, entropy, *grads), None, None
+
+
+def token_logprobs(logits, targets, top: int = 0):
+    """Differentiable ``logprobs`` (in the logits, through logp, entropy and
+    lse).  A training loss with a z term:
+
+        logp, _, lse = token_logprobs(logits, targets)
+        loss = -logp.mean() + 1e-4 * lse.square().mean()
+    """
+    return LogProbFunction.apply(logits, targets, top)
