@@ -10,9 +10,15 @@
 // e^(x - m) and u = sum e^(x - m) (x - m) in fp32; m follows the largest logit
 // only when that passes it by more than kSlack (the sums stay far inside
 // fp32's range, and a change of reference costs a branch of the whole wave).
-// Alternatives: a wave keeps a list of its largest (logit, lowest index) pairs
-// as 64-bit keys and the key of rank k in it; a piece whose largest logit is
-// below that one is passed over, which after the first pieces are nearly all.
+// Alternatives: a thread also keeps its largest logit, the piece of 8 that has
+// it, and the largest of its other pieces.  Where k lanes of a wave hold a logit
+// of at least c, the row's k largest are no less than c: the largest such c of
+// the workgroup's waves is a floor that few logits reach.  The pieces that
+// reach it are read once more (one of a thread as a rule; all of them where its
+// other pieces reach it too), what is not below the floor goes into a list in
+// LDS as 64-bit keys of logit and index, and their ranks are the result.  A
+// list that does not fit (many equal logits at the floor) is found by k passes
+// instead, each for the largest key below the last.
 // Both join over a workgroup's waves, and over the workgroups of a row where
 // there are few rows.
 //
@@ -30,40 +36,45 @@ namespace dd {
 namespace {
 
 typedef uint32_t piece16 __attribute__((ext_vector_type(4), aligned(2)));
+typedef float f32x8 __attribute__((ext_vector_type(8)));
 typedef float piece16f __attribute__((ext_vector_type(4), aligned(4)));
 
 constexpr float kSlack = 10.0f;
-constexpr int kList = 128;  // keys of a wave's list: kMaxTop + 64 at most
+// Keys of a workgroup's list (without a floor there are below 8 k of them).
+template <int NT>
+constexpr int kList = NT < 256 ? 8 * NT : 2048;
 constexpr int kMaxTop = 64;
 
 // Eight logits from element `at` on, of which those below `end` exist; -inf
 // for the others.
-__device__ __forceinline__ void load_logits(const uint16_t *x, int at, int end, float (&f)[8])
+__device__ __forceinline__ f32x8 load_logits(const uint16_t *x, int at, int end)
 {
+    f32x8 f;
     if (at + 8 <= end) {
-        const u32x4 u = *reinterpret_cast<const piece16 *>(x + at);
-        unpack8(u, f);
+        const bf16x8 u = as_bf16x8(*reinterpret_cast<const piece16 *>(x + at));
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            f[i] = static_cast<float>(u[i]);
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
             f[i] = at + i < end ? __uint_as_float(static_cast<uint32_t>(x[at + i]) << 16) : -INFINITY;
     }
+    return f;
 }
-__device__ __forceinline__ void load_logits(const float *x, int at, int end, float (&f)[8])
+__device__ __forceinline__ f32x8 load_logits(const float *x, int at, int end)
 {
+    f32x8 f;
     if (at + 8 <= end) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const piece16f u = *reinterpret_cast<const piece16f *>(x + at + 4 * h);
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                f[4 * h + i] = u[i];
-        }
+        const piece16f a = *reinterpret_cast<const piece16f *>(x + at);
+        const piece16f b = *reinterpret_cast<const piece16f *>(x + at + 4);
+        f = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
             f[i] = at + i < end ? x[at + i] : -INFINITY;
     }
+    return f;
 }
 __device__ __forceinline__ float load_logit(const uint16_t *x, long long at)
 {
@@ -107,66 +118,15 @@ __device__ __forceinline__ float key_logit(uint64_t key)
     return __uint_as_float(k >> 31 ? k & 0x7fffffffu : k ? ~k : 0x7fc00000u);
 }
 
-// A wave's list: `n` keys, of which none is at or below `floor` (its key of
-// rank k once there are k).
-struct Best {
-    uint64_t *keys;
-    int n, k;
-    uint64_t floor;
-    float logit;  // of floor; -inf before
-};
-
-// Keeps the k largest keys, in order.
-__device__ __forceinline__ void compact(Best &t)
+// The largest c that at least k lanes hold a `x` of; 0 if none.
+__device__ __forceinline__ uint32_t wave_floor(uint32_t x, int k)
 {
-    const int lane = threadIdx.x & 63;
-    uint64_t mine[kList / 64];
-    int rank[kList / 64] = {};
+    uint32_t c = 0;
 #pragma unroll
-    for (int i = 0; i < kList / 64; ++i)
-        mine[i] = i * 64 + lane < t.n ? t.keys[i * 64 + lane] : 0u;
-    for (int j = 0; j < t.n; ++j) {
-        const uint64_t other = t.keys[j];
-#pragma unroll
-        for (int i = 0; i < kList / 64; ++i)
-            rank[i] += other > mine[i] ? 1 : 0;
-    }
-    __builtin_amdgcn_wave_barrier();
-#pragma unroll
-    for (int i = 0; i < kList / 64; ++i)
-        if (i * 64 + lane < t.n && rank[i] < t.k)
-            t.keys[rank[i]] = mine[i];
-    __builtin_amdgcn_wave_barrier();
-    if (t.n >= t.k) {
-        t.n = t.k;
-        t.floor = t.keys[t.k - 1];
-        t.logit = key_logit(t.floor);
-        if (t.logit != t.logit)
-            t.logit = -INFINITY;
-    }
-}
-
-__device__ __forceinline__ void offer(Best &t, const float (&f)[8], int at, int end)
-{
-    const int lane = threadIdx.x & 63;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const uint64_t key = pair_key(f[i], at + i);
-        const bool add = at + i < end && key > t.floor;
-        const uint64_t who = __ballot(add);
-        if (who == 0)
-            continue;
-        const int more = __popcll(who);
-        if (t.n + more > kList)
-            compact(t);
-        if (add)
-            t.keys[t.n + __popcll(who & ((1ull << lane) - 1))] = key;
-        __builtin_amdgcn_wave_barrier();
-        t.n += more;
-    }
-    // a floor as soon as there is one
-    if (t.n >= t.k && (t.floor == 0 || t.n > kList - 64))
-        compact(t);
+    for (int b = 31; b >= 0; --b)
+        if (__popcll(__ballot(x >= (c | 1u << b))) >= k)
+            c |= 1u << b;
+    return c;
 }
 
 struct LogitRows {
@@ -209,6 +169,7 @@ __device__ __forceinline__ void rank_keys(const LogitRows &a, int row, const uin
     for (int i = threadIdx.x; i < n; i += blockDim.x) {
         const uint64_t key = keys[i];
         int rank = 0;
+#pragma unroll 8
         for (int j = 0; j < n; ++j)
             rank += keys[j] > key ? 1 : 0;
         if (key == 0 || rank >= a.top)
@@ -227,9 +188,11 @@ template <typename T, int NT, bool TOP>
 __global__ void __launch_bounds__(NT) logits_kernel(LogitRows a)
 {
     constexpr int NW = NT / 64;
-    __shared__ uint64_t lists[TOP ? NW * kList : 1];
-    __shared__ uint64_t tops[TOP ? NW * kMaxTop : 1];
+    __shared__ uint64_t keys[TOP ? kList<NT> : 1];
+    __shared__ int some[TOP ? NT : 1], full[TOP ? NT : 1];
     __shared__ Sums waves[NW];
+    __shared__ uint32_t floors[NW];
+    __shared__ int n_some, n_full, n_keys;
     __shared__ RowLog row_log;
     const int row = static_cast<int>(blockIdx.x / a.splits);
     const int split = static_cast<int>(blockIdx.x % a.splits);
@@ -239,13 +202,15 @@ __global__ void __launch_bounds__(NT) logits_kernel(LogitRows a)
     const long long pieces = (a.V + 7) / 8;
     const int lo = static_cast<int>(pieces * split / a.splits) * 8;
     const int hi = min(static_cast<int>(pieces * (split + 1) / a.splits) * 8, a.V);
+    if (TOP && tid == 0)
+        n_some = n_full = n_keys = 0;
 
     Sums s{-FLT_MAX, 0.f, 0.f};
-    Best best{lists + (TOP ? wave * kList : 0), 0, a.top, 0, -INFINITY};
-    for (int w0 = lo + wave * 512; w0 < hi; w0 += NT * 8) {
-        const int at = w0 + lane * 8;
-        float f[8];
-        load_logits(x, at, hi, f);
+    // the largest logit (a NaN if there are none but NaN), its piece, and the
+    // largest of the other pieces
+    float most = NAN, next = NAN;
+    int where = 0;
+    auto take = [&](f32x8 f) __attribute__((always_inline)) {
         const float mx = fmaxf(fmaxf(fmaxf(f[0], f[1]), fmaxf(f[2], f[3])),
                                fmaxf(fmaxf(f[4], f[5]), fmaxf(f[6], f[7])));
         if (__any(mx > s.m + kSlack))
@@ -256,36 +221,113 @@ __global__ void __launch_bounds__(NT) logits_kernel(LogitRows a)
             s.s += e;
             s.u = fmaf(e, fmaxf(d, kFar), s.u);
         }
-        if constexpr (TOP)
-            if (__any(!(mx < best.logit)))
-                offer(best, f, at, hi);
+        return mx;
+    };
+    auto note = [&](float mx, int at) __attribute__((always_inline)) {
+        const bool more = !(mx <= most);
+        next = more ? most : fmaxf(next, mx);
+        where = more ? at : where;
+        most = more ? fmaxf(most, mx) : most;
+    };
+    // (two pieces of a thread are on their way at once)
+    for (int at = lo + tid * 8; at < hi; at += NT * 16) {
+        const f32x8 f0 = load_logits(x, at, hi), f1 = load_logits(x, at + NT * 8, hi);
+        const float m0 = take(f0), m1 = take(f1);
+        if constexpr (TOP) {
+            note(m0, at);
+            if (at + NT * 8 < hi)
+                note(m1, at + NT * 8);
+        }
     }
+    const uint32_t reach = TOP ? static_cast<uint32_t>(pair_key(most, 0) >> 32) : 0u;
 #pragma unroll
     for (int o = 32; o >= 1; o >>= 1)
         s = joined(s, Sums{__shfl_xor(s.m, o), __shfl_xor(s.s, o), __shfl_xor(s.u, o)});
+    if constexpr (TOP) {
+        const uint32_t c = wave_floor(reach, a.top);
+        if (lane == 0)
+            floors[wave] = c;
+    }
     if (lane == 0)
         waves[wave] = s;
-    if constexpr (TOP) {
-        compact(best);
-        if (lane < a.top)
-            tops[wave * a.top + lane] = lane < best.n ? best.keys[lane] : 0;
-    }
     __syncthreads();
     const long long part = static_cast<long long>(row) * a.splits + split;
-    if (tid == 0) {
-        for (int i = 1; i < NW; ++i)
-            s = joined(s, waves[i]);
-        if (a.splits == 1)
-            row_log = finish_row<T>(a, row, s);
-        else
-            a.part[part] = s;
+    if (wave == 0) {
+        s = waves[lane % NW];
+#pragma unroll
+        for (int o = NW / 2; o >= 1; o >>= 1)
+            s = joined(s, Sums{__shfl_xor(s.m, o), __shfl_xor(s.s, o), __shfl_xor(s.u, o)});
+        if (lane == 0) {
+            if (a.splits == 1)
+                row_log = finish_row<T>(a, row, s);
+            else
+                a.part[part] = s;
+        }
     }
     if constexpr (TOP) {
+        uint32_t floor = floors[0];
+#pragma unroll
+        for (int i = 1; i < NW; ++i)
+            floor = max(floor, floors[i]);
+        if (lo + tid * 8 < hi && reach >= floor) {
+            if (floor == 0 || static_cast<uint32_t>(pair_key(next, 0) >> 32) >= floor)
+                full[atomicAdd(&n_full, 1)] = tid;
+            else
+                some[atomicAdd(&n_some, 1)] = where;
+        }
         uint64_t *list = a.splits == 1 ? nullptr : a.part_keys + part * a.top;
         if (list && tid < a.top)
             list[tid] = 0;  // a part may have fewer
         __syncthreads();
-        rank_keys(a, row, tops, NW * a.top, row_log, list);
+        const int steps = (hi - lo + NT * 8 - 1) / (NT * 8);
+        for (int i = tid; i < n_some + n_full * steps; i += NT) {
+            const int j = i - n_some;
+            const int at = j < 0 ? some[i] : lo + (j / n_full * NT + full[j % n_full]) * 8;
+            const f32x8 f = load_logits(x, at, hi);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const uint64_t key = pair_key(f[e], at + e);
+                if (at + e < hi && static_cast<uint32_t>(key >> 32) >= floor) {
+                    const int k = atomicAdd(&n_keys, 1);
+                    if (k < kList<NT>)
+                        keys[k] = key;
+                }
+            }
+        }
+        __syncthreads();
+        int n = n_keys;
+        if (n > kList<NT>) {
+            // k passes: each thread's largest key below the last, then the row's
+            uint64_t last = ~0ull;
+            for (n = 0; n < a.top; ++n) {
+                uint64_t best = 0;
+                for (int at = lo + tid * 8; at < hi; at += NT * 8) {
+                    const f32x8 f = load_logits(x, at, hi);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const uint64_t key = pair_key(f[j], at + j);
+                        if (at + j < hi && key < last && key > best)
+                            best = key;
+                    }
+                }
+#pragma unroll
+                for (int o = 32; o >= 1; o >>= 1) {
+                    const uint64_t other = __shfl_xor(static_cast<unsigned long long>(best), o);
+                    best = other > best ? other : best;
+                }
+                __syncthreads();  // the pass before has read
+                if (lane == 0)
+                    keys[kMaxTop + wave] = best;
+                __syncthreads();
+                last = keys[kMaxTop];
+                for (int i = 1; i < NW; ++i)
+                    last = keys[kMaxTop + i] > last ? keys[kMaxTop + i] : last;
+                if (tid == 0)
+                    keys[n] = last;
+            }
+            __syncthreads();
+        }
+        rank_keys(a, row, keys, n, row_log, list);
     }
 }
 
@@ -326,11 +368,25 @@ struct GradRows {
     int rows, V, blocks;  // workgroups per row
 };
 
-__device__ __forceinline__ void store_grads(uint16_t *y, int at, int end, const float (&f)[8])
+// STREAM: past the caches.
+template <bool STREAM, typename V>
+__device__ __forceinline__ void store_piece(V *p, V v)
 {
-    const u32x4 u = pack8f(f);
+    if constexpr (STREAM)
+        __builtin_nontemporal_store(v, p);
+    else
+        *p = v;
+}
+template <bool STREAM>
+__device__ __forceinline__ void store_grads(uint16_t *y, int at, int end, f32x8 f)
+{
+    bf16x8 b;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        b[i] = static_cast<__bf16>(f[i]);
+    const piece16 u = __builtin_bit_cast(u32x4, b);
     if (at + 8 <= end) {
-        *reinterpret_cast<piece16 *>(y + at) = u;
+        store_piece<STREAM>(reinterpret_cast<piece16 *>(y + at), u);
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
@@ -338,13 +394,14 @@ __device__ __forceinline__ void store_grads(uint16_t *y, int at, int end, const 
                 y[at + i] = static_cast<uint16_t>(u[i >> 1] >> 16 * (i & 1));
     }
 }
-__device__ __forceinline__ void store_grads(float *y, int at, int end, const float (&f)[8])
+template <bool STREAM>
+__device__ __forceinline__ void store_grads(float *y, int at, int end, f32x8 f)
 {
     if (at + 8 <= end) {
 #pragma unroll
         for (int h = 0; h < 2; ++h)
-            *reinterpret_cast<piece16f *>(y + at + 4 * h) =
-                piece16f{f[4 * h], f[4 * h + 1], f[4 * h + 2], f[4 * h + 3]};
+            store_piece<STREAM>(reinterpret_cast<piece16f *>(y + at + 4 * h),
+                                piece16f{f[4 * h], f[4 * h + 1], f[4 * h + 2], f[4 * h + 3]});
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
@@ -353,12 +410,16 @@ __device__ __forceinline__ void store_grads(float *y, int at, int end, const flo
     }
 }
 
+// Gradients past this size leave the last-level cache (256 MB) before anyone
+// reads them: they are stored past it.
+constexpr long long kStreamBytes = 256LL << 20;
 constexpr int kGradPieces = 4;  // of 8 logits per thread
 
-template <typename T>
+template <typename T, bool STREAM>
 __global__ void __launch_bounds__(256) logits_grad_kernel(GradRows a)
 {
-    const int row = static_cast<int>(blockIdx.x / a.blocks);
+    // from the last row on: what the forward read last is still in the cache
+    const int row = a.rows - 1 - static_cast<int>(blockIdx.x / a.blocks);
     const int block = static_cast<int>(blockIdx.x % a.blocks);
     const T *x = static_cast<const T *>(a.X) + row * a.ldx;
     T *y = static_cast<T *>(a.dX) + row * a.lddx;
@@ -368,12 +429,12 @@ __global__ void __launch_bounds__(256) logits_grad_kernel(GradRows a)
     const float g_h = a.g_entropy ? a.g_entropy[row] : 0.f;
     const float g_p = (a.g_lse ? a.g_lse[row] : 0.f) - g_t;
     const int64_t given = g_t != 0.f ? t : -1;
-    float f[kGradPieces][8];
+    f32x8 f[kGradPieces];
     const int at0 = (block * kGradPieces * 256 + static_cast<int>(threadIdx.x)) * 8;
 #pragma unroll
     for (int k = 0; k < kGradPieces; ++k)
         if (at0 + k * 2048 < a.V)
-            load_logits(x, at0 + k * 2048, a.V, f[k]);
+            f[k] = load_logits(x, at0 + k * 2048, a.V);
 #pragma unroll
     for (int k = 0; k < kGradPieces; ++k) {
         const int at = at0 + k * 2048;
@@ -385,14 +446,27 @@ __global__ void __launch_bounds__(256) logits_grad_kernel(GradRows a)
             const float v = p * (g_p - g_h * (fmaxf(d, kFar) + h));
             f[k][i] = at + i == given ? v + g_t : v;
         }
-        store_grads(y, at, a.V, f[k]);
+        store_grads<STREAM>(y, at, a.V, f[k]);
     }
+}
+
+// Few rows: a row is one workgroup of 1024 threads, or several of them where it
+// is long.  Otherwise it is a workgroup of 256, or a wave.
+constexpr int kFewRows = 512;
+
+int row_threads(int rows, int V, int top)
+{
+    if (rows <= kFewRows && V > 8192)
+        return 1024;
+    return V <= (top ? 2048 : 16384) ? 64 : 256;
 }
 
 int split_rows(int rows, int V, int top)
 {
-    const int most = std::min({kMaxParts, V / 4096, top ? kMaxPartKeys / top : kMaxParts});
-    return std::clamp(512 / rows, 1, std::max(most, 1));
+    if (rows > kFewRows)
+        return 1;
+    const int most = std::min(top ? kMaxPartKeys / top : kMaxParts, kFewRows / rows);
+    return std::clamp((V + 65535) / 65536, 1, most);
 }
 
 template <typename T>
@@ -405,8 +479,12 @@ int launch_logprobs_t(const LogprobArgs &a)
                       reinterpret_cast<Sums *>(keys + parts * a.top), keys, a.ldx, a.rows, a.V,
                       a.top, splits};
     hipStream_t st = static_cast<hipStream_t>(a.stream);
-    hipError_t e = launch_kernel(a.top ? logits_kernel<T, 256, true> : logits_kernel<T, 256, false>,
-                                 dim3(static_cast<unsigned>(parts)), dim3(256), st, r);
+    const int nt = row_threads(a.rows, a.V, a.top);
+    auto kern = nt == 1024 ? (a.top ? logits_kernel<T, 1024, true> : logits_kernel<T, 1024, false>)
+                : nt == 256 ? (a.top ? logits_kernel<T, 256, true> : logits_kernel<T, 256, false>)
+                            : (a.top ? logits_kernel<T, 64, true> : logits_kernel<T, 64, false>);
+    hipError_t e = launch_kernel(kern, dim3(static_cast<unsigned>(parts)),
+                                 dim3(static_cast<unsigned>(nt)), st, r);
     if (e == hipSuccess && splits > 1)
         e = launch_kernel(join_logits_kernel<T>, dim3(static_cast<unsigned>(a.rows)), dim3(256), st,
                           r);
@@ -431,8 +509,10 @@ int launch_logprobs_bwd(const LogprobBackArgs &a)
     const int blocks = (a.V + 2048 * kGradPieces - 1) / (2048 * kGradPieces);
     const GradRows r{a.X, a.targets, a.lse, a.entropy, a.g_logp, a.g_entropy, a.g_lse, a.dX, a.ldx,
                      a.lddx, a.rows, a.V, blocks};
+    const bool stream = static_cast<long long>(a.rows) * a.V * (a.f32 ? 4 : 2) > kStreamBytes;
     const hipError_t e = launch_kernel(
-        a.f32 ? logits_grad_kernel<float> : logits_grad_kernel<uint16_t>,
+        a.f32 ? (stream ? logits_grad_kernel<float, true> : logits_grad_kernel<float, false>)
+              : (stream ? logits_grad_kernel<uint16_t, true> : logits_grad_kernel<uint16_t, false>),
         dim3(static_cast<unsigned>(a.rows) * static_cast<unsigned>(blocks)), dim3(256),
         static_cast<hipStream_t>(a.stream), r);
     return e == hipSuccess ? DD_OK : DD_ERR_HIP;

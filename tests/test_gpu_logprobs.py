@@ -103,6 +103,42 @@ def test_ties_order_and_extremes(cuda, dtype):
     check_forward(x, t, 40, cuda)
 
 
+# a wave, a workgroup of 256 and of 1024, several of them per row
+@pytest.mark.parametrize("rows,V", [(5, 2000), (5, 8000), (5, 30000), (5, 150000), (600, 20000)])
+def test_equal_logits_and_neighbours(cuda, rows, V):
+    """Lists of alternatives that do not fit (all logits equal, or two values),
+    alternatives that lie next to each other, and ones of one thread's pieces."""
+    log(f"logprobs: equal logits {rows} x {V}")
+    x = torch.zeros(rows, V)
+    x[1] = torch.arange(V) % 2
+    x[2:4] = torch.randn(2, V).clamp(max=3)
+    x[2, V // 2:V // 2 + 30] = 8 + torch.arange(30) % 7
+    for step in (64 * 8, 256 * 8, 1024 * 8):
+        x[3, 8:8 + step * 12:step][:12] = 9.0
+    x[4:] = torch.randn(rows - 4, 1)
+    for dtype in (torch.bfloat16, torch.float32):
+        y = x.to(dtype)
+        for top in (1, 20, 64):
+            check_forward(y[:5], torch.zeros(5, dtype=torch.int64), top, cuda)
+        ids = dd.logprobs(y.to(cuda), torch.zeros(rows, dtype=torch.int64, device=cuda), top=9)[4]
+        assert torch.equal(ids[:4].cpu(), O.logprobs(y[:4], torch.zeros(4).long(), 9)[4])
+        assert (ids[4:] == torch.arange(9, device=cuda)).all()
+
+
+def test_large_gradients_are_the_small_ones(cuda):
+    """Past the size from which gradients are stored past the caches."""
+    log("logprobs: gradients of more than 256 MB")
+    for dtype, rows in ((torch.float32, 1400), (torch.bfloat16, 2800)):
+        x = torch.randn(rows, 50277, device=cuda).to(dtype)
+        t = torch.arange(rows, device=cuda)
+        _, h, lse = dd.logprobs(x, t)
+        g = torch.randn(3, rows, device=cuda)
+        all_rows = dd.logprobs_backward(x, t, lse, h, *g)
+        for part in (slice(0, rows // 2), slice(rows // 2, rows)):
+            few = dd.logprobs_backward(x[part], t[part], lse[part], h[part], *(y[part] for y in g))
+            assert torch.equal(all_rows[part], few)
+
+
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 @pytest.mark.parametrize("rows,V", [(2, 700), (2, 9000)])
 def test_rows_out_of_the_ordinary(cuda, rows, V, dtype):
