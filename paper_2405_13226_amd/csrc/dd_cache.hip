@@ -15,7 +15,11 @@
 // order, and no more of them than the result needs.
 //   select: one workgroup per (sequence, head) finds the weight of rank
 //           `budget` by three histograms of 11, 11 and 10 bits of the ordered
-//           weights, then lists holes and survivors in slot order
+//           weights, then lists holes and survivors in slot order.  A thread
+//           holds 16 consecutive slots in registers: the weights are read once,
+//           and a prefix sum over the workgroup orders equal ones, another the
+//           lists.  (Beyond 16,384 slots per sequence they are read again for
+//           each histogram and for the lists.)
 //   move:   the listed rows
 #include "dd_cache.hpp"
 #include "dd_internal.h"
@@ -122,7 +126,8 @@ struct EvictRows {
     int budget, recent, list;
 };
 
-constexpr int kSelectThreads = 1024;
+typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
+typedef int32_t i32x4_any __attribute__((ext_vector_type(4), aligned(4)));
 
 // Weights in order as unsigned numbers: a NaN below all, the slots that stay
 // in any case above all.
@@ -133,10 +138,11 @@ __device__ __forceinline__ uint32_t weight_key(float w, bool stays)
     return stays ? 0xffffffffu : w != w ? 0u : k;
 }
 
-// Exclusive prefix sum of x over the workgroup's threads, and its total.
+// Exclusive prefix sum of x over the workgroup's NT threads, and its total.
+template <int NT>
 __device__ __forceinline__ uint32_t block_prefix(uint32_t x, uint32_t *waves, uint32_t &total)
 {
-    constexpr int NW = kSelectThreads / 64;
+    constexpr int NW = NT / 64;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     uint32_t s = x;
 #pragma unroll
@@ -159,11 +165,14 @@ __device__ __forceinline__ uint32_t block_prefix(uint32_t x, uint32_t *waves, ui
     return before + s - x;
 }
 
-__global__ void __launch_bounds__(kSelectThreads)
-select_kernel(EvictRows a, CacheView c)
+// A thread holds HELD consecutive slots; ONE: the sequence's slots are at most
+// NT * HELD.
+template <int NT, int HELD, bool ONE>
+__global__ void __launch_bounds__(NT) select_kernel(EvictRows a, CacheView c)
 {
-    __shared__ uint32_t hist[2048];
-    __shared__ uint32_t waves[kSelectThreads / 64];
+    constexpr int BINS = 2048, SPAN = NT * HELD;
+    __shared__ uint32_t hist[BINS];
+    __shared__ uint32_t waves[NT / 64];
     __shared__ uint32_t found[2];
     const int bh = static_cast<int>(blockIdx.x), b = bh / c.Hkv, tid = threadIdx.x;
     const int n = min(max(c.lens[b], 0), c.slots());
@@ -176,43 +185,88 @@ select_kernel(EvictRows a, CacheView c)
         if (tid == 0)
             a.count[bh] = 0;
         if (Wout != W || Pout != P)
-            for (int j = tid; j < n; j += kSelectThreads) {
+            for (int j = tid; j < n; j += NT) {
                 Wout[j] = W[j];
                 Pout[j] = P[j];
             }
         return;
     }
-    const long long first = static_cast<long long>(a.seen[b]) - a.recent;
-    auto key_of = [&](int j) __attribute__((always_inline)) {
-        return weight_key(W[j], P[j] >= first);
+    // the first position that stays in any case (or the lowest number)
+    const int first = static_cast<int>(
+        max(static_cast<long long>(a.seen[b]) - a.recent, static_cast<long long>(INT32_MIN)));
+    const bool copy = Wout != W || Pout != P;
+
+    // The keys of the thread's slots from j0 on; those below the budget are
+    // copied on the way (evicted ones are written over by the moves).
+    uint32_t key[HELD];
+    auto load = [&](int j0, bool keep) __attribute__((always_inline)) {
+        f32x4_any w[HELD / 4];
+        i32x4_any p[HELD / 4];
+#pragma unroll
+        for (int q = 0; q < HELD / 4; ++q) {  // (slots: a multiple of 16)
+            const int j = min(j0 + 4 * q, c.slots() - 4);
+            w[q] = *reinterpret_cast<const f32x4_any *>(W + j);
+            p[q] = *reinterpret_cast<const i32x4_any *>(P + j);
+        }
+#pragma unroll
+        for (int q = 0; q < HELD / 4; ++q) {
+            const int j = j0 + 4 * q;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                key[4 * q + e] = weight_key(w[q][e], p[q][e] >= first);
+            if (!keep)
+                continue;
+            if (j + 4 <= a.budget) {
+                *reinterpret_cast<f32x4_any *>(Wout + j) = w[q];
+                *reinterpret_cast<i32x4_any *>(Pout + j) = p[q];
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (j + e < a.budget) {
+                        Wout[j + e] = w[q][e];
+                        Pout[j + e] = p[q][e];
+                    }
+            }
+        }
     };
 
     // The key of rank `budget` (counted from the largest), from its leading
     // bits on, and how many keys equal to it stay.
     uint32_t prefix = 0, need = static_cast<uint32_t>(a.budget);
+    if (ONE && tid * HELD < n)
+        load(tid * HELD, copy);
+#pragma unroll
     for (int part = 0; part < 3; ++part) {
         const int low = part == 0 ? 21 : part == 1 ? 10 : 0, bits = part == 2 ? 10 : 11;
         const uint32_t mask = (1u << bits) - 1;
-        for (int i = tid; i < 2048; i += kSelectThreads)
+        for (int i = tid; i < BINS; i += NT)
             hist[i] = 0;
         __syncthreads();
-        for (int j = tid; j < n; j += kSelectThreads) {
-            const uint32_t k = key_of(j);
-            if (part == 0 || k >> (low + bits) == prefix)
-                atomicAdd(&hist[(k >> low) & mask], 1u);
+        for (int j0 = tid * HELD; j0 < n; j0 += SPAN) {
+            if constexpr (!ONE)
+                load(j0, false);
+#pragma unroll
+            for (int e = 0; e < HELD; ++e)
+                if (j0 + e < n && (part == 0 || key[e] >> (low + bits) == prefix))
+                    atomicAdd(&hist[(key[e] >> low) & mask], 1u);
         }
         __syncthreads();
-        // bins from the largest key down, two per thread
-        const int i0 = 2047 - 2 * tid;
-        const uint32_t h0 = hist[i0], h1 = hist[i0 - 1];
-        uint32_t all;
-        const uint32_t above = block_prefix(h0 + h1, waves, all);
-        if (above < need && need <= above + h0) {
-            found[0] = i0;
-            found[1] = need - above;
-        } else if (above + h0 < need && need <= above + h0 + h1) {
-            found[0] = i0 - 1;
-            found[1] = need - above - h0;
+        // bins from the largest key down, some per thread
+        constexpr int EACH = BINS / NT;
+        uint32_t h[EACH], sum = 0;
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+            h[i] = hist[BINS - 1 - tid * EACH - i];
+            sum += h[i];
+        }
+        uint32_t all, above = block_prefix<NT>(sum, waves, all);
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+            if (above < need && need <= above + h[i]) {
+                found[0] = BINS - 1 - tid * EACH - i;
+                found[1] = need - above;
+            }
+            above += h[i];
         }
         __syncthreads();
         prefix = prefix << bits | found[0];
@@ -224,28 +278,43 @@ select_kernel(EvictRows a, CacheView c)
     int32_t *to = a.to + static_cast<long long>(bh) * a.list;
     int32_t *from = a.from + static_cast<long long>(bh) * a.list;
     uint32_t equal = 0, holes = 0, extra = 0;  // so far
-    for (int j0 = 0; j0 < n; j0 += kSelectThreads) {
-        const int j = j0 + tid;
-        const bool in = j < n;
-        const uint32_t k = in ? key_of(j) : 0u;
-        const bool eq = in && k == prefix;
-        uint32_t all;
-        const uint32_t before = equal + block_prefix(eq ? 1u : 0u, waves, all);
+    for (int s0 = 0; s0 < n; s0 += SPAN) {
+        const int j0 = s0 + tid * HELD;
+        if constexpr (!ONE)
+            load(min(j0, c.slots() - HELD), copy && j0 < n);
+        uint32_t eq = 0, all;
+        if (j0 < n)
+#pragma unroll
+            for (int e = 0; e < HELD; ++e)
+                eq += j0 + e < n && key[e] == prefix ? 1u : 0u;
+        uint32_t before = equal + block_prefix<NT>(eq, waves, all);
         equal += all;
-        const bool keep = in && (k > prefix || (eq && before < need));
-        const bool hole = in && !keep && j < a.budget, moved = keep && j >= a.budget;
-        // holes and moved rows of a step: below 2^16 of each
-        const uint32_t place = block_prefix((hole ? 1u : 0u) | (moved ? 1u << 16 : 0u), waves, all);
-        if (hole)
-            to[holes + (place & 0xffffu)] = j;
-        if (moved)
-            from[extra + (place >> 16)] = j;
+        uint32_t hole = 0, moved = 0;  // bits of the thread's slots
+        if (j0 < n) {
+            uint32_t keep = 0;
+#pragma unroll
+            for (int e = 0; e < HELD; ++e) {
+                const bool same = key[e] == prefix;
+                keep |= (key[e] > prefix || (same && before < need) ? 1u : 0u) << e;
+                before += same ? 1u : 0u;
+            }
+            auto below = [&](int end) __attribute__((always_inline)) {
+                return (1u << min(max(end - j0, 0), HELD)) - 1;
+            };
+            hole = ~keep & below(a.budget);  // (the budget is below n)
+            moved = keep & below(n) & ~below(a.budget);
+        }
+        // (of either at most SPAN <= 2^14 in a step)
+        const uint32_t place =
+            block_prefix<NT>(__popc(hole) | __popc(moved) << 16, waves, all);
+        uint32_t at = holes + (place & 0xffffu);
+        for (; hole; hole &= hole - 1)
+            to[at++] = j0 + __ffs(hole) - 1;
+        at = extra + (place >> 16);
+        for (; moved; moved &= moved - 1)
+            from[at++] = j0 + __ffs(moved) - 1;
         holes += all & 0xffffu;
         extra += all >> 16;
-        if (keep && j < a.budget && (Wout != W || Pout != P)) {
-            Wout[j] = W[j];
-            Pout[j] = P[j];
-        }
     }
     if (tid == 0)
         a.count[bh] = static_cast<int>(holes);
@@ -310,8 +379,12 @@ int launch_cache_evict(const CacheEvictArgs &a)
                       ws + bh + static_cast<size_t>(bh) * list, static_cast<uint16_t *>(a.Kp),
                       static_cast<uint16_t *>(a.Vp), a.budget, a.recent, list};
     hipStream_t st = static_cast<hipStream_t>(a.stream);
-    hipError_t e = launch_kernel(select_kernel, dim3(static_cast<unsigned>(bh)),
-                                 dim3(kSelectThreads), st, r, c);
+    const int slots = c.slots();
+    const dim3 grid(static_cast<unsigned>(bh));
+    hipError_t e = slots <= 2048    ? launch_kernel(select_kernel<256, 8, true>, grid, dim3(256), st, r, c)
+                   : slots <= 8192  ? launch_kernel(select_kernel<1024, 8, true>, grid, dim3(1024), st, r, c)
+                   : slots <= 16384 ? launch_kernel(select_kernel<1024, 16, true>, grid, dim3(1024), st, r, c)
+                                    : launch_kernel(select_kernel<1024, 16, false>, grid, dim3(1024), st, r, c);
     if (e != hipSuccess)
         return DD_ERR_HIP;
     const int rows = 256 / (a.c.D / 8);
