@@ -409,7 +409,8 @@ int dd_cache_attn_fwd(const void *Q, long long ldq, const void *Kp, const void *
                       float *LSE, const float *W_in, float *W_out, int T, int B, int H, int Hkv,
                       int D, int pages, int page, int per, void *workspace, size_t workspace_bytes,
                       void *stream);
-size_t dd_cache_attn_workspace_bytes(int T, int B, int H, int Hkv, int D, int page, int per);
+size_t dd_cache_attn_workspace_bytes(int T, int B, int H, int Hkv, int D, int page, int per,
+                                     int weights); /* whether W_in and W_out are given */
 int dd_cache_evict(void *Kp, void *Vp, const int32_t *table, const int32_t *lens, const float *W_in,
                    const int32_t *P_in, const int32_t *seen, float *W_out, int32_t *P_out,
                    int32_t *lens_out, int B, int Hkv, int D, int pages, int page, int per,

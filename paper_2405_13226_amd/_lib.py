@@ -57,7 +57,7 @@ SIGNATURES = {
     "dd_cache_append": (ctypes.c_int, [_P, _L, _P, _L, _P, _L, _P, _P, _P, _P, _P, _P, _P, _P,
                                        *[_I] * 8, ctypes.c_float, _P]),
     "dd_cache_attn_fwd": (ctypes.c_int, [_P, _L, *[_P] * 9, *[_I] * 8, _P, ctypes.c_size_t, _P]),
-    "dd_cache_attn_workspace_bytes": (ctypes.c_size_t, [_I] * 7),
+    "dd_cache_attn_workspace_bytes": (ctypes.c_size_t, [_I] * 8),
     "dd_cache_evict": (ctypes.c_int, [*[_P] * 10, *[_I] * 8, _P, ctypes.c_size_t, _P]),
     "dd_cache_evict_workspace_bytes": (ctypes.c_size_t, [_I] * 6),
     "dd_cache_check": (ctypes.c_int, [_P, _P, _P, *[_I] * 5]),

@@ -190,7 +190,8 @@ def cache_attention(q, k_pages, v_pages, table, lens, cu_new, weights=None, weig
         if weights_out is not None and weights_out is not weights:
             weights_out.copy_(weights)
         return out, lse
-    need = _need(dev, "dd_cache_attn_workspace_bytes", T, B, H, Hkv, D, page, per)
+    need = _need(dev, "dd_cache_attn_workspace_bytes", T, B, H, Hkv, D, page, per,
+                 weights is not None)
     ws = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
     _call(dev, "dd_cache_attn_fwd", _p(q), ldq, _p(k_pages), _p(v_pages), _p(table), _p(lens),
           _p(cu_new), _p(out), _p(lse), _p(weights),

@@ -144,12 +144,13 @@ int dd_cache_append(const void *Q, long long ldq, const void *K, long long ldk, 
                             Qrot, Kp, Vp, positions, start, ldq, ldk, ldv, H, rope_base, stream});
 }
 
-size_t dd_cache_attn_workspace_bytes(int T, int B, int H, int Hkv, int D, int page, int per)
+size_t dd_cache_attn_workspace_bytes(int T, int B, int H, int Hkv, int D, int page, int per,
+                                     int weights)
 {
     if (shape_status(T, B, H, Hkv, D, 1, page, per) != DD_OK)
         return 0;
     return dd::cache_attn_workspace_bytes(
-        shape(nullptr, nullptr, nullptr, T, B, Hkv, D, 1, page, per), H);
+        shape(nullptr, nullptr, nullptr, T, B, Hkv, D, 1, page, per), H, weights != 0);
 }
 
 int dd_cache_attn_fwd(const void *Q, long long ldq, const void *Kp, const void *Vp,
@@ -172,7 +173,7 @@ int dd_cache_attn_fwd(const void *Q, long long ldq, const void *Kp, const void *
         !aligned(lens, 4) || !aligned(cu_new, 4))
         return DD_ERR_ALIGN;
     const dd::CacheShape c = shape(table, lens, cu_new, T, B, Hkv, D, pages, page, per);
-    const size_t need = dd::cache_attn_workspace_bytes(c, H);
+    const size_t need = dd::cache_attn_workspace_bytes(c, H, W_out != nullptr);
     if (need && (!workspace || workspace_bytes < need))
         return DD_ERR_WORKSPACE;
     if (need && !aligned(workspace, 16))

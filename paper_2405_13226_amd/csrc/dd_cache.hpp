@@ -31,9 +31,17 @@ struct CacheSeq {
     int row0, n, len, total;
 };
 
+// An element of an array that the kernel only reads: a scalar load where the
+// index is the same in all lanes.
+__device__ __forceinline__ int constant(const int32_t *p, long long i)
+{
+    typedef const __attribute__((address_space(4))) int32_t *pointer;
+    return ((pointer)(p))[i];
+}
+
 __device__ __forceinline__ int cache_cu(const CacheView &c, int b)
 {
-    return min(max(c.cu[b], 0), c.T);
+    return min(max(constant(c.cu, b), 0), c.T);
 }
 
 __device__ __forceinline__ CacheSeq cache_seq(const CacheView &c, int b)
@@ -41,7 +49,7 @@ __device__ __forceinline__ CacheSeq cache_seq(const CacheView &c, int b)
     CacheSeq s;
     s.row0 = cache_cu(c, b);
     s.n = max(cache_cu(c, b + 1) - s.row0, 0);
-    s.len = min(max(c.lens[b], 0), c.slots());
+    s.len = min(max(constant(c.lens, b), 0), c.slots());
     s.total = min(s.len + s.n, c.slots());
     return s;
 }
@@ -52,7 +60,7 @@ __device__ __forceinline__ int cache_seq_of(const CacheView &c, int t)
     int lo = 0, hi = c.B - 1;
     while (lo < hi) {
         const int mid = (lo + hi + 1) >> 1;
-        if (c.cu[mid] <= t)
+        if (constant(c.cu, mid) <= t)
             lo = mid;
         else
             hi = mid - 1;
@@ -63,7 +71,7 @@ __device__ __forceinline__ int cache_seq_of(const CacheView &c, int t)
 // The page of a slot, or -1 where the table names none.
 __device__ __forceinline__ int cache_page(const CacheView &c, int b, int slot)
 {
-    const int id = c.table[static_cast<long long>(b) * c.per + (slot >> c.shift)];
+    const int id = constant(c.table, static_cast<long long>(b) * c.per + (slot >> c.shift));
     return id >= 0 && id < c.pages ? id : -1;
 }
 

@@ -19,15 +19,17 @@
 //                joined through LDS at the end
 //
 // Either splits the keys over workgroups where there are too few rows to fill
-// the chip; join_kernel adds the parts.  Tiles arrive by direct global->LDS
+// the chip; finish_kernel adds the parts.  The weights need the rows' final
+// sums: where a sequence has few rows their scores are kept (4 bytes a slot and
+// row, against 2 D bytes of K), else S is formed once more (weights_kernel).  Tiles arrive by direct global->LDS
 // loads; one load instruction covers rows of one page (pages hold at least 16
 // slots), whose number is a scalar load.
 //
 // Slots behind a sequence's last are never read (a tile's rows are clamped to
 // it).  A slot that a row may not see leaves no trace in it, whatever it
-// holds: its score is replaced, and where a boundary tile holds a value that
-// is not finite its keys are added one by one, each only to the rows that see
-// it (zero times infinity would not be zero).
+// holds: its score is replaced, and where a boundary tile holds values that
+// are not finite its slots are added one by one, each to the rows that see it
+// (zero times infinity would not be zero).
 #include "dd_cache.hpp"
 #include "dd_internal.h"
 #include "dd_launch.hpp"
@@ -46,12 +48,15 @@ typedef uint16_t u16x8 __attribute__((ext_vector_type(8)));
 // Rescaling of the accumulator is skipped until the running maximum has grown
 // by this many log2 units (probabilities stay below 2^8).
 constexpr float kSlack = 8.0f;
+constexpr int kMaxSplits = 64;
+constexpr size_t kMaxScores = 256UL << 20;  // bytes of scores kept for the weights
 
 struct AttnRows {
     const uint16_t *Q, *K, *V;
     uint16_t *O;
     float *LSE;
     float *part_o, *part_lse;  // [splits][T * H][D], [splits][T * H] (log2), splits > 1
+    float *scores;             // [T * H][slots] q K_j, or NULL
     long long ldq;
     int H, G, tiles, splits;
     float scale_log2;
@@ -64,12 +69,14 @@ __device__ __forceinline__ void wait_vm()
 }
 
 // One tile of NB x 32 keys for the wave's 32 rows.  MASKED: the lane's row sees
-// the tile's keys 0 .. hi_r only (boundary tiles).
-template <int D, int NB, bool MASKED>
+// the tile's keys 0 .. hi_r only (boundary tiles).  `scores` (optional)
+// receives the lane's row of q K_j, `room` of them (a multiple of 4).
+template <int D, int NB, bool MASKED, bool SCORES = false>
 __device__ __forceinline__ void
 attend_tile(const uint16_t *kt, const uint16_t *vt, const bf16x8 (&qf)[D / 16],
             const int (&koff)[D / 16], const int (&voff)[D / 32][2], int hi_r, int g,
-            float scale_log2, f32x16 (&acc)[D / 32], float &m_i, float &l_i)
+            float scale_log2, f32x16 (&acc)[D / 32], float &m_i, float &l_i,
+            float *scores = nullptr, int room = 0)
 {
     constexpr int KK = D / 16, DB = D / 32;
     f32x16 s[NB];
@@ -86,6 +93,15 @@ attend_tile(const uint16_t *kt, const uint16_t *vt, const bf16x8 (&qf)[D / 16],
 #pragma unroll
             for (int r = 0; r < 16; ++r)
                 s[kb][r] = kb * 32 + 8 * (r >> 2) + (r & 3) <= hi_r - 4 * g ? s[kb][r] : -INFINITY;
+    }
+    if constexpr (SCORES) {
+#pragma unroll
+        for (int kb = 0; kb < NB; ++kb)
+#pragma unroll
+            for (int rg = 0; rg < 4; ++rg)
+                if (kb * 32 + 8 * rg + 4 * g < room)
+                    *reinterpret_cast<f32x4 *>(scores + kb * 32 + 8 * rg + 4 * g) =
+                        f32x4{s[kb][4 * rg], s[kb][4 * rg + 1], s[kb][4 * rg + 2], s[kb][4 * rg + 3]};
     }
     float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
@@ -181,24 +197,30 @@ struct AttnItem {
     int split;
 };
 
+// A value that is the same in every lane, as a scalar.
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
 // The sequences' row tiles lie one after the other: those of sequence b start
 // at cu[b] G / BM + b, which leaves room for each of its parts of BM rows.
 template <int BM, int BN>
 __device__ __forceinline__ bool attn_item(const CacheView &c, const AttnRows &a, AttnItem &it)
 {
-    int j;
-    block_slice(static_cast<int>(blockIdx.x), a.tiles * a.splits, c.Hkv, it.h, j);
+    int h, j;
+    block_slice(static_cast<int>(blockIdx.x), a.tiles * a.splits, c.Hkv, h, j);
+    it.h = uniform(h);
+    j = uniform(j);
     if (it.h >= c.Hkv || j >= a.tiles * a.splits)
         return false;
-    it.split = j % a.splits;
-    const int tile = a.tiles - 1 - j / a.splits;  // a sequence's last rows see the most keys
+    const int tile = a.splits == 1 ? j : uniform(j / a.splits);
+    it.split = j - tile * a.splits;
+    const int from_end = a.tiles - 1 - tile;  // a sequence's last rows see the most keys
     auto first = [&](int b) __attribute__((always_inline)) {
-        return static_cast<int>(static_cast<long long>(cache_cu(c, b)) * a.G / BM) + b;
+        return static_cast<int>(static_cast<unsigned long long>(cache_cu(c, b)) * a.G / BM) + b;
     };
     int lo = 0, hi = c.B - 1;
     while (lo < hi) {
         const int mid = (lo + hi + 1) >> 1;
-        if (first(mid) <= tile)
+        if (first(mid) <= from_end)
             lo = mid;
         else
             hi = mid - 1;
@@ -206,14 +228,17 @@ __device__ __forceinline__ bool attn_item(const CacheView &c, const AttnRows &a,
     it.b = lo;
     it.s = cache_seq(c, lo);
     it.rows = it.s.n * a.G;
-    it.row = (tile - first(lo)) * BM;
+    it.row = (from_end - first(lo)) * BM;
     if (it.row < 0 || it.row >= it.rows)
         return false;
     const int last = min(it.row + BM, it.rows) - 1;
-    const int keys = min(it.s.len + last / a.G + 1, it.s.total);
+    const int keys = min(it.s.len + uniform(last / a.G) + 1, it.s.total);
+    // (tiles: below 2^25 of them, splits at most 64)
     const int tiles = (keys + BN - 1) / BN;
-    it.t0 = static_cast<int>(static_cast<long long>(tiles) * it.split / a.splits);
-    it.t1 = static_cast<int>(static_cast<long long>(tiles) * (it.split + 1) / a.splits);
+    it.t0 = a.splits == 1 ? 0 : uniform(static_cast<int>(static_cast<unsigned>(tiles) * it.split / a.splits));
+    it.t1 = a.splits == 1
+                ? tiles
+                : uniform(static_cast<int>(static_cast<unsigned>(tiles) * (it.split + 1) / a.splits));
     return true;
 }
 
@@ -228,9 +253,7 @@ struct PagedTile {
     {
         const int w = NW == 1 ? 0 : __builtin_amdgcn_readfirstlane(wave);
         const uint32_t slot0 = lds_base_sgpr(lds) + 1024u * static_cast<uint32_t>(w);
-        typedef const __attribute__((address_space(4))) int32_t *scalar_ptr;
-        const scalar_ptr table =
-            (scalar_ptr)(c.table + static_cast<long long>(it.b) * c.per);
+        const int32_t *table = c.table + static_cast<long long>(it.b) * c.per;
         const int lr = lane / CPR;
         const int end = it.s.total - 1;
 #pragma unroll
@@ -238,7 +261,7 @@ struct PagedTile {
             const int r0 = (w + NW * k) * RPI;  // row of the tile
             // an instruction behind the last slot reads the last slot's rows
             const int first = __builtin_amdgcn_readfirstlane(min(j0 + r0, end & -RPI));
-            const uint32_t id = min(static_cast<uint32_t>(table[first >> c.shift]),
+            const uint32_t id = min(static_cast<uint32_t>(constant(table, first >> c.shift)),
                                     static_cast<uint32_t>(c.pages - 1));
             const uint16_t *base = X + cache_row(c, static_cast<int>(id), it.h, first) * D;
             const int row = min(lr, end - first);
@@ -248,16 +271,22 @@ struct PagedTile {
     }
 };
 
+// Row r of the sequence (the last one, where it has fewer) in the outputs: its
+// token times H plus its head.
+__device__ __forceinline__ long long row_out(const AttnRows &a, const AttnItem &it, int r)
+{
+    const int last = min(r, it.rows - 1), i = last / a.G;
+    return static_cast<long long>(it.s.row0 + i) * a.H + it.h * a.G + last - i * a.G;
+}
+
 // The wave's 32 rows from `row` on: its query fragments, and the last slot the
 // lane's row sees.  Rows behind the last read the last one's.
 template <int D>
-__device__ __forceinline__ void load_rows(const CacheView &c, const AttnRows &a, const AttnItem &it,
-                                          int row, int l32, int g, bf16x8 (&qf)[D / 16], int &hi,
-                                          long long &out)
+__device__ __forceinline__ void load_rows(const AttnRows &a, const AttnItem &it, int row, int l32,
+                                          int g, bf16x8 (&qf)[D / 16], int &hi)
 {
     const int r = min(row + l32, it.rows - 1), i = r / a.G, h = it.h * a.G + r - i * a.G;
     hi = min(it.s.len + i, it.s.total - 1);
-    out = static_cast<long long>(it.s.row0 + i) * a.H + h;
     const uint16_t *src = a.Q + (it.s.row0 + i) * a.ldq + h * D + g * 8;
 #pragma unroll
     for (int kk = 0; kk < D / 16; ++kk)
@@ -279,13 +308,16 @@ __device__ __forceinline__ void tile_offsets(int lane, int (&koff)[D / 16], int 
             voff[db][hh] = tile_off<D>(8 * hh + 4 * g + e, db * 32 + 16 * (q & 1) + 4 * x);
 }
 
-// O and the LSE of the lane's row (`ok`: it has one), or a split's part.
+// O and the LSE of the lane's row (the sequence's row `row`, if it has that
+// many), or a split's part.
 template <int D>
-__device__ __forceinline__ void store_rows(const CacheView &c, const AttnRows &a, int split,
-                                           long long out, bool ok, int g, const f32x16 (&acc)[D / 32],
+__device__ __forceinline__ void store_rows(const CacheView &c, const AttnRows &a, const AttnItem &it,
+                                           int row, int g, const f32x16 (&acc)[D / 32],
                                            float m_i, float l_i)
 {
     const float l = halves_sum(l_i);
+    const bool ok = row < it.rows;
+    const long long out = row_out(a, it, row);
     if (a.splits == 1) {
         const float inv = 1.0f / l;
 #pragma unroll
@@ -295,7 +327,7 @@ __device__ __forceinline__ void store_rows(const CacheView &c, const AttnRows &a
             a.LSE[out] = (m_i + log2f(l)) * kLn2;
         return;
     }
-    const long long at = static_cast<long long>(split) * c.T * a.H + out;
+    const long long at = static_cast<long long>(it.split) * c.T * a.H + out;
     const float inv = l == 0.f ? 0.f : 1.0f / l;  // no key in this part
     if (!ok)
         return;
@@ -327,8 +359,7 @@ __global__ void __launch_bounds__(256, 2) tile_kernel(AttnRows a, CacheView c)
 
     bf16x8 qf[KK];
     int hi;
-    long long out;
-    load_rows<D>(c, a, it, row, l32, g, qf, hi, out);
+    load_rows<D>(a, it, row, l32, g, qf, hi);
     const int hi_first = __builtin_amdgcn_readlane(hi, 0), hi_last = __builtin_amdgcn_readlane(hi, 31);
     int koff[KK], voff[DB][2];
     tile_offsets<D>(lane, koff, voff);
@@ -342,6 +373,10 @@ __global__ void __launch_bounds__(256, 2) tile_kernel(AttnRows a, CacheView c)
         PagedTile<D, BN, 4>::issue(c, a.K, stage, it, t * BN, wave, lane);
         PagedTile<D, BN, 4>::issue(c, a.V, stage + TILE, it, t * BN, wave, lane);
     };
+    if (it.t0 < it.t1)
+        issue(it.t0, lds);
+    wait_vmem();
+    __syncthreads();
     auto step = [&](int t, auto bufc) __attribute__((always_inline)) {
         constexpr int BUF = decltype(bufc)::value;
         const uint16_t *kt = lds + BUF * 2 * TILE;
@@ -359,25 +394,23 @@ __global__ void __launch_bounds__(256, 2) tile_kernel(AttnRows a, CacheView c)
         wait_vmem();
         __syncthreads();
     };
-    if (it.t0 < it.t1)
-        issue(it.t0, lds);
-    wait_vmem();
-    __syncthreads();
+    // (the stages as constants: with one body for both 6% slower at 2,048 new
+    // tokens over 16,384 slots)
     for (int t = it.t0; t < it.t1; t += 2) {
         step(t, IC<0>{});
         if (t + 1 < it.t1)
             step(t + 1, IC<1>{});
     }
     if (on)
-        store_rows<D>(c, a, it.split, out, row + l32 < it.rows, g, acc, m_i, l_i);
+        store_rows<D>(c, a, it, row + l32, g, acc, m_i, l_i);
 }
 
-template <int D>
-__global__ void __launch_bounds__(256) few_kernel(AttnRows a, CacheView c)
+template <int D, int NW, bool SCORES>
+__global__ void __launch_bounds__(64 * NW) few_kernel(AttnRows a, CacheView c)
 {
     constexpr int BN = 32, TILE = BN * D, KK = D / 16, DB = D / 32;
     constexpr int LOADS = 2 * PagedTile<D, BN, 1>::PER;  // of a tile's K and V
-    __shared__ __attribute__((aligned(1024))) uint16_t lds[4 * 4 * TILE];
+    __shared__ __attribute__((aligned(1024))) uint16_t lds[NW * 4 * TILE];
     AttnItem it;
     if (!attn_item<32, BN>(c, a, it))
         return;
@@ -386,20 +419,19 @@ __global__ void __launch_bounds__(256) few_kernel(AttnRows a, CacheView c)
     uint16_t *const mine = lds + wave * 4 * TILE;
 
     int t = it.t0 + wave;
-    auto issue = [&](int tile, int buf) __attribute__((always_inline)) {
+    auto issue = [&](int at, int buf) __attribute__((always_inline)) {
         uint16_t *stage = mine + buf * 2 * TILE;
-        PagedTile<D, BN, 1>::issue(c, a.K, stage, it, tile * BN, 0, lane);
-        PagedTile<D, BN, 1>::issue(c, a.V, stage + TILE, it, tile * BN, 0, lane);
+        PagedTile<D, BN, 1>::issue(c, a.K, stage, it, at * BN, 0, lane);
+        PagedTile<D, BN, 1>::issue(c, a.V, stage + TILE, it, at * BN, 0, lane);
     };
     if (t < it.t1)
         issue(t, 0);
-    if (t + 4 < it.t1)
-        issue(t + 4, 1);
+    if (t + NW < it.t1)
+        issue(t + NW, 1);
 
     bf16x8 qf[KK];
     int hi;
-    long long out;
-    load_rows<D>(c, a, it, it.row, l32, g, qf, hi, out);
+    load_rows<D>(a, it, it.row, l32, g, qf, hi);
     const int hi_first = __builtin_amdgcn_readlane(hi, 0);
     int koff[KK], voff[DB][2];
     tile_offsets<D>(lane, koff, voff);
@@ -409,28 +441,31 @@ __global__ void __launch_bounds__(256) few_kernel(AttnRows a, CacheView c)
         acc[db] = f32x16{};
     float m_i = -INFINITY, l_i = 0.f;
 
+    float *const scores = SCORES ? a.scores + row_out(a, it, it.row + l32) * c.slots() : nullptr;
+    const bool mine_ok = it.row + l32 < it.rows;
     int buf = 0;
-    for (; t < it.t1; t += 4, buf ^= 1) {
-        if (t + 4 < it.t1)
+    for (; t < it.t1; t += NW, buf ^= 1) {
+        if (t + NW < it.t1)
             wait_vm<LOADS>();
         else
             wait_vm<0>();
         const uint16_t *kt = mine + buf * 2 * TILE;
         const int j0 = t * BN;
+        const int room = mine_ok ? c.slots() - j0 : 0;
         if (j0 + BN - 1 <= hi_first)
-            attend_tile<D, 1, false>(kt, kt + TILE, qf, koff, voff, 0, g, a.scale_log2, acc, m_i,
-                                     l_i);
+            attend_tile<D, 1, false, SCORES>(kt, kt + TILE, qf, koff, voff, 0, g, a.scale_log2,
+                                             acc, m_i, l_i, scores + j0, room);
         else
-            attend_tile<D, 1, true>(kt, kt + TILE, qf, koff, voff, hi - j0, g, a.scale_log2, acc,
-                                    m_i, l_i);
-        if (t + 8 < it.t1) {
+            attend_tile<D, 1, true, SCORES>(kt, kt + TILE, qf, koff, voff, hi - j0, g,
+                                            a.scale_log2, acc, m_i, l_i, scores + j0, room);
+        if (t + 2 * NW < it.t1) {
             // the stage's last reads have returned before it is filled again
             asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
-            issue(t + 8, buf);
+            issue(t + 2 * NW, buf);
         }
     }
 
-    // Waves 1 to 3 hand over through LDS (every wave is done with its stages).
+    // The other waves hand over through LDS (every wave is done with its stages).
     constexpr int NS = 1 + 4 * DB;
     float *x = reinterpret_cast<float *>(lds) + lane * 4;
     __syncthreads();
@@ -450,7 +485,7 @@ __global__ void __launch_bounds__(256) few_kernel(AttnRows a, CacheView c)
     if (wave > 0)
         return;
 #pragma unroll 1
-    for (int o = 0; o < 3; ++o) {
+    for (int o = 0; o < NW - 1; ++o) {
         const float *y = x + o * NS * 256;
         const f32x4 ml = *reinterpret_cast<const f32x4 *>(y);
         const float m = fmaxf(m_i, ml[0]), ref = m == -INFINITY ? 0.f : m;
@@ -465,39 +500,8 @@ __global__ void __launch_bounds__(256) few_kernel(AttnRows a, CacheView c)
                 acc[r >> 2][4 * (r & 3) + e] = acc[r >> 2][4 * (r & 3) + e] * a0 + v[e] * a1;
         }
     }
-    store_rows<D>(c, a, it.split, out, it.row + l32 < it.rows, g, acc, m_i, l_i);
+    store_rows<D>(c, a, it, it.row + l32, g, acc, m_i, l_i);
 }
-
-// A row's parts on a common maximum: D / 4 lanes per row.
-template <int D>
-__global__ void __launch_bounds__(256) join_kernel(AttnRows a, CacheView c)
-{
-    constexpr int LANES = D / 4, ROWS = 256 / LANES;
-    const long long n = static_cast<long long>(c.T) * a.H;
-    const long long row = static_cast<long long>(blockIdx.x) * ROWS + threadIdx.x / LANES;
-    const int x = threadIdx.x % LANES;
-    if (row < static_cast<long long>(cache_cu(c, 0)) * a.H ||
-        row >= static_cast<long long>(cache_cu(c, c.B)) * a.H)
-        return;
-    float m = -INFINITY;
-    for (int s = 0; s < a.splits; ++s)
-        m = fmaxf(m, a.part_lse[s * n + row]);
-    const float ref = m == -INFINITY ? 0.f : m;
-    float l = 0.f;
-    f32x4 o = {0.f, 0.f, 0.f, 0.f};
-    for (int s = 0; s < a.splits; ++s) {
-        const float w = fast_exp2(a.part_lse[s * n + row] - ref);
-        l += w;
-        o += w * *reinterpret_cast<const f32x4 *>(a.part_o + (s * n + row) * D + 4 * x);
-    }
-    const float inv = 1.0f / l;
-    const bf16x4 y = pack4(o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
-    *reinterpret_cast<u32x2 *>(a.O + row * D + 4 * x) = __builtin_bit_cast(u32x2, y);
-    if (x == 0)
-        a.LSE[row] = (m + log2f(l)) * kLn2;
-}
-
-// ---------------------------------------------------------------------------
 
 struct WeightRows {
     const uint16_t *Q, *K;
@@ -508,54 +512,233 @@ struct WeightRows {
     float scale_log2;
 };
 
-// The weights of 128 slots of one key head, 32 per wave: S = Q K^T puts a slot
-// in a lane column, so a slot's sum stays in its lane; the sequence's rows pass
-// 32 at a time.
+// Blocks below `joins`: rows' parts on a common maximum, D / 4 lanes per row.
+// The others (where scores were kept): the weights of 1024 slots of one key
+// head, from its rows' scores; each block forms its rows' sums itself.
 template <int D>
+__global__ void __launch_bounds__(256) finish_kernel(AttnRows a, WeightRows w, CacheView c, int joins)
+{
+    constexpr int LANES = D / 4, ROWS = 256 / LANES, SETS = kMaxSplits / LANES;
+    constexpr int AT_ONCE = 64;
+    __shared__ float lse2[AT_ONCE];
+    const long long n = static_cast<long long>(c.T) * a.H;
+    if (static_cast<int>(blockIdx.x) < joins) {
+        const long long row = static_cast<long long>(blockIdx.x) * ROWS + threadIdx.x / LANES;
+        const int x = threadIdx.x % LANES;
+        if (row < static_cast<long long>(cache_cu(c, 0)) * a.H ||
+            row >= static_cast<long long>(cache_cu(c, c.B)) * a.H)
+            return;  // (whole groups of lanes)
+        float ls[SETS], m = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < SETS; ++i) {
+            const int s = i * LANES + x;
+            ls[i] = s < a.splits ? a.part_lse[s * n + row] : -INFINITY;
+            m = fmaxf(m, ls[i]);
+        }
+#pragma unroll
+        for (int o = LANES / 2; o >= 1; o >>= 1)
+            m = fmaxf(m, __shfl_xor(m, o));
+        const float ref = m == -INFINITY ? 0.f : m;
+        float l = 0.f;
+#pragma unroll
+        for (int i = 0; i < SETS; ++i) {
+            ls[i] = fast_exp2(ls[i] - ref);
+            l += ls[i];
+        }
+#pragma unroll
+        for (int o = LANES / 2; o >= 1; o >>= 1)
+            l += __shfl_xor(l, o);
+        f32x4 o = {0.f, 0.f, 0.f, 0.f};
+        const float *part = a.part_o + row * D + 4 * x;
+#pragma unroll
+        for (int i = 0; i < SETS; ++i)
+#pragma unroll 4
+            for (int s = i * LANES; s < min((i + 1) * LANES, a.splits); ++s)
+                o += __shfl(ls[i], s - i * LANES, LANES) *
+                     *reinterpret_cast<const f32x4 *>(part + s * n * D);
+        const float inv = 1.0f / l;
+        const bf16x4 y = pack4(o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
+        *reinterpret_cast<u32x2 *>(a.O + row * D + 4 * x) = __builtin_bit_cast(u32x2, y);
+        if (x == 0)
+            a.LSE[row] = (m + log2f(l)) * kLn2;
+        return;
+    }
+    const int blocks = (c.slots() + 1023) / 1024, id = static_cast<int>(blockIdx.x) - joins;
+    const int bh = id / blocks, b = bh / c.Hkv, h = bh % c.Hkv;
+    const CacheSeq s = cache_seq(c, b);
+    const int key = (id % blocks * 256 + static_cast<int>(threadIdx.x)) * 4;
+    if (id % blocks * 1024 >= s.total)
+        return;
+    const bool in = key < s.total;
+    const int rows = s.n * a.G, lane = threadIdx.x & 63;
+    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+    for (int r0 = 0; r0 < rows; r0 += AT_ONCE) {
+        __syncthreads();
+        for (int r = r0 + (threadIdx.x >> 6); r < min(r0 + AT_ONCE, rows); r += 4) {
+            const long long out = static_cast<long long>(s.row0 + r / a.G) * a.H + h * a.G + r % a.G;
+            float z;
+            if (a.splits == 1) {
+                z = a.LSE[out] * kLog2e;
+            } else {
+                const float p = lane < a.splits ? a.part_lse[lane * n + out] : -INFINITY;
+                float m = p;
+#pragma unroll
+                for (int o = 32; o >= 1; o >>= 1)
+                    m = fmaxf(m, __shfl_xor(m, o));
+                float l = fast_exp2(p - (m == -INFINITY ? 0.f : m));
+#pragma unroll
+                for (int o = 32; o >= 1; o >>= 1)
+                    l += __shfl_xor(l, o);
+                z = m + log2f(l);
+            }
+            if (lane == 0)
+                lse2[r - r0] = z;
+        }
+        __syncthreads();
+        if (in)
+#pragma unroll 4
+            for (int r = r0; r < min(r0 + AT_ONCE, rows); ++r) {
+                const int i = r / a.G, hi = min(s.len + i, s.total - 1);
+                const long long out = static_cast<long long>(s.row0 + i) * a.H + h * a.G + r - i * a.G;
+                const f32x4 q = *reinterpret_cast<const f32x4 *>(a.scores + out * c.slots() + key);
+                const float z = lse2[r - r0];
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    sum[e] += key + e <= hi ? fast_exp2(fmaf(q[e], a.scale_log2, -z)) : 0.f;
+            }
+    }
+    const long long at = static_cast<long long>(bh) * c.slots() + key;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        if (key + e < s.total)
+            w.Wout[at + e] = (key + e < s.len ? w.W[at + e] : 0.f) + sum[e];
+}
+
+// ---------------------------------------------------------------------------
+
+// The weights of KB x 128 slots of one key head, from Q and K again (where scores
+// would be more to keep): KB x 32 slots per wave, their K rows in registers as B
+// operands.  S = Q K^T puts a slot in a lane column, so a slot's sum stays in
+// its lane; the sequence's rows pass 32 at a time through LDS, three tiles on
+// their way while one is used, and their sums 1024 at a time.
+template <int D, int KB>
 __global__ void __launch_bounds__(256) weights_kernel(WeightRows a, CacheView c)
 {
-    constexpr int KK = D / 16;
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, l32 = lane & 31, g = lane >> 5;
+    constexpr int KK = D / 16, CPR = D / 8, PER = 32 * CPR / 64 / 4, TILE = 32 * D;
+    constexpr int STAGES = 4, ROWS = 1024;
+    __shared__ __attribute__((aligned(1024))) uint16_t lds[STAGES * TILE];
+    __shared__ __attribute__((aligned(16))) float lse2[ROWS];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63, l32 = lane & 31, g = lane >> 5;
     const int b = static_cast<int>(blockIdx.y) / c.Hkv, h = static_cast<int>(blockIdx.y) % c.Hkv;
     const CacheSeq s = cache_seq(c, b);
-    const int key0 = (static_cast<int>(blockIdx.x) * 4 + wave) * 32, key = key0 + l32;
-    if (key0 >= s.total)
+    const int block0 = static_cast<int>(blockIdx.x) * KB * 128;
+    const int key0 = block0 + wave * KB * 32;
+    if (block0 >= s.total)
         return;
-    const bool live = key < s.total;
-    const int at = min(key, s.total - 1);
-    const int id = max(cache_page(c, b, at), 0);
-    const uint16_t *kp = a.K + cache_row(c, id, h, at) * D + g * 8;
-    bf16x8 kf[KK];
-#pragma unroll
-    for (int kk = 0; kk < KK; ++kk)
-        kf[kk] = as_bf16x8(*reinterpret_cast<const u32x4 *>(kp + kk * 16));
-
     const int rows = s.n * a.G;
-    // the first row that sees the lane's slot, and the wave's first slot
-    const int sees = static_cast<int>(min(static_cast<long long>(max(key - s.len, 0)) * a.G,
-                                          static_cast<long long>(rows)));
-    const int begin = __builtin_amdgcn_readlane(sees, 0), all = wave_max(sees);
-    float sum = 0.f;
-    for (int r0 = begin & ~31; r0 < rows; r0 += 32) {
-        const int r = min(r0 + l32, rows - 1), i = r / a.G, hq = h * a.G + r - i * a.G;
-        const uint16_t *q = a.Q + (s.row0 + i) * a.ldq + hq * D + g * 8;
-        const float lse2 = a.LSE[static_cast<long long>(s.row0 + i) * a.H + hq] * kLog2e;
-        f32x16 p = f32x16{};
+    // the first row that sees a slot
+    auto first = [&](int key) __attribute__((always_inline)) {
+        return static_cast<int>(min(static_cast<long long>(max(key - s.len, 0)) * a.G,
+                                    static_cast<long long>(rows)));
+    };
+    bf16x8 kf[KB][KK];
+    int sees[KB];
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb) {
+        const int key = key0 + kb * 32 + l32, at = min(key, s.total - 1);
+        const int id = max(cache_page(c, b, at), 0);
+        const uint16_t *kp = a.K + cache_row(c, id, h, at) * D + g * 8;
 #pragma unroll
         for (int kk = 0; kk < KK; ++kk)
-            p = mfma32(as_bf16x8(*reinterpret_cast<const u32x4 *>(q + kk * 16)), kf[kk], p);
-        const bool whole = r0 >= all && r0 + 32 <= rows;
+            kf[kb][kk] = as_bf16x8(*reinterpret_cast<const u32x4 *>(kp + kk * 16));
+        sees[kb] = first(key);
+    }
+    const int wave_first = first(key0), wave_all = first(key0 + KB * 32 - 1);
+    const int begin = first(block0) & ~31;
+
+    auto issue = [&](int r0, int buf) __attribute__((always_inline)) {
+        const uint32_t slot = lds_base_sgpr(lds) + static_cast<uint32_t>(buf * TILE * 2 + 1024 * wave);
 #pragma unroll
-        for (int x = 0; x < 16; ++x) {
-            const int rr = 8 * (x >> 2) + 4 * g + (x & 3);
-            const float w = fast_exp2(fmaf(p[x], a.scale_log2, -__shfl(lse2, rr)));
-            sum += whole || (r0 + rr >= sees && r0 + rr < rows) ? w : 0.f;
+        for (int k = 0; k < PER; ++k) {
+            const int q = (wave + 4 * k) * 64 + lane, tr = q / CPR, x = (q % CPR) ^ swz<D>(tr);
+            const int r = min(r0 + tr, rows - 1), i = r / a.G;
+            dma_b128(a.Q + (s.row0 + i) * a.ldq + (h * a.G + r - i * a.G) * D + x * 8,
+                     slot + 4096u * k);
+        }
+    };
+    int koff[KK];
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk)
+        koff[kk] = tile_off<D>(l32, kk * 16 + g * 8);
+    float sum[KB] = {};
+    for (int c0 = begin; c0 < rows; c0 += ROWS) {
+        const int end = min(c0 + ROWS, rows);
+        __syncthreads();  // the sums before have been read
+        for (int r = c0 + static_cast<int>(threadIdx.x); r < c0 + ROWS; r += 256) {
+            const int i = min(r, rows - 1) / a.G;
+            const long long at =
+                static_cast<long long>(s.row0 + i) * a.H + h * a.G + min(r, rows - 1) - i * a.G;
+            lse2[r - c0] = r < rows ? a.LSE[at] * kLog2e : INFINITY;
+        }
+#pragma unroll
+        for (int t = 0; t < STAGES - 1; ++t)
+            if (c0 + 32 * t < end)
+                issue(c0 + 32 * t, t);
+        int buf = 0;
+        for (int r0 = c0; r0 < end; r0 += 32, buf = (buf + 1) % STAGES) {
+            // this tile's loads, and at most two later tiles' outstanding
+            if (r0 + 64 < end)
+                wait_vm<2 * PER>();
+            else if (r0 + 32 < end)
+                wait_vm<PER>();
+            else
+                wait_vm<0>();
+            __syncthreads();  // every wave's loads; and the stage before is free
+            if (r0 + 32 * (STAGES - 1) < end)
+                issue(r0 + 32 * (STAGES - 1), (buf + STAGES - 1) % STAGES);
+            if (r0 + 32 <= wave_first)
+                continue;
+            const uint16_t *qt = lds + buf * TILE;
+            f32x16 p[KB] = {};
+#pragma unroll
+            for (int kk = 0; kk < KK; ++kk) {
+                const bf16x8 q = lds_row8(qt + koff[kk]);
+#pragma unroll
+                for (int kb = 0; kb < KB; ++kb)
+                    p[kb] = mfma32(q, kf[kb][kk], p[kb]);
+            }
+            auto add = [&](auto wholec) __attribute__((always_inline)) {
+                constexpr bool WHOLE = decltype(wholec)::value != 0;
+#pragma unroll
+                for (int rg = 0; rg < 4; ++rg) {
+                    const f32x4 z =
+                        *reinterpret_cast<const f32x4 *>(&lse2[r0 - c0 + 8 * rg + 4 * g]);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int rr = r0 + 8 * rg + 4 * g + e;
+#pragma unroll
+                        for (int kb = 0; kb < KB; ++kb) {
+                            const float v = fast_exp2(fmaf(p[kb][4 * rg + e], a.scale_log2, -z[e]));
+                            sum[kb] += WHOLE || (rr >= sees[kb] && rr < rows) ? v : 0.f;
+                        }
+                    }
+                }
+            };
+            if (r0 >= wave_all && r0 + 32 <= rows)
+                add(IC<1>{});
+            else
+                add(IC<0>{});
         }
     }
-    sum = halves_sum(sum);
-    if (live && g == 0) {
-        const long long w = (static_cast<long long>(b) * c.Hkv + h) * c.slots() + key;
-        a.Wout[w] = (key < s.len ? a.W[w] : 0.f) + sum;
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb) {
+        const float t = halves_sum(sum[kb]);
+        const int key = key0 + kb * 32 + l32;
+        if (key < s.total && g == 0) {
+            const long long at = static_cast<long long>(blockIdx.y) * c.slots() + key;
+            a.Wout[at] = (key < s.len ? a.W[at] : 0.f) + t;
+        }
     }
 }
 
@@ -564,13 +747,20 @@ CacheView view(const CacheShape &c)
     return CacheView{c.table, c.lens, c.cu_new, c.T, c.B, c.Hkv, c.pages, c.shift, c.per};
 }
 
+// Waves of a workgroup with few rows: 64 KB of LDS, two workgroups per CU.  (At
+// D = 128 four waves, one workgroup per CU, read 8 x 8,192 slots of 8 key heads
+// in 46-56 us instead of 41-43: nothing runs while a workgroup begins or ends.)
+template <int D>
+constexpr int few_waves = D == 64 ? 4 : 2;
+
 // How a call runs: by what the host knows of it (rows, sequences, slots).
 struct AttnPlan {
-    bool few;
+    bool few, scores;
     int tiles, splits;
+    size_t rows, part_bytes, bytes;  // of the parts, and of the whole workspace
 };
 
-AttnPlan attn_plan(const CacheShape &c, int H)
+AttnPlan attn_plan(const CacheShape &c, int H, bool weights)
 {
     AttnPlan p;
     const long long rows = static_cast<long long>(c.T) * (H / c.Hkv);
@@ -581,38 +771,57 @@ AttnPlan attn_plan(const CacheShape &c, int H)
     const long long each = (rows + c.B - 1) / c.B;
     const long long work = std::min<long long>(c.B, c.T) * ((each + bm - 1) / bm) * c.Hkv;
     const long long slots = static_cast<long long>(c.per) << c.shift;
-    const long long most = std::max(1LL, slots / (p.few ? 256 : 512));
-    p.splits = static_cast<int>(std::clamp((p.few ? 1024 : 512) / work, 1LL, std::min(most, 64LL)));
+    // few rows: parts of 512 KB of K and V or more, smaller where that leaves
+    // CUs idle, down to 128 slots; many: enough workgroups, of 512 slots or more
+    const long long fill = (512 + work - 1) / work;
+    const long long want = p.few ? std::max(slots * c.D / 131072, std::min(fill, slots / 128))
+                                 : std::min(512 / work, slots / 512);
+    p.splits = static_cast<int>(std::clamp<long long>(want, 1, kMaxSplits));
+    p.rows = static_cast<size_t>(c.T) * H;
+    p.part_bytes = p.splits == 1 ? 0 : p.splits * p.rows * (c.D + 1) * sizeof(float);
+    p.part_bytes = (p.part_bytes + 15) / 16 * 16;
+    const size_t score_bytes = p.rows * slots * sizeof(float);
+    p.scores = weights && p.few && rows <= 8LL * c.B && score_bytes <= kMaxScores;
+    p.bytes = p.part_bytes + (p.scores ? score_bytes : 0);
     return p;
 }
 
 template <int D>
 int launch_attn_d(const CacheAttnArgs &a)
 {
-    const AttnPlan p = attn_plan(a.c, a.H);
+    const AttnPlan p = attn_plan(a.c, a.H, a.Wout != nullptr);
     const CacheView c = view(a.c);
-    const size_t rows = static_cast<size_t>(a.c.T) * a.H;
-    float *ws = static_cast<float *>(a.workspace);
+    char *ws = static_cast<char *>(a.workspace);
+    float *parts = reinterpret_cast<float *>(ws);
     const float scale_log2 = kLog2e / std::sqrt(static_cast<float>(D));
     const AttnRows r{static_cast<const uint16_t *>(a.Q), static_cast<const uint16_t *>(a.Kp),
-                     static_cast<const uint16_t *>(a.Vp), static_cast<uint16_t *>(a.O), a.LSE, ws,
-                     ws ? ws + p.splits * rows * D : nullptr, a.ldq, a.H, a.H / a.c.Hkv, p.tiles,
-                     p.splits, scale_log2};
+                     static_cast<const uint16_t *>(a.Vp), static_cast<uint16_t *>(a.O), a.LSE,
+                     parts, p.splits > 1 ? parts + p.splits * p.rows * D : nullptr,
+                     p.scores ? reinterpret_cast<float *>(ws + p.part_bytes) : nullptr, a.ldq, a.H,
+                     a.H / a.c.Hkv, p.tiles, p.splits, scale_log2};
+    const WeightRows w{r.Q, r.K, a.LSE, a.W, a.Wout, a.ldq, a.H, r.G, scale_log2};
     hipStream_t st = static_cast<hipStream_t>(a.stream);
     const long long items = static_cast<long long>(p.tiles) * p.splits * a.c.Hkv;
     const unsigned grid = static_cast<unsigned>((items + kXcds - 1) / kXcds * kXcds);
-    hipError_t e = launch_kernel(p.few ? few_kernel<D> : tile_kernel<D>, dim3(grid), dim3(256), st, r,
-                                 c);
-    if (e == hipSuccess && p.splits > 1) {
-        constexpr int ROWS = 256 / (D / 4);
-        e = launch_kernel(join_kernel<D>, dim3(static_cast<unsigned>((rows + ROWS - 1) / ROWS)),
-                          dim3(256), st, r, c);
-    }
-    if (e == hipSuccess && a.Wout) {
-        const WeightRows w{r.Q, r.K, a.LSE, a.W, a.Wout, a.ldq, a.H, r.G, scale_log2};
-        e = launch_kernel(weights_kernel<D>,
-                          dim3(static_cast<unsigned>((c.slots() + 127) / 128),
-                               static_cast<unsigned>(a.c.B * a.c.Hkv)),
+    constexpr int NW = few_waves<D>;
+    hipError_t e = launch_kernel(!p.few     ? tile_kernel<D>
+                                 : p.scores ? few_kernel<D, NW, true>
+                                            : few_kernel<D, NW, false>,
+                                 dim3(grid), dim3(p.few ? 64 * NW : 256), st, r, c);
+    constexpr int ROWS = 256 / (D / 4);
+    const unsigned joins = p.splits > 1 ? static_cast<unsigned>((p.rows + ROWS - 1) / ROWS) : 0;
+    const unsigned heads = static_cast<unsigned>(a.c.B * a.c.Hkv);
+    const unsigned more = p.scores ? heads * static_cast<unsigned>((c.slots() + 1023) / 1024) : 0;
+    if (e == hipSuccess && joins + more)
+        e = launch_kernel(finish_kernel<D>, dim3(joins + more), dim3(256), st, r, w, c,
+                          static_cast<int>(joins));
+    if (e == hipSuccess && a.Wout && !p.scores) {
+        // 128 slots a workgroup, or 256 where that still fills the chip twice
+        // over (7 ragged sequences, 4 key heads, 3,000 slots: 35 against 46 us)
+        const unsigned two = static_cast<unsigned>((c.slots() + 255) / 256);
+        const bool wide = static_cast<unsigned long long>(two) * heads >= 2048;
+        e = launch_kernel(wide ? weights_kernel<D, 2> : weights_kernel<D, 1>,
+                          dim3(wide ? two : static_cast<unsigned>((c.slots() + 127) / 128), heads),
                           dim3(256), st, w, c);
     }
     return e == hipSuccess ? DD_OK : DD_ERR_HIP;
@@ -620,11 +829,9 @@ int launch_attn_d(const CacheAttnArgs &a)
 
 }  // namespace
 
-size_t cache_attn_workspace_bytes(const CacheShape &c, int H)
+size_t cache_attn_workspace_bytes(const CacheShape &c, int H, bool weights)
 {
-    const AttnPlan p = attn_plan(c, H);
-    return p.splits == 1 ? 0
-                         : p.splits * static_cast<size_t>(c.T) * H * (c.D + 1) * sizeof(float);
+    return attn_plan(c, H, weights).bytes;
 }
 
 int launch_cache_attn(const CacheAttnArgs &a)

@@ -219,7 +219,7 @@ struct CacheAttnArgs {
     int H;
     void *workspace, *stream;
 };
-size_t cache_attn_workspace_bytes(const CacheShape &c, int H);
+size_t cache_attn_workspace_bytes(const CacheShape &c, int H, bool weights);
 int launch_cache_attn(const CacheAttnArgs &a);
 
 // The `budget` slots of most weight stay (dd_cache.hip).

@@ -82,15 +82,15 @@ def test_attention_refusals(lib):
                dict(W_out=fake(8)), dict(W_in=fake(12))):
         assert call(lib, "dd_cache_attn_fwd", ATTN, **kw) == ALIAS, kw
     big = dict(ATTN, per=64, pages=128)
-    need = lib.dd_cache_attn_workspace_bytes(8, 2, 4, 2, 64, 16, 64)
-    assert need > 0
+    need = lib.dd_cache_attn_workspace_bytes(8, 2, 4, 2, 64, 16, 64, 1)
+    assert need >= lib.dd_cache_attn_workspace_bytes(8, 2, 4, 2, 64, 16, 64, 0) > 0
     assert call(lib, "dd_cache_attn_fwd", big, ws=None) == WORKSPACE
     assert call(lib, "dd_cache_attn_fwd", big, bytes=need - 1) == WORKSPACE
     assert call(lib, "dd_cache_attn_fwd", big, ws=fake(15, 8)) == ALIGN
     assert call(lib, "dd_cache_attn_fwd", big, ws=fake(11)) == ALIAS
-    assert lib.dd_cache_attn_workspace_bytes(0, 2, 4, 2, 64, 16, 64) == 0
-    assert lib.dd_cache_attn_workspace_bytes(8, 2, 4, 2, 80, 16, 64) == 0
-    assert lib.dd_cache_attn_workspace_bytes(8, 2, 5, 2, 64, 16, 64) == 0
+    assert lib.dd_cache_attn_workspace_bytes(0, 2, 4, 2, 64, 16, 64, 0) == 0
+    assert lib.dd_cache_attn_workspace_bytes(8, 2, 4, 2, 80, 16, 64, 1) == 0
+    assert lib.dd_cache_attn_workspace_bytes(8, 2, 5, 2, 64, 16, 64, 0) == 0
 
 
 def test_evict_refusals(lib):

@@ -33,6 +33,10 @@ CASES = [
     ([2500], [65], 3, 1, 64, 64, 0),
     ([700, 64], [66, 190], 4, 2, 64, 1024, 7),
     ([31, 32, 33, 127, 128, 129], [33, 97, 95, 1, 128, 127], 2, 2, 64, 16, 0),
+    # few rows on the average, many in one sequence; scores kept and not
+    ([50] * 15 + [300], [1] * 15 + [100], 1, 1, 64, 16, 0),
+    ([2000] + [5] * 11, [75] + [1] * 11, 2, 2, 128, 32, 0),
+    ([300, 20], [9, 9], 2, 2, 64, 16, 3),
 ]
 
 
@@ -289,6 +293,7 @@ def evict_state(lens, Hkv, slots, seed, ties=False):
 @pytest.mark.parametrize("in_place", [False, True])
 @pytest.mark.parametrize("ties", [False, True])
 @pytest.mark.parametrize("lens,slots,budget,recent", [
+    ([12000, 9000], 12016, 5000, 100), ([20000], 20000, 17000, 3),
     ([100, 7, 0, 64], 112, 40, 8), ([5], 16, 1, 0), ([5], 16, 1, 1), ([48, 47], 48, 47, 47),
     ([48], 48, 48, 3), ([3000, 2999], 3008, 1025, 300), ([2100], 2112, 2000, 0),
     ([1300, 1200], 1312, 64, 64)])
