@@ -397,7 +397,8 @@ size_t dd_gemm_i8_wgrad_workspace_bytes(int T, int M, int N, int n); /* 0: inval
  *                  budget); a sequence with no more slots keeps all of them.
  *                  W_out and P_out (positions) hold lens_out slots, the rest is
  *                  left as it was; W_out may be W_in, P_out P_in, lens_out lens.
- *                  workspace: dd_cache_evict_workspace_bytes(...) bytes.
+ *                  workspace: dd_cache_evict_workspace_bytes(...) bytes, 4-byte
+ *                  aligned.
  */
 int dd_cache_append(const void *Q, long long ldq, const void *K, long long ldk, const void *V,
                     long long ldv, void *Qrot, void *Kp, void *Vp, int32_t *positions,
@@ -415,7 +416,8 @@ int dd_cache_evict(void *Kp, void *Vp, const int32_t *table, const int32_t *lens
                    const int32_t *P_in, const int32_t *seen, float *W_out, int32_t *P_out,
                    int32_t *lens_out, int B, int Hkv, int D, int pages, int page, int per,
                    int budget, int recent, void *workspace, size_t workspace_bytes, void *stream);
-size_t dd_cache_evict_workspace_bytes(int B, int Hkv, int D, int page, int per, int budget);
+size_t dd_cache_evict_workspace_bytes(int B, int Hkv, int D, int page, int per, int budget,
+                                      int in_place); /* whether lens_out is lens */
 int dd_cache_check(const int32_t *host_table, const int32_t *host_lens, const int32_t *host_cu_new,
                    int T, int B, int pages, int page, int per); /* cu_new NULL: no new tokens */
 

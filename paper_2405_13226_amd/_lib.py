@@ -59,7 +59,7 @@ SIGNATURES = {
     "dd_cache_attn_fwd": (ctypes.c_int, [_P, _L, *[_P] * 9, *[_I] * 8, _P, ctypes.c_size_t, _P]),
     "dd_cache_attn_workspace_bytes": (ctypes.c_size_t, [_I] * 8),
     "dd_cache_evict": (ctypes.c_int, [*[_P] * 10, *[_I] * 8, _P, ctypes.c_size_t, _P]),
-    "dd_cache_evict_workspace_bytes": (ctypes.c_size_t, [_I] * 6),
+    "dd_cache_evict_workspace_bytes": (ctypes.c_size_t, [_I] * 7),
     "dd_cache_check": (ctypes.c_int, [_P, _P, _P, *[_I] * 5]),
     "dd_logprobs_fwd": (ctypes.c_int, [_P, _L, _I, *[_P] * 6, _I, _I, _I, _P, ctypes.c_size_t, _P]),
     "dd_logprobs_workspace_bytes": (ctypes.c_size_t, [_I] * 3),

@@ -28,13 +28,43 @@ scratch, and can be captured in a graph.
 from __future__ import annotations
 
 import ctypes
+import functools
 
 import numpy as np
 import torch
 
 from ._lib import check, lib
 from .attention import _ptr as _p
-from .block_ops import _call, _need
+from .block_ops import _call, _entry
+
+_BF16, _F32, _I32 = torch.bfloat16, torch.float32, torch.int32
+
+
+@functools.lru_cache(maxsize=None)
+def _bytes(name, *sizes):
+    """Workspace bytes of a call: of its sizes alone."""
+    return _entry(name)(*sizes)
+
+
+# A call for a few tokens takes a dozen microseconds, most of them here: each
+# wrapper looks at all its tensors in one expression first, and asks the
+# functions below only for the reason of a refusal.
+
+
+def _is(t, shape, dtype, i):
+    """Whether t is a contiguous tensor of this shape and type on device i."""
+    return (t.dtype is dtype and t.shape == shape and t.get_device() == i and t.is_contiguous())
+
+
+def _held(k, v, shape, i):
+    """Whether k and v are the pages of a cache on device i."""
+    return (k.dtype is _BF16 and v.dtype is _BF16 and k.shape == shape == v.shape
+            and k.get_device() == i == v.get_device() and k.is_contiguous() and v.is_contiguous())
+
+
+def _like(q, ld):
+    """A new contiguous tensor of q's shape (the shorter call where q is one)."""
+    return torch.empty_like(q) if ld == q.shape[1] * q.shape[2] else q.new_empty(q.shape)
 
 
 def _rows3(t, name, dev=None, heads=None, dim=None):
@@ -122,39 +152,56 @@ def cache_append(q, k, v, k_pages, v_pages, table, lens, cu_new, rope_base=None,
     which may be a contiguous q; q may be None), new token i of sequence b at
     position start[b] + i (int32 [B]; its slot without ``start``).
     ``positions`` (optional) receives the position of each written slot."""
-    T, Hkv, D, ldk = _rows3(k, "k")
-    dev = k.device
-    ldv = _rows3(v, "v", dev, Hkv, D)[3]
-    if v.shape[0] != T:
-        raise ValueError(f"k has {T} tokens, v has {v.shape[0]}")
-    pages, heads, page, dim = _pages(k_pages, v_pages, dev)
-    if (heads, dim) != (Hkv, D):
-        raise ValueError(f"k has {Hkv} heads of {D}, the pages {heads} of {dim}")
-    B, per = _table(table, lens, dev)
-    _state(cu_new, "cu_new", (B + 1,), torch.int32, dev)
-    if start is not None:
-        _state(start, "start", (B,), torch.int32, dev)
-    if positions is not None:
-        _state(positions, "positions", (B, Hkv, per * page), torch.int32, dev)
+    try:
+        (T, Hkv, D), (ldk, hk, one_k), (ldv, hv, one_v) = k.shape, k.stride(), v.stride()
+        pages, _, page, _ = k_pages.shape
+        B, per = table.shape
+        i = k.get_device()
+        if T == 1:
+            ldk = ldv = Hkv * D
+        fine = (k.dtype is _BF16 and v.dtype is _BF16 and v.shape == k.shape and i >= 0
+                and one_k == one_v == 1 and hk == hv == D and ldk >= Hkv * D <= ldv
+                and v.get_device() == i and _held(k_pages, v_pages, (pages, Hkv, page, D), i)
+                and table.dtype is _I32 and table.get_device() == i and table.is_contiguous()
+                and _is(lens, (B,), _I32, i) and _is(cu_new, (B + 1,), _I32, i)
+                and (start is None or _is(start, (B,), _I32, i))
+                and (positions is None or _is(positions, (B, Hkv, per * page), _I32, i)))
+    except (AttributeError, TypeError, ValueError):
+        fine = False
+    if not fine:
+        T, Hkv, D, ldk = _rows3(k, "k")
+        ldv = _rows3(v, "v", k.device, Hkv, D)[3]
+        if v.shape[0] != T:
+            raise ValueError(f"k has {T} tokens, v has {v.shape[0]}")
+        pages, heads, page, dim = _pages(k_pages, v_pages, k.device)
+        if (heads, dim) != (Hkv, D):
+            raise ValueError(f"k has {Hkv} heads of {D}, the pages {heads} of {dim}")
+        B, per = _table(table, lens, k.device)
+        _state(cu_new, "cu_new", (B + 1,), _I32, k.device)
+        if start is not None:
+            _state(start, "start", (B,), _I32, k.device)
+        if positions is not None:
+            _state(positions, "positions", (B, Hkv, per * page), _I32, k.device)
     H, ldq, rot = Hkv, 0, None
     if q is not None:
-        Tq, H, _, ldq = _rows3(q, "q", dev, None, D)
+        Tq, H, _, ldq = _rows3(q, "q", k.device, None, D)
         if Tq != T:
             raise ValueError(f"q has {Tq} tokens, k has {T}")
-    if rope_base is not None and q is not None:
-        if out is None:
-            out = torch.empty((T, H, D), dtype=torch.bfloat16, device=dev)
-        else:
-            _state(out, "out", (T, H, D), torch.bfloat16, dev)
-        rot = out
-    elif out is not None:
-        raise ValueError("out is the rotated q: it needs rope_base and q")
+    if rope_base is None or q is None:
+        if out is not None:
+            raise ValueError("out is the rotated q: it needs rope_base and q")
+        H = Hkv  # (q is not read)
+    else:
+        rot = _like(q, ldq) if out is None else out
+        if out is not None:
+            _state(out, "out", (T, H, D), _BF16, k.device)
     if rope_base is not None and not rope_base > 0:
         raise ValueError(f"rope_base must be positive (got {rope_base})")
     if T and B:
-        _call(dev, "dd_cache_append", _p(q) if rot is not None else None, ldq, _p(k), ldk, _p(v),
-              ldv, _p(rot), _p(k_pages), _p(v_pages), _p(positions), _p(table), _p(lens), _p(start),
-              _p(cu_new), T, B, H, Hkv, D, pages, page, per, rope_base or 0.0)
+        _call(k.device, "dd_cache_append", q.data_ptr() if rot is not None else None, ldq,
+              k.data_ptr(), ldk, v.data_ptr(), ldv, _p(rot), k_pages.data_ptr(),
+              v_pages.data_ptr(), _p(positions), table.data_ptr(), lens.data_ptr(), _p(start),
+              cu_new.data_ptr(), T, B, H, Hkv, D, pages, page, per, rope_base or 0.0)
     return q if rot is None else rot
 
 
@@ -165,38 +212,55 @@ def cache_attention(q, k_pages, v_pages, table, lens, cu_new, weights=None, weig
     b sees slots 0 .. lens[b] + i.  ``weights`` (optional) is brought up to date
     in place, or into ``weights_out``.  ``out`` and ``lse`` receive the results
     if given (both, or neither)."""
-    T, H, D, ldq = _rows3(q, "q")
-    dev = q.device
-    pages, Hkv, page, dim = _pages(k_pages, v_pages, dev)
-    if dim != D or not Hkv or H % Hkv:
-        raise ValueError(f"q has {H} heads of {D}, the pages {Hkv} of {dim}")
-    B, per = _table(table, lens, dev)
-    _state(cu_new, "cu_new", (B + 1,), torch.int32, dev)
-    if weights is not None:
-        _state(weights, "weights", (B, Hkv, per * page), torch.float32, dev)
-    if weights_out is not None:
-        if weights is None:
-            raise ValueError("weights_out needs weights")
-        _state(weights_out, "weights_out", (B, Hkv, per * page), torch.float32, dev)
+    try:
+        (T, H, D), (ldq, head, one) = q.shape, q.stride()
+        pages, Hkv, page, _ = k_pages.shape
+        B, per = table.shape
+        i = q.get_device()
+        if T == 1:
+            ldq = H * D
+        fine = (q.dtype is _BF16 and i >= 0 and one == 1 and head == D and ldq >= H * D and not H % Hkv
+                and _held(k_pages, v_pages, (pages, Hkv, page, D), i)
+                and table.dtype is _I32 and table.get_device() == i and table.is_contiguous()
+                and _is(lens, (B,), _I32, i) and _is(cu_new, (B + 1,), _I32, i))
+        if fine and weights is not None:
+            slots = (B, Hkv, per * page)
+            fine = _is(weights, slots, _F32, i) and (weights_out is None
+                                                     or _is(weights_out, slots, _F32, i))
+    except (AttributeError, TypeError, ValueError, ZeroDivisionError):
+        fine = False
+    if not fine:
+        T, H, D, ldq = _rows3(q, "q")
+        pages, Hkv, page, dim = _pages(k_pages, v_pages, q.device)
+        if dim != D or not Hkv or H % Hkv:
+            raise ValueError(f"q has {H} heads of {D}, the pages {Hkv} of {dim}")
+        B, per = _table(table, lens, q.device)
+        _state(cu_new, "cu_new", (B + 1,), _I32, q.device)
+        for t, name in ((weights, "weights"), (weights_out, "weights_out")):
+            if t is not None:
+                _state(t, name, (B, Hkv, per * page), _F32, q.device)
+    if weights_out is None:
+        weights_out = weights
+    elif weights is None:
+        raise ValueError("weights_out needs weights")
     if (out is None) != (lse is None):
         raise ValueError("give both out and lse, or neither")
+    dev = q.device
     if out is None:
-        out = torch.empty((T, H, D), dtype=torch.bfloat16, device=dev)
-        lse = torch.empty((T, H), dtype=torch.float32, device=dev)
+        out = _like(q, ldq)
+        lse = q.new_empty((T, H), dtype=_F32)
     else:
-        _state(out, "out", (T, H, D), torch.bfloat16, dev)
-        _state(lse, "lse", (T, H), torch.float32, dev)
+        _state(out, "out", (T, H, D), _BF16, dev)
+        _state(lse, "lse", (T, H), _F32, dev)
     if not (T and B):
-        if weights_out is not None and weights_out is not weights:
+        if weights_out is not weights:
             weights_out.copy_(weights)
         return out, lse
-    need = _need(dev, "dd_cache_attn_workspace_bytes", T, B, H, Hkv, D, page, per,
-                 weights is not None)
+    need = _bytes("dd_cache_attn_workspace_bytes", T, B, H, Hkv, D, page, per, weights is not None)
     ws = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
-    _call(dev, "dd_cache_attn_fwd", _p(q), ldq, _p(k_pages), _p(v_pages), _p(table), _p(lens),
-          _p(cu_new), _p(out), _p(lse), _p(weights),
-          _p(weights if weights_out is None else weights_out), T, B, H, Hkv, D, pages, page, per,
-          _p(ws), need)
+    _call(dev, "dd_cache_attn_fwd", q.data_ptr(), ldq, k_pages.data_ptr(), v_pages.data_ptr(),
+          table.data_ptr(), lens.data_ptr(), cu_new.data_ptr(), out.data_ptr(), lse.data_ptr(),
+          _p(weights), _p(weights_out), T, B, H, Hkv, D, pages, page, per, _p(ws), need)
     return out, lse
 
 
@@ -210,31 +274,46 @@ def cache_evict(k_pages, v_pages, table, lens, weights, positions, seen, budget:
     that stays.  Returns (weights, positions, lens) of the slots that are left
     (new tensors, defined up to the new lens, or ``out``: three tensors, each of
     which may be the input itself)."""
-    pages, Hkv, page, D = _pages(k_pages, v_pages)
-    dev = k_pages.device
-    B, per = _table(table, lens, dev)
-    _state(weights, "weights", (B, Hkv, per * page), torch.float32, dev)
-    _state(positions, "positions", (B, Hkv, per * page), torch.int32, dev)
-    _state(seen, "seen", (B,), torch.int32, dev)
+    try:
+        pages, Hkv, page, D = shape = k_pages.shape
+        B, per = table.shape
+        i = k_pages.get_device()
+        slots = (B, Hkv, per * page)
+        fine = (i >= 0 and _held(k_pages, v_pages, shape, i)
+                and table.dtype is _I32 and table.get_device() == i and table.is_contiguous()
+                and _is(lens, (B,), _I32, i) and _is(seen, (B,), _I32, i)
+                and _is(weights, slots, _F32, i) and _is(positions, slots, _I32, i))
+    except (AttributeError, TypeError, ValueError):
+        fine = False
+    if not fine:
+        pages, Hkv, page, D = _pages(k_pages, v_pages)
+        dev = k_pages.device
+        B, per = _table(table, lens, dev)
+        _state(weights, "weights", (B, Hkv, per * page), _F32, dev)
+        _state(positions, "positions", (B, Hkv, per * page), _I32, dev)
+        _state(seen, "seen", (B,), _I32, dev)
     if not 0 <= recent <= budget or budget < 1:
         raise ValueError(f"need 0 <= recent <= budget and a budget of at least 1 "
                          f"(got {recent} and {budget})")
     budget = min(int(budget), max(per * page, 1))
+    recent = min(int(recent), budget)
+    dev = k_pages.device
     if out is None:
-        out = tuple(torch.empty_like(t) for t in (weights, positions, lens))
+        w, p, n = torch.empty_like(weights), torch.empty_like(positions), torch.empty_like(lens)
     else:
-        out = tuple(out)
-        for t, like, name in zip(out, (weights, positions, lens), ("weights", "positions", "lens")):
+        w, p, n = out
+        for t, like, name in ((w, weights, "weights"), (p, positions, "positions"),
+                              (n, lens, "lens")):
             _state(t, "out " + name, like.shape, like.dtype, dev)
-        if len(out) != 3:
-            raise ValueError("out must hold weights, positions and lens")
     if B and Hkv and per:
-        need = _need(dev, "dd_cache_evict_workspace_bytes", B, Hkv, D, page, per, budget)
-        ws = torch.empty(max(need, 4), dtype=torch.uint8, device=dev)
-        _call(dev, "dd_cache_evict", _p(k_pages), _p(v_pages), _p(table), _p(lens), _p(weights),
-              _p(positions), _p(seen), *(_p(t) for t in out), B, Hkv, D, pages, page, per, budget,
-              min(int(recent), budget), _p(ws), need)
-    return out
+        in_place = n.data_ptr() == lens.data_ptr()
+        need = _bytes("dd_cache_evict_workspace_bytes", B, Hkv, D, page, per, budget, in_place)
+        ws = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
+        _call(dev, "dd_cache_evict", k_pages.data_ptr(), v_pages.data_ptr(), table.data_ptr(),
+              lens.data_ptr(), weights.data_ptr(), positions.data_ptr(), seen.data_ptr(),
+              w.data_ptr(), p.data_ptr(), n.data_ptr(), B, Hkv, D, pages, page, per, budget, recent,
+              _p(ws), need)
+    return w, p, n
 
 
 class PagedCache:

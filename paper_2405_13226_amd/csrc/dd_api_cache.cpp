@@ -192,12 +192,13 @@ int dd_cache_attn_fwd(const void *Q, long long ldq, const void *Kp, const void *
         dd::CacheAttnArgs{c, Q, Kp, Vp, O, LSE, W_in, W_out, ldq, H, workspace, stream});
 }
 
-size_t dd_cache_evict_workspace_bytes(int B, int Hkv, int D, int page, int per, int budget)
+size_t dd_cache_evict_workspace_bytes(int B, int Hkv, int D, int page, int per, int budget,
+                                      int in_place)
 {
     if (shape_status(1, B, Hkv, Hkv, D, 1, page, per) != DD_OK || budget < 1)
         return 0;
     return dd::cache_evict_workspace_bytes(
-        shape(nullptr, nullptr, nullptr, 1, B, Hkv, D, 1, page, per), budget);
+        shape(nullptr, nullptr, nullptr, 1, B, Hkv, D, 1, page, per), budget, in_place != 0);
 }
 
 int dd_cache_evict(void *Kp, void *Vp, const int32_t *table, const int32_t *lens, const float *W_in,
@@ -217,10 +218,10 @@ int dd_cache_evict(void *Kp, void *Vp, const int32_t *table, const int32_t *lens
         !aligned(P_out, 4) || !aligned(lens_out, 4))
         return DD_ERR_ALIGN;
     const dd::CacheShape c = shape(table, lens, nullptr, 1, B, Hkv, D, pages, page, per);
-    const size_t need = dd::cache_evict_workspace_bytes(c, budget);
-    if (!workspace || workspace_bytes < need)
+    const size_t need = dd::cache_evict_workspace_bytes(c, budget, lens == lens_out);
+    if (need && (!workspace || workspace_bytes < need))
         return DD_ERR_WORKSPACE;
-    if (!aligned(workspace, 4))
+    if (need && !aligned(workspace, 4))
         return DD_ERR_ALIGN;
     const long long slots = static_cast<long long>(B) * Hkv * per * page;
     // each state in place, or apart

@@ -20,7 +20,8 @@
 //           and a prefix sum over the workgroup orders equal ones, another the
 //           lists.  (Beyond 16,384 slots per sequence they are read again for
 //           each histogram and for the lists.)
-//   move:   the listed rows
+//   move:   the listed rows (by the workgroup that found them, where they are
+//           few: one launch, no memory for the lists)
 #include "dd_cache.hpp"
 #include "dd_internal.h"
 #include "dd_launch.hpp"
@@ -165,15 +166,45 @@ __device__ __forceinline__ uint32_t block_prefix(uint32_t x, uint32_t *waves, ui
     return before + s - x;
 }
 
+constexpr int kFewMoves = 512;  // entries of a list that stays in LDS
+
+// Moves rows r0, r0 + step, ... of n: row to[r] receives row from[r].
+template <int D>
+__device__ __forceinline__ void move_rows(const EvictRows &a, const CacheView &c, int bh,
+                                          const int32_t *to, const int32_t *from, int n, int r0,
+                                          int step)
+{
+    const int b = bh / c.Hkv, h = bh % c.Hkv, cg = threadIdx.x % (D / 8);
+    const long long base = static_cast<long long>(bh) * c.slots();
+    for (int r = r0; r < n; r += step) {
+        const int d = to[r], s = from[r];
+        const int pd = cache_page(c, b, d), ps = cache_page(c, b, s);
+        if (pd >= 0 && ps >= 0) {
+            const long long rd = cache_row(c, pd, h, d) * D + cg * 8;
+            const long long rs = cache_row(c, ps, h, s) * D + cg * 8;
+            const u32x4 k = *reinterpret_cast<const u32x4 *>(a.Kp + rs);
+            const u32x4 v = *reinterpret_cast<const u32x4 *>(a.Vp + rs);
+            *reinterpret_cast<u32x4 *>(a.Kp + rd) = k;
+            *reinterpret_cast<u32x4 *>(a.Vp + rd) = v;
+        }
+        if (cg == 0) {
+            a.Wout[base + d] = a.W[base + s];
+            a.Pout[base + d] = a.P[base + s];
+        }
+    }
+}
+
 // A thread holds HELD consecutive slots; ONE: the sequence's slots are at most
-// NT * HELD.
-template <int NT, int HELD, bool ONE>
+// NT * HELD.  MOVE (D, or 0): the workgroup moves its rows too; lens_out is not
+// lens then (other heads' workgroups still read that).
+template <int NT, int HELD, bool ONE, int MOVE = 0>
 __global__ void __launch_bounds__(NT) select_kernel(EvictRows a, CacheView c)
 {
     constexpr int BINS = 2048, SPAN = NT * HELD;
     __shared__ uint32_t hist[BINS];
     __shared__ uint32_t waves[NT / 64];
     __shared__ uint32_t found[2];
+    __shared__ int32_t lists[MOVE ? 2 * kFewMoves : 1];
     const int bh = static_cast<int>(blockIdx.x), b = bh / c.Hkv, tid = threadIdx.x;
     const int n = min(max(c.lens[b], 0), c.slots());
     const long long base = static_cast<long long>(bh) * c.slots();
@@ -181,8 +212,10 @@ __global__ void __launch_bounds__(NT) select_kernel(EvictRows a, CacheView c)
     const int32_t *P = a.P + base;
     float *Wout = a.Wout + base;
     int32_t *Pout = a.Pout + base;
+    if (MOVE && tid == 0 && bh % c.Hkv == 0)
+        a.lens_out[b] = min(n, a.budget);
     if (n <= a.budget) {
-        if (tid == 0)
+        if (!MOVE && tid == 0)
             a.count[bh] = 0;
         if (Wout != W || Pout != P)
             for (int j = tid; j < n; j += NT) {
@@ -275,8 +308,8 @@ __global__ void __launch_bounds__(NT) select_kernel(EvictRows a, CacheView c)
     }
 
     // Holes and survivors in slot order.
-    int32_t *to = a.to + static_cast<long long>(bh) * a.list;
-    int32_t *from = a.from + static_cast<long long>(bh) * a.list;
+    int32_t *to = MOVE ? lists : a.to + static_cast<long long>(bh) * a.list;
+    int32_t *from = MOVE ? lists + kFewMoves : a.from + static_cast<long long>(bh) * a.list;
     uint32_t equal = 0, holes = 0, extra = 0;  // so far
     for (int s0 = 0; s0 < n; s0 += SPAN) {
         const int j0 = s0 + tid * HELD;
@@ -316,38 +349,26 @@ __global__ void __launch_bounds__(NT) select_kernel(EvictRows a, CacheView c)
         holes += all & 0xffffu;
         extra += all >> 16;
     }
-    if (tid == 0)
+    if constexpr (MOVE != 0) {
+        // (the barrier also orders the copies of evicted weights before the moves)
+        __syncthreads();
+        move_rows<MOVE>(a, c, bh, to, from, static_cast<int>(holes), tid / (MOVE / 8), NT / (MOVE / 8));
+    } else if (tid == 0) {
         a.count[bh] = static_cast<int>(holes);
+    }
 }
 
 template <int D>
 __global__ void __launch_bounds__(256) move_kernel(EvictRows a, CacheView c)
 {
-    constexpr int CG = D / 8, ROWS = 256 / CG;
-    const int bh = static_cast<int>(blockIdx.y), b = bh / c.Hkv, h = bh % c.Hkv;
-    if (blockIdx.x == 0 && h == 0 && threadIdx.x == 0)
+    constexpr int ROWS = 256 / (D / 8);
+    const int bh = static_cast<int>(blockIdx.y), b = bh / c.Hkv;
+    if (blockIdx.x == 0 && bh % c.Hkv == 0 && threadIdx.x == 0)
         a.lens_out[b] = min(min(max(c.lens[b], 0), c.slots()), a.budget);
-    const int n = a.count[bh], cg = threadIdx.x % CG;
-    const long long base = static_cast<long long>(bh) * c.slots();
-    const int32_t *to = a.to + static_cast<long long>(bh) * a.list;
-    const int32_t *from = a.from + static_cast<long long>(bh) * a.list;
-    for (int r = static_cast<int>(blockIdx.x) * ROWS + threadIdx.x / CG; r < n;
-         r += static_cast<int>(gridDim.x) * ROWS) {
-        const int d = to[r], s = from[r];
-        const int pd = cache_page(c, b, d), ps = cache_page(c, b, s);
-        if (pd >= 0 && ps >= 0) {
-            const long long rd = cache_row(c, pd, h, d) * D + cg * 8;
-            const long long rs = cache_row(c, ps, h, s) * D + cg * 8;
-            const u32x4 k = *reinterpret_cast<const u32x4 *>(a.Kp + rs);
-            const u32x4 v = *reinterpret_cast<const u32x4 *>(a.Vp + rs);
-            *reinterpret_cast<u32x4 *>(a.Kp + rd) = k;
-            *reinterpret_cast<u32x4 *>(a.Vp + rd) = v;
-        }
-        if (cg == 0) {
-            a.Wout[base + d] = a.W[base + s];
-            a.Pout[base + d] = a.P[base + s];
-        }
-    }
+    const long long list = static_cast<long long>(bh) * a.list;
+    move_rows<D>(a, c, bh, a.to + list, a.from + list, a.count[bh],
+                 static_cast<int>(blockIdx.x) * ROWS + threadIdx.x / (D / 8),
+                 static_cast<int>(gridDim.x) * ROWS);
 }
 
 // Entries of a list: holes lie below the budget, survivors behind it.
@@ -363,8 +384,10 @@ int launch_cache_append(const CacheAppendArgs &a)
     return a.c.D == 64 ? launch_append_d<64>(a) : launch_append_d<128>(a);
 }
 
-size_t cache_evict_workspace_bytes(const CacheShape &c, int budget)
+size_t cache_evict_workspace_bytes(const CacheShape &c, int budget, bool in_place)
 {
+    if (evict_list(c, budget) <= kFewMoves && !in_place)
+        return 0;
     return static_cast<size_t>(c.B) * c.Hkv * (1 + 2 * static_cast<size_t>(evict_list(c, budget))) *
            sizeof(int32_t);
 }
@@ -381,6 +404,15 @@ int launch_cache_evict(const CacheEvictArgs &a)
     hipStream_t st = static_cast<hipStream_t>(a.stream);
     const int slots = c.slots();
     const dim3 grid(static_cast<unsigned>(bh));
+    if (list <= kFewMoves && a.lens_out != a.c.lens) {
+        const bool narrow = a.c.D == 64;
+        const hipError_t e =
+            slots <= 2048 ? launch_kernel(narrow ? select_kernel<256, 8, true, 64> : select_kernel<256, 8, true, 128>, grid, dim3(256), st, r, c)
+            : slots <= 8192 ? launch_kernel(narrow ? select_kernel<1024, 8, true, 64> : select_kernel<1024, 8, true, 128>, grid, dim3(1024), st, r, c)
+            : slots <= 16384 ? launch_kernel(narrow ? select_kernel<1024, 16, true, 64> : select_kernel<1024, 16, true, 128>, grid, dim3(1024), st, r, c)
+                             : launch_kernel(narrow ? select_kernel<1024, 16, false, 64> : select_kernel<1024, 16, false, 128>, grid, dim3(1024), st, r, c);
+        return e == hipSuccess ? DD_OK : DD_ERR_HIP;
+    }
     hipError_t e = slots <= 2048    ? launch_kernel(select_kernel<256, 8, true>, grid, dim3(256), st, r, c)
                    : slots <= 8192  ? launch_kernel(select_kernel<1024, 8, true>, grid, dim3(1024), st, r, c)
                    : slots <= 16384 ? launch_kernel(select_kernel<1024, 16, true>, grid, dim3(1024), st, r, c)

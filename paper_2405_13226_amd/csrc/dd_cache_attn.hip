@@ -28,8 +28,8 @@
 // Slots behind a sequence's last are never read (a tile's rows are clamped to
 // it).  A slot that a row may not see leaves no trace in it, whatever it
 // holds: its score is replaced, and where a boundary tile holds values that
-// are not finite its slots are added one by one, each to the rows that see it
-// (zero times infinity would not be zero).
+// are not finite its keys are added one by one, each only to the rows that see
+// it (zero times infinity would not be zero).
 #include "dd_cache.hpp"
 #include "dd_internal.h"
 #include "dd_launch.hpp"
@@ -465,42 +465,63 @@ __global__ void __launch_bounds__(64 * NW) few_kernel(AttnRows a, CacheView c)
         }
     }
 
-    // The other waves hand over through LDS (every wave is done with its stages).
+    // The waves' sums on a common maximum, through LDS (every wave is done with
+    // its stages): each wave adds up and stores every NW-th piece of 4 values.
     constexpr int NS = 1 + 4 * DB;
     float *x = reinterpret_cast<float *>(lds) + lane * 4;
     __syncthreads();
-    if (wave > 0) {
-        float *y = x + (wave - 1) * NS * 256;
-        *reinterpret_cast<f32x4 *>(y) = f32x4{m_i, l_i, 0.f, 0.f};
+    float *y = x + wave * NS * 256;
+    *reinterpret_cast<f32x4 *>(y) = f32x4{m_i, l_i, 0.f, 0.f};
 #pragma unroll
-        for (int r = 0; r < 4 * DB; ++r) {
-            f32x4 v;
+    for (int r = 0; r < 4 * DB; ++r) {
+        f32x4 v;
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                v[e] = acc[r >> 2][4 * (r & 3) + e];
-            *reinterpret_cast<f32x4 *>(y + (r + 1) * 256) = v;
-        }
+        for (int e = 0; e < 4; ++e)
+            v[e] = acc[r >> 2][4 * (r & 3) + e];
+        *reinterpret_cast<f32x4 *>(y + (r + 1) * 256) = v;
     }
     __syncthreads();
-    if (wave > 0)
-        return;
-#pragma unroll 1
-    for (int o = 0; o < NW - 1; ++o) {
-        const float *y = x + o * NS * 256;
-        const f32x4 ml = *reinterpret_cast<const f32x4 *>(y);
-        const float m = fmaxf(m_i, ml[0]), ref = m == -INFINITY ? 0.f : m;
-        const float a0 = fast_exp2(m_i - ref), a1 = fast_exp2(ml[0] - ref);
-        m_i = m;
-        l_i = l_i * a0 + ml[1] * a1;
+    float scale[NW], m = -INFINITY, l = 0.f;
 #pragma unroll
-        for (int r = 0; r < 4 * DB; ++r) {
-            const f32x4 v = *reinterpret_cast<const f32x4 *>(y + (r + 1) * 256);
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                acc[r >> 2][4 * (r & 3) + e] = acc[r >> 2][4 * (r & 3) + e] * a0 + v[e] * a1;
-        }
+    for (int w = 0; w < NW; ++w) {
+        scale[w] = x[w * NS * 256];
+        m = fmaxf(m, scale[w]);
     }
-    store_rows<D>(c, a, it, it.row + l32, g, acc, m_i, l_i);
+    const float ref = m == -INFINITY ? 0.f : m;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+        scale[w] = fast_exp2(scale[w] - ref);
+        l += scale[w] * x[w * NS * 256 + 1];
+    }
+    l = halves_sum(l);
+    const int row = it.row + l32;
+    const bool one = a.splits == 1;
+    // (a part without a key of the row has l = 0)
+    const float inv = !one && l == 0.f ? 0.f : 1.0f / l;
+    const long long out = row_out(a, it, row);
+    const long long part = static_cast<long long>(it.split) * c.T * a.H + out;
+#pragma unroll
+    for (int i = 0; i < 4 * DB / NW; ++i) {
+        const int r = wave + i * NW;
+        f32x4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < NW; ++w)
+            v += scale[w] * *reinterpret_cast<const f32x4 *>(x + (w * NS + r + 1) * 256);
+        v *= inv;
+        const int at = 8 * r + 4 * g;
+        if (row >= it.rows)
+            continue;
+        if (one)
+            *reinterpret_cast<bf16x4 *>(a.O + out * D + at) = pack4(v[0], v[1], v[2], v[3]);
+        else
+            *reinterpret_cast<f32x4 *>(a.part_o + part * D + at) = v;
+    }
+    if (wave == 0 && g == 0 && row < it.rows) {
+        if (one)
+            a.LSE[out] = (m + log2f(l)) * kLn2;
+        else
+            a.part_lse[part] = m + log2f(l);
+    }
 }
 
 struct WeightRows {
@@ -528,6 +549,16 @@ __global__ void __launch_bounds__(256) finish_kernel(AttnRows a, WeightRows w, C
         if (row < static_cast<long long>(cache_cu(c, 0)) * a.H ||
             row >= static_cast<long long>(cache_cu(c, c.B)) * a.H)
             return;  // (whole groups of lanes)
+        // (the first parts are on their way while the sums are joined)
+        constexpr int BATCH = 8;
+        f32x4 v[BATCH];
+        auto load = [&](int s0) __attribute__((always_inline)) {
+            const float *part = a.part_o + row * D + 4 * x;
+#pragma unroll
+            for (int i = 0; i < BATCH; ++i)
+                v[i] = *reinterpret_cast<const f32x4 *>(part + min(s0 + i, a.splits - 1) * n * D);
+        };
+        load(0);
         float ls[SETS], m = -INFINITY;
 #pragma unroll
         for (int i = 0; i < SETS; ++i) {
@@ -549,13 +580,18 @@ __global__ void __launch_bounds__(256) finish_kernel(AttnRows a, WeightRows w, C
         for (int o = LANES / 2; o >= 1; o >>= 1)
             l += __shfl_xor(l, o);
         f32x4 o = {0.f, 0.f, 0.f, 0.f};
-        const float *part = a.part_o + row * D + 4 * x;
+        for (int s0 = 0; s0 < a.splits; s0 += BATCH) {
+            float w = ls[0];  // of the batch's parts, and others
 #pragma unroll
-        for (int i = 0; i < SETS; ++i)
-#pragma unroll 4
-            for (int s = i * LANES; s < min((i + 1) * LANES, a.splits); ++s)
-                o += __shfl(ls[i], s - i * LANES, LANES) *
-                     *reinterpret_cast<const f32x4 *>(part + s * n * D);
+            for (int i = 1; i < SETS; ++i)
+                w = s0 / LANES == i ? ls[i] : w;
+#pragma unroll
+            for (int i = 0; i < BATCH; ++i)
+                if (s0 + i < a.splits)
+                    o += __shfl(w, s0 % LANES + i, LANES) * v[i];
+            if (s0 + BATCH < a.splits)
+                load(s0 + BATCH);
+        }
         const float inv = 1.0f / l;
         const bf16x4 y = pack4(o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
         *reinterpret_cast<u32x2 *>(a.O + row * D + 4 * x) = __builtin_bit_cast(u32x2, y);
@@ -750,12 +786,15 @@ CacheView view(const CacheShape &c)
 // Waves of a workgroup with few rows: 64 KB of LDS, two workgroups per CU.  (At
 // D = 128 four waves, one workgroup per CU, read 8 x 8,192 slots of 8 key heads
 // in 46-56 us instead of 41-43: nothing runs while a workgroup begins or ends.)
+// Twice as many where a sequence's slots are few enough to be one part, which
+// saves the launch that joins parts and the memory for them.
 template <int D>
 constexpr int few_waves = D == 64 ? 4 : 2;
+constexpr long long kOnePart = 256 << 10;  // bytes of K and V
 
 // How a call runs: by what the host knows of it (rows, sequences, slots).
 struct AttnPlan {
-    bool few, scores;
+    bool few, scores, wide;
     int tiles, splits;
     size_t rows, part_bytes, bytes;  // of the parts, and of the whole workspace
 };
@@ -774,7 +813,8 @@ AttnPlan attn_plan(const CacheShape &c, int H, bool weights)
     // few rows: parts of 512 KB of K and V or more, smaller where that leaves
     // CUs idle, down to 128 slots; many: enough workgroups, of 512 slots or more
     const long long fill = (512 + work - 1) / work;
-    const long long want = p.few ? std::max(slots * c.D / 131072, std::min(fill, slots / 128))
+    p.wide = p.few && slots * c.D * 4 <= kOnePart && work < 512;
+    const long long want = p.wide ? 1 : p.few ? std::max(slots * c.D / 131072, std::min(fill, slots / 128))
                                  : std::min(512 / work, slots / 512);
     p.splits = static_cast<int>(std::clamp<long long>(want, 1, kMaxSplits));
     p.rows = static_cast<size_t>(c.T) * H;
@@ -803,11 +843,15 @@ int launch_attn_d(const CacheAttnArgs &a)
     hipStream_t st = static_cast<hipStream_t>(a.stream);
     const long long items = static_cast<long long>(p.tiles) * p.splits * a.c.Hkv;
     const unsigned grid = static_cast<unsigned>((items + kXcds - 1) / kXcds * kXcds);
-    constexpr int NW = few_waves<D>;
-    hipError_t e = launch_kernel(!p.few     ? tile_kernel<D>
-                                 : p.scores ? few_kernel<D, NW, true>
-                                            : few_kernel<D, NW, false>,
-                                 dim3(grid), dim3(p.few ? 64 * NW : 256), st, r, c);
+    constexpr int NW = few_waves<D>, WIDE = 2 * NW;
+    auto kern = p.scores ? few_kernel<D, NW, true> : few_kernel<D, NW, false>;
+    if (p.wide)
+        kern = p.scores ? few_kernel<D, WIDE, true> : few_kernel<D, WIDE, false>;
+    if (!p.few)
+        kern = tile_kernel<D>;
+    hipError_t e = launch_kernel(kern, dim3(grid),
+                                 dim3(static_cast<unsigned>(p.wide ? 64 * WIDE : p.few ? 64 * NW : 256)),
+                                 st, r, c);
     constexpr int ROWS = 256 / (D / 4);
     const unsigned joins = p.splits > 1 ? static_cast<unsigned>((p.rows + ROWS - 1) / ROWS) : 0;
     const unsigned heads = static_cast<unsigned>(a.c.B * a.c.Hkv);

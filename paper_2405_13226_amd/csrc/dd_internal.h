@@ -233,7 +233,8 @@ struct CacheEvictArgs {
     int budget, recent;
     void *workspace, *stream;
 };
-size_t cache_evict_workspace_bytes(const CacheShape &c, int budget);
+// in_place: lens_out is lens
+size_t cache_evict_workspace_bytes(const CacheShape &c, int budget, bool in_place);
 int launch_cache_evict(const CacheEvictArgs &a);
 
 // Log probabilities of given tokens (dd_logprobs.hip); X and dX bf16 or fp32.

@@ -14,7 +14,8 @@ from __future__ import annotations
 import torch
 
 from .attention import _ptr as _p
-from .block_ops import _call, _need, _vec
+from .block_ops import _call, _vec
+from .cache import _bytes
 
 MAX_TOP = 64
 
@@ -40,21 +41,30 @@ def logprobs(logits, targets, top: int = 0):
     entropy, and the log of the sum of exponentials; with ``top`` also the log
     probabilities (fp32 [rows, top]) and ids (int64) of the most likely tokens,
     in order, equal ones by the lowest id."""
+    return _logprobs(logits, targets, top, True)
+
+
+def _logprobs(logits, targets, top, shared):
+    """shared: logp, entropy and lse are rows of one tensor (one allocation)."""
     rows, V, ldx, f32 = _logits(logits, "logits")
     dev = logits.device
     _vec(targets, "targets", rows, torch.int64, dev)
     if not 0 <= top <= min(V, MAX_TOP):
         raise ValueError(f"top must be at most {min(V, MAX_TOP)} (got {top})")
-    logp, entropy, lse = (torch.empty(rows, dtype=torch.float32, device=dev) for _ in range(3))
+    if shared:
+        logp, entropy, lse = torch.empty((3, rows), dtype=torch.float32, device=dev).unbind()
+    else:
+        logp, entropy, lse = (torch.empty(rows, dtype=torch.float32, device=dev) for _ in range(3))
     best = ids = None
     if top:
         best = torch.empty((rows, top), dtype=torch.float32, device=dev)
         ids = torch.empty((rows, top), dtype=torch.int64, device=dev)
     if rows:
-        need = _need(dev, "dd_logprobs_workspace_bytes", rows, V, top)
+        need = _bytes("dd_logprobs_workspace_bytes", rows, V, top)
         ws = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
-        _call(dev, "dd_logprobs_fwd", _p(logits), ldx, f32, _p(targets), _p(logp), _p(entropy),
-              _p(lse), _p(best), _p(ids), rows, V, top, _p(ws), need)
+        _call(dev, "dd_logprobs_fwd", logits.data_ptr(), ldx, f32, targets.data_ptr(),
+              logp.data_ptr(), entropy.data_ptr(), lse.data_ptr(), _p(best), _p(ids), rows, V, top,
+              _p(ws), need)
     return (logp, entropy, lse, best, ids) if top else (logp, entropy, lse)
 
 
@@ -87,7 +97,7 @@ class LogProbFunction(torch.autograd.Function):
 
     @staticmethod
     def forward(ctx, logits, targets, top):
-        res = logprobs(logits, targets, top)
+        res = _logprobs(logits, targets, top, False)
         ctx.save_for_backward(logits, targets, res[2], res[1])
         ctx.set_materialize_grads(False)
         ctx.mark_non_differentiable(*res[3:])

@@ -81,9 +81,9 @@ def test_attention_refusals(lib):
     for kw in (dict(O=fake(0)), dict(O=fake(4)), dict(LSE=fake(11)), dict(W_out=fake(13, 4)),
                dict(W_out=fake(8)), dict(W_in=fake(12))):
         assert call(lib, "dd_cache_attn_fwd", ATTN, **kw) == ALIAS, kw
-    big = dict(ATTN, per=64, pages=128)
-    need = lib.dd_cache_attn_workspace_bytes(8, 2, 4, 2, 64, 16, 64, 1)
-    assert need >= lib.dd_cache_attn_workspace_bytes(8, 2, 4, 2, 64, 16, 64, 0) > 0
+    big = dict(ATTN, per=640, pages=1280)
+    need = lib.dd_cache_attn_workspace_bytes(8, 2, 4, 2, 64, 16, 640, 1)
+    assert need >= lib.dd_cache_attn_workspace_bytes(8, 2, 4, 2, 64, 16, 640, 0) > 0
     assert call(lib, "dd_cache_attn_fwd", big, ws=None) == WORKSPACE
     assert call(lib, "dd_cache_attn_fwd", big, bytes=need - 1) == WORKSPACE
     assert call(lib, "dd_cache_attn_fwd", big, ws=fake(15, 8)) == ALIGN
@@ -100,13 +100,20 @@ def test_evict_refusals(lib):
                dict(recent=-1), dict(recent=41), dict(B=40000), dict(budget=-3)):
         assert call(lib, "dd_cache_evict", EVICT, **kw) == SHAPE, kw
     assert call(lib, "dd_cache_evict", EVICT, D=96) == HEADDIM
-    need = lib.dd_cache_evict_workspace_bytes(2, 2, 64, 16, 5, 40)
-    assert need > 0 and lib.dd_cache_evict_workspace_bytes(2, 2, 64, 16, 5, 0) == 0
-    assert call(lib, "dd_cache_evict", EVICT, ws=None) == WORKSPACE
-    assert call(lib, "dd_cache_evict", EVICT, bytes=need - 1) == WORKSPACE
-    assert call(lib, "dd_cache_evict", EVICT, ws=fake(15, 2)) == ALIGN
+    # lists for the moves: in place, or long
+    assert lib.dd_cache_evict_workspace_bytes(2, 2, 64, 16, 5, 0, 1) == 0
+    assert lib.dd_cache_evict_workspace_bytes(2, 2, 64, 16, 5, 40, 0) == 0
+    for kw in (dict(lens_out=EVICT["lens"]), dict(per=200, pages=400, budget=1600)):
+        args = {**EVICT, **kw}
+        need = lib.dd_cache_evict_workspace_bytes(2, 2, 64, 16, args["per"], args["budget"],
+                                                  int("lens_out" in kw))
+        assert need > 0
+        assert call(lib, "dd_cache_evict", args, ws=None) == WORKSPACE
+        assert call(lib, "dd_cache_evict", args, bytes=need - 1) == WORKSPACE
+        assert call(lib, "dd_cache_evict", args, ws=fake(15, 2)) == ALIGN
+        assert call(lib, "dd_cache_evict", args, ws=fake(4)) == ALIAS
     for kw in (dict(W_out=fake(13, 4)), dict(P_out=fake(6, 8)), dict(lens_out=fake(8, 4)),
-               dict(Kp=fake(5)), dict(W_out=fake(9)), dict(ws=fake(4)), dict(W_out=fake(6)),
+               dict(Kp=fake(5)), dict(W_out=fake(9)), dict(W_out=fake(6)),
                dict(P_out=fake(14))):
         assert call(lib, "dd_cache_evict", EVICT, **kw) == ALIAS, kw
 
@@ -154,9 +161,9 @@ def test_logprob_refusals(lib):
     for kw in (dict(logp=fake(0, 4)), dict(lse=fake(3, 8)), dict(top_ids=fake(1)),
                dict(top_logp=fake(6))):
         assert call(lib, "dd_logprobs_fwd", LOGP, **kw) == ALIAS, kw
-    need = lib.dd_logprobs_workspace_bytes(8, 50432, 4)
+    need = lib.dd_logprobs_workspace_bytes(8, 150432, 4)
     assert need > 0 and lib.dd_logprobs_workspace_bytes(8, 0, 0) == 0
-    wide = dict(LOGP, V=50432, ldx=50432)
+    wide = dict(LOGP, V=150432, ldx=150432)
     assert call(lib, "dd_logprobs_fwd", wide, ws=None) == WORKSPACE
     assert call(lib, "dd_logprobs_fwd", wide, bytes=need - 1) == WORKSPACE
     assert call(lib, "dd_logprobs_fwd", wide, ws=fake(7, 4)) == ALIGN
