@@ -377,6 +377,16 @@ __global__ void __launch_bounds__(256, 2) tile_kernel(AttnRows a, CacheView c)
         issue(it.t0, lds);
     wait_vmem();
     __syncthreads();
+    // The last slot the lane's row sees, formed anew for each boundary tile, as
+    // the row's place is for the results: held over the loop they would spill.
+    auto place = [&]() __attribute__((always_inline)) {
+        int tid = static_cast<int>(threadIdx.x);
+        asm volatile("" : "+v"(tid));
+        return it.row + (tid >> 6) * 32 + (tid & 31);
+    };
+    auto last_seen = [&]() __attribute__((always_inline)) {
+        return min(it.s.len + min(place(), it.rows - 1) / a.G, it.s.total - 1);
+    };
     auto step = [&](int t, auto bufc) __attribute__((always_inline)) {
         constexpr int BUF = decltype(bufc)::value;
         const uint16_t *kt = lds + BUF * 2 * TILE;
@@ -388,8 +398,8 @@ __global__ void __launch_bounds__(256, 2) tile_kernel(AttnRows a, CacheView c)
                 attend_tile<D, 2, false>(kt, kt + TILE, qf, koff, voff, 0, g, a.scale_log2, acc, m_i,
                                          l_i);
             else
-                attend_tile<D, 2, true>(kt, kt + TILE, qf, koff, voff, hi - j0, g, a.scale_log2, acc,
-                                        m_i, l_i);
+                attend_tile<D, 2, true>(kt, kt + TILE, qf, koff, voff, last_seen() - j0, g,
+                                        a.scale_log2, acc, m_i, l_i);
         }
         wait_vmem();
         __syncthreads();
@@ -402,7 +412,7 @@ __global__ void __launch_bounds__(256, 2) tile_kernel(AttnRows a, CacheView c)
             step(t + 1, IC<1>{});
     }
     if (on)
-        store_rows<D>(c, a, it, row + l32, g, acc, m_i, l_i);
+        store_rows<D>(c, a, it, place(), g, acc, m_i, l_i);
 }
 
 template <int D, int NW, bool SCORES>
@@ -803,7 +813,7 @@ AttnPlan attn_plan(const CacheShape &c, int H, bool weights)
 {
     AttnPlan p;
     const long long rows = static_cast<long long>(c.T) * (H / c.Hkv);
-    p.few = rows <= 64LL * c.B;
+    p.few = rows <= 32LL * c.B;
     const int bm = p.few ? 32 : 128;
     p.tiles = static_cast<int>(rows / bm) + c.B;
     // workgroups with work in them, if the rows are spread evenly
@@ -821,7 +831,9 @@ AttnPlan attn_plan(const CacheShape &c, int H, bool weights)
     p.part_bytes = p.splits == 1 ? 0 : p.splits * p.rows * (c.D + 1) * sizeof(float);
     p.part_bytes = (p.part_bytes + 15) / 16 * 16;
     const size_t score_bytes = p.rows * slots * sizeof(float);
-    p.scores = weights && p.few && rows <= 8LL * c.B && score_bytes <= kMaxScores;
+    // (written and read: at most half of K's bytes)
+    p.scores = weights && p.few && rows * 8 <= static_cast<long long>(c.D) * c.B &&
+               score_bytes <= kMaxScores;
     p.bytes = p.part_bytes + (p.scores ? score_bytes : 0);
     return p;
 }

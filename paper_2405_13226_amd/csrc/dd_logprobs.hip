@@ -118,12 +118,14 @@ __device__ __forceinline__ float key_logit(uint64_t key)
     return __uint_as_float(k >> 31 ? k & 0x7fffffffu : k ? ~k : 0x7fc00000u);
 }
 
-// The largest c that at least k lanes hold a `x` of; 0 if none.
+// The largest c, of multiples of 2^LOW, that at least k lanes hold a larger or
+// equal x than; 0 if none.
+template <int LOW>
 __device__ __forceinline__ uint32_t wave_floor(uint32_t x, int k)
 {
     uint32_t c = 0;
 #pragma unroll
-    for (int b = 31; b >= 0; --b)
+    for (int b = 31; b >= LOW; --b)
         if (__popcll(__ballot(x >= (c | 1u << b))) >= k)
             c |= 1u << b;
     return c;
@@ -244,7 +246,8 @@ __global__ void __launch_bounds__(NT) logits_kernel(LogitRows a)
     for (int o = 32; o >= 1; o >>= 1)
         s = joined(s, Sums{__shfl_xor(s.m, o), __shfl_xor(s.s, o), __shfl_xor(s.u, o)});
     if constexpr (TOP) {
-        const uint32_t c = wave_floor(reach, a.top);
+        // (bf16 logits differ in their upper halves only)
+        const uint32_t c = wave_floor<sizeof(T) == 2 ? 16 : 0>(reach, a.top);
         if (lane == 0)
             floors[wave] = c;
     }

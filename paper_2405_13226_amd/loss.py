@@ -15,25 +15,28 @@ import torch
 
 from .attention import _ptr as _p
 from .block_ops import _call, _vec
-from .cache import _bytes
+from .cache import _bytes, _is
 
 MAX_TOP = 64
+_TYPES = (torch.bfloat16, torch.float32)
 
 
 def _logits(t, name, dev=None):
     """(rows, V, row stride, whether fp32)."""
+    if isinstance(t, torch.Tensor) and t.dim() == 2:
+        (rows, V), (ld, one) = t.shape, t.stride()
+        if (V and (one == 1 or V == 1) and t.is_cuda and t.dtype in _TYPES
+                and (dev is None or t.device == dev)):
+            return rows, V, ld if rows > 1 else V, t.dtype is torch.float32
     if not isinstance(t, torch.Tensor) or t.dim() != 2:
         raise ValueError(f"{name} must be a 2-D tensor")
-    if t.dtype not in (torch.bfloat16, torch.float32) or not t.is_cuda:
+    if t.dtype not in _TYPES or not t.is_cuda:
         raise ValueError(f"{name} must be a bf16 or fp32 GPU tensor")
     if dev is not None and t.device != dev:
         raise ValueError(f"{name} is on {t.device}, not on {dev}")
-    rows, V = t.shape
-    if V < 1:
+    if not t.shape[1]:
         raise ValueError(f"the rows of {name} are empty")
-    if V > 1 and t.stride(1) != 1:
-        raise ValueError(f"{name} must have unit column stride")
-    return rows, V, t.stride(0) if rows > 1 else V, t.dtype is torch.float32
+    raise ValueError(f"{name} must have unit column stride")
 
 
 def logprobs(logits, targets, top: int = 0):
@@ -74,20 +77,31 @@ def logprobs_backward(logits, targets, lse, entropy, g_logp=None, g_entropy=None
     (fp32 [rows], each optional), of their type; ``out`` (optional) receives it
     and may be the logits themselves."""
     rows, V, ldx, f32 = _logits(logits, "logits")
-    dev = logits.device
-    _vec(targets, "targets", rows, torch.int64, dev)
-    for t, name in ((lse, "lse"), (entropy, "entropy"), (g_logp, "g_logp"),
-                    (g_entropy, "g_entropy"), (g_lse, "g_lse")):
-        if t is not None or name in ("lse", "entropy"):
-            _vec(t, name, rows, torch.float32, dev)
+    dev, i = logits.device, logits.get_device()
+    try:
+        fine = (_is(targets, (rows,), torch.int64, i) and _is(lse, (rows,), torch.float32, i)
+                and _is(entropy, (rows,), torch.float32, i)
+                and all(g is None or _is(g, (rows,), torch.float32, i)
+                        for g in (g_logp, g_entropy, g_lse)))
+    except AttributeError:
+        fine = False
+    if not fine:
+        _vec(targets, "targets", rows, torch.int64, dev)
+        for t, name in ((lse, "lse"), (entropy, "entropy"), (g_logp, "g_logp"),
+                        (g_entropy, "g_entropy"), (g_lse, "g_lse")):
+            if t is not None or name in ("lse", "entropy"):
+                _vec(t, name, rows, torch.float32, dev)
+    ldd = V
     if out is None:
         out = torch.empty((rows, V), dtype=logits.dtype, device=dev)
-    r, c, ldd, same = _logits(out, "out", dev)
-    if (r, c, same) != (rows, V, f32):
-        raise ValueError(f"out must be a {logits.dtype} tensor of shape {(rows, V)}")
+    else:
+        r, c, ldd, same = _logits(out, "out", dev)
+        if (r, c, same) != (rows, V, f32):
+            raise ValueError(f"out must be a {logits.dtype} tensor of shape {(rows, V)}")
     if rows:
-        _call(dev, "dd_logprobs_bwd", _p(logits), ldx, f32, _p(targets), _p(lse), _p(entropy),
-              _p(g_logp), _p(g_entropy), _p(g_lse), _p(out), ldd, rows, V)
+        _call(dev, "dd_logprobs_bwd", logits.data_ptr(), ldx, f32, targets.data_ptr(),
+              lse.data_ptr(), entropy.data_ptr(), _p(g_logp), _p(g_entropy), _p(g_lse),
+              out.data_ptr(), ldd, rows, V)
     return out
 
 
