@@ -70,9 +70,12 @@ __device__ __forceinline__ void wait_vm()
 
 // One tile of NB x 32 keys for the wave's 32 rows.  MASKED: the lane's row sees
 // the tile's keys 0 .. hi_r only (boundary tiles).  `scores` (optional)
-// receives the lane's row of q K_j, `room` of them (a multiple of 4).
-template <int D, int NB, bool MASKED, bool SCORES = false>
-__device__ __forceinline__ void
+// receives the lane's row of q K_j, `room` of them (a multiple of 4).  Where a
+// boundary tile holds values that are not finite: EXACT adds its keys one by
+// one, each only to the rows that see it; otherwise the result is true, and the
+// sums are not to be used.
+template <int D, int NB, bool MASKED, bool EXACT, bool SCORES = false>
+__device__ __forceinline__ bool
 attend_tile(const uint16_t *kt, const uint16_t *vt, const bf16x8 (&qf)[D / 16],
             const int (&koff)[D / 16], const int (&voff)[D / 32][2], int hi_r, int g,
             float scale_log2, f32x16 (&acc)[D / 32], float &m_i, float &l_i,
@@ -141,7 +144,7 @@ attend_tile(const uint16_t *kt, const uint16_t *vt, const bf16x8 (&qf)[D / 16],
         const uint16_t *vr = vt + (kb * 32 + 16 * t2) * D;
         return join(lds_tr4(vr + voff[db][0]), lds_tr4(vr + voff[db][1]));
     };
-    if constexpr (MASKED) {
+    if constexpr (MASKED && EXACT) {
         u16x8 top = {};
 #pragma unroll
         for (int kb = 0; kb < NB; ++kb)
@@ -176,16 +179,23 @@ attend_tile(const uint16_t *kt, const uint16_t *vt, const bf16x8 (&qf)[D / 16],
                                 acc[db][r] += sees ? one[r] : 0.f;
                         }
                     }
-            return;
+            return false;
         }
     }
+    u16x8 top = {};
 #pragma unroll
     for (int kb = 0; kb < NB; ++kb)
 #pragma unroll
         for (int t2 = 0; t2 < 2; ++t2)
 #pragma unroll
-            for (int db = 0; db < DB; ++db)
-                acc[db] = mfma32(value(kb, t2, db), pb[kb][t2], acc[db]);
+            for (int db = 0; db < DB; ++db) {
+                const bf16x8 a = value(kb, t2, db);
+                if constexpr (MASKED && !EXACT)
+                    top = __builtin_elementwise_max(
+                        top, __builtin_bit_cast(u16x8, __builtin_bit_cast(u32x4, a) & 0x7fff7fffu));
+                acc[db] = mfma32(a, pb[kb][t2], acc[db]);
+            }
+    return MASKED && !EXACT && __any(__builtin_reduce_max(top) >= 0x7f80);
 }
 
 // A work item: BM rows of one sequence and key head, and the part of the key
@@ -345,10 +355,15 @@ __device__ __forceinline__ void store_rows(const CacheView &c, const AttnRows &a
         a.part_lse[at] = m_i + log2f(l);
 }
 
+// At D = 64 values that are not finite in a boundary tile make the item start
+// over in a loop of its own: within the main one they cost it a wave per SIMD
+// (4 x 2,048 tokens over 8,192 slots of 16 heads 341-349 us instead of 370; at
+// D = 128 it is the other way round, 1,185 instead of 1,110 over 16,384).
 template <int D>
-__global__ void __launch_bounds__(256, 2) tile_kernel(AttnRows a, CacheView c)
+__global__ void __launch_bounds__(256, D == 64 ? 3 : 2) tile_kernel(AttnRows a, CacheView c)
 {
     constexpr int BM = 128, BN = 64, TILE = BN * D, KK = D / 16, DB = D / 32;
+    constexpr bool EXACT = D == 128;
     __shared__ __attribute__((aligned(1024))) uint16_t lds[4 * TILE];
     AttnItem it;
     if (!attn_item<BM, BN>(c, a, it))
@@ -387,6 +402,7 @@ __global__ void __launch_bounds__(256, 2) tile_kernel(AttnRows a, CacheView c)
     auto last_seen = [&]() __attribute__((always_inline)) {
         return min(it.s.len + min(place(), it.rows - 1) / a.G, it.s.total - 1);
     };
+    bool again = false;
     auto step = [&](int t, auto bufc) __attribute__((always_inline)) {
         constexpr int BUF = decltype(bufc)::value;
         const uint16_t *kt = lds + BUF * 2 * TILE;
@@ -395,11 +411,12 @@ __global__ void __launch_bounds__(256, 2) tile_kernel(AttnRows a, CacheView c)
         const int j0 = t * BN;
         if (on && j0 <= hi_last) {
             if (j0 + BN - 1 <= hi_first)
-                attend_tile<D, 2, false>(kt, kt + TILE, qf, koff, voff, 0, g, a.scale_log2, acc, m_i,
-                                         l_i);
+                attend_tile<D, 2, false, false>(kt, kt + TILE, qf, koff, voff, 0, g, a.scale_log2,
+                                                acc, m_i, l_i);
             else
-                attend_tile<D, 2, true>(kt, kt + TILE, qf, koff, voff, last_seen() - j0, g,
-                                        a.scale_log2, acc, m_i, l_i);
+                again |= attend_tile<D, 2, true, EXACT>(kt, kt + TILE, qf, koff, voff,
+                                                        last_seen() - j0, g, a.scale_log2, acc, m_i,
+                                                        l_i);
         }
         wait_vmem();
         __syncthreads();
@@ -410,6 +427,36 @@ __global__ void __launch_bounds__(256, 2) tile_kernel(AttnRows a, CacheView c)
         step(t, IC<0>{});
         if (t + 1 < it.t1)
             step(t + 1, IC<1>{});
+    }
+    if constexpr (!EXACT) {
+        if (__syncthreads_or(again)) {  // from the start
+#pragma unroll
+            for (int db = 0; db < DB; ++db)
+                acc[db] = f32x16{};
+            m_i = -INFINITY;
+            l_i = 0.f;
+#pragma unroll 1
+            for (int t = it.t0; t < it.t1; ++t) {
+                issue(t, lds);
+                wait_vmem();
+                __syncthreads();
+#pragma unroll 1
+                for (int p = 0; p < 2; ++p) {
+                    const uint16_t *kt = lds + p * 32 * D;
+                    const int j0 = t * BN + p * 32;
+                    if (!on || j0 > hi_last)
+                        continue;
+                    if (j0 + 31 <= hi_first)
+                        attend_tile<D, 1, false, true>(kt, kt + TILE, qf, koff, voff, 0, g,
+                                                       a.scale_log2, acc, m_i, l_i);
+                    else
+                        attend_tile<D, 1, true, true>(kt, kt + TILE, qf, koff, voff,
+                                                      last_seen() - j0, g, a.scale_log2, acc, m_i,
+                                                      l_i);
+                }
+                __syncthreads();
+            }
+        }
     }
     if (on)
         store_rows<D>(c, a, it, place(), g, acc, m_i, l_i);
@@ -463,10 +510,10 @@ __global__ void __launch_bounds__(64 * NW) few_kernel(AttnRows a, CacheView c)
         const int j0 = t * BN;
         const int room = mine_ok ? c.slots() - j0 : 0;
         if (j0 + BN - 1 <= hi_first)
-            attend_tile<D, 1, false, SCORES>(kt, kt + TILE, qf, koff, voff, 0, g, a.scale_log2,
+            attend_tile<D, 1, false, true, SCORES>(kt, kt + TILE, qf, koff, voff, 0, g, a.scale_log2,
                                              acc, m_i, l_i, scores + j0, room);
         else
-            attend_tile<D, 1, true, SCORES>(kt, kt + TILE, qf, koff, voff, hi - j0, g,
+            attend_tile<D, 1, true, true, SCORES>(kt, kt + TILE, qf, koff, voff, hi - j0, g,
                                             a.scale_log2, acc, m_i, l_i, scores + j0, room);
         if (t + 2 * NW < it.t1) {
             // the stage's last reads have returned before it is filled again
