@@ -395,8 +395,10 @@ size_t dd_gemm_i8_wgrad_workspace_bytes(int T, int M, int N, int n); /* 0: inval
  *                  n-th slot behind it that does: slots are in no order after it,
  *                  which attention does not depend on.  lens_out = min(lens,
  *                  budget); a sequence with no more slots keeps all of them.
- *                  W_out and P_out (positions) hold lens_out slots, the rest is
- *                  left as it was; W_out may be W_in, P_out P_in, lens_out lens.
+ *                  W_out and P_out (positions) hold the first min(budget, per *
+ *                  page) slots (behind lens_out what the inputs hold there), the
+ *                  rest is left as it was; W_out may be W_in, P_out P_in,
+ *                  lens_out lens.
  *                  workspace: dd_cache_evict_workspace_bytes(...) bytes, 4-byte
  *                  aligned.
  */

@@ -253,8 +253,9 @@ def cache_attention(q, k_pages, v_pages, table, lens, cu_new, weights=None, weig
         _state(out, "out", (T, H, D), _BF16, dev)
         _state(lse, "lse", (T, H), _F32, dev)
     if not (T and B):
-        if weights_out is not weights:
-            weights_out.copy_(weights)
+        if weights_out is not weights and B and per:  # the slots in use
+            used = torch.arange(per * page, device=dev) < lens[:, None, None]
+            weights_out.copy_(torch.where(used, weights, weights_out))
         return out, lse
     need = _bytes("dd_cache_attn_workspace_bytes", T, B, H, Hkv, D, page, per, weights is not None)
     ws = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
@@ -272,8 +273,9 @@ def cache_evict(k_pages, v_pages, table, lens, weights, positions, seen, budget:
     equal weights go by the lowest slot.  Keys and values move within the pages:
     the n-th slot below the budget that goes receives the n-th one behind it
     that stays.  Returns (weights, positions, lens) of the slots that are left
-    (new tensors, defined up to the new lens, or ``out``: three tensors, each of
-    which may be the input itself)."""
+    (new tensors, or ``out``: three tensors, each of which may be the input
+    itself); weights and positions hold the first ``budget`` slots, behind the
+    new lens what the inputs hold there, and are not written behind the budget."""
     try:
         pages, Hkv, page, D = shape = k_pages.shape
         B, per = table.shape

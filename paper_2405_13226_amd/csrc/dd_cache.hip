@@ -218,7 +218,7 @@ __global__ void __launch_bounds__(NT) select_kernel(EvictRows a, CacheView c)
         if (!MOVE && tid == 0)
             a.count[bh] = 0;
         if (Wout != W || Pout != P)
-            for (int j = tid; j < n; j += NT) {
+            for (int j = tid; j < min(a.budget, c.slots()); j += NT) {
                 Wout[j] = W[j];
                 Pout[j] = P[j];
             }

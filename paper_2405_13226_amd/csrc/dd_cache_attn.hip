@@ -867,13 +867,17 @@ AttnPlan attn_plan(const CacheShape &c, int H, bool weights)
     const long long each = (rows + c.B - 1) / c.B;
     const long long work = std::min<long long>(c.B, c.T) * ((each + bm - 1) / bm) * c.Hkv;
     const long long slots = static_cast<long long>(c.per) << c.shift;
-    // few rows: parts of 512 KB of K and V or more, smaller where that leaves
-    // CUs idle, down to 128 slots; many: enough workgroups, of 512 slots or more
+    // Few rows: parts of 512 KB of K and V or more while there are less than
+    // 8,192 (32 x 8,192 slots of 16 heads in 2, 4, 8 and 16 parts: 314, 293, 281
+    // and 293 us), smaller where that leaves CUs idle, down to 128 slots (8
+    // sequences, 8 key heads in 4, 8 and 16 parts: 64, 52 and 53).  Many: enough
+    // workgroups, of 512 slots or more.
     const long long fill = (512 + work - 1) / work;
     p.wide = p.few && slots * c.D * 4 <= kOnePart && work < 512;
-    const long long want = p.wide ? 1 : p.few ? std::max(slots * c.D / 131072, std::min(fill, slots / 128))
-                                 : std::min(512 / work, slots / 512);
-    p.splits = static_cast<int>(std::clamp<long long>(want, 1, kMaxSplits));
+    long long want = std::min(512 / work, slots / 512);
+    if (p.few)
+        want = std::max(std::min(slots * c.D / 131072, 8192 / work), std::min(fill, slots / 128));
+    p.splits = p.wide ? 1 : static_cast<int>(std::clamp<long long>(want, 1, kMaxSplits));
     p.rows = static_cast<size_t>(c.T) * H;
     p.part_bytes = p.splits == 1 ? 0 : p.splits * p.rows * (c.D + 1) * sizeof(float);
     p.part_bytes = (p.part_bytes + 15) / 16 * 16;

@@ -12,6 +12,7 @@ ignored.  Statistics are fp32.
 from __future__ import annotations
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from .attention import _ptr as _p
 from .block_ops import _call, _vec
@@ -118,6 +119,7 @@ class LogProbFunction(torch.autograd.Function):
         return res
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, g_logp, g_entropy, g_lse, *_):
         logits, targets, lse, entropy = ctx.saved_tensors
         if g_logp is None and g_entropy is None and g_lse is None:

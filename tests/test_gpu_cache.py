@@ -1,6 +1,8 @@
 """GPU parity of the paged cache (append, attention with slot weights,
 eviction) against its float64 definitions.  Tolerances: tests/cache_oracle.py;
 rows that are only moved, positions and lengths are exact."""
+import random
+
 import pytest
 import torch
 
@@ -37,6 +39,11 @@ CASES = [
     ([50] * 15 + [300], [1] * 15 + [100], 1, 1, 64, 16, 0),
     ([2000] + [5] * 11, [75] + [1] * 11, 2, 2, 128, 32, 0),
     ([300, 20], [9, 9], 2, 2, 64, 16, 3),
+    # one part per head, several; scores kept and not
+    ([3000, 200, 0], [1, 2, 1], 4, 2, 128, 32, 0),
+    ([5000, 17], [1, 1], 4, 4, 64, 16, 1),
+    ([6000], [20], 1, 1, 64, 64, 0),
+    ([2500], [31], 1, 1, 128, 16, 2),
 ]
 
 
@@ -87,6 +94,20 @@ def test_attention(cuda, case):
     lens, news, H, Hkv, D, page, tail = case
     log(f"cache attention {case}")
     check(O.Batch(lens, news, H, Hkv, D, page, seed=sum(lens) + sum(news), tail=tail), cuda)
+
+
+@pytest.mark.parametrize("seed", range(12))
+def test_attention_of_random_batches(cuda, seed):
+    g = random.Random(seed)
+    H, Hkv = g.choice([(1, 1), (2, 1), (3, 3), (6, 2), (8, 8), (10, 2), (8, 1)])
+    B = g.choice([1, 2, 3, 9])
+    top = g.choice([1, 1, 4, 40, 150])
+    lens = [g.choice([0, 1, g.randint(0, 700)]) for _ in range(B)]
+    news = [g.randint(0 if B > 1 else 1, top) for _ in range(B)]
+    news[0] = max(news[0], 1)
+    case = (lens, news, H, Hkv, g.choice([64, 128]), g.choice([16, 32, 64, 128]), g.choice([0, 5]))
+    log(f"cache attention {case}")
+    check(O.Batch(*case[:6], seed=seed, tail=case[6]), cuda)
 
 
 @pytest.mark.parametrize("D", [64, 128])
@@ -271,7 +292,10 @@ def evict_case(cuda, lens, w, pos, seen, budget, recent, D=64, page=16, in_place
         assert torch.equal(res[0][b, :, :n].cpu().view(torch.int32),
                            want[2][b, :, :n].view(torch.int32))
         assert torch.equal(res[1][b, :, :n].cpu(), want[3][b, :, :n])
-        rest = (w, pos) if in_place else (torch.full_like(w, 9.0), torch.full_like(pos, 9))
+        # behind the new lens: the inputs' up to the budget, then what was there
+        rest = (w.clone(), pos.clone())
+        if not in_place:
+            rest[0][..., budget:], rest[1][..., budget:] = 9.0, 9
         assert torch.equal(res[0][b, :, n:].cpu().view(torch.int32),
                            rest[0][b, :, n:].view(torch.int32))
         assert torch.equal(res[1][b, :, n:].cpu(), rest[1][b, :, n:])
