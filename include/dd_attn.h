@@ -367,7 +367,8 @@ size_t dd_gemm_i8_wgrad_workspace_bytes(int T, int M, int N, int n); /* 0: inval
  *
  * table, lens, cu_new (and start, seen) are device memory and not validated;
  * callers check host copies with dd_cache_check: offsets in order, slots within
- * the table, every page in use named once.  Malformed contents cannot make a
+ * the table, every page in use named once (dd_cache_attn_fwd, which only reads
+ * pages, also takes pages that sequences share).  Malformed contents cannot make a
  * kernel access memory out of bounds, but results are then unspecified; a token
  * without a slot, or whose page the cache does not have, is not written.
  *

@@ -19,7 +19,9 @@ dd_cache_* functions of include/dd_attn.h.
 Query rows are bf16 [T, H, D], H a multiple of the kv heads, a token's heads
 contiguous (columns of a wider matrix are fine).  Rows behind cu_new[B] are left
 as they were.  The calls read these tensors on the device and check their types
-and shapes only: ``check_cache`` checks the contents of host copies.  Calls run
+and shapes only: ``check_cache`` checks the contents of host copies (it wants
+every page in one sequence; attention, which only reads them, may be given
+pages that sequences share).  Forward only.  Calls run
 on the tensors' device, on its current stream, allocate only their results and
 scratch, and can be captured in a graph.
 
@@ -29,6 +31,7 @@ from __future__ import annotations
 
 import ctypes
 import functools
+import itertools
 
 import numpy as np
 import torch
@@ -350,11 +353,11 @@ class PagedCache:
 
     def _set_tables(self):
         rows = [own + [-1] * (self.per - len(own)) for own in self.owned]
-        self.table.copy_(self._device_ints(rows))
+        self.table.copy_(self._device_ints(rows).view(self.table.shape))
 
     def _reserve(self, news):
         slots = [n + m for n, m in zip(self.lengths, news)]
-        if max(slots) > self.per * self.page:
+        if max(slots, default=0) > self.per * self.page:
             raise RuntimeError(f"a sequence would need {max(slots)} slots of "
                                f"{self.per * self.page}")
         more = [-(-n // self.page) - len(own) for n, own in zip(slots, self.owned)]
@@ -375,7 +378,7 @@ class PagedCache:
         if sum(news) > q.shape[0]:
             raise ValueError(f"{sum(news)} new tokens, but q has {q.shape[0]} rows")
         self._reserve(news)
-        cu = self._device_ints(np.concatenate([[0], np.cumsum(news)]))
+        cu = self._device_ints([0, *itertools.accumulate(news)])
         q = cache_append(q, k, v, self.k_pages, self.v_pages, self.table, self.lens, cu,
                          rope_base=rope_base, start=self.seen, positions=self.positions)
         o, lse = cache_attention(q, self.k_pages, self.v_pages, self.table, self.lens, cu,

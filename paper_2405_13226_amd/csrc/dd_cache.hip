@@ -4,7 +4,9 @@
 // chunk's queries) rotated at their positions (dd_rope.hpp: bit-identical to a
 // dd_rope pass at these positions).  One workgroup per token: thread t holds
 // the 8-element chunk t % (D/8) of its heads, so an angle is formed once per
-// token and thread.  Bytes only: each row is read and written once.
+// token and thread.  Bytes only: each row is read and written once (24,927 tokens
+// of 16 heads of 128 with their queries: 613 MB in 115 us, 5.3 TB/s; a copy of
+// 2 GiB reaches 4.9).
 //
 // Eviction: per sequence and key head, the `budget` slots of most weight stay
 // (slots of the last `recent` positions before all others; equal ones by the
@@ -22,6 +24,9 @@
 //           each histogram and for the lists.)
 //   move:   the listed rows (by the workgroup that found them, where they are
 //           few: one launch, no memory for the lists)
+// 16 sequences of 8,192 slots, 16 heads of 128, thinned out to 4,096: 17 us for
+// the lists, bound by the latency of three histograms and two prefix sums, and 87
+// for the rows, 4.6 TB/s (a copy 4.9; pieces of 256 bytes at random).
 #include "dd_cache.hpp"
 #include "dd_internal.h"
 #include "dd_launch.hpp"
@@ -166,7 +171,10 @@ __device__ __forceinline__ uint32_t block_prefix(uint32_t x, uint32_t *waves, ui
     return before + s - x;
 }
 
-constexpr int kFewMoves = 512;  // entries of a list that stays in LDS
+// Entries of a list that stays in LDS, for the workgroup that made it to move the
+// rows.  (12 heads of 1,100 slots, up to 100 of them moved: 9.4 us, 8.6 + 4.0 in
+// two launches; with longer lists one workgroup per head moves too slowly.)
+constexpr int kFewMoves = 512;
 
 // Moves rows r0, r0 + step, ... of n: row to[r] receives row from[r].
 template <int D>
@@ -377,6 +385,22 @@ int evict_list(const CacheShape &c, int budget)
     return std::max(std::min(budget, (c.per << c.shift) - budget), 0);
 }
 
+// As many threads as hold the sequence's slots, where that is possible.
+template <int MOVE>
+hipError_t launch_select(const EvictRows &r, const CacheView &c, hipStream_t st)
+{
+    const int slots = c.slots();
+    auto kern = select_kernel<1024, 16, false, MOVE>;
+    if (slots <= 2048)
+        kern = select_kernel<256, 8, true, MOVE>;
+    else if (slots <= 8192)
+        kern = select_kernel<1024, 8, true, MOVE>;
+    else if (slots <= 16384)
+        kern = select_kernel<1024, 16, true, MOVE>;
+    return launch_kernel(kern, dim3(static_cast<unsigned>(c.B * c.Hkv)),
+                         dim3(slots <= 2048 ? 256u : 1024u), st, r, c);
+}
+
 }  // namespace
 
 int launch_cache_append(const CacheAppendArgs &a)
@@ -402,21 +426,12 @@ int launch_cache_evict(const CacheEvictArgs &a)
                       ws + bh + static_cast<size_t>(bh) * list, static_cast<uint16_t *>(a.Kp),
                       static_cast<uint16_t *>(a.Vp), a.budget, a.recent, list};
     hipStream_t st = static_cast<hipStream_t>(a.stream);
-    const int slots = c.slots();
-    const dim3 grid(static_cast<unsigned>(bh));
     if (list <= kFewMoves && a.lens_out != a.c.lens) {
         const bool narrow = a.c.D == 64;
-        const hipError_t e =
-            slots <= 2048 ? launch_kernel(narrow ? select_kernel<256, 8, true, 64> : select_kernel<256, 8, true, 128>, grid, dim3(256), st, r, c)
-            : slots <= 8192 ? launch_kernel(narrow ? select_kernel<1024, 8, true, 64> : select_kernel<1024, 8, true, 128>, grid, dim3(1024), st, r, c)
-            : slots <= 16384 ? launch_kernel(narrow ? select_kernel<1024, 16, true, 64> : select_kernel<1024, 16, true, 128>, grid, dim3(1024), st, r, c)
-                             : launch_kernel(narrow ? select_kernel<1024, 16, false, 64> : select_kernel<1024, 16, false, 128>, grid, dim3(1024), st, r, c);
+        const hipError_t e = narrow ? launch_select<64>(r, c, st) : launch_select<128>(r, c, st);
         return e == hipSuccess ? DD_OK : DD_ERR_HIP;
     }
-    hipError_t e = slots <= 2048    ? launch_kernel(select_kernel<256, 8, true>, grid, dim3(256), st, r, c)
-                   : slots <= 8192  ? launch_kernel(select_kernel<1024, 8, true>, grid, dim3(1024), st, r, c)
-                   : slots <= 16384 ? launch_kernel(select_kernel<1024, 16, true>, grid, dim3(1024), st, r, c)
-                                    : launch_kernel(select_kernel<1024, 16, false>, grid, dim3(1024), st, r, c);
+    hipError_t e = launch_select<0>(r, c, st);
     if (e != hipSuccess)
         return DD_ERR_HIP;
     const int rows = 256 / (a.c.D / 8);

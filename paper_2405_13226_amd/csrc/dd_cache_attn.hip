@@ -21,9 +21,16 @@
 // Either splits the keys over workgroups where there are too few rows to fill
 // the chip; finish_kernel adds the parts.  The weights need the rows' final
 // sums: where a sequence has few rows their scores are kept (4 bytes a slot and
-// row, against 2 D bytes of K), else S is formed once more (weights_kernel).  Tiles arrive by direct global->LDS
-// loads; one load instruction covers rows of one page (pages hold at least 16
-// slots), whose number is a scalar load.
+// row, against 2 D bytes of K), else S is formed once more (weights_kernel).
+// Tiles arrive by direct global->LDS loads; one load instruction covers rows of
+// one page (pages hold at least 16 slots), whose number is a scalar load.
+//
+// Few rows are bound by the cache's bytes: 32 sequences of 8,192 slots, 16 heads
+// of 128, a token each: 1,564 MB in 275 us and 5 us for the parts, 5.6 TB/s (a
+// copy of 2 GiB: 4.9).  Many by the matrix cores: 4 x 2,048 tokens over 14,336
+// slots and each other, 16 heads of 128: 1.03 TFLOP in 1,090 us, 0.95 PFLOP/s
+// (the library's largest products 1.37); matrix cores busy 50% of the time, the
+// exponentials take most of the rest; no LDS conflicts.
 //
 // Slots behind a sequence's last are never read (a tile's rows are clamped to
 // it).  A slot that a row may not see leaves no trace in it, whatever it
@@ -840,11 +847,19 @@ CacheView view(const CacheShape &c)
     return CacheView{c.table, c.lens, c.cu_new, c.T, c.B, c.Hkv, c.pages, c.shift, c.per};
 }
 
+// Up to 32 rows per sequence on the average go to few_kernel, more to
+// tile_kernel: 4 sequences of 4,096 slots, 16 heads of 128, with 16, 32, 48, 64
+// and 96 rows each take 31, 31, 39, 38 and 67 us in few_kernel, which reads K and V
+// once for 32 rows, and 30, 31, 34, 34 and 39 in tile_kernel; one sequence 19.1,
+// 19.8, 19.1, 20.5 and 31.2 against 21.3, 21.5, 22.4, 22.8 and 24.9.
+constexpr int kFewRows = 32;
+
 // Waves of a workgroup with few rows: 64 KB of LDS, two workgroups per CU.  (At
 // D = 128 four waves, one workgroup per CU, read 8 x 8,192 slots of 8 key heads
 // in 46-56 us instead of 41-43: nothing runs while a workgroup begins or ends.)
 // Twice as many where a sequence's slots are few enough to be one part, which
-// saves the launch that joins parts and the memory for them.
+// saves the launch that joins parts and the memory for them (1,024 slots, 12
+// heads of 64: 8.5 us instead of 5.5 + 3.8 in two launches).
 template <int D>
 constexpr int few_waves = D == 64 ? 4 : 2;
 constexpr long long kOnePart = 256 << 10;  // bytes of K and V
@@ -860,7 +875,7 @@ AttnPlan attn_plan(const CacheShape &c, int H, bool weights)
 {
     AttnPlan p;
     const long long rows = static_cast<long long>(c.T) * (H / c.Hkv);
-    p.few = rows <= 32LL * c.B;
+    p.few = rows <= static_cast<long long>(kFewRows) * c.B;
     const int bm = p.few ? 32 : 128;
     p.tiles = static_cast<int>(rows / bm) + c.B;
     // workgroups with work in them, if the rows are spread evenly
@@ -882,7 +897,9 @@ AttnPlan attn_plan(const CacheShape &c, int H, bool weights)
     p.part_bytes = p.splits == 1 ? 0 : p.splits * p.rows * (c.D + 1) * sizeof(float);
     p.part_bytes = (p.part_bytes + 15) / 16 * 16;
     const size_t score_bytes = p.rows * slots * sizeof(float);
-    // (written and read: at most half of K's bytes)
+    // Scores are kept where they are at most half of K's bytes, written and read
+    // (8 sequences of 8,192 slots, 8 key heads with 4 heads each, a token: 65 us in
+    // all, 91 with S formed once more).
     p.scores = weights && p.few && rows * 8 <= static_cast<long long>(c.D) * c.B &&
                score_bytes <= kMaxScores;
     p.bytes = p.part_bytes + (p.scores ? score_bytes : 0);

@@ -23,6 +23,12 @@
 // there are few rows.
 //
 // Backward: elementwise, each logit read and each gradient written once.
+//
+// Both are bound by the logits' bytes: 1,501 x 50,277 in fp32 with 5 alternatives
+// 302 MB in 59 us, 5.1 TB/s; 16,384 x 50,432 in bf16 296 us forward, 5.6 TB/s, and
+// 556 back, 5.9 (what the cache still holds of the forward's among it; a copy of
+// 2 GiB 4.9).  16 rows with 8 alternatives, 11.7 us, by latency: the sums 5, the
+// alternatives 7.
 #include "dd_device.hpp"
 #include "dd_internal.h"
 #include "dd_launch.hpp"
@@ -414,7 +420,9 @@ __device__ __forceinline__ void store_grads(float *y, int at, int end, f32x8 f)
 }
 
 // Gradients past this size leave the last-level cache (256 MB) before anyone
-// reads them: they are stored past it.
+// reads them: they are stored past it (16,384 x 50,432, in turn with the forward:
+// 599 us through the cache and 345 for the next forward, past it 579 and 320; rows
+// taken from the last one on 566 and 316).
 constexpr long long kStreamBytes = 256LL << 20;
 constexpr int kGradPieces = 4;  // of 8 logits per thread
 
@@ -453,15 +461,29 @@ __global__ void __launch_bounds__(256) logits_grad_kernel(GradRows a)
     }
 }
 
-// Few rows: a row is one workgroup of 1024 threads, or several of them where it
-// is long.  Otherwise it is a workgroup of 256, or a wave.
+// Few long rows: a row is one workgroup of 1024 threads, or several of them where
+// it is very long.  Otherwise it is a wave, up to a length that grows with the
+// number of rows (a wave takes long over its row, and many rows hide that), or a
+// workgroup of 256.  In us with a wave, 256 and 1024 threads, without
+// alternatives / with 8:
+//      16 x 50,432   31 / 38     11 / 15     7.3 / 11.2
+//     512 x 50,432   47 / 55     17 / 20      14 / 18
+//     768 x 50,432   49 / 56     19 / 23      18 / 25
+//      16 x  1,000  3.3 / 5.6   3.5 / 6.0    3.7 / 6.2
+//      16 x  8,000  7.3 / 10.0  4.2 / 7.1    4.8 / 8.3
+//   2,048 x  4,000  7.6 / 10.3  7.6 / 11.0    16 / 28
+//   2,048 x  8,000   12 / 15     10 / 14      21 / 35
+//  16,384 x  1,000   13 / 20     29 / 49
+//  16,384 x 16,000  102 / 111   101 / 124
+//  16,384 x 24,000  144 / 154   138 / 163
+// (16 x 50,432 in 12 parts of 256 threads and a join: 7.4 + 3.6, and a launch.)
 constexpr int kFewRows = 512;
 
-int row_threads(int rows, int V, int top)
+int row_threads(int rows, int V)
 {
     if (rows <= kFewRows && V > 8192)
         return 1024;
-    return V <= (top ? 2048 : 16384) ? 64 : 256;
+    return V <= std::clamp(2 * rows, 1024, 16384) ? 64 : 256;
 }
 
 int split_rows(int rows, int V, int top)
@@ -482,7 +504,7 @@ int launch_logprobs_t(const LogprobArgs &a)
                       reinterpret_cast<Sums *>(keys + parts * a.top), keys, a.ldx, a.rows, a.V,
                       a.top, splits};
     hipStream_t st = static_cast<hipStream_t>(a.stream);
-    const int nt = row_threads(a.rows, a.V, a.top);
+    const int nt = row_threads(a.rows, a.V);
     auto kern = nt == 1024 ? (a.top ? logits_kernel<T, 1024, true> : logits_kernel<T, 1024, false>)
                 : nt == 256 ? (a.top ? logits_kernel<T, 256, true> : logits_kernel<T, 256, false>)
                             : (a.top ? logits_kernel<T, 64, true> : logits_kernel<T, 64, false>);

@@ -134,5 +134,9 @@ def token_logprobs(logits, targets, top: int = 0):
 
         logp, _, lse = token_logprobs(logits, targets)
         loss = -logp.mean() + 1e-4 * lse.square().mean()
+
+    Where a captured graph shall hold the backward pass while eager autograd
+    graphs of the same leaves live, capture ``logprobs`` and
+    ``logprobs_backward``: autograd would join the two graphs' streams.
     """
     return LogProbFunction.apply(logits, targets, top)

@@ -29,7 +29,8 @@ pytestmark = pytest.mark.gpu
 # nothing divides; rows split over workgroups and not
 SHAPES = [(1, 1, 1), (3, 2, 2), (5, 7, 3), (4, 64, 64), (33, 65, 0), (2, 511, 5), (7, 513, 20),
           (1, 2049, 8), (600, 1000, 4), (1, 4096, 1), (3, 12345, 64), (16, 50432, 8), (2, 50277, 20),
-          (1, 131072, 33), (700, 9001, 3)]
+          (1, 131072, 33), (700, 9001, 3),
+          (1100, 2200, 6), (1100, 2201, 6)]
 
 
 def tolerances(x, ref):
@@ -104,7 +105,8 @@ def test_ties_order_and_extremes(cuda, dtype):
 
 
 # a wave, a workgroup of 256 and of 1024, several of them per row
-@pytest.mark.parametrize("rows,V", [(5, 2000), (5, 8000), (5, 30000), (5, 150000), (600, 20000)])
+@pytest.mark.parametrize("rows,V", [(5, 2000), (5, 8000), (5, 30000), (5, 150000), (600, 20000),
+                                    (2100, 4200)])
 def test_equal_logits_and_neighbours(cuda, rows, V):
     """Lists of alternatives that do not fit (all logits equal, or two values),
     alternatives that lie next to each other, and ones of one thread's pieces."""
