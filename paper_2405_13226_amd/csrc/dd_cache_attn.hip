@@ -886,10 +886,16 @@ AttnPlan attn_plan(const CacheShape &c, int H, bool weights)
     // 8,192 (32 x 8,192 slots of 16 heads in 2, 4, 8 and 16 parts: 314, 293, 281
     // and 293 us), smaller where that leaves CUs idle, down to 128 slots (8
     // sequences, 8 key heads in 4, 8 and 16 parts: 64, 52 and 53).  Many: enough
-    // workgroups, of 512 slots or more.
+    // workgroups, of 512 slots or more; at D = 64, where 768 run at once and a
+    // part's sums are half as many bytes, two rounds of them where they keep 2,048
+    // slots, for ragged sequences (in us with 1 and 2-3 parts, up to so many new
+    // tokens: 3 x 1,399 over 7,053 slots of one key head with 16 124 and 88, 16 x
+    // 256 over 8,000 of 16 207 and 156; at D = 128 gains and losses of 10%).
     const long long fill = (512 + work - 1) / work;
     p.wide = p.few && slots * c.D * 4 <= kOnePart && work < 512;
     long long want = std::min(512 / work, slots / 512);
+    if (c.D == 64)
+        want = std::max(want, std::min((1536 + work / 2) / work, slots / 2048));
     if (p.few)
         want = std::max(std::min(slots * c.D / 131072, 8192 / work), std::min(fill, slots / 128));
     p.splits = p.wide ? 1 : static_cast<int>(std::clamp<long long>(want, 1, kMaxSplits));

@@ -44,6 +44,9 @@ CASES = [
     ([5000, 17], [1, 1], 4, 4, 64, 16, 1),
     ([6000], [20], 1, 1, 64, 64, 0),
     ([2500], [31], 1, 1, 128, 16, 2),
+    # many rows of D = 64, long sequences and short: two and more parts
+    ([4500, 10, 2000], [60, 45, 1], 1, 1, 64, 64, 1),
+    ([6500], [300], 4, 1, 64, 16, 0),
 ]
 
 
