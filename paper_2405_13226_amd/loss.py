@@ -16,7 +16,7 @@ from torch.autograd.function import once_differentiable
 
 from .attention import _ptr as _p
 from .block_ops import _call, _vec
-from .cache import _bytes, _is
+from .cache import _F32, _bytes, _is
 
 MAX_TOP = 64
 _TYPES = (torch.bfloat16, torch.float32)
@@ -56,13 +56,13 @@ def _logprobs(logits, targets, top, shared):
     if not 0 <= top <= min(V, MAX_TOP):
         raise ValueError(f"top must be at most {min(V, MAX_TOP)} (got {top})")
     if shared:
-        logp, entropy, lse = torch.empty((3, rows), dtype=torch.float32, device=dev).unbind()
+        logp, entropy, lse = logits.new_empty((3, rows), dtype=_F32).unbind()
     else:
-        logp, entropy, lse = (torch.empty(rows, dtype=torch.float32, device=dev) for _ in range(3))
+        logp, entropy, lse = (logits.new_empty(rows, dtype=_F32) for _ in range(3))
     best = ids = None
     if top:
-        best = torch.empty((rows, top), dtype=torch.float32, device=dev)
-        ids = torch.empty((rows, top), dtype=torch.int64, device=dev)
+        best = logits.new_empty((rows, top), dtype=_F32)
+        ids = targets.new_empty((rows, top))
     if rows:
         need = _bytes("dd_logprobs_workspace_bytes", rows, V, top)
         ws = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
@@ -80,10 +80,11 @@ def logprobs_backward(logits, targets, lse, entropy, g_logp=None, g_entropy=None
     rows, V, ldx, f32 = _logits(logits, "logits")
     dev, i = logits.device, logits.get_device()
     try:
-        fine = (_is(targets, (rows,), torch.int64, i) and _is(lse, (rows,), torch.float32, i)
-                and _is(entropy, (rows,), torch.float32, i)
-                and all(g is None or _is(g, (rows,), torch.float32, i)
-                        for g in (g_logp, g_entropy, g_lse)))
+        n = (rows,)
+        fine = (_is(targets, n, torch.int64, i) and _is(lse, n, _F32, i) and _is(entropy, n, _F32, i)
+                and (g_logp is None or _is(g_logp, n, _F32, i))
+                and (g_entropy is None or _is(g_entropy, n, _F32, i))
+                and (g_lse is None or _is(g_lse, n, _F32, i)))
     except AttributeError:
         fine = False
     if not fine:
@@ -94,7 +95,7 @@ def logprobs_backward(logits, targets, lse, entropy, g_logp=None, g_entropy=None
                 _vec(t, name, rows, torch.float32, dev)
     ldd = V
     if out is None:
-        out = torch.empty((rows, V), dtype=logits.dtype, device=dev)
+        out = torch.empty_like(logits) if ldx == V else logits.new_empty((rows, V))
     else:
         r, c, ldd, same = _logits(out, "out", dev)
         if (r, c, same) != (rows, V, f32):
