@@ -4,8 +4,8 @@
 // chunk's queries) rotated at their positions (dd_rope.hpp: bit-identical to a
 // dd_rope pass at these positions).  One workgroup per token: thread t holds
 // the 8-element chunk t % (D/8) of its heads, so an angle is formed once per
-// token and thread.  Bytes only: each row is read and written once (24,927 tokens
-// of 16 heads of 128 with their queries: 613 MB in 115 us, 5.3 TB/s; a copy of
+// token and thread.  Bytes only: each row is read and written once (24,863 tokens
+// of 16 heads of 128 with their queries: 611 MB in 115 us, 5.3 TB/s; a copy of
 // 2 GiB reaches 4.9).
 //
 // Eviction: per sequence and key head, the `budget` slots of most weight stay
