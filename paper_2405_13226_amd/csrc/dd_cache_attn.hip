@@ -129,6 +129,11 @@ attend_tile(const uint16_t *kt, const uint16_t *vt, const bf16x8 (&qf)[D / 16],
             acc[db] *= alpha;
         m_i = m_new;
     }
+    // A wave that has its scores goes before one that forms them: two on a SIMD
+    // then alternate between the vector unit and the matrix cores (1,000 us instead
+    // of 1,095 for 4 x 2,048 tokens over 14,336, 119 instead of 139 for 8 x up to
+    // 512 over 4,000; with the products V P alone before the others 1,068 and 130).
+    __builtin_amdgcn_s_setprio(1);
     const float neg_m = m_i == -INFINITY ? 0.f : -m_i;
     float psum = 0.f;
 #pragma unroll
@@ -186,6 +191,7 @@ attend_tile(const uint16_t *kt, const uint16_t *vt, const bf16x8 (&qf)[D / 16],
                                 acc[db][r] += sees ? one[r] : 0.f;
                         }
                     }
+            __builtin_amdgcn_s_setprio(0);
             return false;
         }
     }
@@ -202,6 +208,7 @@ attend_tile(const uint16_t *kt, const uint16_t *vt, const bf16x8 (&qf)[D / 16],
                         top, __builtin_bit_cast(u16x8, __builtin_bit_cast(u32x4, a) & 0x7fff7fffu));
                 acc[db] = mfma32(a, pb[kb][t2], acc[db]);
             }
+    __builtin_amdgcn_s_setprio(0);
     return MASKED && !EXACT && __any(__builtin_reduce_max(top) >= 0x7f80);
 }
 
