@@ -764,14 +764,28 @@ __global__ void __launch_bounds__(256) weights_kernel(WeightRows a, CacheView c)
     const int wave_first = first(key0), wave_all = first(key0 + KB * 32 - 1);
     const int begin = first(block0) & ~31;
 
-    auto issue = [&](int r0, int buf) __attribute__((always_inline)) {
+    // The next tile's rows of the lane: their tokens and heads, stepped from tile
+    // to tile (divisions cost 7 ragged sequences with 4 heads a key head 2 us of 35).
+    // Behind the last token they are rows of that one.
+    int token[PER], head[PER];
+    const int step_token = 32 / a.G, step_head = 32 - step_token * a.G;
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+        const int r = begin + ((wave + 4 * k) * 64 + lane) / CPR;
+        token[k] = r / a.G;
+        head[k] = r - token[k] * a.G;
+    }
+    auto issue = [&](int buf) __attribute__((always_inline)) {
         const uint32_t slot = lds_base_sgpr(lds) + static_cast<uint32_t>(buf * TILE * 2 + 1024 * wave);
 #pragma unroll
         for (int k = 0; k < PER; ++k) {
             const int q = (wave + 4 * k) * 64 + lane, tr = q / CPR, x = (q % CPR) ^ swz<D>(tr);
-            const int r = min(r0 + tr, rows - 1), i = r / a.G;
-            dma_b128(a.Q + (s.row0 + i) * a.ldq + (h * a.G + r - i * a.G) * D + x * 8,
+            dma_b128(a.Q + (s.row0 + min(token[k], s.n - 1)) * a.ldq + (h * a.G + head[k]) * D +
+                         x * 8,
                      slot + 4096u * k);
+            head[k] += step_head;
+            token[k] += step_token + (head[k] >= a.G ? 1 : 0);
+            head[k] -= head[k] >= a.G ? a.G : 0;
         }
     };
     int koff[KK];
@@ -791,7 +805,7 @@ __global__ void __launch_bounds__(256) weights_kernel(WeightRows a, CacheView c)
 #pragma unroll
         for (int t = 0; t < STAGES - 1; ++t)
             if (c0 + 32 * t < end)
-                issue(c0 + 32 * t, t);
+                issue(t);
         int buf = 0;
         for (int r0 = c0; r0 < end; r0 += 32, buf = (buf + 1) % STAGES) {
             // this tile's loads, and at most two later tiles' outstanding
@@ -803,7 +817,7 @@ __global__ void __launch_bounds__(256) weights_kernel(WeightRows a, CacheView c)
                 wait_vm<0>();
             __syncthreads();  // every wave's loads; and the stage before is free
             if (r0 + 32 * (STAGES - 1) < end)
-                issue(r0 + 32 * (STAGES - 1), (buf + STAGES - 1) % STAGES);
+                issue((buf + STAGES - 1) % STAGES);
             if (r0 + 32 <= wave_first)
                 continue;
             const uint16_t *qt = lds + buf * TILE;
