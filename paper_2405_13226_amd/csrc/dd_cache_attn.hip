@@ -25,12 +25,12 @@
 // Tiles arrive by direct global->LDS loads; one load instruction covers rows of
 // one page (pages hold at least 16 slots), whose number is a scalar load.
 //
-// Few rows are bound by the cache's bytes: 32 sequences of 8,192 slots, 16 heads
-// of 128, a token each: 1,564 MB in 275 us and 5 us for the parts, 5.6 TB/s (a
-// copy of 2 GiB: 4.9).  Many by the matrix cores: 4 x 2,048 tokens over 14,336
-// slots and each other, 16 heads of 128: 1.03 TFLOP in 1,090 us, 0.95 PFLOP/s
-// (the library's largest products 1.37); matrix cores busy 50% of the time, the
-// exponentials take most of the rest; no LDS conflicts.
+// Few rows are bound by the cache's bytes: 32 sequences of up to 8,192 slots, 16
+// heads of 128, a token each: 1,564 MB in 273 us and 5 us for the parts, 5.6 TB/s
+// (a copy of 2 GiB: 4.9).  Many by the matrix cores and the exponentials: 4 x 2,048
+// tokens over 14,336 slots and each other, 16 heads of 128: 1.03 TFLOP in 1,000 to
+// 1,058 us on different cards, 0.97-1.03 PFLOP/s (the library's largest products
+// 1.37); matrix cores busy 57% of the time, no LDS conflicts.
 //
 // Slots behind a sequence's last are never read (a tile's rows are clamped to
 // it).  A slot that a row may not see leaves no trace in it, whatever it
@@ -868,12 +868,19 @@ CacheView view(const CacheShape &c)
     return CacheView{c.table, c.lens, c.cu_new, c.T, c.B, c.Hkv, c.pages, c.shift, c.per};
 }
 
-// Up to 32 rows per sequence on the average go to few_kernel, more to
-// tile_kernel: 4 sequences of 4,096 slots, 16 heads of 128, with 16, 32, 48, 64
-// and 96 rows each take 31, 31, 39, 38 and 67 us in few_kernel, which reads K and V
-// once for 32 rows, and 30, 31, 34, 34 and 39 in tile_kernel; one sequence 19.1,
-// 19.8, 19.1, 20.5 and 31.2 against 21.3, 21.5, 22.4, 22.8 and 24.9.
-constexpr int kFewRows = 32;
+// Up to so many rows per sequence on the average go to few_kernel, more to
+// tile_kernel.  In us by rows per sequence, few_kernel / tile_kernel, 16 heads of
+// 4,096 slots (the last: 8,192):
+//            16            24            32            48            96
+//   D = 128, 1 sequence
+//       19.1 / 20.0               19.7 / 20.3   19.9 / 21.2   32 / 24
+//   16   108 / 102     109 / 103   112 / 104     150 / 110     211 / 121
+//   32   416 / 363     429 / 364
+//   D = 64, 1 sequence
+//       14.1 / 15.4               15.1 / 15.6   14.4 / 16.4   19 / 18
+//   16    55 / 57       56 / 57     67 / 58       67 / 61      111 / 67
+//   32   200 / 194     207 / 228
+constexpr int few_rows(int D) { return D == 64 ? 24 : 16; }
 
 // Waves of a workgroup with few rows: 64 KB of LDS, two workgroups per CU.  (At
 // D = 128 four waves, one workgroup per CU, read 8 x 8,192 slots of 8 key heads
@@ -892,33 +899,60 @@ struct AttnPlan {
     size_t rows, part_bytes, bytes;  // of the parts, and of the whole workspace
 };
 
+// Parts of a sequence's keys for few rows, `work` of them to be split: the time of
+// `work` x p workgroups, 512 at once, is estimated for those p that fill 1, 2, 3
+// ... rounds.  Together they read 5.6 TB/s, one alone up to 17 GB/s; a round costs
+// a microsecond to begin and end, ragged sequences a quarter of one (within one
+// round the others go faster instead), the join a launch and its bytes.  (32 x
+// 8,192 slots of 16 heads of 128 in 2, 4, 8 and 16 parts: 314, 293, 281 and 293
+// us; 8 sequences and 8 key heads in 4, 8 and 16: 64, 52 and 53; 6 and 8 in 10
+// and 11: 43 and 60.)
+int few_parts(long long work, long long slots, int D, long long rows)
+{
+    const int most = static_cast<int>(std::clamp<long long>(slots / 128, 1, kMaxSplits));
+    int best = 1;
+    double least = 0;
+    for (int m = 0; m <= 16; ++m) {
+        const int p = static_cast<int>(std::clamp<long long>(512 * m / work, 1, most));
+        const long long n = work * p, full = n / 512, rest = n % 512;
+        const double bytes = static_cast<double>(slots) * D * 4 / p, round = bytes * 512 / 5.6e6;
+        const double us = static_cast<double>(full) * round +
+                          (rest ? bytes / std::min(17e3, 5.6e6 / static_cast<double>(rest)) : 0) +
+                          (n > 512 ? 0.25 : 0.06) * round + static_cast<double>(full + (rest > 0)) +
+                          (p > 1 ? 2 + static_cast<double>(p) * rows * D * 8 / 5.6e6 : 0);
+        if (m == 0 || us < least) {
+            best = p;
+            least = us;
+        }
+        if (p == most)
+            break;
+    }
+    return best;
+}
+
 AttnPlan attn_plan(const CacheShape &c, int H, bool weights)
 {
     AttnPlan p;
     const long long rows = static_cast<long long>(c.T) * (H / c.Hkv);
-    p.few = rows <= static_cast<long long>(kFewRows) * c.B;
+    p.few = rows <= static_cast<long long>(few_rows(c.D)) * c.B;
     const int bm = p.few ? 32 : 128;
     p.tiles = static_cast<int>(rows / bm) + c.B;
     // workgroups with work in them, if the rows are spread evenly
     const long long each = (rows + c.B - 1) / c.B;
     const long long work = std::min<long long>(c.B, c.T) * ((each + bm - 1) / bm) * c.Hkv;
     const long long slots = static_cast<long long>(c.per) << c.shift;
-    // Few rows: parts of 512 KB of K and V or more while there are less than
-    // 8,192 (32 x 8,192 slots of 16 heads in 2, 4, 8 and 16 parts: 314, 293, 281
-    // and 293 us), smaller where that leaves CUs idle, down to 128 slots (8
-    // sequences, 8 key heads in 4, 8 and 16 parts: 64, 52 and 53).  Many: enough
-    // workgroups, of 512 slots or more; at D = 64, where 768 run at once and a
-    // part's sums are half as many bytes, two rounds of them where they keep 2,048
-    // slots, for ragged sequences (in us with 1 and 2-3 parts, up to so many new
-    // tokens: 3 x 1,399 over 7,053 slots of one key head with 16 124 and 88, 16 x
-    // 256 over 8,000 of 16 207 and 156; at D = 128 gains and losses of 10%).
-    const long long fill = (512 + work - 1) / work;
+    // Many rows: enough workgroups, of 512 slots or more; at D = 64, where 768 run
+    // at once and a part's sums are half as many bytes, two rounds of them where
+    // they keep 2,048 slots, for ragged sequences (in us with 1 and 2-3 parts, up to
+    // so many new tokens: 3 x 1,399 over 7,053 slots of one key head with 16 124 and
+    // 88, 16 x 256 over 8,000 of 16 207 and 156; at D = 128 192 and 179 at best, but
+    // 124 and 140, 295 and 342).
     p.wide = p.few && slots * c.D * 4 <= kOnePart && work < 512;
     long long want = std::min(512 / work, slots / 512);
     if (c.D == 64)
         want = std::max(want, std::min((1536 + work / 2) / work, slots / 2048));
-    if (p.few)
-        want = std::max(std::min(slots * c.D / 131072, 8192 / work), std::min(fill, slots / 128));
+    if (p.few && !p.wide)
+        want = few_parts(work, slots, c.D, rows);
     p.splits = p.wide ? 1 : static_cast<int>(std::clamp<long long>(want, 1, kMaxSplits));
     p.rows = static_cast<size_t>(c.T) * H;
     p.part_bytes = p.splits == 1 ? 0 : p.splits * p.rows * (c.D + 1) * sizeof(float);

@@ -47,6 +47,12 @@ CASES = [
     # many rows of D = 64, long sequences and short: two and more parts
     ([4500, 10, 2000], [60, 45, 1], 1, 1, 64, 64, 1),
     ([6500], [300], 4, 1, 64, 16, 0),
+    # around the most rows that count as few, one part and several
+    ([900, 40], [16, 16], 1, 1, 128, 32, 0),
+    ([900, 40], [17, 16], 1, 1, 128, 32, 0),
+    ([3100, 40], [24, 24], 1, 1, 64, 32, 0),
+    ([3100, 40], [24, 25], 1, 1, 64, 32, 0),
+    ([9000, 100, 7000], [1, 2, 1], 8, 2, 128, 64, 0),
 ]
 
 
