@@ -1,6 +1,8 @@
 """The paged cache's calls as a serving program makes them: two at once on
 streams of their own, captured and replayed with many rows, over pages that
 sequences share, under a batch of prompts and single tokens."""
+import random
+
 import pytest
 import torch
 
@@ -8,7 +10,7 @@ import paper_2405_13226_amd as dd
 
 import cache_oracle as O
 from parity import log
-from test_gpu_cache import close
+from test_gpu_cache import check, close
 
 pytestmark = pytest.mark.gpu
 
@@ -146,6 +148,18 @@ def test_prompts_among_single_tokens(cuda, H, Hkv, D):
                                      t["lens_t"][b:b + 1], cu)
         close(one, o[at:at + 1], to[at:at + 1], "o of its own")
         close(z1, lse[at:at + 1], tl[at:at + 1], "lse of its own")
+
+
+@pytest.mark.parametrize("most", [1, 40])
+@pytest.mark.parametrize("D", [64, 128])
+def test_many_sequences(cuda, D, most):
+    """More sequences than a wave has lanes, many of them without new tokens or
+    without slots."""
+    log(f"cache: 150 sequences, D {D}, up to {most} new tokens")
+    rng = random.Random(D + most)
+    lens = [rng.choice([0, 1, 15, 16, 17, 40, 130]) for _ in range(150)]
+    news = [rng.choice([0, 1, rng.randint(1, most)]) for _ in lens]
+    check(O.Batch(lens, news, 2, 1, D, 16, seed=most, tail=3), cuda)
 
 
 def test_empty_batch(cuda):
