@@ -369,12 +369,17 @@ class PagedCache:
         if need:
             self._set_tables()
 
-    def extend(self, q, k, v, news, rope_base=None, out=None, lse=None):
-        """Appends the chunk (news[b] rows of sequence b, one after the other)
-        and returns its attention (o, lse) over the cache."""
+    def counts(self, news):
+        """The numbers of new tokens as a list, one for each sequence."""
         news = [int(n) for n in news]
         if len(news) != len(self.lengths) or min(news, default=0) < 0:
             raise ValueError(f"need {len(self.lengths)} numbers of new tokens")
+        return news
+
+    def extend(self, q, k, v, news, rope_base=None, out=None, lse=None):
+        """Appends the chunk (news[b] rows of sequence b, one after the other)
+        and returns its attention (o, lse) over the cache."""
+        news = self.counts(news)
         if sum(news) > q.shape[0]:
             raise ValueError(f"{sum(news)} new tokens, but q has {q.shape[0]} rows")
         self._reserve(news)

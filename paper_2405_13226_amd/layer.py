@@ -176,10 +176,13 @@ class OpenLMBlock(torch.nn.Module):
     @torch.no_grad()
     def extend(self, x, cache, news):
         """The block on a ragged chunk of new tokens: x [tokens, d] holds news[b]
-        rows of sequence b, one after the other; ``cache`` (a PagedCache of H
-        heads of d / H) receives their keys and values and holds what they
-        attend to.  Forward only."""
+        rows of sequence b, one after the other, and no others; ``cache`` (a
+        PagedCache of H heads of d / H) receives their keys and values and holds
+        what they attend to.  Forward only."""
         T, d = x.shape
+        news = cache.counts(news)
+        if sum(news) != T:
+            raise ValueError(f"{sum(news)} new tokens, but x has {T} rows")
         rows = -(-T // 256) * 256  # the products take whole tiles of rows
         if not T:
             return x.clone()

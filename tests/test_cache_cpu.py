@@ -226,3 +226,16 @@ def test_paged_cache_bookkeeping():
         c.extend(torch.zeros(2, 1, 64), None, None, [1])
     with pytest.raises(ValueError):
         c.extend(torch.zeros(2, 1, 64), None, None, [2, 1])
+
+
+def test_block_extend_wants_as_many_rows_as_new_tokens():
+    from paper_2405_13226_amd.layer import OpenLMBlock
+    block = OpenLMBlock(d=512, H=8, hidden=256, device="cpu")
+    c = cache.PagedCache(2, 8, 64, 64, page=16, device="cpu")
+    x = torch.zeros(3, 512, dtype=torch.bfloat16)
+    for rows, news in ((3, [10, 0]), (3, [2, 2]), (3, [1, 1]), (3, [3]), (3, [4, -1]), (3, [1, 1, 1]),
+                       (0, [1, 0]), (0, [1, -1]), (0, [0])):
+        with pytest.raises(ValueError, match="new tokens"):
+            block.extend(x[:rows], c, news)
+        assert c.lengths == [0, 0] and c.owned == [[], []] and not c.lens.any()
+    assert block.extend(x[:0], c, [0, 0]).shape == (0, 512)
