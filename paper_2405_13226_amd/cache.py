@@ -378,10 +378,14 @@ class PagedCache:
 
     def extend(self, q, k, v, news, rope_base=None, out=None, lse=None):
         """Appends the chunk (news[b] rows of sequence b, one after the other)
-        and returns its attention (o, lse) over the cache."""
+        and returns its attention (o, lse) over the cache.  Rows behind the
+        chunk's last are left as they were in ``out`` and ``lse``."""
         news = self.counts(news)
-        if sum(news) > q.shape[0]:
-            raise ValueError(f"{sum(news)} new tokens, but q has {q.shape[0]} rows")
+        rows, n = q.shape[0], sum(news)
+        if n > rows:
+            raise ValueError(f"{n} new tokens, but q has {rows} rows")
+        if n < rows:
+            return self._extend_first(q, k, v, news, rope_base, out, lse)
         self._reserve(news)
         cu = self._device_ints([0, *itertools.accumulate(news)])
         q = cache_append(q, k, v, self.k_pages, self.v_pages, self.table, self.lens, cu,
@@ -394,6 +398,23 @@ class PagedCache:
         self.lens += step
         self.seen += step
         return o, lse
+
+    def _extend_first(self, q, k, v, news, rope_base, out, lse):
+        """``extend`` where rows lie behind the chunk's: the operators, which
+        choose their kernels by the number of rows, get the chunk's alone."""
+        n, rows = sum(news), q.shape[0]
+        for t, name in ((k, "k"), (v, "v")):
+            if t.shape[0] != rows:
+                raise ValueError(f"q has {rows} rows, {name} has {t.shape[0]}")
+        if (out is None) != (lse is None):
+            raise ValueError("give both out and lse, or neither")
+        if out is None:
+            out, lse = q.new_empty(q.shape), q.new_empty(q.shape[:2], dtype=_F32)
+        else:
+            _state(out, "out", q.shape, _BF16, q.device)
+            _state(lse, "lse", q.shape[:2], _F32, q.device)
+        self.extend(q[:n], k[:n], v[:n], news, rope_base, out[:n], lse[:n])
+        return out, lse
 
     def evict(self, budget: int, recent: int = 0):
         """Thins every sequence out to ``budget`` slots and frees their pages."""

@@ -239,3 +239,38 @@ def test_block_extend_wants_as_many_rows_as_new_tokens():
             block.extend(x[:rows], c, news)
         assert c.lengths == [0, 0] and c.owned == [[], []] and not c.lens.any()
     assert block.extend(x[:0], c, [0, 0]).shape == (0, 512)
+
+
+def test_the_cache_hands_over_the_chunks_rows_only(monkeypatch):
+    """Rows behind the chunk's last are no tokens: the operators, whose plans go
+    by the number of rows, get the chunk's; results have all rows, those behind
+    as they were."""
+    seen = []
+
+    def append(q, k, v, *_, **kw):
+        seen.append([t.shape[0] for t in (q, k, v)])
+        return q
+
+    def attention(q, *_, out=None, lse=None, **kw):
+        seen.append([t.shape[0] for t in (q, out, lse)])
+        out.fill_(1)
+        lse.fill_(1)
+        return out, lse
+    monkeypatch.setattr(cache, "cache_append", append)
+    monkeypatch.setattr(cache, "cache_attention", attention)
+    c = cache.PagedCache(2, 2, 64, 64, page=16, device="cpu")
+    q, k, v = (torch.zeros(256, h, 64, dtype=torch.bfloat16) for h in (4, 2, 2))
+    out, lse = torch.full_like(q, 7.0), torch.full((256, 4), 7.0)
+    o, z = c.extend(q, k, v, [2, 1], out=out, lse=lse)
+    assert seen == [[3, 3, 3], [3, 3, 3]] and c.lens.tolist() == [2, 1] == c.lengths
+    assert o is out and z is lse
+    assert (out[:3] == 1).all() and (out[3:] == 7).all() and (lse[3:] == 7).all()
+    o, z = c.extend(q, k, v, [0, 5])
+    assert seen[2:] == [[5, 5, 5], [5, 5, 5]] and o.shape == q.shape and z.shape == (256, 4)
+    state = [list(c.lengths), [list(p) for p in c.owned], list(c.free)]
+    for bad in (dict(k=k[:200]), dict(v=v[:5]), dict(out=out[:3], lse=lse), dict(out=out),
+                dict(out=out, lse=lse[:3]), dict(out=out, lse=lse.double())):
+        args = dict(dict(k=k, v=v), **bad)
+        with pytest.raises(ValueError):
+            c.extend(q, args.pop("k"), args.pop("v"), [30, 1], **args)
+        assert state == [c.lengths, c.owned, c.free], bad

@@ -579,3 +579,55 @@ def test_malformed_contents_stay_inside(cuda):
         torch.cuda.synchronize()
         for buf in (kp, vp, w, p, o, z):
             assert buf.intact()
+
+
+def test_rows_behind_the_chunk_do_not_change_the_plan(cuda):
+    """The cache's results for a token each are bit for bit those without the
+    rows of padding behind them."""
+    log("cache: padding rows")
+    g = torch.Generator().manual_seed(3)
+    caches = [dd.PagedCache(2, 4, 128, 4096, page=16, weights=True, device=cuda) for _ in range(2)]
+    for news in ([900, 400], [1, 1], [1, 0], [1, 1]):
+        n = sum(news)
+        q, k, v = (torch.randn(n, 4, 128, generator=g).to(torch.bfloat16).to(cuda) for _ in range(3))
+        o, z = caches[0].extend(q, k, v, news, rope_base=BASE)
+        wide = [torch.nn.functional.pad(t, (0, 0, 0, 0, 0, 256)) for t in (q, k, v)]
+        out, lse = torch.full_like(wide[0], 7.0), torch.full((n + 256, 4), 7.0, device=cuda)
+        caches[1].extend(*wide, news, rope_base=BASE, out=out, lse=lse)
+        assert torch.equal(out[:n], o) and torch.equal(lse[:n], z)
+        assert (out[n:] == 7).all() and (lse[n:] == 7).all()
+        for b in range(2):
+            m = caches[0].lengths[b]
+            assert torch.equal(*(c.weights[b, :, :m] for c in caches))
+
+
+def test_block_extend_of_several_sequences_with_weights(cuda):
+    """Chunks of three sequences through a cache with weights: the block on each
+    whole row; rows of padding leave nothing in the cache, and a token each takes
+    the plan of its rows alone."""
+    log("block: extend of several sequences")
+    from paper_2405_13226_amd.layer import OpenLMBlock
+    block = OpenLMBlock(d=512, H=8, hidden=1024, device=cuda)
+    x = torch.randn(3, 256, 512, device=cuda, dtype=torch.bfloat16)
+    with torch.no_grad():
+        y = block(x).float()
+    cache = dd.PagedCache(3, 8, 64, 512, page=16, weights=True, device=cuda)
+    at, got = [0, 0, 0], torch.zeros_like(y)
+    for news in ([200, 0, 3], [1, 1, 1], [1, 1, 1], [0, 150, 0], [54, 104, 251]):
+        rows = torch.cat([x[b, a:a + n] for b, (a, n) in enumerate(zip(at, news))])
+        out = block.extend(rows, cache, news).float()
+        assert out.shape == rows.shape
+        i = 0
+        for b, n in enumerate(news):
+            got[b, at[b]:at[b] + n] = out[i:i + n]
+            i, at[b] = i + n, at[b] + n
+        assert cache.lengths == at == cache.lens.tolist()
+    assert at == [256, 256, 256]
+    # the two differ by roundings of the attention's output (2^-8 each) and what follows
+    assert float((got - y).norm() / y.norm()) < 2.0 ** -7
+    # a token's probabilities add up to 1 a head, each sum within 1e-4 (see cache_oracle)
+    total = cache.weights.double().sum(dim=2)
+    assert ((total[:, :, None] - 256).abs() <= 256 * 1e-4).all()
+    cache.evict(100, 20)
+    block.extend(x[:, 0], cache, [1, 1, 1])
+    assert cache.lengths == [101] * 3
