@@ -340,3 +340,76 @@ def test_empty(cuda):
     assert [tuple(o.shape) for o in out] == [(0,), (0,), (0,), (0, 2), (0, 2)]
     z = torch.zeros(0, device=cuda)
     assert dd.logprobs_backward(x, t, z, z).shape == (0, 10)
+
+
+def exact_grad(x, t, g_logp, g_entropy, g_lse):
+    """(gradient, magnitudes, p, |log p|, entropy) in float64, log p = (x - m) -
+    log sum e^(x - m): an lse in float64 does not hold that sum either where the
+    logits are near fp32's largest."""
+    a = x.double() - x.double().amax(dim=1, keepdim=True)
+    lp = a - torch.log(torch.exp(a).sum(dim=1, keepdim=True))
+    p = torch.exp(lp)
+    lp = torch.where(p > 0, lp, 0.0)
+    h = -(p * lp).sum(dim=1, keepdim=True)
+    gl = torch.where(t < 0, 0.0, g_logp.double())[:, None]
+    ge, gz = g_entropy.double()[:, None], g_lse.double()[:, None]
+    one = torch.zeros_like(p)
+    one.scatter_(1, t.clamp(min=0)[:, None], 1.0)
+    size = gl.abs() * (one + p) + gz.abs() * p + ge.abs() * p * (lp.abs() + h)
+    return gl * (one - p) + gz * p - ge * p * (lp + h), size, p, lp.abs(), h[:, 0]
+
+
+def check_far(x, t, g, dx):
+    """dx against exact_grad.  Up to |lse| = 64 the lse's rounding is 64 u of every
+    p; beyond it p is formed from the row's sum again (r as above): in no row
+    does the tolerance grow with |lse|."""
+    V = x.shape[1]
+    ref, size, p, lp, h = exact_grad(x, t, *g)
+    r = (200 + V / 256 + 110) * U
+    th = r * (100 + math.log(V)) / 10 + 4 * U * (h.abs() + 20)
+    tz = r + 84 * U
+    tol = (2 * tz + 4 * U * (lp.clamp(max=200) + 1) + 8 * U) * size
+    tol = tol + p * (tz + th[:, None]) * g[1].double().abs()[:, None]
+    tol = tol + (HB if x.dtype is torch.bfloat16 else U) * (ref.abs() + tol) + 1e-38
+    close(dx, ref, tol, "gradient")
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("V", [40, 1001, 20003])
+def test_gradient_of_logits_far_from_zero(cuda, V, dtype):
+    """An offset of a row's logits, however large, changes p by no more than its
+    own roundings; rows of one value, and of the type's lowest and largest."""
+    log(f"logprobs: gradients of far logits {V} {dtype}")
+    least, most = torch.finfo(dtype).min, torch.finfo(dtype).max
+    base, _, _ = case(1, V, torch.float32, V)
+    half = torch.arange(V) % 2 == 0
+    rows = [base[0] + c for c in (0.0, 45.0, 52.0, 58.0, 70.0, -60.0, -90.0, 1e3, -1e3, 1e5, -1e5, 1e7,
+                                  -1e7, 1e20, -1e30)]
+    rows += [torch.full((V,), c) for c in (least, most, 80.0, -1e6)]
+    rows += [torch.where(half, base[0] + 1e4, least), torch.where(half, base[0] - 1e4, float("-inf"))]
+    one = torch.full((V,), least)
+    one[V - 1] = most
+    x = torch.stack(rows + [one]).to(dtype)
+    n = len(x)
+    gen = torch.Generator().manual_seed(V)
+    t = torch.randint(0, V, (n,), generator=gen)
+    t[::5] = -1
+    g = [torch.randn(n, generator=gen) for _ in range(3)]
+    xd, td, gd = x.to(cuda), t.to(cuda), [y.to(cuda) for y in g]
+    _, h, lse = dd.logprobs(xd, td)
+    dx = dd.logprobs_backward(xd, td, lse, h, *gd)
+    check_far(x, t, g, dx)
+    # each p by itself: no target, the gradient of the lse alone
+    ones = torch.ones(n)
+    p = dd.logprobs_backward(xd, torch.full_like(td, -1), lse, h, g_lse=ones.to(cuda))
+    check_far(x, torch.full_like(t, -1), [0 * ones, 0 * ones, ones], p)
+    # in place, several workgroups to a row
+    wide = torch.zeros(n, V + 3, dtype=dtype, device=cuda)
+    part = wide[:, 1:V + 1]
+    part.copy_(xd)
+    dd.logprobs_backward(part, td, lse, h, *gd, out=part)
+    assert torch.equal(part, dx) and not wide[:, 0].any() and not wide[:, V + 1:].any()
+    leaf = xd.clone().requires_grad_()
+    logp, h, lse = dd.token_logprobs(leaf, td)
+    (logp * gd[0] + h * gd[1] + lse * gd[2]).sum().backward()
+    assert torch.equal(leaf.grad, dx)
