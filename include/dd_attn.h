@@ -428,7 +428,8 @@ int dd_cache_check(const int32_t *host_table, const int32_t *host_lens, const in
  * Log probabilities of given tokens.  X: logits [rows][V], bf16 (f32 = 0) or
  * fp32 (f32 = 1), row stride ldx >= V, any alignment of their type; targets
  * int64 [rows], a negative one is ignored (log probability and its gradient 0),
- * one of V or more gives NaN.  1 <= rows <= 2^23, 1 <= V <= 2^30, rows *
+ * one of V or more gives NaN (the log probability, and with g_logp the row of
+ * the gradient).  1 <= rows <= 2^23, 1 <= V <= 2^30, rows *
  * ceil(V / 8192) < 2^24, top <= min(V, 64).  fp32 throughout; sums in a fixed
  * order.
  *

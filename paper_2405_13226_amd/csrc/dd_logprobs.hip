@@ -447,7 +447,8 @@ __global__ void __launch_bounds__(256) logits_grad_kernel(GradRows a)
     T *y = static_cast<T *>(a.dX) + row * a.lddx;
     const float lse = a.lse[row], h = a.entropy[row];
     const int64_t t = a.targets[row];
-    const float g_t = a.g_logp && t >= 0 ? a.g_logp[row] : 0.f;
+    // (a target of V or more has no log probability: its row becomes NaN)
+    const float g_t = a.g_logp && t >= 0 ? (t < a.V ? a.g_logp[row] : NAN) : 0.f;
     const float g_h = a.g_entropy ? a.g_entropy[row] : 0.f;
     const float g_p = (a.g_lse ? a.g_lse[row] : 0.f) - g_t;
     const int64_t given = g_t != 0.f ? t : -1;

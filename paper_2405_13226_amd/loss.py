@@ -7,7 +7,8 @@ dd_logprobs_fwd and dd_logprobs_bwd of include/dd_attn.h.
 
 Logits are [rows, V] in bf16 or fp32 with unit column stride (the columns of a
 wider, padded matrix are fine), targets int64 [rows]; a negative target is
-ignored.  Statistics are fp32.
+ignored, one of V or more makes its log probability and that one's gradient NaN.
+Statistics are fp32.
 """
 from __future__ import annotations
 

@@ -413,3 +413,21 @@ def test_gradient_of_logits_far_from_zero(cuda, V, dtype):
     logp, h, lse = dd.token_logprobs(leaf, td)
     (logp * gd[0] + h * gd[1] + lse * gd[2]).sum().backward()
     assert torch.equal(leaf.grad, dx)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("V", [700, 9000])
+def test_gradient_of_a_target_out_of_range(cuda, V, dtype):
+    """A target of V or more: NaN where the log probability has a gradient, in its
+    row alone."""
+    log(f"logprobs: gradient of targets out of range {V} {dtype}")
+    x, _, g = case(5, V, dtype, 9)
+    x[4] += 100
+    t = torch.tensor([0, V, -1, 2 ** 40, V])
+    xd, td, gd = x.to(cuda), t.to(cuda), [y.to(cuda) for y in g]
+    logp, h, lse = dd.logprobs(xd, td)
+    assert torch.equal(logp.isnan().cpu(), t >= V)
+    dx = dd.logprobs_backward(xd, td, lse, h, *gd).cpu()
+    assert dx[t >= V].isnan().all() and torch.isfinite(dx[t < V]).all()
+    dx = dd.logprobs_backward(xd, td, lse, h, None, *gd[1:])
+    check_far(x, torch.full_like(t, -1), [torch.zeros(5), *g[1:]], dx)
