@@ -427,6 +427,10 @@ __device__ __forceinline__ void store_grads(float *y, int at, int end, f32x8 f)
 constexpr long long kStreamBytes = 256LL << 20;
 constexpr int kGradPieces = 4;  // of 8 logits per thread
 
+// Below this log p there is no p (e^-1000 is 0 in fp32): what multiplies that 0
+// stays finite for a g_entropy of up to 1e35.
+constexpr float kNone = -1000.0f;
+
 // The lse is rounded to its own size, and every p_j = e^(x_j - lse) carries that
 // rounding.  Up to this |lse| it is at most 2^-18 of p.  Beyond it the row's first
 // workgroup takes the whole row: S = sum_j e^(x_j - lse), which the rounding moved
@@ -475,7 +479,7 @@ __global__ void __launch_bounds__(256) logits_grad_kernel(GradRows a)
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const float d = f[i] - lse, p = fast_exp2(d * kLog2e) * scale;
-                const float v = p * (g_p - g_h * (fmaxf(d - log_s, kFar) + h));
+                const float v = p * (g_p - g_h * (fmaxf(d - log_s, kNone) + h));
                 f[i] = at + i == given ? v + g_t : v;
             }
             store_grads<STREAM>(y, at, a.V, f);
@@ -496,7 +500,7 @@ __global__ void __launch_bounds__(256) logits_grad_kernel(GradRows a)
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const float d = f[k][i] - lse, p = fast_exp2(d * kLog2e);
-            const float v = p * (g_p - g_h * (fmaxf(d, kFar) + h));
+            const float v = p * (g_p - g_h * (fmaxf(d, kNone) + h));
             f[k][i] = at + i == given ? v + g_t : v;
         }
         store_grads<STREAM>(y, at, a.V, f[k]);

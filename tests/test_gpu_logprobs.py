@@ -431,3 +431,19 @@ def test_gradient_of_a_target_out_of_range(cuda, V, dtype):
     assert dx[t >= V].isnan().all() and torch.isfinite(dx[t < V]).all()
     dx = dd.logprobs_backward(xd, td, lse, h, None, *gd[1:])
     check_far(x, torch.full_like(t, -1), [torch.zeros(5), *g[1:]], dx)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_large_entropy_gradients_of_masked_logits(cuda, dtype):
+    log(f"logprobs: large entropy gradients {dtype}")
+    x, t, _ = case(6, 3001, dtype, 12)
+    mask = torch.rand(6, 3001, generator=torch.Generator().manual_seed(1)) < 0.5
+    mask[torch.arange(6), t.clamp(min=0)] = False
+    g = torch.tensor([1e9, -1e9, 1e20, -1e20, 3e30, 1.0])
+    for value in (float("-inf"), torch.finfo(dtype).min, -1e30):
+        y = x.masked_fill(mask, value)
+        yd, td = y.to(cuda), t.to(cuda)
+        _, h, lse = dd.logprobs(yd, td)
+        dx = dd.logprobs_backward(yd, td, lse, h, g_entropy=g.to(cuda)).cpu()
+        assert (dx[mask] == 0).all() and torch.isfinite(dx).all()
+        check_far(y, t, [torch.zeros(6), g, torch.zeros(6)], dx)
