@@ -43,9 +43,10 @@ from .block_ops import _call, _entry
 _BF16, _F32, _I32 = torch.bfloat16, torch.float32, torch.int32
 
 
-@functools.lru_cache(maxsize=None)
+@functools.lru_cache(maxsize=1024)
 def _bytes(name, *sizes):
-    """Workspace bytes of a call: of its sizes alone."""
+    """Workspace bytes of a call: of its sizes alone (the latest 1024 of them: a
+    program that scores texts has ever new numbers of rows)."""
     return _entry(name)(*sizes)
 
 

@@ -274,3 +274,9 @@ def test_the_cache_hands_over_the_chunks_rows_only(monkeypatch):
         with pytest.raises(ValueError):
             c.extend(q, args.pop("k"), args.pop("v"), [30, 1], **args)
         assert state == [c.lengths, c.owned, c.free], bad
+
+
+def test_workspace_sizes_that_are_remembered_are_bounded():
+    for rows in range(1, 3000):
+        cache._bytes("dd_logprobs_workspace_bytes", rows, 100, 0)
+    assert cache._bytes.cache_info().currsize <= 1024
