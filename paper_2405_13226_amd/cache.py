@@ -319,6 +319,8 @@ def cache_evict(k_pages, v_pages, table, lens, weights, positions, seen, budget:
               lens.data_ptr(), weights.data_ptr(), positions.data_ptr(), seen.data_ptr(),
               w.data_ptr(), p.data_ptr(), n.data_ptr(), B, Hkv, D, pages, page, per, budget, recent,
               _p(ws), need)
+    elif B:  # no heads, or no slots
+        torch.clamp(lens, 0, budget if per else 0, out=n)
     return w, p, n
 
 

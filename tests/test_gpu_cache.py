@@ -631,3 +631,20 @@ def test_block_extend_of_several_sequences_with_weights(cuda):
     cache.evict(100, 20)
     block.extend(x[:, 0], cache, [1, 1, 1])
     assert cache.lengths == [101] * 3
+
+
+def test_evict_without_slots_or_heads(cuda):
+    """Nothing to thin out: the lengths that are left all the same."""
+    log("evict: no slots, no heads")
+    lens = torch.tensor([7, 0, 90], dtype=torch.int32, device=cuda)
+    seen = torch.zeros_like(lens)
+    for Hkv, per, want in ((0, 6, [7, 0, 40]), (2, 0, [0, 0, 0])):
+        pages = torch.zeros(4, Hkv, 16, 64, dtype=torch.bfloat16, device=cuda)
+        table = torch.zeros(3, per, dtype=torch.int32, device=cuda)
+        w = torch.zeros(3, Hkv, per * 16, device=cuda)
+        n = torch.full_like(lens, -9)
+        out = dd.cache_evict(pages, pages.clone(), table, lens, w, w.int(), seen, 40, 3,
+                             out=(w.clone(), w.int(), n))
+        assert out[2] is n and n.tolist() == want
+        out = dd.cache_evict(pages, pages.clone(), table, lens, w, w.int(), seen, 40, 3)
+        assert out[2].tolist() == want
