@@ -199,8 +199,8 @@ def cache_append(q, k, v, k_pages, v_pages, table, lens, cu_new, rope_base=None,
         rot = _like(q, ldq) if out is None else out
         if out is not None:
             _state(out, "out", (T, H, D), _BF16, k.device)
-    if rope_base is not None and not rope_base > 0:
-        raise ValueError(f"rope_base must be positive (got {rope_base})")
+    if rope_base is not None and not 2.0 ** -126 <= rope_base < 2.0 ** 128:
+        raise ValueError(f"rope_base must be positive and fit fp32 (got {rope_base})")
     if T and B:
         _call(k.device, "dd_cache_append", q.data_ptr() if rot is not None else None, ldq,
               k.data_ptr(), ldk, v.data_ptr(), ldv, _p(rot), k_pages.data_ptr(),

@@ -648,3 +648,15 @@ def test_evict_without_slots_or_heads(cuda):
         assert out[2] is n and n.tolist() == want
         out = dd.cache_evict(pages, pages.clone(), table, lens, w, w.int(), seen, 40, 3)
         assert out[2].tolist() == want
+
+
+def test_append_refuses_a_base_that_fp32_does_not_hold(cuda):
+    log("append: rope bases that leave fp32")
+    x = O.Batch([3], [2], 2, 2, 64, 16)
+    t = x.to(cuda)
+    for base in (1e-50, 1e39, -1.0, 0.0, float("nan"), float("inf")):
+        for q in (None, t["q"]):
+            with pytest.raises((ValueError, dd.DDError)):
+                dd.cache_append(q, t["q"], t["q"], t["k"], t["v"], t["table"], t["lens_t"], t["cu"],
+                                rope_base=base)
+    assert torch.equal(t["k"].cpu(), x.k)
