@@ -960,9 +960,11 @@ AttnPlan attn_plan(const CacheShape &c, int H, bool weights)
     const size_t score_bytes = p.rows * slots * sizeof(float);
     // Scores are kept where they are at most half of K's bytes, written and read
     // (8 sequences of 8,192 slots, 8 key heads with 4 heads each, a token: 65 us in
-    // all, 91 with S formed once more).
+    // all, 91 with S formed once more), and where a launch has as many workgroups of
+    // 256 as finish_kernel takes (below 2^32 threads, half of them for the joins).
     p.scores = weights && p.few && rows * 8 <= static_cast<long long>(c.D) * c.B &&
-               score_bytes <= kMaxScores;
+               score_bytes <= kMaxScores &&
+               static_cast<long long>(c.B) * c.Hkv * ((slots + 1023) / 1024) < 1 << 23;
     p.bytes = p.part_bytes + (p.scores ? score_bytes : 0);
     return p;
 }

@@ -280,3 +280,14 @@ def test_workspace_sizes_that_are_remembered_are_bounded():
     for rows in range(1, 3000):
         cache._bytes("dd_logprobs_workspace_bytes", rows, 100, 0)
     assert cache._bytes.cache_info().currsize <= 1024
+
+
+def test_scores_are_not_kept_for_more_slots_than_a_launch_has_blocks(lib):
+    """A block of 256 threads turns the scores of 1024 slots into weights, and a
+    launch ends at 2^32 threads (weights of 68 GB); half of them are left to the
+    joins.  On either side of the bound: the workspace with and without weights."""
+    for per, kept in ((1 << 12, True), (1 << 14, False)):
+        sizes = (1, 65535, 1, 1, 64, 16, per)
+        more = lib.dd_cache_attn_workspace_bytes(*sizes, 1) - \
+            lib.dd_cache_attn_workspace_bytes(*sizes, 0)
+        assert more == (4 * 16 * per if kept else 0)
