@@ -660,3 +660,34 @@ def test_append_refuses_a_base_that_fp32_does_not_hold(cuda):
                 dd.cache_append(q, t["q"], t["q"], t["k"], t["v"], t["table"], t["lens_t"], t["cu"],
                                 rope_base=base)
     assert torch.equal(t["k"].cpu(), x.k)
+
+
+# many rows over capacities from which a workgroup forms the weights of 256 slots:
+# chunks across such a border, sequences shorter than a block and without slots
+@pytest.mark.parametrize("H,Hkv,D,page,spare", [(8, 8, 64, 1024, 22), (16, 8, 128, 1024, 22),
+                                                (8, 8, 128, 16, 1400), (32, 16, 64, 64, 175)])
+def test_weights_of_large_capacities(cuda, H, Hkv, D, page, spare):
+    log(f"cache attention, large capacity, {H} {Hkv} {D} page {page}")
+    x = O.Batch([200, 0, 700], [100, 40, 70], H, Hkv, D, page, seed=D + page, spare=spare, tail=2)
+    assert -(-x.slots // 256) * x.B * Hkv >= 2048
+    check(x, cuda)
+
+
+# few rows, short caches, more (sequence, key head) pairs than run at once: a
+# part each, the usual waves; scores kept and not
+@pytest.mark.parametrize("H,D", [(8, 64), (8, 128), (96, 64), (128, 128)])
+def test_many_heads_of_short_caches(cuda, H, D):
+    log(f"cache attention, 80 sequences of 8 key heads, {H} heads of {D}")
+    g = random.Random(H)
+    lens = [g.choice([0, 1, 15, 16, 33, 64, 100]) for _ in range(80)]
+    news = [g.choice([0, 1, 1, 2]) for _ in lens]
+    check(O.Batch(lens, news, H, 8, D, 16, seed=H, tail=1), cuda)
+
+
+@pytest.mark.parametrize("ties", [False, True])
+@pytest.mark.parametrize("budget", [300, 19700])
+@pytest.mark.parametrize("D", [64, 128])
+def test_evict_few_rows_of_long_sequences(cuda, D, budget, ties):
+    """Beyond 16,384 slots, moved by the workgroup that selects them."""
+    log(f"evict 20000 to {budget}, D {D}, ties {ties}")
+    evict_case(cuda, *evict_state([20000, 18000, 5], 2, 20000, budget, ties), budget, 40, D=D)
