@@ -331,7 +331,9 @@ class PagedCache:
 
     Lengths and pages in use are kept on the host as well, so that nothing has
     to be read back; a call that finds no free page raises RuntimeError and
-    changes nothing."""
+    changes nothing.  ``extend``, ``evict`` and ``clear`` bring the device's
+    offsets and tables up to date from the host, which waits for the stream:
+    they are not for a captured graph."""
 
     def __init__(self, batch: int, kv_heads: int, dim: int, capacity: int, page: int = 64,
                  pages: int = None, weights: bool = False, device="cuda"):

@@ -146,6 +146,11 @@ attend_tile(const uint16_t *kt, const uint16_t *vt, const bf16x8 (&qf)[D / 16],
         }
     l_i += psum;
 
+    // The one rounding to fewer bits before the output's: the matrix cores take P in
+    // V's type, and its roundings, one a key, average out where many keys count
+    // (o of one token over 1,024 slots is 0.00164 from float64, relative, and 0.00161
+    // if only o itself is rounded; of 4 x 2,048 tokens over 14,336 0.00168 and
+    // 0.00167).  The row's sum is of the fp32 values.
     bf16x8 pb[NB][2];
 #pragma unroll
     for (int kb = 0; kb < NB; ++kb)

@@ -17,8 +17,10 @@
 // reach it are read once more (one of a thread as a rule; all of them where its
 // other pieces reach it too), what is not below the floor goes into a list in
 // LDS as 64-bit keys of logit and index, and their ranks are the result.  A
-// list that does not fit (many equal logits at the floor) is found by k passes
-// instead, each for the largest key below the last.
+// list that does not fit is found by k passes instead, each for the largest key
+// below the last: many equal logits at the floor, or so many masked ones that no
+// wave has k lanes with another (the floor is the mask then; 16 x 50,432 with 30
+// logits that are not -inf and 8 alternatives 77 us, with 300 of them 13.7).
 // Both join over a workgroup's waves, and over the workgroups of a row where
 // there are few rows.
 //
