@@ -446,8 +446,9 @@ int dd_cache_check(const int32_t *host_table, const int32_t *host_lens, const in
  *                  lse) (each gradient fp32 [rows] or NULL): dX_j = p_j (g_lse -
  *                  g_logp - g_entropy (log p_j + entropy)) + g_logp [j = t], of
  *                  X's type, rounded once; lse and entropy from the forward (a
- *                  row's p add up to 1 whatever the size of its lse).  dX may be X
- *                  (with lddx = ldx).
+ *                  row's p add up to 1 whatever the size of its lse; where X holds
+ *                  some columns of the row whose lse and entropy are given, they
+ *                  are e^(x - lse)).  dX may be X (with lddx = ldx).
  */
 int dd_logprobs_fwd(const void *X, long long ldx, int f32, const int64_t *targets, float *logp,
                     float *entropy, float *lse, float *top_logp, int64_t *top_ids, int rows, int V,

@@ -475,7 +475,11 @@ __global__ void __launch_bounds__(256) logits_grad_kernel(GradRows a)
             waves[tid >> 6] = s;
         __syncthreads();
         s = (waves[0] + waves[1]) + (waves[2] + waves[3]);
-        const float scale = 1.f / s, log_s = logf(s);
+        // (half a step of the lse, or little more; further off, the lse is that of a
+        // row of which these columns are a part, and counts as it is)
+        const float off = logf(s);
+        const bool rounding = fabsf(off) <= fabsf(lse) * 0x1p-21f;
+        const float scale = rounding ? 1.f / s : 1.f, log_s = rounding ? off : 0.f;
         for (int at = tid * 8; at < a.V; at += 2048) {
             f32x8 f = load_logits(x, at, a.V);
 #pragma unroll

@@ -447,3 +447,28 @@ def test_large_entropy_gradients_of_masked_logits(cuda, dtype):
         dx = dd.logprobs_backward(yd, td, lse, h, g_entropy=g.to(cuda)).cpu()
         assert (dx[mask] == 0).all() and torch.isfinite(dx).all()
         check_far(y, t, [torch.zeros(6), g, torch.zeros(6)], dx)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("offset", [0.0, 90.0, -200.0])
+def test_gradient_of_a_part_of_the_columns(cuda, offset, dtype):
+    """A row's lse and entropy with some of its columns (a vocabulary in parts):
+    the columns' share of the row's gradient, also where the lse lies far from
+    zero.  Tolerance: the lse's own rounding, |lse| u of p, is in it twice."""
+    log(f"logprobs: gradient of a part of the columns, offset {offset} {dtype}")
+    V, cuts = 12000, [0, 500, 9500, 12000]
+    x, _, g = case(6, V, dtype, 21)
+    x = (x.float() + offset).to(dtype)
+    none = torch.full((6,), -1)
+    xd, nd, gd = x.to(cuda), none.to(cuda), [y.to(cuda) for y in g]
+    _, h, lse = dd.logprobs(xd, nd)
+    whole = dd.logprobs_backward(xd, nd, lse, h, None, *gd[1:])
+    check_far(x, none, g, whole)
+    parts = [dd.logprobs_backward(xd[:, a:b], nd, lse, h, None, *gd[1:])
+             for a, b in zip(cuts, cuts[1:])]
+    ref, size, p, lp, hr = exact_grad(x, none, torch.zeros(6), *g[1:])
+    z = lse.double().cpu().abs()[:, None]
+    tol = (2 * (200 + V / 256 + 194) * U + 2 * U * z + 4 * U * (lp.clamp(max=200) + 1)) * size
+    tol = tol + (2 * U * z + 1e-4) * p * g[1].double().abs()[:, None]
+    tol = tol + (HB if dtype is torch.bfloat16 else U) * (ref.abs() + tol) + 1e-38
+    close(torch.cat(parts, dim=1), ref, tol, "parts")
