@@ -409,8 +409,8 @@ class PagedCache:
         choose their kernels by the number of rows, get the chunk's alone."""
         n, rows = sum(news), q.shape[0]
         for t, name in ((k, "k"), (v, "v")):
-            if t.shape[0] != rows:
-                raise ValueError(f"q has {rows} rows, {name} has {t.shape[0]}")
+            if not isinstance(t, torch.Tensor) or t.shape[:1] != q.shape[:1]:
+                raise ValueError(f"q has {rows} rows, {name} must have as many")
         if (out is None) != (lse is None):
             raise ValueError("give both out and lse, or neither")
         if out is None:

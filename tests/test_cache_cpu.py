@@ -291,3 +291,13 @@ def test_scores_are_not_kept_for_more_slots_than_a_launch_has_blocks(lib):
         more = lib.dd_cache_attn_workspace_bytes(*sizes, 1) - \
             lib.dd_cache_attn_workspace_bytes(*sizes, 0)
         assert more == (4 * 16 * per if kept else 0)
+
+
+def test_the_cache_compares_its_rows_first():
+    """What is no tensor of q's rows is refused before pages change hands."""
+    c = cache.PagedCache(1, 2, 64, 64, page=16, device="cpu")
+    q = torch.zeros(8, 2, 64, dtype=torch.bfloat16)
+    for k, v in ((None, q), (q, None), (q[0, 0, 0], q), (q, q[:3])):
+        with pytest.raises(ValueError):
+            c.extend(q, k, v, [5])
+    assert c.owned == [[]] and len(c.free) == 4
